@@ -253,13 +253,12 @@ def _inputs(case, seed):
         s["q"] = _normal(g, (sum(q_lens), Hq, D), 1.5)                   # scores of a spread of 1.5
         s["k"], s["v"] = _normal(g, (sum(k_lens), Hk, D)), _normal(g, (sum(k_lens), Hk, D))
         s["cu_q"], s["cu_k"] = _cu(q_lens), _cu(k_lens)
-        s["max_q"], s["max_k"] = max(q_lens), max(k_lens)
         if op == "train":
             s["dout"] = _normal(g, (sum(q_lens), Hq, D))
     elif op == "store":
         lens, before = _ints(case["q_lens"]), _ints(case["before"])
         s["k"], s["v"] = _normal(g, (sum(lens), Hk, D)) + 0.5 * _normal(g, (Hk, D)), _normal(g, (sum(lens), Hk, D))
-        s["cu_q"], s["max_q"] = _cu(lens), max(lens)
+        s["cu_q"] = _cu(lens)
         s["before"] = torch.tensor(before, dtype=torch.int32, device="cuda")
         s["table"], pages = _table(g, [a + n for a, n in zip(before, lens)])
         s["cache"] = _empty_cache(pages, Hk, D)
@@ -464,13 +463,13 @@ def run(state):
         return swz.qk_norm_rope_backward(s["dq"], s["dk"], s["q"], s["k"], s["q_weight"], s["k_weight"], s["cos"], s["sin"], s["positions"], eps=EPS,
                                          interleaved=case["interleaved"])
     if op == "prompt":
-        return swz.attention(s["q"], s["k"], s["v"], s["cu_q"], s["cu_k"], s["max_q"], s["max_k"], causal=case["causal"])[0]
+        return swz.attention(s["q"], s["k"], s["v"], s["cu_q"], s["cu_k"], causal=case["causal"])[0]
     if op == "train":
-        out, lse = swz.attention(s["q"], s["k"], s["v"], s["cu_q"], s["cu_k"], s["max_q"], s["max_k"], causal=case["causal"])
-        return (out, *swz.attention_backward(s["dout"], s["q"], s["k"], s["v"], out, lse, s["cu_q"], s["cu_k"], s["max_q"], s["max_k"], causal=case["causal"]))
+        out, lse = swz.attention(s["q"], s["k"], s["v"], s["cu_q"], s["cu_k"], causal=case["causal"])
+        return (out, *swz.attention_backward(s["dout"], s["q"], s["k"], s["v"], out, lse, s["cu_q"], s["cu_k"], causal=case["causal"]))
     if op == "store":
-        swz.cache4_append(s["cache"], s["k"], s["v"], s["cu_q"], s["before"], s["table"], s["max_q"])
-        return swz.cache4_read(s["cache"], s["cu_q"], s["before"], s["table"], s["max_q"], s["k"].shape[0])
+        swz.cache4_append(s["cache"], s["k"], s["v"], s["cu_q"], s["before"], s["table"])
+        return swz.cache4_read(s["cache"], s["cu_q"], s["before"], s["table"], s["k"].shape[0])
     return swz.cache4_attention(s["q"], s["cache"], s["lens"], s["table"], s["max_len"])
 
 
