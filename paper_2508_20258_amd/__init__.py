@@ -9,3 +9,6 @@ from .binding import (  # noqa: F401
     gemm_launch_map, gemm_plan, lib, pid_map, pid_map_device, pid_map_persistent, pid_map_persistent_device, status_string, transpose,
     layernorm, mfma_peak, softmax, gemm_probe, PROBE_WORDS,
 )
+from .attention_layer import (  # noqa: F401
+    CACHE_GROUP, Cache4, attention, attention_backward, cache4_append, cache4_attention, cache4_read, kv_cache4, qk_norm_rope, qk_norm_rope_backward,
+)

@@ -1,0 +1,339 @@
+// libswz: C-ABI entry points of attention layers (declared in include/swz_attention.h).  Host side: argument checks, the split of the
+// work, launches.  Nothing here allocates device memory or synchronises.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/swz_attention.h"
+#include "attention_backward_kernel.h"
+#include "attention_kernel.h"
+#include "cache4_kernel.h"
+#include "launch.h"
+#include "pid_decode.h"
+#include "qk_norm_kernel.h"
+
+namespace {
+
+using swz::DeviceFacts;
+using swz::kWholeCus;
+using swz::launch;
+using swz::query_device;
+
+constexpr int64_t kTokens = (int64_t)1 << 31;      // fewer than these
+
+swz::Heads device_heads(const swz_heads& h) { return {static_cast<uint16_t*>(h.data), h.token, h.head}; }
+
+bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+// Heads that a call reads or writes: there, aligned, and distances that keep 16-byte pieces aligned.
+int check_heads(const swz_heads& h) {
+  if (h.data == nullptr || h.token < 0 || h.head < 0) return SWZ_ERR_INVALID_ARG;
+  return aligned(h.data, 16) && h.token % 8 == 0 && h.head % 8 == 0 ? SWZ_OK : SWZ_ERR_UNSUPPORTED;
+}
+template <class... H>
+int check_heads(const swz_heads& h, const H&... more) {
+  const int st = check_heads(h);
+  return st != SWZ_OK ? st : check_heads(more...);
+}
+
+bool head_dim_ok(int d) { return d == 64 || d == 128; }
+
+// f(integral_constant<int, D>) for the two sizes of a head.
+template <class F>
+int for_head_dim(int d, F&& f) {
+  return d == 128 ? f(std::integral_constant<int, 128>{}) : f(std::integral_constant<int, 64>{});
+}
+template <class F>
+int for_flag(bool flag, F&& f) {
+  return flag ? f(std::true_type{}) : f(std::false_type{});
+}
+
+int compute_units() {
+  DeviceFacts f;
+  return query_device(&f) == SWZ_OK && f.cus > 0 ? f.cus : kWholeCus;
+}
+
+// XCDs that the workgroups are dealt to; 1 (their order as it is) where the device does not say.
+int xcds() {
+  DeviceFacts f;
+  return query_device(&f) == SWZ_OK && f.num_xcd > 0 ? f.num_xcd : 1;
+}
+
+// ---------------------------------------------------------------- norm and rotation
+
+int check_norm(const swz_norm_args* a) {
+  if (a == nullptr || a->q_weight == nullptr || a->k_weight == nullptr || a->cos == nullptr || a->sin == nullptr || a->positions == nullptr) return SWZ_ERR_INVALID_ARG;
+  if (a->tokens < 0 || a->q_heads < 1 || a->k_heads < 1 || a->table_rows < 0 || !(a->eps >= 0.f)) return SWZ_ERR_INVALID_ARG;
+  const int st = check_heads(a->q, a->k, a->q_out, a->k_out);
+  if (st != SWZ_OK) return st;
+  if (!head_dim_ok(a->head_dim) || a->rotary_dim < 16 || a->rotary_dim > a->head_dim || a->rotary_dim % 16 != 0) return SWZ_ERR_UNSUPPORTED;
+  if (!aligned(a->q_weight, 16) || !aligned(a->k_weight, 16) || !aligned(a->cos, 16) || !aligned(a->sin, 16) || !aligned(a->positions, 4)) return SWZ_ERR_UNSUPPORTED;
+  if (a->q_heads > 65536 || a->k_heads > 65536 || a->table_rows >= kTokens) return SWZ_ERR_OVERFLOW;
+  if (a->tokens >= kTokens || a->tokens * a->q_heads >= kTokens || a->tokens * a->k_heads >= kTokens) return SWZ_ERR_OVERFLOW;
+  return SWZ_OK;
+}
+
+swz::NormArgs norm_args(const swz_norm_args& a) {
+  swz::NormArgs n{};
+  n.x[0] = device_heads(a.q), n.x[1] = device_heads(a.k);
+  n.z[0] = device_heads(a.q_out), n.z[1] = device_heads(a.k_out);
+  n.weight[0] = static_cast<const uint16_t*>(a.q_weight), n.weight[1] = static_cast<const uint16_t*>(a.k_weight);
+  n.cos = a.cos, n.sin = a.sin, n.positions = a.positions;
+  n.heads[0] = a.q_heads, n.heads[1] = a.k_heads;
+  n.rows[0] = (int)(a.tokens * a.q_heads), n.rows[1] = (int)(a.tokens * a.k_heads);
+  n.rotary = a.rotary_dim, n.table_rows = (int)a.table_rows, n.eps = a.eps;
+  return n;
+}
+
+// Workgroups of the backward pass: as many as have rows, at most eight to a compute unit.
+int norm_backward_blocks(const swz_norm_args& a) {
+  const int64_t rows = a.tokens * (a.q_heads > a.k_heads ? a.q_heads : a.k_heads), per = 2 * swz::kNormThreads / (a.head_dim / 8);
+  const int64_t blocks = (rows + per - 1) / per, most = 8 * (int64_t)compute_units();
+  return (int)(blocks < 1 ? 1 : blocks < most ? blocks : most);
+}
+
+// ---------------------------------------------------------------- prompts
+
+int check_prompt(const swz_attention_args* a) {
+  if (a == nullptr || a->lse == nullptr || a->cu_q == nullptr || a->cu_k == nullptr) return SWZ_ERR_INVALID_ARG;
+  if (a->total_q < 0 || a->total_k < 0 || a->sequences < 1 || a->q_heads < 1 || a->k_heads < 1 || a->q_heads % a->k_heads != 0) return SWZ_ERR_INVALID_ARG;
+  if (!(a->scale > 0.f) || !isfinite(a->scale)) return SWZ_ERR_INVALID_ARG;
+  const int st = check_heads(a->q, a->k, a->v, a->out);
+  if (st != SWZ_OK) return st;
+  if (!head_dim_ok(a->head_dim) || !aligned(a->lse, 4) || !aligned(a->cu_q, 4) || !aligned(a->cu_k, 4)) return SWZ_ERR_UNSUPPORTED;
+  return a->total_q >= kTokens || a->total_k >= kTokens ? SWZ_ERR_OVERFLOW : SWZ_OK;
+}
+
+swz::PromptArgs prompt_args(const swz_attention_args& a) {
+  swz::PromptArgs p{};
+  p.q = device_heads(a.q), p.k = device_heads(a.k), p.v = device_heads(a.v), p.out = device_heads(a.out);
+  p.lse = a.lse, p.cu_q = a.cu_q, p.cu_k = a.cu_k;
+  p.total_q = (int)a.total_q, p.total_k = (int)a.total_k, p.sequences = a.sequences;
+  p.q_heads = a.q_heads, p.k_heads = a.k_heads, p.num_xcd = xcds(), p.scale = a.scale;
+  return p;
+}
+
+// Workgroups for tiles of `rows` tokens (see find_slot) and `heads` heads; the launch refuses what is too many threads.
+int64_t slots_of(int64_t total, int sequences, int rows, int per = 1) { return total / rows + (int64_t)per * sequences; }
+
+template <class Kernel, class Args>
+int launch_slots(Kernel kernel, int64_t slots, int heads, int threads, hipStream_t stream, const Args& args) {
+  if (slots * heads >= kTokens) return SWZ_ERR_OVERFLOW;
+  return launch(kernel, dim3((unsigned)(slots * heads)), dim3((unsigned)threads), 0, stream, args);
+}
+
+constexpr int kForwardWaves = 4, kDqWaves = 4, kDkvWaves = 4;
+
+// ---------------------------------------------------------------- the cache
+
+int check_cache(const swz_cache4* c) {
+  if (c == nullptr || c->k_words == nullptr || c->v_words == nullptr || c->k_scales == nullptr || c->v_scales == nullptr || c->pages < 1 || c->k_heads < 1) return SWZ_ERR_INVALID_ARG;
+  if (!head_dim_ok(c->head_dim) || c->page_tokens < 32 || (c->page_tokens & (c->page_tokens - 1)) != 0) return SWZ_ERR_UNSUPPORTED;
+  if (!aligned(c->k_words, 16) || !aligned(c->v_words, 16) || !aligned(c->k_scales, 16) || !aligned(c->v_scales, 16)) return SWZ_ERR_UNSUPPORTED;
+  return c->pages >= kTokens ? SWZ_ERR_OVERFLOW : SWZ_OK;
+}
+
+swz::CacheArgs cache_args(const swz_cache4& c, const int32_t* table, int table_width) {
+  swz::CacheArgs a{};
+  a.k_words = reinterpret_cast<uint32_t*>(c.k_words), a.v_words = reinterpret_cast<uint32_t*>(c.v_words);
+  a.k_scales = static_cast<uint32_t*>(c.k_scales), a.v_scales = static_cast<uint32_t*>(c.v_scales);
+  a.table = table, a.pages = c.pages, a.page_shift = __builtin_ctz((unsigned)c.page_tokens), a.k_heads = c.k_heads, a.table_width = table_width;
+  return a;
+}
+
+template <bool READ>
+int store_or_read(const swz_cache4* cache, const swz_heads* k, const swz_heads* v, int64_t tokens, const int32_t* cu, const int32_t* before, const int32_t* table,
+                  int32_t table_width, int32_t sequences, hipStream_t stream) {
+  int st = check_cache(cache);
+  if (st != SWZ_OK) return st;
+  if (k == nullptr || v == nullptr || cu == nullptr || before == nullptr || table == nullptr || tokens < 0 || sequences < 1 || table_width < 1) return SWZ_ERR_INVALID_ARG;
+  if (tokens == 0) return SWZ_OK;
+  st = check_heads(*k, *v);
+  if (st != SWZ_OK) return st;
+  if (!aligned(cu, 4) || !aligned(before, 4) || !aligned(table, 4)) return SWZ_ERR_UNSUPPORTED;
+  if (tokens >= kTokens) return SWZ_ERR_OVERFLOW;
+  return for_head_dim(cache->head_dim, [&](auto dim) {
+    constexpr int D = decltype(dim)::value;
+    swz::StoreArgs a{};
+    a.c = cache_args(*cache, table, table_width);
+    a.k = device_heads(*k), a.v = device_heads(*v);
+    a.cu = cu, a.before = before, a.total = (int)tokens, a.sequences = sequences;
+    a.head_blocks = (cache->k_heads + swz::StoreShape<D>::kHeads - 1) / swz::StoreShape<D>::kHeads;
+    auto kernel = READ ? swz::cache4_read_kernel<D> : swz::cache4_append_kernel<D>;
+    return launch_slots(kernel, slots_of(tokens, sequences, 8, 2), a.head_blocks, 256, stream, a);
+  });
+}
+
+// How the sequences of a decoding step are split: parts of part_tokens tokens, a workgroup each.
+struct DecodeSplit {
+  int columns, parts, part_tokens;
+};
+constexpr int kDecodeWaves = 4;
+DecodeSplit decode_split(const swz_cache4& c, int sequences, int q_heads, int table_width, int max_length) {
+  const int group = q_heads / c.k_heads, columns = (group + 15) / 16;
+  const int64_t cut = (int64_t)table_width * c.page_tokens, longest = max_length > 0 && max_length < cut ? max_length : cut;
+  const int64_t pairs = (int64_t)sequences * c.k_heads * columns, step = 32 * kDecodeWaves;
+  int64_t parts = 4 * (int64_t)compute_units() / pairs;                  // as many as give every compute unit four workgroups
+  if (parts > (longest + 2 * step - 1) / (2 * step)) parts = (longest + 2 * step - 1) / (2 * step);
+  if (parts < 1) parts = 1;
+  int64_t tokens = (longest + parts - 1) / parts;
+  tokens = (tokens + step - 1) / step * step;
+  // sequences longer than the caller said (never longer than the table) must still be covered
+  parts = (cut + tokens - 1) / tokens;
+  return {columns, (int)parts, (int)tokens};
+}
+
+int check_decode(const swz_cache4* c, int sequences, int q_heads, int table_width, int max_length) {
+  const int st = check_cache(c);
+  if (st != SWZ_OK) return st;
+  if (sequences < 1 || q_heads < 1 || q_heads % c->k_heads != 0 || table_width < 1 || max_length < 0) return SWZ_ERR_INVALID_ARG;
+  if ((int64_t)table_width * c->page_tokens >= kTokens || (int64_t)sequences * q_heads >= kTokens) return SWZ_ERR_OVERFLOW;
+  return SWZ_OK;
+}
+
+int64_t decode_floats(const swz_cache4& c, const DecodeSplit& s, int sequences, int q_heads) {
+  return s.parts == 1 ? 0 : (int64_t)sequences * q_heads * s.parts * (c.head_dim + 2);
+}
+
+}  // namespace
+
+extern "C" {
+
+int swz_qk_norm_rope(const swz_norm_args* args, hipStream_t stream) {
+  const int st = check_norm(args);
+  if (st != SWZ_OK || args->tokens == 0) return st;
+  swz::NormArgs n = norm_args(*args);
+  return for_head_dim(args->head_dim, [&](auto dim) {
+    return for_flag(args->interleaved != 0, [&](auto interleaved) {
+      constexpr int D = decltype(dim)::value;
+      const int per = swz::kNormUnroll * swz::kNormThreads / (D / 8);
+      n.blocks_q = (n.rows[0] + per - 1) / per;
+      const int blocks_k = (n.rows[1] + per - 1) / per;
+      return launch(swz::qk_norm_kernel<D, decltype(interleaved)::value>, dim3((unsigned)(n.blocks_q + blocks_k)), dim3(swz::kNormThreads), 0, stream, n);
+    });
+  });
+}
+
+int64_t swz_qk_norm_rope_backward_workspace(const swz_norm_args* args) {
+  const int st = check_norm(args);
+  return st != SWZ_OK ? st : (int64_t)norm_backward_blocks(*args) * 2 * args->head_dim * 4;
+}
+
+int swz_qk_norm_rope_backward(const swz_norm_args* args, const swz_heads* dq, const swz_heads* dk, float* dq_weight, float* dk_weight,
+                              void* workspace, int64_t workspace_bytes, hipStream_t stream) {
+  int st = check_norm(args);
+  if (st != SWZ_OK) return st;
+  if (dq == nullptr || dk == nullptr || dq_weight == nullptr || dk_weight == nullptr || workspace == nullptr) return SWZ_ERR_INVALID_ARG;
+  st = check_heads(*dq, *dk);
+  if (st != SWZ_OK) return st;
+  if (!aligned(dq_weight, 4) || !aligned(dk_weight, 4) || !aligned(workspace, 16)) return SWZ_ERR_UNSUPPORTED;
+  if (workspace_bytes < swz_qk_norm_rope_backward_workspace(args)) return SWZ_ERR_INVALID_ARG;
+  swz::NormArgs n = norm_args(*args);
+  n.dx[0] = device_heads(*dq), n.dx[1] = device_heads(*dk);
+  n.partial = static_cast<float*>(workspace);
+  const int blocks = norm_backward_blocks(*args);
+  st = for_head_dim(args->head_dim, [&](auto dim) {
+    return for_flag(args->interleaved != 0, [&](auto interleaved) {
+      return launch(swz::qk_norm_backward_kernel<decltype(dim)::value, decltype(interleaved)::value>, dim3((unsigned)blocks), dim3(swz::kNormThreads), 0, stream, n);
+    });
+  });
+  if (st != SWZ_OK) return st;
+  return launch(swz::norm_weights_kernel, dim3((unsigned)(2 * args->head_dim / 16)), dim3(256), 0, stream, n.partial, blocks, args->head_dim, dq_weight, dk_weight);
+}
+
+int swz_attention(const swz_attention_args* args, hipStream_t stream) {
+  const int st = check_prompt(args);
+  if (st != SWZ_OK || args->total_q == 0) return st;
+  swz::PromptArgs p = prompt_args(*args);
+  return for_head_dim(args->head_dim, [&](auto dim) {
+    return for_flag(args->causal != 0, [&](auto causal) {
+      constexpr int D = decltype(dim)::value;
+      const int64_t slots = slots_of(args->total_q, args->sequences, 32 * kForwardWaves);
+      if (slots >= kTokens) return (int)SWZ_ERR_OVERFLOW;
+      p.slots = (int)slots;
+      return launch_slots(swz::attention_kernel<D, kForwardWaves, decltype(causal)::value>, slots, args->q_heads, 64 * kForwardWaves, stream, p);
+    });
+  });
+}
+
+int64_t swz_attention_backward_workspace(const swz_attention_args* args) {
+  const int st = check_prompt(args);
+  if (st != SWZ_OK) return st;
+  return args->total_q * args->q_heads * 4;
+}
+
+int swz_attention_backward(const swz_attention_args* args, const swz_heads* dout, const swz_heads* dq, const swz_heads* dk, const swz_heads* dv,
+                           void* workspace, int64_t workspace_bytes, hipStream_t stream) {
+  int st = check_prompt(args);
+  if (st != SWZ_OK) return st;
+  if (dout == nullptr || dq == nullptr || dk == nullptr || dv == nullptr || workspace == nullptr) return SWZ_ERR_INVALID_ARG;
+  st = check_heads(*dout, *dq, *dk, *dv);
+  if (st != SWZ_OK) return st;
+  if (!aligned(workspace, 16)) return SWZ_ERR_UNSUPPORTED;
+  if (workspace_bytes < swz_attention_backward_workspace(args)) return SWZ_ERR_INVALID_ARG;
+  swz::PromptBackArgs p{};
+  p.f = prompt_args(*args);
+  p.dout = device_heads(*dout), p.dq = device_heads(*dq), p.dk = device_heads(*dk), p.dv = device_heads(*dv);
+  p.delta = static_cast<float*>(workspace);
+  return for_head_dim(args->head_dim, [&](auto dim) {
+    return for_flag(args->causal != 0, [&](auto causal) {
+      constexpr int D = decltype(dim)::value;
+      constexpr bool kCausal = decltype(causal)::value;
+      const int64_t q_slots = slots_of(args->total_q, args->sequences, 32 * kDqWaves), k_slots = slots_of(args->total_k, args->sequences, 32 * kDkvWaves);
+      if (q_slots * args->q_heads * 64 * kDqWaves > swz::kLaunchThreads || k_slots * args->k_heads * 64 * kDkvWaves > swz::kLaunchThreads) return (int)SWZ_ERR_OVERFLOW;
+      int status = SWZ_OK;
+      p.f.slots = (int)q_slots;
+      if (args->total_q > 0) status = launch_slots(swz::attention_dq_kernel<D, kDqWaves, kCausal>, q_slots, args->q_heads, 64 * kDqWaves, stream, p);
+      if (status != SWZ_OK || args->total_k == 0) return status;
+      p.f.slots = (int)k_slots;
+      return launch_slots(swz::attention_dkv_kernel<D, kDkvWaves, kCausal>, k_slots, args->k_heads, 64 * kDkvWaves, stream, p);
+    });
+  });
+}
+
+int swz_cache4_append(const swz_cache4* cache, const swz_heads* k, const swz_heads* v, int64_t tokens, const int32_t* cu, const int32_t* before,
+                      const int32_t* block_table, int32_t table_width, int32_t sequences, hipStream_t stream) {
+  return store_or_read<false>(cache, k, v, tokens, cu, before, block_table, table_width, sequences, stream);
+}
+
+int swz_cache4_read(const swz_cache4* cache, const swz_heads* k, const swz_heads* v, int64_t tokens, const int32_t* cu, const int32_t* first,
+                    const int32_t* block_table, int32_t table_width, int32_t sequences, hipStream_t stream) {
+  return store_or_read<true>(cache, k, v, tokens, cu, first, block_table, table_width, sequences, stream);
+}
+
+int64_t swz_cache4_attention_workspace(const swz_cache4* cache, int32_t sequences, int32_t q_heads, int32_t table_width, int32_t max_length) {
+  const int st = check_decode(cache, sequences, q_heads, table_width, max_length);
+  if (st != SWZ_OK) return st;
+  return 4 * decode_floats(*cache, decode_split(*cache, sequences, q_heads, table_width, max_length), sequences, q_heads);
+}
+
+int swz_cache4_attention(const swz_cache4* cache, const swz_heads* q, const swz_heads* out, const int32_t* lengths, const int32_t* block_table,
+                         int32_t table_width, int32_t sequences, int32_t q_heads, int32_t max_length, float scale, void* workspace, int64_t workspace_bytes,
+                         hipStream_t stream) {
+  int st = check_decode(cache, sequences, q_heads, table_width, max_length);
+  if (st != SWZ_OK) return st;
+  if (q == nullptr || out == nullptr || lengths == nullptr || block_table == nullptr || !(scale > 0.f) || !isfinite(scale)) return SWZ_ERR_INVALID_ARG;
+  st = check_heads(*q, *out);
+  if (st != SWZ_OK) return st;
+  const DecodeSplit s = decode_split(*cache, sequences, q_heads, table_width, max_length);
+  const int64_t floats = decode_floats(*cache, s, sequences, q_heads);
+  if (floats > 0 && (workspace == nullptr || workspace_bytes < 4 * floats)) return SWZ_ERR_INVALID_ARG;
+  if (!aligned(lengths, 4) || !aligned(block_table, 4) || !aligned(workspace, 16)) return SWZ_ERR_UNSUPPORTED;
+  swz::DecodeArgs a{};
+  a.c = cache_args(*cache, block_table, table_width);
+  a.q = device_heads(*q), a.out = device_heads(*out);
+  a.lengths = lengths, a.sequences = sequences, a.q_heads = q_heads;
+  a.columns = s.columns, a.parts = s.parts, a.part_tokens = s.part_tokens, a.scale = scale;
+  a.sums = static_cast<float*>(workspace);
+  a.stats = a.sums + (floats > 0 ? (int64_t)sequences * q_heads * s.parts * cache->head_dim : 0);
+  return for_head_dim(cache->head_dim, [&](auto dim) {
+    constexpr int D = decltype(dim)::value;
+    const int64_t blocks = (int64_t)sequences * cache->k_heads * s.columns * s.parts;
+    if (blocks >= kTokens) return (int)SWZ_ERR_OVERFLOW;
+    int status = launch(swz::cache4_attention_kernel<D, kDecodeWaves>, dim3((unsigned)blocks), dim3(64 * kDecodeWaves), 0, stream, a);
+    if (status != SWZ_OK || s.parts == 1) return status;
+    return launch(swz::cache4_join_kernel<D>, dim3((unsigned)(((int64_t)sequences * q_heads + 3) / 4)), dim3(256), 0, stream, a);
+  });
+}
+
+}  // extern "C"
