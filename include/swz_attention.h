@@ -74,7 +74,10 @@ typedef struct {
   float scale;
 } swz_attention_args;
 
-int swz_attention(const swz_attention_args* args, hipStream_t stream);
+/*   workspace : swz_attention_workspace(args) bytes, 16-byte aligned; may be null where that is 0 (it is not where few queries look at many keys, which are then
+ *   cut among workgroups and joined by a second launch). */
+int64_t swz_attention_workspace(const swz_attention_args* args);
+int swz_attention(const swz_attention_args* args, void* workspace, int64_t workspace_bytes, hipStream_t stream);
 
 /* The gradient of swz_attention: args as in the forward call, with its out and lse (read).
  *   dout : gradient of out.   dq, dk, dv : receive those of q, k, v, for all tokens of the sequences (must not overlap anything that is read).

@@ -12,7 +12,7 @@ from typing import NamedTuple
 
 from .binding import _check, _launch_stream, lib, torch
 
-EXPORTS = ("swz_qk_norm_rope", "swz_qk_norm_rope_backward_workspace", "swz_qk_norm_rope_backward", "swz_attention", "swz_attention_backward_workspace",
+EXPORTS = ("swz_qk_norm_rope", "swz_qk_norm_rope_backward_workspace", "swz_qk_norm_rope_backward", "swz_attention_workspace", "swz_attention", "swz_attention_backward_workspace",
            "swz_attention_backward", "swz_cache4_append", "swz_cache4_read", "swz_cache4_attention_workspace", "swz_cache4_attention")
 CACHE_GROUP = 64            # values of a head that share a step and a low
 
@@ -45,8 +45,8 @@ def _declare() -> None:
     lib.swz_qk_norm_rope.argtypes = [n, vp]
     lib.swz_qk_norm_rope_backward_workspace.argtypes = [n]
     lib.swz_qk_norm_rope_backward.argtypes = [n, h, h, vp, vp, vp, i64, vp]
-    lib.swz_attention.argtypes = [a, vp]
-    lib.swz_attention_backward_workspace.argtypes = [a]
+    lib.swz_attention.argtypes = [a, vp, i64, vp]
+    lib.swz_attention_workspace.argtypes = lib.swz_attention_backward_workspace.argtypes = [a]
     lib.swz_attention_backward.argtypes = [a, h, h, h, h, vp, i64, vp]
     lib.swz_cache4_append.argtypes = lib.swz_cache4_read.argtypes = [c, h, h, i64, vp, vp, vp, i32, i32, vp]
     lib.swz_cache4_attention_workspace.argtypes = [c, i32, i32, i32, i32]
@@ -170,7 +170,10 @@ def attention(q, k, v, cu_q, cu_k=None, out=None, lse=None, causal: bool = True,
         return out, lse
     if k.shape[0] == 0:                                   # nothing to look at: no memory that a pointer could name either
         k = v = q[:1, :1].expand(1, k.shape[1], -1)
-    _check(lib.swz_attention(ctypes.byref(_attention_args(q, k, v, out, lse, cu_q, cu_k, causal, scale)), h), "swz_attention")
+    a = _attention_args(q, k, v, out, lse, cu_q, cu_k, causal, scale)
+    work = _workspace(lib.swz_attention_workspace(ctypes.byref(a)), "swz_attention", q)
+    _check(lib.swz_attention(ctypes.byref(a), _pointer(work), 0 if work is None else work.numel(), h), "swz_attention")
+    _keep(stream, work)
     return out, lse
 
 

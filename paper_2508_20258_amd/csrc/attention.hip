@@ -109,7 +109,7 @@ swz::PromptArgs prompt_args(const swz_attention_args& a) {
   p.q = device_heads(a.q), p.k = device_heads(a.k), p.v = device_heads(a.v), p.out = device_heads(a.out);
   p.lse = a.lse, p.cu_q = a.cu_q, p.cu_k = a.cu_k;
   p.total_q = (int)a.total_q, p.total_k = (int)a.total_k, p.sequences = a.sequences;
-  p.q_heads = a.q_heads, p.k_heads = a.k_heads, p.num_xcd = xcds(), p.scale = a.scale;
+  p.q_heads = a.q_heads, p.k_heads = a.k_heads, p.num_xcd = xcds(), p.sets = swz::prompt_sets(a.k_heads, p.num_xcd), p.scale = a.scale;
   return p;
 }
 
@@ -122,7 +122,40 @@ int launch_slots(Kernel kernel, int64_t slots, int heads, int threads, hipStream
   return launch(kernel, dim3((unsigned)(slots * heads)), dim3((unsigned)threads), 0, stream, args);
 }
 
-constexpr int kForwardWaves = 4, kDqWaves = 4, kDkvWaves = 4;
+// The launch of a kernel over prompts: `slots` turns, of `splits` workgroups each, `group` query heads of a key head apart or (1) together.
+template <auto KERNEL, class Args>
+int launch_prompt(Args& args, swz::PromptArgs& p, int64_t slots, int splits, int group, int threads, hipStream_t stream) {
+  const int64_t workgroups = slots * splits < kTokens ? swz::prompt_workgroups(slots * splits, p.k_heads, group, p.num_xcd) : kTokens;
+  if (workgroups >= kTokens) return SWZ_ERR_OVERFLOW;
+  p.slots = (int)slots;
+  p.splits = splits;
+  return launch(KERNEL, dim3((unsigned)workgroups), dim3((unsigned)threads), 0, stream, args);
+}
+bool too_many_threads(int64_t slots, int heads_k, int group, int num_xcd, int threads) {
+  return slots >= kTokens || swz::prompt_workgroups(slots, heads_k, group, num_xcd) * threads > swz::kLaunchThreads;
+}
+
+// Forward: rows of a workgroup, and into how many pieces the keys of a row are cut.
+struct ForwardPlan {
+  int waves, splits;
+};
+ForwardPlan forward_plan(const swz_attention_args& a) {
+  const int64_t cus = compute_units(), group = a.q_heads / a.k_heads;
+  const int xcd = xcds();
+  const int64_t few = swz::prompt_workgroups(slots_of(a.total_q, 1, 128), a.k_heads, (int)group, xcd);       // workgroups of 128 rows, if the sequences were one
+  ForwardPlan p{4, 1};
+  if (a.head_dim == 128 && few >= 8 * cus) p.waves = 8;
+  const int64_t tiles = a.total_k / a.sequences / swz::kPromptKeys;                                      // of an average sequence
+  if (few < cus && tiles >= 16) {
+    int64_t splits = 2 * cus / few;
+    if (splits > tiles / 8) splits = tiles / 8;
+    p.splits = (int)(splits < 32 ? splits : 32);
+  }
+  return p;
+}
+int64_t forward_floats(const swz_attention_args& a, const ForwardPlan& p) { return p.splits == 1 ? 0 : (int64_t)p.splits * a.total_q * a.q_heads * (a.head_dim + 2); }
+
+constexpr int kDqWaves = 4, kDkvWaves = 4;
 
 // ---------------------------------------------------------------- the cache
 
@@ -241,17 +274,40 @@ int swz_qk_norm_rope_backward(const swz_norm_args* args, const swz_heads* dq, co
   return launch(swz::norm_weights_kernel, dim3((unsigned)(2 * args->head_dim / 16)), dim3(256), 0, stream, n.partial, blocks, args->head_dim, dq_weight, dk_weight);
 }
 
-int swz_attention(const swz_attention_args* args, hipStream_t stream) {
+int64_t swz_attention_workspace(const swz_attention_args* args) {
+  const int st = check_prompt(args);
+  return st != SWZ_OK ? st : 4 * forward_floats(*args, forward_plan(*args));
+}
+
+int swz_attention(const swz_attention_args* args, void* workspace, int64_t workspace_bytes, hipStream_t stream) {
   const int st = check_prompt(args);
   if (st != SWZ_OK || args->total_q == 0) return st;
+  const ForwardPlan plan = forward_plan(*args);
+  const int64_t floats = forward_floats(*args, plan);
+  if (floats > 0 && (workspace == nullptr || workspace_bytes < 4 * floats)) return SWZ_ERR_INVALID_ARG;
+  if (!aligned(workspace, 16)) return SWZ_ERR_UNSUPPORTED;
   swz::PromptArgs p = prompt_args(*args);
+  p.splits = plan.splits;
+  p.part_sums = static_cast<float*>(workspace);
+  p.part_stats = p.part_sums + (floats > 0 ? floats / (args->head_dim + 2) * args->head_dim : 0);
   return for_head_dim(args->head_dim, [&](auto dim) {
     return for_flag(args->causal != 0, [&](auto causal) {
       constexpr int D = decltype(dim)::value;
-      const int64_t slots = slots_of(args->total_q, args->sequences, 32 * kForwardWaves);
-      if (slots >= kTokens) return (int)SWZ_ERR_OVERFLOW;
+      constexpr bool kCausal = decltype(causal)::value;
+      const int group = args->q_heads / args->k_heads;
+      auto go = [&](auto waves) {
+        constexpr int W = decltype(waves)::value;
+        return launch_prompt<swz::attention_kernel<D, W, kCausal>>(p, p, slots_of(args->total_q, args->sequences, 32 * W), plan.splits, group, 64 * W, stream);
+      };
+      int status = SWZ_ERR_UNSUPPORTED;
+      if constexpr (D == 128) status = plan.waves == 8 ? go(std::integral_constant<int, 8>{}) : go(std::integral_constant<int, 4>{});
+      else status = go(std::integral_constant<int, 4>{});
+      if (status != SWZ_OK || plan.splits == 1) return status;
+      p.sets = swz::prompt_sets(args->q_heads, p.num_xcd);
+      const int64_t slots = slots_of(args->total_q, args->sequences, swz::kJoinRows);
+      if (slots >= kTokens || swz::prompt_workgroups(slots, args->q_heads, 1, p.num_xcd) >= kTokens) return (int)SWZ_ERR_OVERFLOW;
       p.slots = (int)slots;
-      return launch_slots(swz::attention_kernel<D, kForwardWaves, decltype(causal)::value>, slots, args->q_heads, 64 * kForwardWaves, stream, p);
+      return launch(swz::attention_join_kernel<D>, dim3((unsigned)swz::prompt_workgroups(slots, args->q_heads, 1, p.num_xcd)), dim3(64 * swz::kJoinRows), 0, stream, p);
     });
   });
 }
@@ -280,13 +336,12 @@ int swz_attention_backward(const swz_attention_args* args, const swz_heads* dout
       constexpr int D = decltype(dim)::value;
       constexpr bool kCausal = decltype(causal)::value;
       const int64_t q_slots = slots_of(args->total_q, args->sequences, 32 * kDqWaves), k_slots = slots_of(args->total_k, args->sequences, 32 * kDkvWaves);
-      if (q_slots * args->q_heads * 64 * kDqWaves > swz::kLaunchThreads || k_slots * args->k_heads * 64 * kDkvWaves > swz::kLaunchThreads) return (int)SWZ_ERR_OVERFLOW;
+      const int group = args->q_heads / args->k_heads;
+      if (too_many_threads(q_slots, args->k_heads, group, p.f.num_xcd, 64 * kDqWaves) || too_many_threads(k_slots, args->k_heads, 1, p.f.num_xcd, 64 * kDkvWaves)) return (int)SWZ_ERR_OVERFLOW;
       int status = SWZ_OK;
-      p.f.slots = (int)q_slots;
-      if (args->total_q > 0) status = launch_slots(swz::attention_dq_kernel<D, kDqWaves, kCausal>, q_slots, args->q_heads, 64 * kDqWaves, stream, p);
+      if (args->total_q > 0) status = launch_prompt<swz::attention_dq_kernel<D, kDqWaves, kCausal>>(p, p.f, q_slots, 1, group, 64 * kDqWaves, stream);
       if (status != SWZ_OK || args->total_k == 0) return status;
-      p.f.slots = (int)k_slots;
-      return launch_slots(swz::attention_dkv_kernel<D, kDkvWaves, kCausal>, k_slots, args->k_heads, 64 * kDkvWaves, stream, p);
+      return launch_prompt<swz::attention_dkv_kernel<D, kDkvWaves, kCausal>>(p, p.f, k_slots, 1, 1, 64 * kDkvWaves, stream);
     });
   });
 }

@@ -21,13 +21,13 @@ __global__ void __launch_bounds__(NW * 64, 2) attention_dq_kernel(PromptBackArgs
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
 
   const int group = a.q_heads / a.k_heads;
-  const int l = swz_xcd_renumber((int)blockIdx.x, (int)gridDim.x, a.num_xcd);
-  const int k_head = l / (a.slots * group), rest = l - k_head * (a.slots * group), turn = rest / group;
-  const int head = k_head * group + (rest - turn * group);
-  const SlotPlace place = find_slot(a.cu_q, a.sequences, a.total_q, S::kRows, a.slots - 1 - turn);
-  const Span q = sequence_span(a.cu_q, place.sequence, a.total_q), k = sequence_span(a.cu_k, place.sequence, a.total_k);
-  const int first = place.tile * S::kRows;
-  if (place.tile < 0 || first >= q.length) return;
+  const PromptPiece piece = prompt_piece((int)blockIdx.x, a.slots, a.k_heads, group, a.num_xcd, a.sets);
+  if (piece.turn < 0) return;
+  const int k_head = piece.k_head, head = k_head * group + piece.member;
+  const TurnPlace place = find_turn(a.cu_q, a.total_q, a.cu_k, a.total_k, a.sequences, S::kRows, piece.turn);
+  const Span q = place.mine, k = place.other;
+  const int first = ((q.length + S::kRows - 1) / S::kRows - 1 - place.tile) * S::kRows;
+  if (place.tile < 0 || first < 0) return;
 
   const int row0 = first + wave * 32, row = row0 + (lane & 31);
   const bool real = row < q.length;
@@ -38,11 +38,11 @@ __global__ void __launch_bounds__(NW * 64, 2) attention_dq_kernel(PromptBackArgs
   const int last_key = keys_of(row) - 1;
   const int tiles = (keys + kPromptKeys - 1) / kPromptKeys;
 
-  const uint16_t *k_rows = a.k.at(k.first, k_head), *v_rows = a.v.at(k.first, k_head);
+  const RowLoader<D, kPromptKeys, NW> load_k(a.k.at(k.first, k_head), a.k.token, k.length, wave, lane), load_v(a.v.at(k.first, k_head), a.v.token, k.length, wave, lane);
   auto fetch = [&](int t) {
     const uint32_t at = lds + (uint32_t)((t & 1) * S::kTileBytes);
-    load_rows<D, kPromptKeys, NW>(k_rows, a.k.token, t * kPromptKeys, k.length, at, wave, lane);
-    load_rows<D, kPromptKeys, NW>(v_rows, a.v.token, t * kPromptKeys, k.length, at + 2 * S::kTileBytes, wave, lane);
+    load_k(t * kPromptKeys, at);
+    load_v(t * kPromptKeys, at + 2 * S::kTileBytes);
   };
   if (tiles > 0) fetch(0);
 
@@ -112,10 +112,11 @@ __global__ void __launch_bounds__(NW * 64, 2) attention_dkv_kernel(PromptBackArg
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
 
   const int group = a.q_heads / a.k_heads;
-  const int l = swz_xcd_renumber((int)blockIdx.x, (int)gridDim.x, a.num_xcd);
-  const int k_head = l / a.slots;
-  const SlotPlace place = find_slot(a.cu_k, a.sequences, a.total_k, kKeys, l - k_head * a.slots);
-  const Span q = sequence_span(a.cu_q, place.sequence, a.total_q), k = sequence_span(a.cu_k, place.sequence, a.total_k);
+  const PromptPiece piece = prompt_piece((int)blockIdx.x, a.slots, a.k_heads, 1, a.num_xcd, a.sets);
+  if (piece.turn < 0) return;
+  const int k_head = piece.k_head;
+  const TurnPlace place = find_turn(a.cu_k, a.total_k, a.cu_q, a.total_q, a.sequences, kKeys, piece.turn);
+  const Span q = place.other, k = place.mine;
   const int first = place.tile * kKeys;
   if (place.tile < 0 || first >= k.length) return;
 
@@ -133,12 +134,15 @@ __global__ void __launch_bounds__(NW * 64, 2) attention_dkv_kernel(PromptBackArg
   for (int i = 0; i < D / 32; ++i) dk[i] = dv[i] = f32x16{};
   const float c = a.scale * kLog2E;
 
+  RowLoader<D, kBackRows, NW> load_q(a.q.data, a.q.token, q.length, wave, lane), load_g(args.dout.data, args.dout.token, q.length, wave, lane);
   float stat = 0.f;                                         // thread i < 32: lse of row i, in units of log2; i < 64: delta of row i - 32
   auto fetch = [&](int n) {
     const int m = n / tiles, r0 = (from + n - m * tiles) * kBackRows, head = k_head * group + m;
     const uint32_t at = lds + (uint32_t)((n & 1) * kTileBytes);
-    load_rows<D, kBackRows, NW>(a.q.at(q.first, head), a.q.token, r0, q.length, at, wave, lane);
-    load_rows<D, kBackRows, NW>(args.dout.at(q.first, head), args.dout.token, r0, q.length, at + 2 * kTileBytes, wave, lane);
+    load_q.head = a.q.at(q.first, head);
+    load_g.head = args.dout.at(q.first, head);
+    load_q(r0, at);
+    load_g(r0, at + 2 * kTileBytes);
     if (threadIdx.x < 64) {
       const int r = r0 + (lane & 31);
       const float* from_stat = lane < 32 ? a.lse : args.delta;

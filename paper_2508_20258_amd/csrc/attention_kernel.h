@@ -8,32 +8,34 @@ namespace swz {
 constexpr int kPromptKeys = 64;        // keys of a tile
 constexpr float kLazyRise = 8.f;       // a maximum that rises by less than 2^8 does not rescale what has been summed
 
-template <int D, int NW>
-struct PromptShape {
-  static constexpr int kRows = 32 * NW;
-  static constexpr int kTileBytes = kPromptKeys * 2 * D;
-  static constexpr int kLdsBytes = 4 * kTileBytes;
+template <int D, int QW>
+struct PromptShape {                   // a workgroup: QW waves of 32 rows each
+  static constexpr int kRows = 32 * QW;
+  static constexpr int kTileBytes = kPromptKeys * 2 * D, kLdsBytes = 4 * kTileBytes;      // two tiles of keys, two of values
 };
 
-// o += p v for the 32 keys from `first` on of a tile that the lane's row looks at (up to `last` of the tile), one at a time; p as the score product leaves it.
+// o += p v for the 64 keys of a tile that the lane's row looks at (up to `last` of the tile), one at a time; p as the product with the values takes it.
 template <int D>
-__device__ __forceinline__ void add_by_key(f32x16 (&o)[D / 32], const f32x16& p, const uint16_t* v_tile, int first, int last, int lane) {
+__device__ __forceinline__ void add_by_key(f32x16 (&o)[D / 32], const u32x4 (&p)[4], const unsigned char* v_tile, int last, int lane) {
   const int h = lane >> 5;
 #pragma unroll 1
-  for (int key = 0; key < 32; ++key) {
-    float mine = 0.f;
+  for (int key = 0; key < kPromptKeys; ++key) {
+    // key 16 j + 8 a + 4 h + e is number 4 a + e of operand j in lane half h
+    uint32_t word = 0;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) mine = key == 8 * (r / 4) + 4 * h + r % 4 ? p[r] : mine;
-    const float w = (float)(__bf16)across_halves(mine, [](float x, float y) { return x + y; });
-    const int row = first + key;
-    const bool seen = row <= last;
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) word = j == key >> 4 && e == 2 * (key >> 3 & 1) + (key >> 1 & 1) ? p[j][e] : word;
+    const float mine = (key >> 2 & 1) == h ? __uint_as_float(key & 1 ? word & 0xffff0000u : word << 16) : 0.f;
+    const float w = across_halves(mine, [](float x, float y) { return x + y; });
+    const bool seen = key <= last;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
       for (int part = 0; part < 4; ++part) {
         typedef __attribute__((ext_vector_type(4))) uint16_t u16x4;
         const int d = 32 * i + 8 * part + 4 * h;
-        const u16x4 v = *reinterpret_cast<const u16x4*>(v_tile + row * D + (((d >> 3) ^ tile_key<D>(row)) << 3) + (d & 7));
+        const u16x4 v = *reinterpret_cast<const u16x4*>(v_tile + key * 2 * D + (((d >> 3) ^ tile_key<D>(key)) << 4) + (d & 7) * 2);
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[i][4 * part + e] += seen ? w * __uint_as_float((uint32_t)v[e] << 16) : 0.f;
         __builtin_amdgcn_sched_barrier(0);                  // few registers at a time: this path is rare, and they are the kernel's
@@ -41,21 +43,21 @@ __device__ __forceinline__ void add_by_key(f32x16 (&o)[D / 32], const f32x16& p,
   }
 }
 
-template <int D, int NW, bool CAUSAL>
-__global__ void __launch_bounds__(NW * 64, D == 64 ? 4 : 2) attention_kernel(PromptArgs a) {
-  using S = PromptShape<D, NW>;
+template <int D, int QW, bool CAUSAL>
+__global__ void __launch_bounds__(64 * QW, D == 64 ? 3 : 2) attention_kernel(PromptArgs a) {
+  using S = PromptShape<D, QW>;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[S::kLdsBytes];
+  const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
 
   const int group = a.q_heads / a.k_heads;
-  const int l = swz_xcd_renumber((int)blockIdx.x, (int)gridDim.x, a.num_xcd);
-  const int k_head = l / (a.slots * group), rest = l - k_head * (a.slots * group), turn = rest / group;
-  const int head = k_head * group + (rest - turn * group);
-  const SlotPlace place = find_slot(a.cu_q, a.sequences, a.total_q, S::kRows, a.slots - 1 - turn);
-  const Span q = sequence_span(a.cu_q, place.sequence, a.total_q), k = sequence_span(a.cu_k, place.sequence, a.total_k);
-  const int first = place.tile * S::kRows;
-  if (place.tile < 0 || first >= q.length) return;
+  const PromptPiece piece = prompt_piece((int)blockIdx.x, a.slots * a.splits, a.k_heads, group, a.num_xcd, a.sets);
+  if (piece.turn < 0) return;
+  const int k_head = piece.k_head, head = k_head * group + piece.member, split = a.splits == 1 ? 0 : piece.turn % a.splits;
+  const TurnPlace place = find_turn(a.cu_q, a.total_q, a.cu_k, a.total_k, a.sequences, S::kRows, a.splits == 1 ? piece.turn : piece.turn / a.splits);
+  const Span q = place.mine, k = place.other;
+  const int first = ((q.length + S::kRows - 1) / S::kRows - 1 - place.tile) * S::kRows;      // a sequence's last rows look at the most keys
+  if (place.tile < 0 || first < 0) return;
 
   const int row0 = first + wave * 32, row = row0 + (lane & 31);
   const int ahead = k.length - q.length;                    // causal: query i looks at keys 0 .. i + ahead
@@ -63,99 +65,265 @@ __global__ void __launch_bounds__(NW * 64, D == 64 ? 4 : 2) attention_kernel(Pro
   const int keys = keys_of(min(first + S::kRows, q.length) - 1);              // of any row of the workgroup,
   const int wave_keys = row0 < q.length ? keys_of(min(row0 + 32, q.length) - 1) : 0, all_keys = keys_of(row0);   // any and every row of the wave
   const int last_key = keys_of(row) - 1;
-  const int tiles = (keys + kPromptKeys - 1) / kPromptKeys;
+  // with splits, this workgroup's share of the tiles: `per` of them from `before` on
+  const int every = (keys + kPromptKeys - 1) / kPromptKeys, per = a.splits == 1 ? every : (every + a.splits - 1) / a.splits, before = split * per;
+  auto my_tiles = [&](int n) { return clamp_to(n - before, 0, per); };       // of the first n
+  const int tiles = my_tiles(every), wave_tiles = my_tiles((wave_keys + kPromptKeys - 1) / kPromptKeys);
+  auto first_key = [&](int t) { return (before + t) * kPromptKeys; };
 
-  const uint16_t *k_rows = a.k.at(k.first, k_head), *v_rows = a.v.at(k.first, k_head);
-  auto fetch = [&](int t) {
-    const uint32_t at = lds + (uint32_t)((t & 1) * S::kTileBytes);
-    load_rows<D, kPromptKeys, NW>(k_rows, a.k.token, t * kPromptKeys, k.length, at, wave, lane);
-    load_rows<D, kPromptKeys, NW>(v_rows, a.v.token, t * kPromptKeys, k.length, at + 2 * S::kTileBytes, wave, lane);
-  };
+  const RowLoader<D, kPromptKeys, QW> load_k(a.k.at(k.first, k_head), a.k.token, k.length, wave, lane), load_v(a.v.at(k.first, k_head), a.v.token, k.length, wave, lane);
+  auto fetch_k = [&](int t) { load_k(first_key(t), lds + (uint32_t)((t & 1) * S::kTileBytes)); };
+  auto fetch_v = [&](int t) { load_v(first_key(t), lds + (uint32_t)((2 + (t & 1)) * S::kTileBytes)); };
+  if (tiles > 0) fetch_k(0), fetch_v(0);
+  if (tiles > 1) fetch_k(1);
+
   bf16x8 qf[D / 16];
   load_fragments<D>(qf, a.q.at(q.first + min(row, q.length - 1), head), lane);
-  f32x16 o[D / 32];
+  f32x16 o[D / 32], s[2], next[2];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) o[i] = f32x16{};
   const float c = a.scale * kLog2E;
-  float top, sum;                                           // of scores times c; this lane's half of the sum
+  float top = -FLT_MAX, sum = 0.f;                          // of scores times c; this lane's half of the sum
+
+  auto score = [&](f32x16 (&x)[2], int t) __attribute__((always_inline)) {
+    const uint32_t k_lane = row_address<D>(lds + (uint32_t)((t & 1) * S::kTileBytes), lane);
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      x[b] = f32x16{};
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) x[b] = mfma32(read_rows<D>(k_lane, b, i), qf[i], x[b]);
+    }
+  };
+  auto mask = [&](f32x16 (&x)[2], int t) __attribute__((always_inline)) {
+    if (first_key(t) + kPromptKeys <= all_keys) return;
+    const int last = last_key - first_key(t) - 4 * h;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[b][r] = 32 * b + 8 * (r / 4) + r % 4 <= last ? x[b][r] : -INFINITY;
+  };
+  auto highest = [&](const f32x16 (&x)[2]) __attribute__((always_inline)) {
+    float high = x[0][0];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) high = fmaxf(high, x[b][r]);
+    return high;
+  };
+  auto raise = [&](float high) __attribute__((always_inline)) {
+    high = across_halves(high, [](float x, float y) { return fmaxf(x, y); }) * c;
+    if (!__any(high > top + kLazyRise)) return;
+    const float now = fmaxf(top, high), less = __builtin_amdgcn_exp2f(top - now);
+    sum *= less;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) o[i] *= less;
+    top = now;
+  };
+  // A tile of scores has 32 weights a lane: 16 pairs, each two exponentials, sums and one rounding.
+  constexpr int kSteps = D / 16, kParts = D / 32, kScoreSlots = 2 * kSteps, kSlots = kScoreSlots + 4 * kParts;
+  uint32_t k_at[kSteps], v_at[kParts][2];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) keep(k_at[i] = row_address<D>(lds, lane) ^ (uint32_t)(i << 5));
+#pragma unroll
+  for (int i = 0; i < kParts; ++i) {
+    keep(v_at[i][0] = column_address<D>(lds, lane) ^ (uint32_t)(i << 6));
+    keep(v_at[i][1] = (column_address<D>(lds, lane) ^ (uint32_t)(i << 6) ^ 32u) + 16u * D);
+  }
+  // One tile: kSlots products, first the next tile's scores (MORE: there is one), then the values, weighted.  The vector unit has about as much to do as the
+  // matrix unit, so every slot gets its share of it, in a fixed order (the compiler would move all reads ahead of all products): pair n of weights by slot
+  // 7 n / 128 of all, which is before the products with its 16 keys, and in the slots of the values the next tile's maximum.
+  // PARITY: of the tile's number, -1 where it is not a constant (t says).
+  auto tile_pass = [&](f32x16 (&now)[2], f32x16 (&then)[2], int t, auto parity, auto more, auto masked) __attribute__((always_inline)) {
+    constexpr bool MORE = decltype(more)::value, MASKED = decltype(masked)::value;
+    constexpr int PARITY = decltype(parity)::value, kFirst = MORE ? 0 : kScoreSlots;
+    const uint32_t keys_at = (uint32_t)(((PARITY < 0 ? t : PARITY) & 1 ? 0 : 1) * S::kTileBytes), values_at = (uint32_t)((2 + ((PARITY < 0 ? t : PARITY) & 1)) * S::kTileBytes);
+    auto read = [&](auto slot) __attribute__((always_inline)) {
+      constexpr int i = decltype(slot)::value, v = i - kScoreSlots;
+      if constexpr (i < kScoreSlots) return read_rows_at<D>(k_at[i % kSteps], keys_at + (uint32_t)(i / kSteps * 64 * D));
+      else return read_columns_at<D>(v_at[v % kParts][0], v_at[v % kParts][1], values_at + (uint32_t)(v / kParts * 32 * D));
+    };
+    u32x4 p[4];
+    bf16x8 f[3];
+    f[kFirst % 3] = read(std::integral_constant<int, kFirst>{});
+    f[(kFirst + 1) % 3] = read(std::integral_constant<int, kFirst + 1>{});
+    if constexpr (MORE) then[0] = then[1] = f32x16{};
+    float sums[2] = {sum, 0.f}, high[2] = {-INFINITY, -INFINITY};
+    now[0][0] = __builtin_fmaf(now[0][0], c, -top);
+    now[0][1] = __builtin_fmaf(now[0][1], c, -top);
+    __builtin_amdgcn_sched_barrier(0);
+    for_each_index([&](auto slot) __attribute__((always_inline)) {
+      constexpr int i = kFirst + decltype(slot)::value, v = i - kScoreSlots;
+      if constexpr (i + 2 < kSlots) f[(i + 2) % 3] = read(std::integral_constant<int, i + 2>{});
+      if constexpr (i < kScoreSlots) then[i / kSteps] = mfma32(f[i % 3], qf[i % kSteps], then[i / kSteps]);
+      if constexpr (MORE && i >= kScoreSlots) o[v % kParts] = mfma32(f[i % 3], __builtin_bit_cast(bf16x8, p[v / kParts]), o[v % kParts]);
+      constexpr auto kPairs = [](int before) constexpr {                // pairs taken before a slot
+        if (MORE) return before >= kSlots ? 16 : before <= 0 ? 0 : (before * 128 + 7 * kSlots - 1) / (7 * kSlots) < 16 ? (before * 128 + 7 * kSlots - 1) / (7 * kSlots) : 16;
+        const int w = before - kScoreSlots;
+        return w <= 0 ? 0 : w < kParts ? 8 : w < 2 * kParts ? 12 : 16;
+      };
+#pragma unroll
+      for (int n = kPairs(i); n < kPairs(i + 1); ++n) {
+        const int b = n / 8, r = n % 8 * 2, m = n + 1;
+        if (m < 16) {
+          now[m / 8][m % 8 * 2] = __builtin_fmaf(now[m / 8][m % 8 * 2], c, -top);
+          now[m / 8][m % 8 * 2 + 1] = __builtin_fmaf(now[m / 8][m % 8 * 2 + 1], c, -top);
+        }
+        const float w0 = __builtin_amdgcn_exp2f(now[b][r]), w1 = __builtin_amdgcn_exp2f(now[b][r + 1]);
+        sums[0] += w0;
+        sums[1] += w1;
+        p[n / 4][n % 4] = pack_bf16(w0, w1);
+      }
+      if constexpr (!MORE) o[v % kParts] = mfma32(f[i % 3], __builtin_bit_cast(bf16x8, p[v / kParts]), o[v % kParts]);
+      if constexpr (MASKED && i == kScoreSlots - 1) mask(then, t + 1);
+      if constexpr (MORE && i >= kScoreSlots) {
+#pragma unroll
+        for (int e = v * 32 / (4 * kParts); e < (v + 1) * 32 / (4 * kParts); e += 2)
+          high[e / 2 % 2] = fmaxf(high[e / 2 % 2], fmaxf(then[e / 16][e % 16], then[e / 16][e % 16 + 1]));
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }, std::make_integer_sequence<int, kSlots - kFirst>{});
+    sum = sums[0] + sums[1];
+    return fmaxf(high[0], high[1]);
+  };
+  constexpr std::integral_constant<int, 0> kEven{};
+  constexpr std::integral_constant<int, 1> kOdd{};
+  constexpr std::integral_constant<int, -1> kEither{};
+
+  // The scores of the first tile; then, tile by tile, this one's weights and values beside the scores of the next.  Two sets of scores take turns.
+  auto turn = [&](int t) __attribute__((always_inline)) {
+    publish();
+    if (t + 2 < tiles) fetch_k(t + 2);
+    if (t + 1 < tiles) fetch_v(t + 1);
+  };
+  publish();
+  if (wave_tiles > 0) {
+    score(s, 0);
+    mask(s, 0);
+    raise(highest(s));
+  }
+  const int whole = min(my_tiles(all_keys / kPromptKeys), wave_tiles);          // tiles without a mask
+  int t = 0;
+  for (; t + 2 < whole; t += 2) {
+    turn(t);
+    raise(tile_pass(s, next, t, kEven, std::true_type{}, std::false_type{}));
+    turn(t + 1);
+    raise(tile_pass(next, s, t + 1, kOdd, std::true_type{}, std::false_type{}));
+  }
+  for (; t + 1 < wave_tiles; ++t) {
+    turn(t);
+    raise(tile_pass(s, next, t, kEither, std::true_type{}, std::true_type{}));
+    s[0] = next[0];
+    s[1] = next[1];
+  }
+  if (t < wave_tiles) {
+    turn(t);
+    tile_pass(s, next, t, kEither, std::false_type{}, std::false_type{});
+    ++t;
+  }
+  for (; t < tiles; ++t) turn(t);
 
   // A weight of 0 times an infinity or NaN is NaN: where a value that only some rows of a tile look at is no finite number, the products carry it into the others.
   // The result shows it, and the tiles are then taken a second time, the masked ones key by key.
-  auto all_tiles = [&](auto careful) __attribute__((always_inline)) {
-    if (tiles > 0) fetch(0);
-    top = -FLT_MAX;
-    sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) o[i] = f32x16{};
-    for (int t = 0; t < tiles; ++t) {
-      publish();
-      if (t + 1 < tiles) fetch(t + 1);
-      const int k0 = t * kPromptKeys;
-      if (k0 >= wave_keys) continue;
-      const uint32_t at = lds + (uint32_t)((t & 1) * S::kTileBytes);
-      const uint32_t k_lane = row_address<D>(at, lane), v_lane = column_address<D>(at + 2 * S::kTileBytes, lane);
-      f32x16 s[2];
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        s[b] = f32x16{};
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) s[b] = mfma32(read_rows<D>(k_lane, b, i), qf[i], s[b]);
-      }
-      const bool masked = k0 + kPromptKeys > all_keys;
-      if (masked) {
-        const int last = last_key - k0 - 4 * h;
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[b][r] = 32 * b + 8 * (r / 4) + r % 4 <= last ? s[b][r] : -INFINITY;
-      }
-      float high = s[0][0];
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) high = fmaxf(high, s[b][r]);
-      high = across_halves(high, [](float x, float y) { return fmaxf(x, y); }) * c;
-      if (__any(high > top + kLazyRise)) {
-        const float now = fmaxf(top, high), less = __builtin_amdgcn_exp2f(top - now);
-        sum *= less;
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) o[i] *= less;
-        top = now;
-      }
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], c, -top));
-#pragma unroll
-        for (int r = 0; r < 16; ++r) sum += s[b][r];
-      }
-      if (decltype(careful)::value && masked) {
-        const uint16_t* v_tile = reinterpret_cast<const uint16_t*>(smem + (t & 1) * S::kTileBytes + 2 * S::kTileBytes);
-        add_by_key<D>(o, s[0], v_tile, 0, last_key - k0, lane);
-        add_by_key<D>(o, s[1], v_tile, 32, last_key - k0, lane);
-        continue;
-      }
-      bf16x8 p[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) p[j] = as_operand(s[j / 2], j % 2);
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) o[i] = mfma32(read_columns<D>(v_lane, j, i), p[j], o[i]);
-    }
-  };
-  all_tiles(std::false_type{});
   if constexpr (CAUSAL) {
     float odd = 0.f;
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i)
+    for (int i = 0; i < kParts; ++i)
 #pragma unroll
       for (int r = 0; r < 16; ++r) odd = __builtin_fmaf(o[i][r], 0.f, odd);
-    if (__builtin_expect(__syncthreads_or(odd != 0.f), 0)) all_tiles(std::true_type{});
+    const bool mine = __any(odd != 0.f);
+    publish();
+    uint32_t* flags = reinterpret_cast<uint32_t*>(smem);
+    if (lane == 0) flags[wave] = mine;
+    publish();
+    uint32_t again = 0;
+#pragma unroll
+    for (int i = 0; i < QW; ++i) again |= flags[i];
+    publish();
+    if (__builtin_expect(__builtin_amdgcn_readfirstlane((int)again) != 0, 0)) {
+      if (tiles > 0) fetch_k(0), fetch_v(0);
+      top = -FLT_MAX;
+      sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) o[i] = f32x16{};
+      for (t = 0; t < tiles; ++t) {
+        publish();
+        if (t + 1 < tiles) fetch_k(t + 1), fetch_v(t + 1);
+        if (t >= wave_tiles) continue;
+        score(s, t);
+        mask(s, t);
+        raise(highest(s));
+        u32x4 p[4];
+#pragma unroll
+        for (int n = 0; n < 16; ++n) {
+          const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n / 8][n % 8 * 2], c, -top)), w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n / 8][n % 8 * 2 + 1], c, -top));
+          sum += w0 + w1;
+          p[n / 4][n % 4] = pack_bf16(w0, w1);
+        }
+        if (t >= whole) {
+          add_by_key<D>(o, p, smem + (2 + (t & 1)) * S::kTileBytes, last_key - first_key(t), lane);
+        } else {
+          const uint32_t v_lane = column_address<D>(lds + (uint32_t)((2 + (t & 1)) * S::kTileBytes), lane);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < kParts; ++i) o[i] = mfma32(read_columns<D>(v_lane, j, i), __builtin_bit_cast(bf16x8, p[j]), o[i]);
+        }
+      }
+    }
   }
 
   sum = across_halves(sum, [](float x, float y) { return x + y; });
   const bool real = row < q.length;
+  if (a.splits > 1) {
+    if (!real) return;
+    const int64_t at = ((int64_t)split * a.total_q + q.first + row) * a.q_heads + head;
+    if (h == 0) *reinterpret_cast<float2*>(a.part_stats + 2 * at) = float2{top, sum};
+    if (tiles == 0) return;
+#pragma unroll
+    for (int i = 0; i < kParts; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) *reinterpret_cast<f32x4*>(a.part_sums + at * D + 32 * i + 2 * r + 4 * h) = f32x4{o[i][r], o[i][r + 1], o[i][r + 2], o[i][r + 3]};
+    return;
+  }
   store_columns<D>(o, sum == 0.f ? 0.f : 1.f / sum, a.out.at(q.first + min(row, q.length - 1), head), real, lane);
   if (real && h == 0) a.lse[(int64_t)head * a.total_q + q.first + row] = sum == 0.f ? -INFINITY : __builtin_fmaf(top, kLn2, __logf(sum));
+}
+
+// What the splits of a row (at most 64) have, joined: a wave for each row of a head, D / 64 dimensions a lane.
+constexpr int kJoinRows = 4;
+template <int D>
+__global__ void __launch_bounds__(64 * kJoinRows) attention_join_kernel(PromptArgs a) {
+  constexpr int kPer = D / 64;
+  typedef __attribute__((ext_vector_type(kPer))) float vec;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const PromptPiece piece = prompt_piece((int)blockIdx.x, a.slots, a.q_heads, 1, a.num_xcd, a.sets);
+  if (piece.turn < 0) return;
+  const int head = piece.k_head;
+  const TurnPlace place = find_turn(a.cu_q, a.total_q, a.cu_k, a.total_k, a.sequences, kJoinRows, piece.turn);
+  const int row = place.tile * kJoinRows + wave;
+  if (place.tile < 0 || row >= place.mine.length) return;
+  const int64_t token = place.mine.first + row, step = (int64_t)a.total_q * a.q_heads, at = token * a.q_heads + head;
+  float my_top = -FLT_MAX, my_sum = 0.f;                    // of split `lane`
+  if (lane < a.splits) {
+    const float2 x = *reinterpret_cast<const float2*>(a.part_stats + 2 * (at + lane * step));
+    my_top = x.x;
+    my_sum = x.y;
+  }
+  const float top = over_wave(my_top, [](float x, float y) { return fmaxf(x, y); });
+  // a split without keys has a sum of 0 and has written nothing else
+  const float weight = __builtin_amdgcn_exp2f(my_top - top), sum = over_wave(my_sum * weight, [](float x, float y) { return x + y; });
+  vec o = 0.f;
+#pragma unroll 4
+  for (int s = 0; s < a.splits; ++s) {
+    const float w = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(weight), s));
+    if (__uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(my_sum), s)) != 0.f)
+      o += *reinterpret_cast<const vec*>(a.part_sums + (at + s * step) * D + lane * kPer) * w;
+  }
+  const float f = sum == 0.f ? 0.f : 1.f / sum;
+  uint16_t* to = a.out.at(token, head) + lane * kPer;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) to[i] = __builtin_bit_cast(uint16_t, (__bf16)(o[i] * f));
+  if (lane == 0) a.lse[(int64_t)head * a.total_q + token] = sum == 0.f ? -INFINITY : __builtin_fmaf(top, kLn2, __logf(sum));
 }
 
 }  // namespace swz

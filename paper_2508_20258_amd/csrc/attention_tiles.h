@@ -16,6 +16,7 @@
 #include <stdint.h>
 
 #include "gemm_kernel.h"
+#include "prompt_order.h"
 
 namespace swz {
 
@@ -37,8 +38,10 @@ struct PromptArgs {
   Heads q, k, v, out;
   float* lse;
   const int32_t *cu_q, *cu_k;
-  int total_q, total_k, sequences, slots, q_heads, k_heads, num_xcd;
+  int total_q, total_k, sequences, slots, q_heads, k_heads, num_xcd, sets;
   float scale;
+  int splits;                        // of a row's keys, in the forward pass: each writes what it has (splits x total_q x q_heads x head_dim, and maximum and sum)
+  float *part_sums, *part_stats;
 };
 
 __device__ __forceinline__ int clamp_to(int x, int lo, int hi) { return x < lo ? lo : (x > hi ? hi : x); }
@@ -69,10 +72,54 @@ __device__ __forceinline__ SlotPlace find_slot(const int32_t* cu, int sequences,
 struct Span {
   int first, length;
 };
+__device__ __forceinline__ Span span_of(int from, int to, int total) {
+  const int a = clamp_to(from, 0, total);
+  return {a, clamp_to(to, a, total) - a};
+}
 __device__ __forceinline__ Span sequence_span(const int32_t* cu, int sequence, int total) {
-  const int a = clamp_to(__builtin_amdgcn_readfirstlane(cu[sequence]), 0, total);
-  const int b = clamp_to(__builtin_amdgcn_readfirstlane(cu[sequence + 1]), a, total);
-  return {a, b - a};
+  return span_of(__builtin_amdgcn_readfirstlane(cu[sequence]), __builtin_amdgcn_readfirstlane(cu[sequence + 1]), total);
+}
+
+// Sum of x over this lane and those before it.
+__device__ __forceinline__ int sum_before(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);       // row_shr:1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);       // row_bcast:15, to rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);       // row_bcast:31, to rows 2 and 3
+  return x;
+}
+
+// The turn-th tile of `rows` tokens of all sequences: which of its sequence's (-1: there is none), and the sequence's tokens on this side and the other.  Up to 64 sequences have a
+// lane each.  Up to 16 take turns by the length of the other side, the longest first, as each is compared with all (30 clocks a sequence); more of them even out as they come.
+struct TurnPlace {
+  Span mine, other;
+  int tile;
+};
+__device__ __forceinline__ TurnPlace find_turn(const int32_t* cu, int total, const int32_t* other, int other_total, int sequences, int rows, int turn) {
+  const int lane = threadIdx.x & 63;
+  if (sequences > 64) {
+    const SlotPlace p = find_slot(cu, sequences, total, rows, turn);
+    return {sequence_span(cu, p.sequence, total), sequence_span(other, p.sequence, other_total), p.tile};
+  }
+  const int at = min(lane, sequences - 1);
+  const Span a = span_of(cu[at], cu[at + 1], total), b = span_of(other[at], other[at + 1], other_total);
+  const int tiles = lane < sequences ? (a.length + rows - 1) / rows : 0;
+  int start = 0;
+  if (sequences <= 16) {
+    for (int j = 0; j < sequences; ++j) {
+      const int longer = __builtin_amdgcn_readlane(b.length, j), n = __builtin_amdgcn_readlane(tiles, j);
+      start += longer > b.length || (longer == b.length && j < lane) ? n : 0;
+    }
+  } else {
+    start = sum_before(tiles) - tiles;
+  }
+  const uint64_t found = __ballot(turn >= start && turn < start + tiles);
+  if (found == 0) return {{0, 0}, {0, 0}, -1};
+  const int s = __ffsll((unsigned long long)found) - 1;
+  return {{__builtin_amdgcn_readlane(a.first, s), __builtin_amdgcn_readlane(a.length, s)}, {__builtin_amdgcn_readlane(b.first, s), __builtin_amdgcn_readlane(b.length, s)},
+          turn - __builtin_amdgcn_readlane(start, s)};
 }
 
 template <int D>
@@ -81,18 +128,37 @@ __device__ __forceinline__ int tile_key(int row) {
   else return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
 }
 
-// ROWS rows of a head, from `first` on, into LDS by all NW waves: 1024 bytes an instruction.  Rows at or past `length` come as zeros.
+// ROWS rows of a head into LDS by NW waves, 1024 bytes an instruction.  Rows past the end are copies of the last one, which what uses them masks.  An instruction's rows
+// are named by a wave-uniform base and 32-bit offsets, so the distance between tokens is less than 2^28 elements (7 rows of it fit 2^32 bytes).
 template <int D, int ROWS, int NW>
-__device__ __forceinline__ void load_rows(const uint16_t* head, int64_t token, int first, int length, uint32_t lds, int wave, int lane) {
-  constexpr int kChunks = D / 8, kRows = 64 / kChunks, kLoads = ROWS / kRows / NW;
+struct RowLoader {
+  static constexpr int kChunks = D / 8, kRows = 64 / kChunks, kLoads = ROWS / kRows / NW;
   static_assert(kLoads * kRows * NW == ROWS, "whole instructions for every wave");
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    const int row = (wave * kLoads + i) * kRows + lane / kChunks, chunk = (lane % kChunks) ^ tile_key<D>(row), r = first + row;
-    const void* from = r < length ? static_cast<const void*>(head + (int64_t)r * token + chunk * 8) : static_cast<const void*>(&kZeroChunk);
-    load_to_lds(from, lds + (uint32_t)((wave * kLoads + i) * 1024));
+  const uint16_t* head;
+  int64_t token;
+  int length, wave, lane;
+  uint32_t whole[kLoads];            // offsets where all rows are there
+
+  __device__ __forceinline__ uint32_t offset(int i, int most) const {          // most: the last row of the instruction that is there
+    const int r = lane / kChunks, row = (wave * kLoads + i) * kRows + r;
+    return (uint32_t)min(r, most) * (uint32_t)(token * 2) + (uint32_t)(((lane % kChunks) ^ tile_key<D>(row)) << 4);
   }
-}
+  __device__ __forceinline__ RowLoader(const uint16_t* head_, int64_t token_, int length_, int wave_, int lane_) : head(head_), token(token_), length(length_), wave(wave_), lane(lane_) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) whole[i] = offset(i, kRows);
+  }
+  // first: of the tile, less than length
+  __device__ __forceinline__ void operator()(int first, uint32_t lds) const {
+    const bool all = first + ROWS <= length;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = (wave * kLoads + i) * kRows, from = min(first + at, length - 1);
+      const uint64_t at_row = reinterpret_cast<uint64_t>(head + (int64_t)from * token);
+      const uint64_t base = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at_row >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)at_row);
+      load_to_lds_base_off(reinterpret_cast<const void*>(base), all ? whole[i] : offset(i, length - 1 - from), lds + (uint32_t)((wave * kLoads + i) * 1024));
+    }
+  }
+};
 
 // This wave's loads have landed and its reads are done; then so are all waves'.
 __device__ __forceinline__ void publish() {
@@ -131,6 +197,22 @@ __device__ __forceinline__ bf16x8 read_columns(uint32_t lane_column, int j, int 
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
+// The same with the lane's part of the address, a register, apart from the offset that is an instruction's constant.
+template <int D>
+__device__ __forceinline__ bf16x8 read_rows_at(uint32_t lane_step, uint32_t offset) {
+  typedef __attribute__((address_space(3))) const bf16x8* ptr;
+  return *(ptr)(uintptr_t)(lane_step + offset);
+}
+template <int D>
+__device__ __forceinline__ bf16x8 read_columns_at(uint32_t lane_part, uint32_t lane_part_8, uint32_t offset) {
+  typedef __attribute__((address_space(3))) s16x4* ptr;
+  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr)(uintptr_t)(lane_part + offset));
+  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr)(uintptr_t)(lane_part_8 + offset));
+  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+// Keeps the compiler from working a value out again where it is used.
+__device__ __forceinline__ void keep(uint32_t& x) { asm volatile("" : "+v"(x)); }
+
 // A head's row as B (columns are rows of the tensor), dimensions 16 step + 8 h .. + 7 for all steps.
 template <int D>
 __device__ __forceinline__ void load_fragments(bf16x8 (&f)[D / 16], const uint16_t* row, int lane) {
@@ -158,6 +240,20 @@ template <class Op>
 __device__ __forceinline__ float across_halves(float x, Op op) {
   const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return op(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+
+// x of all lanes.
+template <class Op>
+__device__ __forceinline__ float over_wave(float x, Op op) {
+  auto dpp = [](float v, auto ctrl) __attribute__((always_inline)) {
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, false));
+  };
+  x = op(x, dpp(x, std::integral_constant<int, 0xB1>{}));        // quad_perm [1,0,3,2]
+  x = op(x, dpp(x, std::integral_constant<int, 0x4E>{}));        // quad_perm [2,3,0,1]
+  x = op(x, dpp(x, std::integral_constant<int, 0x141>{}));       // row_half_mirror
+  x = op(x, dpp(x, std::integral_constant<int, 0x140>{}));       // row_mirror
+  const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return across_halves(op(__uint_as_float(s[0]), __uint_as_float(s[1])), op);
 }
 
 // Column i of D / 32 products (dimensions 32 part + row) times `factor`, rounded and stored as a head's row: the halves trade registers so that each lane has 16 bytes.

@@ -138,10 +138,18 @@ def test_norm_backward_refusals():
     (dict(head_dim=32), UNSUPPORTED), (dict(cu_k=P + 2), UNSUPPORTED), (dict(total_k=1 << 31), OVERFLOW), (dict(total_q=(1 << 31) - 1, q_heads=1024, k_heads=1024), OVERFLOW)])
 def test_attention_refusals(change, status):
     a, h = prompt_args(**change), ctypes.byref(heads())
-    assert layer.lib.swz_attention(ctypes.byref(a), None) == status
+    assert layer.lib.swz_attention(ctypes.byref(a), P, 1 << 60, None) == status
     assert layer.lib.swz_attention_backward(ctypes.byref(a), h, h, h, h, P, 1 << 60, None) == status
     if status != OVERFLOW:
-        assert layer.lib.swz_attention_backward_workspace(ctypes.byref(a)) == status
+        assert layer.lib.swz_attention_backward_workspace(ctypes.byref(a)) == layer.lib.swz_attention_workspace(ctypes.byref(a)) == status
+
+
+def test_attention_workspace_refusals():
+    many = ctypes.byref(prompt_args(total_k=100000))         # few queries, many keys: cut among workgroups
+    need = layer.lib.swz_attention_workspace(many)
+    assert need > 0 and layer.lib.swz_attention_workspace(ctypes.byref(prompt_args())) == 0
+    assert layer.lib.swz_attention(many, None, need, None) == layer.lib.swz_attention(many, P, need - 1, None) == INVALID
+    assert layer.lib.swz_attention(many, P + 8, need, None) == UNSUPPORTED
 
 
 def test_attention_backward_refusals():
@@ -154,7 +162,7 @@ def test_attention_backward_refusals():
     assert layer.lib.swz_attention_backward(a, r(h), r(h), None, r(h), P, need, None) == INVALID
     assert layer.lib.swz_attention_backward(a, r(h), r(h), r(heads(head=1)), r(h), P, need, None) == UNSUPPORTED
     assert layer.lib.swz_attention_backward(a, r(h), r(h), r(h), r(h), P + 4, need, None) == UNSUPPORTED
-    assert layer.lib.swz_attention(ctypes.byref(prompt_args(total_q=0)), None) == 0
+    assert layer.lib.swz_attention(ctypes.byref(prompt_args(total_q=0)), None, 0, None) == 0
 
 
 @pytest.mark.parametrize("change,status", [(dict(k_words=None), INVALID), (dict(v_scales=None), INVALID), (dict(pages=0), INVALID), (dict(k_heads=0), INVALID),

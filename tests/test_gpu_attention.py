@@ -75,6 +75,7 @@ PROMPTS = [
     ([1], None, 1, 1), ([2], None, 3, 1), ([31], None, 2, 2), ([32], None, 1, 1), ([33], None, 4, 2), ([63, 64, 65], None, 2, 1), ([127], None, 1, 1), ([129], None, 2, 1),
     ([257], None, 1, 1), ([300, 0, 1, 70], None, 8, 2), ([0, 5], None, 1, 1),
     ([5], [200], 2, 1), ([64], [65], 1, 1), ([130], [300], 2, 2), ([1], [129], 4, 1),                     # the next piece of a prompt
+    ([3], [2100], 2, 1), ([70, 1, 0], [1500, 1600, 900], 2, 2),                                         # few queries and many keys: cut among workgroups
     ([40], [7], 2, 1), ([200, 3], [70, 0], 1, 1), ([70], [1], 3, 1),                                     # rows that look at nothing
 ]
 
@@ -155,6 +156,14 @@ def test_what_is_not_looked_at_does_not_matter(swz, dim, bad):
     long = torch.full((300, 2, dim), bad, dtype=torch.bfloat16, device="cuda")
     lk, lv = long.clone(), long.clone()
     lk[:177], lv[:177] = k, v
+    # few queries and many keys, cut among workgroups
+    q3, k3, v3 = randn(17, 40, 2, dim), randn(18, 1500, 2, dim), randn(19, 1500, 2, dim)
+    cq, ck = cu_of([40]), cu_of([1500])
+    first = swz.attention(q3, k3, v3, cq, ck)[0]
+    v3[1480, 1] = bad
+    got = swz.attention(q3, k3, v3, cq, ck)[0]
+    assert torch.equal(got[:, 0], first[:, 0]) and torch.isfinite(got[:20, 1]).all() and not torch.isfinite(got[20:, 1]).any()
+    assert (got[:20, 1].float() - first[:20, 1].float()).abs().max() <= 2 ** -6
     for causal in (True, False):
         a, b = swz.attention(q, lk, lv, cu, causal=causal), swz.attention(q, k, v, cu, causal=causal)
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
