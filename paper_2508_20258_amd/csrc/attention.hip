@@ -144,7 +144,7 @@ ForwardPlan forward_plan(const swz_attention_args& a) {
   const int xcd = xcds();
   const int64_t few = swz::prompt_workgroups(slots_of(a.total_q, 1, 128), a.k_heads, (int)group, xcd);       // workgroups of 128 rows, if the sequences were one
   ForwardPlan p{4, 1};
-  if (a.head_dim == 128 && few >= 8 * cus) p.waves = 8;
+  if (a.head_dim == 128 && few >= 16 * cus) p.waves = 8;
   const int64_t tiles = a.total_k / a.sequences / swz::kPromptKeys;                                      // of an average sequence
   if (few < cus && tiles >= 16) {
     int64_t splits = 2 * cus / few;
@@ -155,7 +155,13 @@ ForwardPlan forward_plan(const swz_attention_args& a) {
 }
 int64_t forward_floats(const swz_attention_args& a, const ForwardPlan& p) { return p.splits == 1 ? 0 : (int64_t)p.splits * a.total_q * a.q_heads * (a.head_dim + 2); }
 
-constexpr int kDqWaves = 4, kDkvWaves = 4;
+constexpr int kDqWaves = 4;
+
+template <int D>
+struct DkvShape {
+  static constexpr int kKeyWaves = D == 128 ? 4 : 2, kBlocks = 1, kParts = 2;
+  static constexpr int kKeys = 32 * kKeyWaves * kBlocks, kThreads = 64 * kKeyWaves * kParts;
+};
 
 // ---------------------------------------------------------------- the cache
 
@@ -315,7 +321,7 @@ int swz_attention(const swz_attention_args* args, void* workspace, int64_t works
 int64_t swz_attention_backward_workspace(const swz_attention_args* args) {
   const int st = check_prompt(args);
   if (st != SWZ_OK) return st;
-  return args->total_q * args->q_heads * 4;
+  return 2 * args->total_q * args->q_heads * 4;
 }
 
 int swz_attention_backward(const swz_attention_args* args, const swz_heads* dout, const swz_heads* dq, const swz_heads* dk, const swz_heads* dv,
@@ -330,18 +336,20 @@ int swz_attention_backward(const swz_attention_args* args, const swz_heads* dout
   swz::PromptBackArgs p{};
   p.f = prompt_args(*args);
   p.dout = device_heads(*dout), p.dq = device_heads(*dq), p.dk = device_heads(*dk), p.dv = device_heads(*dv);
-  p.delta = static_cast<float*>(workspace);
+  p.log_sums = static_cast<float*>(workspace);
+  p.deltas = p.log_sums + args->total_q * args->q_heads;
   return for_head_dim(args->head_dim, [&](auto dim) {
     return for_flag(args->causal != 0, [&](auto causal) {
       constexpr int D = decltype(dim)::value;
       constexpr bool kCausal = decltype(causal)::value;
-      const int64_t q_slots = slots_of(args->total_q, args->sequences, 32 * kDqWaves), k_slots = slots_of(args->total_k, args->sequences, 32 * kDkvWaves);
+      using K = DkvShape<D>;
+      const int64_t q_slots = slots_of(args->total_q, args->sequences, 32 * kDqWaves), k_slots = slots_of(args->total_k, args->sequences, K::kKeys);
       const int group = args->q_heads / args->k_heads;
-      if (too_many_threads(q_slots, args->k_heads, group, p.f.num_xcd, 64 * kDqWaves) || too_many_threads(k_slots, args->k_heads, 1, p.f.num_xcd, 64 * kDkvWaves)) return (int)SWZ_ERR_OVERFLOW;
+      if (too_many_threads(q_slots, args->k_heads, group, p.f.num_xcd, 64 * kDqWaves) || too_many_threads(k_slots, args->k_heads, 1, p.f.num_xcd, K::kThreads)) return (int)SWZ_ERR_OVERFLOW;
       int status = SWZ_OK;
       if (args->total_q > 0) status = launch_prompt<swz::attention_dq_kernel<D, kDqWaves, kCausal>>(p, p.f, q_slots, 1, group, 64 * kDqWaves, stream);
       if (status != SWZ_OK || args->total_k == 0) return status;
-      return launch_prompt<swz::attention_dkv_kernel<D, kDkvWaves, kCausal>>(p, p.f, k_slots, 1, 1, 64 * kDkvWaves, stream);
+      return launch_prompt<swz::attention_dkv_kernel<D, K::kKeyWaves, K::kBlocks, K::kParts, kCausal>>(p, p.f, k_slots, 1, 1, K::kThreads, stream);
     });
   });
 }

@@ -8,7 +8,7 @@ namespace swz {
 struct PromptBackArgs {
   PromptArgs f;                    // slots: of this launch
   Heads dout, dq, dk, dv;
-  float* delta;                    // q_heads x total_q: sum over the dimensions of dout * out
+  float *log_sums, *deltas;        // q_heads x total_q each: -lse / scale, and -(sum over the dimensions of dout * out)
 };
 
 // dq, and delta for the other kernel.  As the forward kernel, with a third product: dq^T += k^T dS^T.
@@ -57,8 +57,11 @@ __global__ void __launch_bounds__(NW * 64, 2) attention_dq_kernel(PromptBackArgs
     for (int e = 0; e < 8; ++e) delta = __builtin_fmaf((float)gf[i][e], (float)qf[i][e], delta);
   delta = across_halves(delta, [](float x, float y) { return x + y; });
   const int64_t stat = (int64_t)head * a.total_q + token;
-  if (real && h == 0) args.delta[stat] = delta;
   const float lse = a.lse[stat] * kLog2E;                   // -inf where a row looks at nothing: all of it is masked below
+  if (real && h == 0) {
+    args.log_sums[stat] = lse == -INFINITY ? -INFINITY : -lse / (a.scale * kLog2E);
+    args.deltas[stat] = -delta;
+  }
   load_fragments<D>(qf, a.q.at(token, head), lane);
   f32x16 acc[D / 32];
 #pragma unroll
@@ -98,107 +101,227 @@ __global__ void __launch_bounds__(NW * 64, 2) attention_dq_kernel(PromptBackArgs
   store_columns<D>(acc, a.scale, args.dq.at(token, head), real, lane);
 }
 
-// dk and dv of 32 NW keys of a key head, summed over the queries of all its query heads.  A wave has 32 keys, as columns: their rows of k
-// and v are B of S = q k^T and dP = dout v^T, whose rows are queries, so that P and dS are B of dv^T += dout^T P and dk^T += q^T dS.
+// dk and dv of 32 KW keys of a key head, summed over the queries of all its query heads.  A wave has 32 keys, as columns: with them as B, S = q k^T and dP = dout v^T have
+// queries as rows, so that P and dS are B of dv^T += dout^T P and dk^T += q^T dS.  QP groups of KW waves take tiles of 32 queries in turn and add up what they have
+// at the end: more waves for a key tile than one group of them would give, so that a tile that many queries look at is done sooner, and no atomics.
+// The products start from the rows' -lse / scale and -delta, so that P = exp2(c S) and dS = P dP as they come.
 constexpr int kBackRows = 32;      // queries of a tile
+__device__ const float kMinusInfinity = -INFINITY;
 
-template <int D, int NW, bool CAUSAL>
-__global__ void __launch_bounds__(NW * 64, 2) attention_dkv_kernel(PromptBackArgs args) {
+template <int D, int KW, int KB, int QP>
+struct BackShape {
+  static constexpr int kKeys = 32 * KW * KB, kThreads = 64 * KW * QP;
+  static constexpr int kTileBytes = kBackRows * 2 * D;       // of q, or of dout
+  static constexpr int kGroupBytes = 4 * kTileBytes;         // q and dout of one tile, then of the next
+  static constexpr int kKeyBytes = kKeys * 2 * D, kKeysAt = QP * kGroupBytes, kStatsAt = kKeysAt + 2 * kKeyBytes;      // keys, values, statistics
+  static constexpr int kLdsBytes = kStatsAt + QP * 2 * 2 * kBackRows * 4;
+  static constexpr int kAccBytes = KB * (D / 32) * 4096;     // of a wave: dk or dv
+  static_assert(kLdsBytes <= 160 * 1024 && (QP == 1 || QP / 2 * KW * kAccBytes <= kLdsBytes), "LDS");
+};
+
+template <int D, int KW, int KB, int QP, bool CAUSAL>
+__global__ void __launch_bounds__(64 * KW * QP, D == 64 ? (KB == 2 ? 2 : 3) : (KB == 2 ? 1 : 2)) attention_dkv_kernel(PromptBackArgs args) {
   const PromptArgs& a = args.f;
-  constexpr int kKeys = 32 * NW, kTileBytes = kBackRows * 2 * D;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * kTileBytes];
-  __shared__ __attribute__((aligned(16))) float stats[2][2][kBackRows];
+  using S = BackShape<D, KW, KB, QP>;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[S::kLdsBytes];
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
+  const int lane = threadIdx.x & 63, h = lane >> 5, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int wave = w % KW, part = QP == 1 ? 0 : w / KW;
 
   const int group = a.q_heads / a.k_heads;
   const PromptPiece piece = prompt_piece((int)blockIdx.x, a.slots, a.k_heads, 1, a.num_xcd, a.sets);
   if (piece.turn < 0) return;
   const int k_head = piece.k_head;
-  const TurnPlace place = find_turn(a.cu_k, a.total_k, a.cu_q, a.total_q, a.sequences, kKeys, piece.turn);
+  const TurnPlace place = find_turn(a.cu_k, a.total_k, a.cu_q, a.total_q, a.sequences, S::kKeys, piece.turn);
   const Span q = place.other, k = place.mine;
-  const int first = place.tile * kKeys;
+  const int first = place.tile * S::kKeys;
   if (place.tile < 0 || first >= k.length) return;
 
-  const int key0 = first + wave * 32, key = key0 + (lane & 31);
+  const int key0 = first + wave * 32 * KB, key = key0 + (lane & 31);       // and with KB = 2 the key 32 behind it
   const int ahead = k.length - q.length;
   const int from = CAUSAL ? clamp_to(first - ahead, 0, q.length) / kBackRows : 0;      // the first tile of queries that looks at a key of the workgroup
-  const int tiles = (q.length + kBackRows - 1) / kBackRows - from, steps = tiles > 0 ? tiles * group : 0;
+  const int tiles = (q.length + kBackRows - 1) / kBackRows - from, steps = tiles > 0 ? tiles * group : 0, rounds = (steps + QP - 1) / QP;
 
-  const int64_t token = k.first + min(key, k.length - 1);
-  bf16x8 kf[D / 16], vf[D / 16];
-  load_fragments<D>(kf, a.k.at(token, k_head), lane);
-  load_fragments<D>(vf, a.v.at(token, k_head), lane);
-  f32x16 dk[D / 32], dv[D / 32];
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i) dk[i] = dv[i] = f32x16{};
-  const float c = a.scale * kLog2E;
+  const RowLoader<D, S::kKeys, KW * QP> load_k(a.k.at(k.first, k_head), a.k.token, k.length, w, lane), load_v(a.v.at(k.first, k_head), a.v.token, k.length, w, lane);
+  if (rounds > 0) load_k(first, lds + S::kKeysAt), load_v(first, lds + S::kKeysAt + S::kKeyBytes);
 
-  RowLoader<D, kBackRows, NW> load_q(a.q.data, a.q.token, q.length, wave, lane), load_g(args.dout.data, args.dout.token, q.length, wave, lane);
-  float stat = 0.f;                                         // thread i < 32: lse of row i, in units of log2; i < 64: delta of row i - 32
-  auto fetch = [&](int n) {
-    const int m = n / tiles, r0 = (from + n - m * tiles) * kBackRows, head = k_head * group + m;
-    const uint32_t at = lds + (uint32_t)((n & 1) * kTileBytes);
+  // this group's steps: query head k_head * group + member, tile `tile` of it, QP further each round
+  RowLoader<D, kBackRows, KW> load_q(a.q.data, a.q.token, q.length, wave, lane), load_g(args.dout.data, args.dout.token, q.length, wave, lane);
+  const uint32_t tile_lds = lds + (uint32_t)(part * S::kGroupBytes), stats_lds = lds + (uint32_t)(S::kStatsAt + part * 4 * kBackRows * 4);
+  int member = tiles > 0 ? part / tiles : 0, tile = part - member * tiles;
+  auto advance = [&]() {
+    tile += QP;
+    while (tile >= tiles) tile -= tiles, ++member;
+  };
+  auto fetch = [&](int round) __attribute__((always_inline)) {         // of (member, tile), the round's
+    if (member >= group) return;
+    const int head = k_head * group + member, r0 = (from + tile) * kBackRows;
+    const uint32_t at = tile_lds + (uint32_t)((round & 1) * 2 * S::kTileBytes);
     load_q.head = a.q.at(q.first, head);
     load_g.head = args.dout.at(q.first, head);
     load_q(r0, at);
-    load_g(r0, at + 2 * kTileBytes);
-    if (threadIdx.x < 64) {
+    load_g(r0, at + S::kTileBytes);
+    if (wave == 0) {
       const int r = r0 + (lane & 31);
-      const float* from_stat = lane < 32 ? a.lse : args.delta;
-      stat = r < q.length ? from_stat[(int64_t)head * a.total_q + q.first + r] : 0.f;
-      // rows past the end, and rows that look at nothing, get weights of 0
-      if (lane < 32) stat = r < q.length && stat != -INFINITY ? stat * kLog2E : INFINITY;
+      const float* stat = (lane < 32 ? args.log_sums : args.deltas) + (int64_t)head * a.total_q + q.first + r;
+      load_word_to_lds(r < q.length ? stat : lane < 32 ? &kMinusInfinity : reinterpret_cast<const float*>(&kZeroChunk), stats_lds + (uint32_t)((round & 1) * 2 * kBackRows * 4));
     }
   };
-  if (steps > 0) fetch(0);
-  for (int n = 0; n < steps; ++n) {
-    if (threadIdx.x < 64) stats[n & 1][lane >> 5][lane & 31] = stat;
-    publish();
-    if (n + 1 < steps) fetch(n + 1);
-    const int m = n / tiles, r0 = (from + n - m * tiles) * kBackRows;
-    if (CAUSAL && r0 + kBackRows - 1 + ahead < key0) continue;               // none of these rows looks at a key of this wave
-    const uint32_t at = lds + (uint32_t)((n & 1) * kTileBytes);
-    const uint32_t q_lane = row_address<D>(at, lane), g_lane = row_address<D>(at + 2 * kTileBytes, lane);
-    f32x16 s = f32x16{}, dp = f32x16{};
+  if (rounds > 0) fetch(0);
+
+  constexpr int kSteps = D / 16, kParts = D / 32;
+  f32x16 dk[KB][kParts], dv[KB][kParts];
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) s = mfma32(read_rows<D>(q_lane, 0, i), kf[i], s);
+  for (int b = 0; b < KB; ++b)
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) dp = mfma32(read_rows<D>(g_lane, 0, i), vf[i], dp);
-    const bool masked = (CAUSAL && r0 + ahead < key0 + 31) || key0 + 32 > k.length;
+    for (int i = 0; i < kParts; ++i) dk[b][i] = dv[b][i] = f32x16{};
+  const float c = a.scale * kLog2E;
+  uint32_t q_at = row_address<D>(tile_lds, lane), g_at = q_at + S::kTileBytes, column_at[kParts][2];
+  keep(g_at);                        // or the compiler shares their steps' addresses, and has no registers for them
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const f32x4 lse = *reinterpret_cast<const f32x4*>(&stats[n & 1][0][8 * i + 4 * h]);
-      const f32x4 delta = *reinterpret_cast<const f32x4*>(&stats[n & 1][1][8 * i + 4 * h]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int r = 4 * i + e;
-        s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -lse[e]));
-        dp[r] = s[r] * (dp[r] - delta[e]);
-      }
-    }
-    if (masked) {
-      const int first_row = CAUSAL ? key - ahead - r0 - 4 * h : -1;          // of this key
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const bool looked_at = 8 * (r / 4) + r % 4 >= first_row && key < k.length;
-        s[r] = looked_at ? s[r] : 0.f;
-        dp[r] = looked_at ? dp[r] : 0.f;
-      }
-    }
-    const uint32_t qt_lane = column_address<D>(at, lane), gt_lane = column_address<D>(at + 2 * kTileBytes, lane);
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const bf16x8 p = as_operand(s, j), ds = as_operand(dp, j);
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i) dv[i] = mfma32(read_columns<D>(gt_lane, j, i), p, dv[i]);
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i) dk[i] = mfma32(read_columns<D>(qt_lane, j, i), ds, dk[i]);
-    }
+  for (int i = 0; i < kParts; ++i) {
+    keep(column_at[i][0] = column_address<D>(tile_lds, lane) ^ (uint32_t)(i << 6));
+    keep(column_at[i][1] = (column_address<D>(tile_lds, lane) ^ (uint32_t)(i << 6) ^ 32u) + 16u * D);
   }
-  const bool real = key < k.length;
-  store_columns<D>(dk, a.scale, args.dk.at(token, k_head), real, lane);
-  store_columns<D>(dv, 1.f, args.dv.at(token, k_head), real, lane);
+  const uint32_t key_at = row_address<D>(lds + (uint32_t)(S::kKeysAt + wave * KB * 64 * D), lane);
+  uint32_t value_at = key_at + S::kKeyBytes;
+  keep(value_at);
+  typedef __attribute__((address_space(3))) const f32x4* stat_ptr;
+  uint32_t stat_at = stats_lds + (uint32_t)(16 * h);
+
+  for (int round = 0; round < rounds; ++round) {
+    publish();
+    const int r0 = (from + tile) * kBackRows;
+    const bool mine = member < group && !(CAUSAL && r0 + kBackRows - 1 + ahead < key0);       // some of these rows look at a key of this wave
+    advance();
+    if (round + 1 < rounds) fetch(round + 1);
+    if (mine) {
+      f32x16 s[KB], dp[KB];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4 x = *(stat_ptr)(uintptr_t)(stat_at + (uint32_t)(32 * i)), y = *(stat_ptr)(uintptr_t)(stat_at + (uint32_t)(32 * i + kBackRows * 4));
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int b = 0; b < KB; ++b) s[b][4 * i + e] = x[e], dp[b][4 * i + e] = y[e];
+      }
+      // Slots of KB products with one A: S, dP, dv, dk.
+      constexpr int kAhead = 2, kRing = kAhead + 1;
+      bf16x8 f[kRing], kf[kRing][KB];
+      auto read_a = [&](auto slot) __attribute__((always_inline)) {
+        constexpr int i = decltype(slot)::value, j = i - 2 * kSteps;
+        if constexpr (i < 2 * kSteps) return read_rows<D>(i < kSteps ? q_at : g_at, 0, i % kSteps);
+        else return read_columns_at<D>(column_at[j % kParts][0], column_at[j % kParts][1], (uint32_t)((j < 2 * kParts ? S::kTileBytes : 0) + j / kParts % 2 * 32 * D));
+      };
+      auto read_k = [&](auto slot) __attribute__((always_inline)) {
+        constexpr int i = decltype(slot)::value;
+#pragma unroll
+        for (int b = 0; b < KB; ++b) kf[i % kRing][b] = read_rows<D>(i < kSteps ? key_at : value_at, b, i % kSteps);
+      };
+      constexpr int kSlots = 2 * kSteps + 4 * kParts, kPairs = 8 * KB;       // pairs of weights, of blocks 0 and 1 in turn
+      for_each_index([&](auto slot) __attribute__((always_inline)) {
+        f[decltype(slot)::value] = read_a(slot);
+        read_k(slot);
+      }, std::make_integer_sequence<int, kAhead>{});
+      __builtin_amdgcn_sched_barrier(0);
+      for_each_index([&](auto slot) __attribute__((always_inline)) {
+        constexpr int i = decltype(slot)::value;
+        f[(i + kAhead) % kRing] = read_a(std::integral_constant<int, i + kAhead>{});
+        read_k(std::integral_constant<int, i + kAhead>{});
+#pragma unroll
+        for (int b = 0; b < KB; ++b) s[b] = mfma32(f[i % kRing], kf[i % kRing][b], s[b]);
+        __builtin_amdgcn_sched_barrier(0);
+      }, std::make_integer_sequence<int, kSteps>{});
+      if ((CAUSAL && r0 + ahead < key0 + 32 * KB - 1) || key0 + 32 * KB > k.length) {
+#pragma unroll
+        for (int b = 0; b < KB; ++b) {
+          const int at = key + 32 * b, first_row = (at < k.length ? (CAUSAL ? at - ahead - r0 : 0) : 64) - 4 * h;          // of those that look at this key
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[b][r] = 8 * (r / 4) + r % 4 >= first_row ? s[b][r] : -INFINITY;
+        }
+      }
+      u32x4 p[KB][2], ds[KB][2];
+      for_each_index([&](auto slot) __attribute__((always_inline)) {
+        constexpr int u = decltype(slot)::value, i = kSteps + u, j = i - 2 * kSteps;
+        if constexpr (i + kAhead < kSlots) f[(i + kAhead) % kRing] = read_a(std::integral_constant<int, i + kAhead>{});
+        if constexpr (i + kAhead < 2 * kSteps) read_k(std::integral_constant<int, i + kAhead>{});
+#pragma unroll
+        for (int b = 0; b < KB; ++b) {
+          if constexpr (i < 2 * kSteps) dp[b] = mfma32(f[i % kRing], kf[i % kRing][b], dp[b]);
+          else if constexpr (j < 2 * kParts) dv[b][j % kParts] = mfma32(f[i % kRing], __builtin_bit_cast(bf16x8, p[b][j / kParts]), dv[b][j % kParts]);
+          else dk[b][j % kParts] = mfma32(f[i % kRing], __builtin_bit_cast(bf16x8, ds[b][j / kParts - 2]), dk[b][j % kParts]);
+        }
+        // weights while dP and the first half of dv are multiplied (half of them before any of dv, all before its second half), then the gradients of
+        // the scores, half of them before any of dk
+        constexpr int kW = kSteps + kParts, kD = 3 * kParts;
+        constexpr auto weights_before = [](int n) constexpr { return n >= kW ? kPairs : n <= 0 ? 0 : (n * kPairs + kW - 1) / kW; };
+        constexpr auto slopes_before = [](int n) constexpr { return n >= kD ? kPairs : n <= 0 ? 0 : (n * kPairs + kD - 1) / kD; };
+#pragma unroll
+        for (int n = weights_before(u); n < weights_before(u + 1); ++n) {
+          const int b = n % KB, e = n / KB * 2;
+          s[b][e] = __builtin_amdgcn_exp2f(s[b][e] * c);
+          s[b][e + 1] = __builtin_amdgcn_exp2f(s[b][e + 1] * c);
+          p[b][e / 8][e % 8 / 2] = pack_bf16(s[b][e], s[b][e + 1]);
+        }
+#pragma unroll
+        for (int n = slopes_before(j); n < slopes_before(j + 1); ++n) {
+          const int b = n % KB, e = n / KB * 2;
+          ds[b][e / 8][e % 8 / 2] = pack_bf16(s[b][e] * dp[b][e], s[b][e + 1] * dp[b][e + 1]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }, std::make_integer_sequence<int, kSlots - kSteps>{});
+    }
+    // to the other tile
+    q_at ^= 2 * S::kTileBytes;
+    g_at ^= 2 * S::kTileBytes;
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+      column_at[i][0] ^= 2 * S::kTileBytes;
+      column_at[i][1] ^= 2 * S::kTileBytes;
+    }
+    stat_at ^= 2 * kBackRows * 4;
+  }
+
+  // the groups in halves, first dk, then dv: the upper one's sums go to the lower one
+  auto join = [&](f32x16 (&x)[KB][kParts]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int half = QP / 2; half > 0; half /= 2) {
+      publish();
+      f32x4* held = reinterpret_cast<f32x4*>(smem) + lane;
+      auto at = [&](int p, int b, int i, int r) { return ((((p * KW + wave) * KB + b) * kParts + i) * 4 + r) * 64; };
+      if (part >= half && part < 2 * half) {
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+          for (int i = 0; i < kParts; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) held[at(part - half, b, i, r)] = f32x4{x[b][i][4 * r], x[b][i][4 * r + 1], x[b][i][4 * r + 2], x[b][i][4 * r + 3]};
+      }
+      publish();
+      if (part < half) {
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+          for (int i = 0; i < kParts; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const f32x4 y = held[at(part, b, i, r)];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) x[b][i][4 * r + e] += y[e];
+            }
+      }
+    }
+  };
+  join(dk);
+  join(dv);
+  if (part > 0) return;
+#pragma unroll
+  for (int b = 0; b < KB; ++b) {
+    const bool real = key + 32 * b < k.length;
+    const int64_t token = k.first + min(key + 32 * b, k.length - 1);
+    store_columns<D>(dk[b], a.scale, args.dk.at(token, k_head), real, lane);
+    store_columns<D>(dv[b], 1.f, args.dv.at(token, k_head), real, lane);
+  }
 }
 
 }  // namespace swz

@@ -143,9 +143,12 @@ __global__ void __launch_bounds__(64 * QW, D == 64 ? 3 : 2) attention_kernel(Pro
       else return read_columns_at<D>(v_at[v % kParts][0], v_at[v % kParts][1], values_at + (uint32_t)(v / kParts * 32 * D));
     };
     u32x4 p[4];
-    bf16x8 f[3];
-    f[kFirst % 3] = read(std::integral_constant<int, kFirst>{});
-    f[(kFirst + 1) % 3] = read(std::integral_constant<int, kFirst + 1>{});
+    constexpr int kAhead = 2, kRing = kAhead + 1;            // reads on their way
+    bf16x8 f[kRing];
+    for_each_index([&](auto slot) __attribute__((always_inline)) {
+      constexpr int i = kFirst + decltype(slot)::value;
+      f[i % kRing] = read(std::integral_constant<int, i>{});
+    }, std::make_integer_sequence<int, kAhead>{});
     if constexpr (MORE) then[0] = then[1] = f32x16{};
     float sums[2] = {sum, 0.f}, high[2] = {-INFINITY, -INFINITY};
     now[0][0] = __builtin_fmaf(now[0][0], c, -top);
@@ -153,9 +156,9 @@ __global__ void __launch_bounds__(64 * QW, D == 64 ? 3 : 2) attention_kernel(Pro
     __builtin_amdgcn_sched_barrier(0);
     for_each_index([&](auto slot) __attribute__((always_inline)) {
       constexpr int i = kFirst + decltype(slot)::value, v = i - kScoreSlots;
-      if constexpr (i + 2 < kSlots) f[(i + 2) % 3] = read(std::integral_constant<int, i + 2>{});
-      if constexpr (i < kScoreSlots) then[i / kSteps] = mfma32(f[i % 3], qf[i % kSteps], then[i / kSteps]);
-      if constexpr (MORE && i >= kScoreSlots) o[v % kParts] = mfma32(f[i % 3], __builtin_bit_cast(bf16x8, p[v / kParts]), o[v % kParts]);
+      if constexpr (i + kAhead < kSlots) f[(i + kAhead) % kRing] = read(std::integral_constant<int, i + kAhead>{});
+      if constexpr (i < kScoreSlots) then[i / kSteps] = mfma32(f[i % kRing], qf[i % kSteps], then[i / kSteps]);
+      if constexpr (MORE && i >= kScoreSlots) o[v % kParts] = mfma32(f[i % kRing], __builtin_bit_cast(bf16x8, p[v / kParts]), o[v % kParts]);
       constexpr auto kPairs = [](int before) constexpr {                // pairs taken before a slot
         if (MORE) return before >= kSlots ? 16 : before <= 0 ? 0 : (before * 128 + 7 * kSlots - 1) / (7 * kSlots) < 16 ? (before * 128 + 7 * kSlots - 1) / (7 * kSlots) : 16;
         const int w = before - kScoreSlots;
@@ -173,7 +176,7 @@ __global__ void __launch_bounds__(64 * QW, D == 64 ? 3 : 2) attention_kernel(Pro
         sums[1] += w1;
         p[n / 4][n % 4] = pack_bf16(w0, w1);
       }
-      if constexpr (!MORE) o[v % kParts] = mfma32(f[i % 3], __builtin_bit_cast(bf16x8, p[v / kParts]), o[v % kParts]);
+      if constexpr (!MORE) o[v % kParts] = mfma32(f[i % kRing], __builtin_bit_cast(bf16x8, p[v / kParts]), o[v % kParts]);
       if constexpr (MASKED && i == kScoreSlots - 1) mask(then, t + 1);
       if constexpr (MORE && i >= kScoreSlots) {
 #pragma unroll
@@ -313,7 +316,6 @@ __global__ void __launch_bounds__(64 * kJoinRows) attention_join_kernel(PromptAr
   // a split without keys has a sum of 0 and has written nothing else
   const float weight = __builtin_amdgcn_exp2f(my_top - top), sum = over_wave(my_sum * weight, [](float x, float y) { return x + y; });
   vec o = 0.f;
-#pragma unroll 4
   for (int s = 0; s < a.splits; ++s) {
     const float w = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(weight), s));
     if (__uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(my_sum), s)) != 0.f)

@@ -137,28 +137,40 @@ struct RowLoader {
   const uint16_t* head;
   int64_t token;
   int length, wave, lane;
-  uint32_t whole[kLoads];            // offsets where all rows are there
+  uint32_t row_part, chunk;          // bytes of the lane's row of an instruction; its chunk where the instruction starts at a row whose key is 0
 
-  __device__ __forceinline__ uint32_t offset(int i, int most) const {          // most: the last row of the instruction that is there
-    const int r = lane / kChunks, row = (wave * kLoads + i) * kRows + r;
-    return (uint32_t)min(r, most) * (uint32_t)(token * 2) + (uint32_t)(((lane % kChunks) ^ tile_key<D>(row)) << 4);
-  }
   __device__ __forceinline__ RowLoader(const uint16_t* head_, int64_t token_, int length_, int wave_, int lane_) : head(head_), token(token_), length(length_), wave(wave_), lane(lane_) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) whole[i] = offset(i, kRows);
+    const int r = lane / kChunks;
+    row_part = (uint32_t)r * (uint32_t)(token * 2);
+    chunk = (uint32_t)((lane % kChunks) ^ tile_key<D>(r)) << 4;
   }
   // first: of the tile, less than length
   __device__ __forceinline__ void operator()(int first, uint32_t lds) const {
-    const bool all = first + ROWS <= length;
+    const uint32_t to = lds + (uint32_t)(wave * kLoads * 1024);
+    if (first + ROWS <= length) {
+      const uint16_t* base = head + (int64_t)(first + wave * kLoads * kRows) * token;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int at = (wave * kLoads + i) * kRows, from = min(first + at, length - 1);
-      const uint64_t at_row = reinterpret_cast<uint64_t>(head + (int64_t)from * token);
-      const uint64_t base = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at_row >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)at_row);
-      load_to_lds_base_off(reinterpret_cast<const void*>(base), all ? whole[i] : offset(i, length - 1 - from), lds + (uint32_t)((wave * kLoads + i) * 1024));
+      for (int i = 0; i < kLoads; ++i) load(base + i * kRows * token, row_part, i, to);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int from = min(first + (wave * kLoads + i) * kRows, length - 1);
+        load(head + (int64_t)from * token, (uint32_t)min(lane / kChunks, length - 1 - from) * (uint32_t)(token * 2), i, to);
+      }
     }
   }
+  __device__ __forceinline__ void load(const uint16_t* row, uint32_t rows, int i, uint32_t to) const {
+    const uint64_t at = reinterpret_cast<uint64_t>(row);
+    const uint64_t base = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)at);
+    load_to_lds_base_off(reinterpret_cast<const void*>(base), rows + (chunk ^ (uint32_t)(tile_key<D>((wave * kLoads + i) * kRows) << 4)), to + (uint32_t)(i * 1024));
+  }
 };
+
+// 4 bytes a lane, global -> LDS at lds + lane * 4 (load_to_lds has 16).
+__device__ __forceinline__ void load_word_to_lds(const void* gptr, uint32_t lds_base) {
+  const uint32_t lds_addr = __builtin_amdgcn_readfirstlane(lds_base);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(lds_addr), "v"(gptr) : "memory", "m0");
+}
 
 // This wave's loads have landed and its reads are done; then so are all waves'.
 __device__ __forceinline__ void publish() {
