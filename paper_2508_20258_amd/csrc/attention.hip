@@ -203,23 +203,17 @@ int store_or_read(const swz_cache4* cache, const swz_heads* k, const swz_heads* 
   });
 }
 
-// How the sequences of a decoding step are split: parts of part_tokens tokens, a workgroup each.
-struct DecodeSplit {
-  int columns, parts, part_tokens;
+// A decoding step: waves that share the steps of a key head (of each block of 16 of its query heads), rows that a product has for queries.
+struct DecodePlan {
+  int columns, rows, shares;
 };
-constexpr int kDecodeWaves = 4;
-DecodeSplit decode_split(const swz_cache4& c, int sequences, int q_heads, int table_width, int max_length) {
-  const int group = q_heads / c.k_heads, columns = (group + 15) / 16;
+DecodePlan decode_plan(const swz_cache4& c, int sequences, int q_heads, int table_width, int max_length) {
+  const int group = q_heads / c.k_heads, columns = (group + 15) / 16, rows = group <= 4 ? 4 : group <= 8 ? 8 : 16;
   const int64_t cut = (int64_t)table_width * c.page_tokens, longest = max_length > 0 && max_length < cut ? max_length : cut;
-  const int64_t pairs = (int64_t)sequences * c.k_heads * columns, step = 32 * kDecodeWaves;
-  int64_t parts = 4 * (int64_t)compute_units() / pairs;                  // as many as give every compute unit four workgroups
-  if (parts > (longest + 2 * step - 1) / (2 * step)) parts = (longest + 2 * step - 1) / (2 * step);
-  if (parts < 1) parts = 1;
-  int64_t tokens = (longest + parts - 1) / parts;
-  tokens = (tokens + step - 1) / step * step;
-  // sequences longer than the caller said (never longer than the table) must still be covered
-  parts = (cut + tokens - 1) / tokens;
-  return {columns, (int)parts, (int)tokens};
+  // as many as run together; fewer where there are fewer steps
+  const int64_t together = (int64_t)compute_units() * 4 * (c.head_dim == 64 ? 3 : rows >= 8 ? 2 : 3) / ((int64_t)c.k_heads * columns);
+  const int64_t steps = (longest + swz::kDecodeStep - 1) / swz::kDecodeStep * sequences;
+  return {columns, rows, (int)(together < 1 ? 1 : steps < together ? steps : together)};
 }
 
 int check_decode(const swz_cache4* c, int sequences, int q_heads, int table_width, int max_length) {
@@ -230,9 +224,9 @@ int check_decode(const swz_cache4* c, int sequences, int q_heads, int table_widt
   return SWZ_OK;
 }
 
-int64_t decode_floats(const swz_cache4& c, const DecodeSplit& s, int sequences, int q_heads) {
-  return s.parts == 1 ? 0 : (int64_t)sequences * q_heads * s.parts * (c.head_dim + 2);
-}
+// The parts' sums, their statistics, and where they are.
+int64_t decode_parts(const swz_cache4& c, const DecodePlan& p) { return (int64_t)p.shares * c.k_heads * p.columns * 2 * p.rows; }
+int64_t decode_bytes(const swz_cache4& c, const DecodePlan& p, int sequences) { return 4 * decode_parts(c, p) * (c.head_dim + 2) + (int64_t)8 * sequences * c.k_heads * p.columns; }
 
 }  // namespace
 
@@ -367,7 +361,7 @@ int swz_cache4_read(const swz_cache4* cache, const swz_heads* k, const swz_heads
 int64_t swz_cache4_attention_workspace(const swz_cache4* cache, int32_t sequences, int32_t q_heads, int32_t table_width, int32_t max_length) {
   const int st = check_decode(cache, sequences, q_heads, table_width, max_length);
   if (st != SWZ_OK) return st;
-  return 4 * decode_floats(*cache, decode_split(*cache, sequences, q_heads, table_width, max_length), sequences, q_heads);
+  return decode_bytes(*cache, decode_plan(*cache, sequences, q_heads, table_width, max_length), sequences);
 }
 
 int swz_cache4_attention(const swz_cache4* cache, const swz_heads* q, const swz_heads* out, const int32_t* lengths, const int32_t* block_table,
@@ -378,24 +372,26 @@ int swz_cache4_attention(const swz_cache4* cache, const swz_heads* q, const swz_
   if (q == nullptr || out == nullptr || lengths == nullptr || block_table == nullptr || !(scale > 0.f) || !isfinite(scale)) return SWZ_ERR_INVALID_ARG;
   st = check_heads(*q, *out);
   if (st != SWZ_OK) return st;
-  const DecodeSplit s = decode_split(*cache, sequences, q_heads, table_width, max_length);
-  const int64_t floats = decode_floats(*cache, s, sequences, q_heads);
-  if (floats > 0 && (workspace == nullptr || workspace_bytes < 4 * floats)) return SWZ_ERR_INVALID_ARG;
+  const DecodePlan p = decode_plan(*cache, sequences, q_heads, table_width, max_length);
+  if (workspace == nullptr || workspace_bytes < decode_bytes(*cache, p, sequences)) return SWZ_ERR_INVALID_ARG;
   if (!aligned(lengths, 4) || !aligned(block_table, 4) || !aligned(workspace, 16)) return SWZ_ERR_UNSUPPORTED;
   swz::DecodeArgs a{};
   a.c = cache_args(*cache, block_table, table_width);
   a.q = device_heads(*q), a.out = device_heads(*out);
   a.lengths = lengths, a.sequences = sequences, a.q_heads = q_heads;
-  a.columns = s.columns, a.parts = s.parts, a.part_tokens = s.part_tokens, a.scale = scale;
+  a.columns = p.columns, a.shares = p.shares, a.scale = scale;
   a.sums = static_cast<float*>(workspace);
-  a.stats = a.sums + (floats > 0 ? (int64_t)sequences * q_heads * s.parts * cache->head_dim : 0);
+  a.stats = a.sums + decode_parts(*cache, p) * cache->head_dim;
+  a.parts = reinterpret_cast<int2*>(a.stats + decode_parts(*cache, p) * 2);
   return for_head_dim(cache->head_dim, [&](auto dim) {
     constexpr int D = decltype(dim)::value;
-    const int64_t blocks = (int64_t)sequences * cache->k_heads * s.columns * s.parts;
-    if (blocks >= kTokens) return (int)SWZ_ERR_OVERFLOW;
-    int status = launch(swz::cache4_attention_kernel<D, kDecodeWaves>, dim3((unsigned)blocks), dim3(64 * kDecodeWaves), 0, stream, a);
-    if (status != SWZ_OK || s.parts == 1) return status;
-    return launch(swz::cache4_join_kernel<D>, dim3((unsigned)(((int64_t)sequences * q_heads + 3) / 4)), dim3(256), 0, stream, a);
+    const int64_t waves = (int64_t)p.shares * cache->k_heads * p.columns;
+    const dim3 grid((unsigned)((waves + swz::kDecodeWaves - 1) / swz::kDecodeWaves)), block(64 * swz::kDecodeWaves);
+    if (2 * waves >= kTokens || (int64_t)sequences * cache->k_heads * p.columns >= kTokens || (int64_t)sequences * q_heads * 64 * swz::kJoinWaves > swz::kLaunchThreads) return (int)SWZ_ERR_OVERFLOW;
+    auto kernel = p.rows == 4 ? swz::cache4_attention_kernel<D, 4> : p.rows == 8 ? swz::cache4_attention_kernel<D, 8> : swz::cache4_attention_kernel<D, 16>;
+    const int status = launch(kernel, grid, block, 0, stream, a);
+    if (status != SWZ_OK) return status;
+    return launch(swz::cache4_join_kernel<D>, dim3((unsigned)((int64_t)sequences * q_heads)), dim3(64 * swz::kJoinWaves), 0, stream, a, p.rows);
   });
 }
 

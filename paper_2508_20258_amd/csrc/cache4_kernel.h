@@ -179,24 +179,56 @@ __global__ void __launch_bounds__(256) cache4_read_kernel(StoreArgs a) {
 }
 
 // ---------------------------------------------------------------- attention of one token of each sequence
-
+//
+// A wave takes 64 tokens of a key head at a time.  Scores: queries (A, rows) times keys (B, columns), a product for 16 tokens and 32 dimensions.  A matrix instruction has room
+// for 16 queries, a key head has often 4: the queries then stand in all four groups of 4 rows, and lanes 16 g .. + 15 keep what they have of tokens 16 g .. + 15, so that
+// each lane has one token and all that is done for a weight (scales, exponential, sums) is done once.  R rows: 4, 8 or 16, 64 R / 64 weights a lane.
+// The weights go through LDS to the layout in which the product with the values takes them: values (A, rows are dimensions) times weights (B, columns are queries).
+//
+// Numbers n of a word become bfloat16 128 + n (0x4300 | n, two an instruction); products of scores start from -128 sum(q), and what the values' 136 adds is taken off with
+// the rounded weights themselves.
+//
+// The steps of all sequences, in their order, are dealt evenly to the waves that a key head has, whatever the lengths: of `shares` waves, wave i has steps
+// total * i / shares and up.  All key heads are dealt alike and neighbouring waves have neighbouring heads, whose tokens are neighbours in a page.  What a wave has of a sequence goes to
+// `out` where that is all of it, else into one of two places of its own (the first sequence it works on, or the last), and cache4_join_kernel joins them.  Waves share nothing, and wait for
+// nothing but their own loads; the loads of the next step's keys are issued when this one's are used up, and so for the values.
 struct DecodeArgs {
   CacheArgs c;
   Heads q, out;
   const int32_t* lengths;
-  float *sums, *stats;               // of the parts of a sequence: sequences x q_heads x parts x D, and x 2 (maximum, sum)
-  int sequences, q_heads, columns;   // columns: blocks of 16 query heads of a key head
-  int parts, part_tokens;
+  float *sums, *stats;               // shares x heads x 2 x R x D, and x 2 (maximum, sum)
+  int2* parts;                       // sequences x heads: place of the first part, share of the last
+  int sequences, q_heads, columns;   // columns: blocks of 16 query heads of a key head, each a head of its own here
+  int shares;
   float scale;
 };
 
-// Numbers n of a word as bfloat16 128 + n, which is 0x4300 | n: a pair of them an instruction.
-__device__ __forceinline__ bf16x8 numbers_128(uint32_t w) {
-  u32x4 x;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] = ((w >> (4 * i)) & 0x000f000fu) | 0x43004300u;
-  return __builtin_bit_cast(bf16x8, x);
+constexpr int kDecodeStep = 64, kDecodeWaves = 4;
+
+__device__ __forceinline__ int cached_length(const DecodeArgs& a, int sequence) {
+  return (int)min((int64_t)max(a.lengths[sequence], 0), (int64_t)a.c.table_width << a.c.page_shift);
 }
+__device__ __forceinline__ int steps_of(int length) { return (length + kDecodeStep - 1) / kDecodeStep; }
+// f(first sequence, steps of the lane's sequence, steps of the lane's and those before it) for 64 sequences at a time, until it says false.
+template <class F>
+__device__ __forceinline__ void over_sequences(const DecodeArgs& a, F&& f) {
+  for (int first = 0; first < a.sequences; first += 64) {
+    const int b = first + (int)(threadIdx.x & 63), n = b < a.sequences ? steps_of(cached_length(a, b)) : 0;
+    if (!f(first, n, sum_before(n))) return;
+  }
+}
+
+// The instruction takes no two constants, so they are kept in registers.
+struct Numbers {
+  uint32_t mask = 0x000f000fu, one = 0x43004300u;
+  __device__ __forceinline__ Numbers() { asm volatile("" : "+s"(mask), "+v"(one)); }
+  __device__ __forceinline__ bf16x8 operator()(uint32_t w) const {
+    u32x4 x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = ((w >> (4 * i)) & mask) | one;
+    return __builtin_bit_cast(bf16x8, x);
+  }
+};
 
 __device__ __forceinline__ float scale_step(uint32_t s) { return __uint_as_float(s << 16); }
 __device__ __forceinline__ float scale_low(uint32_t s) { return __uint_as_float(s & 0xffff0000u); }
@@ -207,238 +239,361 @@ __device__ __forceinline__ float over_rows(float x, Op op) {
   const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return across_halves(op(__uint_as_float(s[0]), __uint_as_float(s[1])), op);
 }
-
-// What 32 tokens of a head are in the cache, as the lanes of a wave take them (lane 16 g + m).
-template <int D>
-struct Raw {
-  uint32_t k[2][D / 32];             // token 8 (m / 4) + 4 b + m % 4, words D / 32 * g ..
-  u32x4 v[D / 64];                   // tokens 8 g .. + 7, dimensions 64 i + 4 m .. + 3
-  uint32_t ks[8][D / 64], vs[8][D / 64];   // scales of tokens 8 g .. + 7
-};
-
-template <int D>
-__device__ __forceinline__ void load_raw(Raw<D>& r, const CacheArgs& c, int page, int head, int position, int lane) {
-  const int m = lane & 15, g = lane >> 4;
-  const int64_t at = c.token_at(page, head, position);
-  typedef __attribute__((ext_vector_type(D / 32))) uint32_t k_vec;
-#pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    const k_vec w = *reinterpret_cast<const k_vec*>(c.k_words + (at + 8 * (m >> 2) + 4 * b + (m & 3)) * (D / 8) + (D / 32) * g);
-#pragma unroll
-    for (int s = 0; s < D / 32; ++s) r.k[b][s] = w[s];
+// op over the lanes that hold one query's weights: those of a row of 16, and of the rows R / 4 apart.
+template <int R, class Op>
+__device__ __forceinline__ float over_tokens(float x, Op op) {
+  auto dpp = [](float v, auto ctrl) __attribute__((always_inline)) {
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, false));
+  };
+  x = op(x, dpp(x, std::integral_constant<int, 0xB1>{}));        // quad_perm [1,0,3,2]
+  x = op(x, dpp(x, std::integral_constant<int, 0x4E>{}));        // quad_perm [2,3,0,1]
+  x = op(x, dpp(x, std::integral_constant<int, 0x141>{}));       // row_half_mirror
+  x = op(x, dpp(x, std::integral_constant<int, 0x140>{}));       // row_mirror
+  if constexpr (R == 4) {
+    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = op(__uint_as_float(s[0]), __uint_as_float(s[1]));
   }
-#pragma unroll
-  for (int i = 0; i < D / 64; ++i) r.v[i] = *reinterpret_cast<const u32x4*>(c.v_words + ((at >> 3) + g) * D + 64 * i + 4 * m);
-#pragma unroll
-  for (int i = 0; i < 2 * (D / 64); ++i) {
-    const u32x4 k = *reinterpret_cast<const u32x4*>(c.k_scales + (at + 8 * g) * (D / 64) + 4 * i), v = *reinterpret_cast<const u32x4*>(c.v_scales + (at + 8 * g) * (D / 64) + 4 * i);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      r.ks[(4 * i + e) / (D / 64)][(4 * i + e) % (D / 64)] = k[e];
-      r.vs[(4 * i + e) / (D / 64)][(4 * i + e) % (D / 64)] = v[e];
-    }
-  }
+  if constexpr (R <= 8) x = across_halves(x, op);
+  return x;
 }
 
-template <int D, int NW>
-__global__ void __launch_bounds__(NW * 64) cache4_attention_kernel(DecodeArgs a) {
+template <int D, int R>
+__global__ void __launch_bounds__(64 * kDecodeWaves, D == 128 && R >= 8 ? 2 : 3) cache4_attention_kernel(DecodeArgs a) {
   constexpr int kGroups = D / 64, kSteps = D / 32;
-  __shared__ f32x4 merge[NW / 2][4 * kGroups][64];
-  __shared__ float merge_stats[NW / 2][2][64];
+  constexpr int kQuads = R / 4, kSets = R / 4, kBlocks = 16 / R;      // row groups that a query's four rows take part in; sets of 4 weights a lane; blocks of 16 tokens of a set
+  __shared__ __attribute__((aligned(16))) uint16_t weights[kDecodeWaves][kGroups][kDecodeStep][R];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
-  int rest = (int)blockIdx.x;
-  const int column = rest % a.columns;
-  rest /= a.columns;
-  const int k_head = rest % a.c.k_heads;
-  rest /= a.c.k_heads;
-  const int sequence = rest % a.sequences, part = rest / a.sequences;
-  const int group = a.q_heads / a.c.k_heads, head = k_head * group + column * 16 + n;
-  const bool real = column * 16 + n < group;
-  const int length = (int)min((int64_t)max(__builtin_amdgcn_readfirstlane(a.lengths[sequence]), 0), (int64_t)a.c.table_width << a.c.page_shift);
-  const int begin = part * a.part_tokens, end = (int)min((int64_t)length, (int64_t)begin + a.part_tokens);
-  if (part > 0 && begin >= length) return;
+  const int heads = a.c.k_heads * a.columns, group = a.q_heads / a.c.k_heads;
+  const int id = (int)blockIdx.x * kDecodeWaves + wave, share = id / heads, pair = id - share * heads;
+  int64_t total = 0;
+  over_sequences(a, [&](int, int, int sum) {
+    total += __builtin_amdgcn_readlane(sum, 63);
+    return true;
+  });
+  const int shares = (int)min((int64_t)a.shares, total);
+  if (share >= shares) return;
+  const int64_t my_start = total * share / shares, my_end = total * (share + 1) / shares;
+  int sequence = 0;
+  int64_t before = 0;                                        // steps of the sequences before it
+  over_sequences(a, [&](int first, int n, int sum) {
+    const uint64_t found = __ballot(my_start < before + sum);
+    if (found == 0) {
+      before += __builtin_amdgcn_readlane(sum, 63);
+      return true;
+    }
+    const int s = __ffsll((unsigned long long)found) - 1;
+    sequence = first + s;
+    before += __builtin_amdgcn_readlane(sum - n, s);
+    return false;
+  });
+  const int k_head = pair / a.columns, column = pair - k_head * a.columns;
+  const int head0 = k_head * group + column * 16, queries = min(16, group - column * 16);
 
-  bf16x8 q[kSteps];
-  float q_sum[kGroups];
-#pragma unroll
-  for (int j = 0; j < kGroups; ++j) q_sum[j] = 0.f;
-#pragma unroll
-  for (int s = 0; s < kSteps; ++s) {
-    q[s] = bf16x8{};
-    if (real) q[s] = *reinterpret_cast<const bf16x8*>(a.q.at(sequence, head) + 32 * s + 8 * g);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) q_sum[s / 2] += (float)q[s][e];
-  }
-#pragma unroll
-  for (int j = 0; j < kGroups; ++j) q_sum[j] = over_rows(q_sum[j], [](float x, float y) { return x + y; });
-
+  typedef __attribute__((ext_vector_type(kSteps))) uint32_t k_vec;
+  typedef __attribute__((ext_vector_type(kGroups))) uint32_t scale_vec;
+  typedef __attribute__((address_space(3))) s16x4* tr_ptr;
+  const Numbers numbers;
   const float c = a.scale * kLog2E;
-  const u32x4 minus_136 = {0xc308c308u, 0xc308c308u, 0xc308c308u, 0xc308c308u};
-  f32x4 o[kGroups][4], shift[kGroups];
-  float mids[kGroups], top = -FLT_MAX, sum = 0.f;
+  const uint32_t weights_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)&weights[wave][0][0][0];
+  // transposing reads: 4 tokens of a row each; columns from R on are what they may be, nothing reads them
+  const uint32_t read_at = weights_at + (uint32_t)((8 * g + (n >> 2)) * 2 * R + (n & 3) % kQuads * 8);
+  auto token_of = [&](int u) { return 16 * (u * kBlocks + g / kQuads) + n; };            // of a step: the lane's in set u
+  // of what the lanes hold for their queries (4 (g mod kQuads) + r): that of query n
+  auto of_query = [&](const float (&x)[4]) __attribute__((always_inline)) {
+    float mine = 0.f;
 #pragma unroll
-  for (int i = 0; i < kGroups; ++i) {
-    mids[i] = 0.f;
-    shift[i] = f32x4{};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) o[i][j] = f32x4{};
-  }
+    for (int r = 0; r < 4; ++r) {
+      const float f = __int_as_float(__builtin_amdgcn_ds_bpermute(n / 4 % kQuads * 64, __float_as_int(x[r])));
+      mine = (n & 3) == r ? f : mine;
+    }
+    return mine;
+  };
 
-  for (int t = begin + 32 * wave; t < end; t += 32 * NW) {
-    const int page = a.c.page_of(sequence, t);
-    Raw<D> r;
-    load_raw<D>(r, a.c, page < 0 ? 0 : page, k_head, t, lane);
-    if (page < 0) {
+  for (int64_t step = my_start; step < my_end; ++sequence) {
+    const int length = __builtin_amdgcn_readfirstlane(cached_length(a, sequence)), all = steps_of(length);
+    if (all == 0) continue;
+    const int from = (int)(step - before), count = (int)min((int64_t)(all - from), my_end - step);
+    const int begin = from * kDecodeStep, end = min(length, (from + count) * kDecodeStep);
+
+    // queries, in all groups of R rows, and -128 times their sums over a group of dimensions: of the lane's four, 4 (g mod kQuads) + r
+    bf16x8 q[kSteps];
+    f32x4 start[kGroups];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) r.ks[e][0] = 0x7fc07fc0u;
+    for (int s = 0; s < kSteps; ++s) {
+      q[s] = bf16x8{};
+      if (n % R < queries) q[s] = *reinterpret_cast<const bf16x8*>(a.q.at(sequence, head0 + n % R) + 32 * s + 8 * g);
     }
-    if (t + 32 > end) {
+
+    // keys and values of a step; pages have 32 tokens and more: one for each half of it, looked up a step ahead
+    int page[2], next_page[2];
+    int64_t at[2];
+    k_vec k[4];
+    u32x4 v[2][kGroups];
+    scale_vec ks[kSets], vs[kSets];
+    auto look_up = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
+      for (int half = 0; half < 2; ++half) next_page[half] = t + 32 * half < end ? a.c.page_of(sequence, t + 32 * half) : 0;
+    };
+    auto scale_place = [&](int u) {
+      const int token = token_of(u);
+      return ((token < 32 ? at[0] : at[1]) + (token & 31)) * kGroups;
+    };
+    auto load_keys = [&](int t) __attribute__((always_inline)) {       // of step t and what places its values; page stays that of the step before
 #pragma unroll
-        for (int i = 0; i < kGroups; ++i) r.vs[e][i] = t + 8 * g + e < end ? r.vs[e][i] : 0u;
+      for (int half = 0; half < 2; ++half) at[half] = a.c.token_at(max(next_page[half], 0), k_head, t + 32 * half);
+#pragma unroll
+      for (int b = 0; b < 4; ++b) k[b] = *reinterpret_cast<const k_vec*>(a.c.k_words + (at[b / 2] + 16 * (b & 1) + n) * (D / 8) + kSteps * g);
+#pragma unroll
+      for (int u = 0; u < kSets; ++u) ks[u] = *reinterpret_cast<const scale_vec*>(a.c.k_scales + scale_place(u));
+    };
+    auto load_values = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < kSets; ++u) vs[u] = *reinterpret_cast<const scale_vec*>(a.c.v_scales + scale_place(u));
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i) v[half][i] = *reinterpret_cast<const u32x4*>(a.c.v_words + ((at[half] >> 3) + g) * D + 64 * i + 4 * n);
+    };
+    look_up(begin);
+    load_keys(begin);
+    load_values();
+    page[0] = next_page[0];
+    page[1] = next_page[1];
+    look_up(begin + kDecodeStep);
+
+#pragma unroll
+    for (int j = 0; j < kGroups; ++j) {
+      float mine = 0.f;                                      // of query n % R
+#pragma unroll
+      for (int s = 2 * j; s < 2 * j + 2; ++s)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) mine += (float)q[s][e];
+      mine = -128.f * over_rows(mine, [](float x, float y) { return x + y; });
+#pragma unroll
+      for (int r = 0; r < 4; ++r) start[j][r] = __int_as_float(__builtin_amdgcn_ds_bpermute((4 * (g % kQuads) + r) * 4, __float_as_int(mine)));
     }
-    float x[8];
+    f32x4 o[kGroups][4];
+    float mids[kGroups][4], top[4], sum[4];                  // of the lane's queries; sums over the lane's tokens
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int i = 0; i < kGroups; ++i)
 #pragma unroll
-      for (int i = 0; i < kGroups; ++i) {
-        f32x4 s = f32x4{};
+      for (int j = 0; j < 4; ++j) o[i][j] = f32x4{}, mids[i][j] = 0.f;
 #pragma unroll
-        for (int u = 2 * i; u < 2 * i + 2; ++u) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(numbers_128(r.k[b][u]), q[u], s, 0, 0, 0);
+    for (int r = 0; r < 4; ++r) top[r] = -FLT_MAX, sum[r] = 0.f;
+
+    for (int t = begin; t < end; t += kDecodeStep) {
+      float x[kSets][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t w = r.ks[4 * b + e][i];
-          const float part_score = __builtin_fmaf(scale_step(w), __builtin_fmaf(q_sum[i], -128.f, s[e]), scale_low(w) * q_sum[i]);
-          x[4 * b + e] = i == 0 ? part_score : x[4 * b + e] + part_score;
+      for (int u = 0; u < kSets; ++u) {
+        f32x4 y[2][kGroups], s[kGroups];
+        auto take = [&](int p) __attribute__((always_inline)) {        // of block p, by the lanes that keep it
+#pragma unroll
+          for (int i = 0; i < kGroups; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[i][r] = p == 0 || g / kQuads == p ? y[p % 2][i][r] : s[i][r];
+        };
+#pragma unroll
+        for (int p = 0; p < kBlocks; ++p) {
+#pragma unroll
+          for (int i = 0; i < kGroups; ++i) {
+            y[p % 2][i] = start[i];
+#pragma unroll
+            for (int w = 2 * i; w < 2 * i + 2; ++w) y[p % 2][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[w], numbers(k[u * kBlocks + p][w]), y[p % 2][i], 0, 0, 0);
+          }
+          if (p > 0) take(p - 1);
+          __builtin_amdgcn_sched_barrier(0);                // or all words are taken apart at once, and registers run out
+        }
+        take(kBlocks - 1);
+        const int token = token_of(u);
+        if (t + 32 * (token / 32) < end && (token < 32 ? page[0] : page[1]) < 0) ks[u][0] = 0x7fc07fc0u;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          x[u][r] = 0.f;
+#pragma unroll
+          for (int i = 0; i < kGroups; ++i) x[u][r] = __builtin_fmaf(scale_step(ks[u][i]), s[i][r], __builtin_fmaf(scale_low(ks[u][i]) * (-1.f / 128), start[i][r], x[u][r]));
+          x[u][r] *= c;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      const bool more = t + kDecodeStep < end;
+      if (more) load_keys(t + kDecodeStep);
+      if (!more && t + kDecodeStep > end) {
+#pragma unroll
+        for (int u = 0; u < kSets; ++u) {
+          const bool real = t + token_of(u) < end;
+#pragma unroll
+          for (int i = 0; i < kGroups; ++i) vs[u][i] = real ? vs[u][i] : 0u;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) x[u][r] = real ? x[u][r] : -INFINITY;
         }
       }
-    }
-    if (t + 32 > end) {
+      bool higher = false;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = t + 8 * g + e < end ? x[e] : -INFINITY;
-    }
-    float high = x[0];
+      for (int u = 0; u < kSets; ++u)
 #pragma unroll
-    for (int e = 1; e < 8; ++e) high = fmaxf(high, x[e]);
-    high = over_rows(high, [](float y, float z) { return fmaxf(y, z); }) * c;
-    if (__any(high > top + kLazyRise)) {
-      const float now = fmaxf(top, high), less = __builtin_amdgcn_exp2f(top - now);
-      sum *= less;
+        for (int r = 0; r < 4; ++r) higher |= x[u][r] > top[r] + kLazyRise;
+      if (__any(higher)) {
+        float less[4];
 #pragma unroll
-      for (int i = 0; i < kGroups; ++i) {
-        mids[i] *= less;
-        shift[i] *= less;
+        for (int r = 0; r < 4; ++r) {
+          float high = x[0][r];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[i][j] *= less;
+          for (int u = 1; u < kSets; ++u) high = fmaxf(high, x[u][r]);
+          const float now = fmaxf(top[r], over_tokens<R>(high, [](float y, float z) { return fmaxf(y, z); }));
+          less[r] = __builtin_amdgcn_exp2f(top[r] - now);
+          top[r] = now;
+          sum[r] *= less[r];
+#pragma unroll
+          for (int i = 0; i < kGroups; ++i) mids[i][r] *= less[r];
+        }
+        const float mine = of_query(less);
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[i][j] *= mine;
       }
-      top = now;
-    }
+      // value = mid + step (n - 8): the rounding of a weight times step then costs in proportion to the value, not to the range of its group
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], c, -top));
-      sum += x[e];
+      for (int u = 0; u < kSets; ++u) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          x[u][r] = __builtin_amdgcn_exp2f(x[u][r] - top[r]);
+          sum[r] += x[u][r];
+        }
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i) {
+          const float size = scale_step(vs[u][i]), mid = __builtin_fmaf(size, 8.f, scale_low(vs[u][i]));
+#pragma unroll
+          for (int r = 0; r < 4; ++r) mids[i][r] = __builtin_fmaf(x[u][r], mid, mids[i][r]);
+          const u32x2 w = {pack_bf16(x[u][0] * size, x[u][1] * size), pack_bf16(x[u][2] * size, x[u][3] * size)};
+          *reinterpret_cast<u32x2*>(&weights[wave][i][token_of(u)][4 * (g % kQuads)]) = w;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) mids[i][r] = __builtin_fmaf(-136.f, r % 2 == 0 ? __uint_as_float(w[r / 2] << 16) : __uint_as_float(w[r / 2] & 0xffff0000u), mids[i][r]);
+        }
+      }
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i) {
+          const uint32_t w_at = read_at + (uint32_t)((i * kDecodeStep + 32 * half) * 2 * R);
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(uintptr_t)w_at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(uintptr_t)(w_at + 8 * R));
+          const bf16x8 p = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            o[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(numbers(v[half][i][j]), p, o[i][j], 0, 0, 0);
+            if (j % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+      if (more) {
+        load_values();
+        page[0] = next_page[0];
+        page[1] = next_page[1];
+        look_up(t + 2 * kDecodeStep);
+      }
     }
-    // value = mid + step (n - 8): the rounding of a weight times step then costs in proportion to the value, not to the range of its group
+
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      sum[r] = over_tokens<R>(sum[r], [](float x, float y) { return x + y; });
+#pragma unroll
+      for (int i = 0; i < kGroups; ++i) mids[i][r] = over_tokens<R>(mids[i][r], [](float x, float y) { return x + y; });
+    }
+    const float my_sum = of_query(sum), my_top = of_query(top);
+    const bool whole = count == all;
+    const float f = !whole ? 1.f : my_sum == 0.f ? 0.f : 1.f / my_sum;
 #pragma unroll
     for (int i = 0; i < kGroups; ++i) {
-      u32x4 w;
+      const float mid = of_query(mids[i]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = pack_bf16(x[2 * e] * scale_step(r.vs[2 * e][i]), x[2 * e + 1] * scale_step(r.vs[2 * e + 1][i]));
-      const bf16x8 p = __builtin_bit_cast(bf16x8, w);
+      for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) mids[i] = __builtin_fmaf(x[e], __builtin_fmaf(scale_step(r.vs[e][i]), 8.f, scale_low(r.vs[e][i])), mids[i]);
-      shift[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, minus_136), p, shift[i], 0, 0, 0);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) o[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(numbers_128(r.v[i][j]), p, o[i][j], 0, 0, 0);
+        for (int e = 0; e < 4; ++e) o[i][j][e] = (o[i][j][e] + mid) * f;
     }
-  }
-
+    // query n's dimensions 64 i + 16 g + 4 e + j
+    if (n < queries) {
+      if (whole) {
 #pragma unroll
-  for (int i = 0; i < kGroups; ++i) {
-    mids[i] = over_rows(mids[i], [](float x, float y) { return x + y; });
+        for (int i = 0; i < kGroups; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+          for (int half = 0; half < 2; ++half) {
+            float y[8];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[i][j][e] += shift[i][e] + mids[i];
-  }
-  sum = over_rows(sum, [](float x, float y) { return x + y; });
-
-  // the waves in halves: the upper one's sums go to the lower one
+            for (int z = 0; z < 8; ++z) y[z] = o[i][z % 4][2 * half + z / 4];
+            *reinterpret_cast<u32x4*>(a.out.at(sequence, head0 + n) + 64 * i + 16 * g + 8 * half) = pack8(y);
+          }
+      } else {
+        const int part = id * 2 + (step == my_start ? 0 : 1);
+        const int64_t to = (int64_t)part * R + n;
 #pragma unroll
-  for (int half = NW / 2; half > 0; half /= 2) {
-    if (wave >= half && wave < 2 * half) {
+        for (int i = 0; i < kGroups; ++i)
 #pragma unroll
-      for (int i = 0; i < kGroups; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) merge[wave - half][4 * i + j][lane] = o[i][j];
-      merge_stats[wave - half][0][lane] = top;
-      merge_stats[wave - half][1][lane] = sum;
-    }
-    __syncthreads();
-    if (wave < half) {
-      const float their_top = merge_stats[wave][0][lane], now = fmaxf(top, their_top);
-      const float mine = __builtin_amdgcn_exp2f(top - now), theirs = __builtin_amdgcn_exp2f(their_top - now);
-      sum = sum * mine + merge_stats[wave][1][lane] * theirs;
-#pragma unroll
-      for (int i = 0; i < kGroups; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) o[i][j] = o[i][j] * mine + merge[wave][4 * i + j][lane] * theirs;
-      top = now;
-    }
-    __syncthreads();
-  }
-  if (wave > 0 || !real) return;
-  // query n's dimensions 64 i + 16 g + 4 e + j
-  if (a.parts == 1) {
-    const float f = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-    for (int i = 0; i < kGroups; ++i)
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        float y[8];
-#pragma unroll
-        for (int x = 0; x < 8; ++x) y[x] = o[i][x % 4][2 * half + x / 4] * f;
-        *reinterpret_cast<u32x4*>(a.out.at(sequence, head) + 64 * i + 16 * g + 8 * half) = pack8(y);
+          for (int e = 0; e < 4; ++e)
+            *reinterpret_cast<f32x4*>(a.sums + to * D + 64 * i + 16 * g + 4 * e) = f32x4{o[i][0][e], o[i][1][e], o[i][2][e], o[i][3][e]};
+        if (g == 0) *reinterpret_cast<float2*>(a.stats + to * 2) = float2{my_top, my_sum};
+        if (lane == 0 && from == 0) a.parts[sequence * heads + pair].x = part;
       }
-  } else {
-    const int64_t at = ((int64_t)sequence * a.q_heads + head) * a.parts + part;
-#pragma unroll
-    for (int i = 0; i < kGroups; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        *reinterpret_cast<f32x4*>(a.sums + at * D + 64 * i + 16 * g + 4 * e) = f32x4{o[i][0][e], o[i][1][e], o[i][2][e], o[i][3][e]};
-    if (g == 0) {
-      a.stats[at * 2] = top;
-      a.stats[at * 2 + 1] = sum;
     }
+    if (lane == 0 && from + count == all) a.parts[sequence * heads + pair].y = whole ? -1 : share;
+    step += count;
+    before += all;
   }
 }
 
-// The parts of a sequence joined, a wave for each query head.
+// What several waves have of a sequence's key head joined, a workgroup for each query head; and zeros for sequences without tokens.
+constexpr int kJoinWaves = 4;
 template <int D>
-__global__ void __launch_bounds__(256) cache4_join_kernel(DecodeArgs a) {
+__global__ void __launch_bounds__(64 * kJoinWaves) cache4_join_kernel(DecodeArgs a, int rows) {
   constexpr int kPer = D / 64;
   typedef __attribute__((ext_vector_type(kPer))) float vec;
-  const int lane = threadIdx.x & 63, id = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  if (id >= a.sequences * a.q_heads) return;
-  const int sequence = id / a.q_heads, head = id - sequence * a.q_heads;
-  const int length = (int)min((int64_t)max(__builtin_amdgcn_readfirstlane(a.lengths[sequence]), 0), (int64_t)a.c.table_width << a.c.page_shift);
-  const int parts = (int)min((int64_t)a.parts, ((int64_t)length + a.part_tokens - 1) / a.part_tokens);
-  const float* stats = a.stats + (int64_t)id * a.parts * 2;
-  const float* sums = a.sums + (int64_t)id * a.parts * D + lane * kPer;
-  float top = -FLT_MAX;
-  for (int p = 0; p < parts; ++p) top = fmaxf(top, stats[2 * p]);
-  float total = 0.f;
+  __shared__ float joined[kJoinWaves][D], joined_stats[kJoinWaves][2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int sequence = (int)blockIdx.x / a.q_heads, head = (int)blockIdx.x - sequence * a.q_heads;
+  const int heads = a.c.k_heads * a.columns, group = a.q_heads / a.c.k_heads, k_head = head / group, member = head - k_head * group;
+  uint16_t* to = a.out.at(sequence, head) + lane * kPer;
+  const int pair = k_head * a.columns + member / 16;
+  const int2 parts = a.parts[sequence * heads + pair];
+  if (__builtin_amdgcn_readfirstlane(cached_length(a, sequence)) == 0) {
+    if (wave == 0)
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) to[i] = 0;
+    return;
+  }
+  const int last = __builtin_amdgcn_readfirstlane(parts.y);
+  if (last < 0) return;                                     // one wave had all of it
+  const int first_part = __builtin_amdgcn_readfirstlane(parts.x), first = first_part / 2 / heads;
+  auto place = [&](int share) { return (int64_t)(share == first ? first_part : (share * heads + pair) * 2) * rows + member % 16; };
+  float top = -FLT_MAX, sum = 0.f;
   vec o = 0.f;
+  // 64 of a wave's parts at a time, a lane each for their statistics
+  for (int from = first + wave; from <= last; from += 64 * kJoinWaves) {
+    const int mine = from + lane * kJoinWaves;
+    float2 x = {-FLT_MAX, 0.f};
+    if (mine <= last) x = *reinterpret_cast<const float2*>(a.stats + 2 * place(mine));
+    const float now = fmaxf(top, over_wave(x.x, [](float y, float z) { return fmaxf(y, z); })), less = __builtin_amdgcn_exp2f(top - now);
+    const float weight = __builtin_amdgcn_exp2f(x.x - now);
+    sum = sum * less + over_wave(x.y * weight, [](float y, float z) { return y + z; });
+    o *= less;
+    top = now;
+    const int parts = min(64, (last - from) / kJoinWaves + 1);
 #pragma unroll 4
-  for (int p = 0; p < parts; ++p) {
-    const float f = __builtin_amdgcn_exp2f(stats[2 * p] - top);
-    total += stats[2 * p + 1] * f;
-    o += *reinterpret_cast<const vec*>(sums + (int64_t)p * D) * f;
+    for (int p = 0; p < parts; ++p)
+      o += *reinterpret_cast<const vec*>(a.sums + place(from + p * kJoinWaves) * D + lane * kPer) * __int_as_float(__builtin_amdgcn_readlane(__float_as_int(weight), p));
+  }
+  *reinterpret_cast<vec*>(&joined[wave][lane * kPer]) = o;
+  if (lane == 0) joined_stats[wave][0] = top, joined_stats[wave][1] = sum;
+  __syncthreads();
+  if (wave > 0) return;
+  float highest = -FLT_MAX, total = 0.f;
+#pragma unroll
+  for (int w = 0; w < kJoinWaves; ++w) highest = fmaxf(highest, joined_stats[w][0]);
+  o = 0.f;
+#pragma unroll
+  for (int w = 0; w < kJoinWaves; ++w) {
+    const float f = __builtin_amdgcn_exp2f(joined_stats[w][0] - highest);
+    total += joined_stats[w][1] * f;
+    o += *reinterpret_cast<const vec*>(&joined[w][lane * kPer]) * f;
   }
   const float f = total == 0.f ? 0.f : 1.f / total;
-  uint16_t* to = a.out.at(sequence, head) + lane * kPer;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) to[i] = __builtin_bit_cast(uint16_t, (__bf16)(o[i] * f));
 }
