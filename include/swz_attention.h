@@ -52,7 +52,7 @@ typedef struct {
 int swz_qk_norm_rope(const swz_norm_args* args, hipStream_t stream);
 
 /* The gradient of swz_qk_norm_rope.  args->q, k and the tables as in the forward call; q_out, k_out hold the gradients of its
- * outputs (read), dq, dk receive those of q and k (may be q_out, k_out themselves), dq_weight, dk_weight (head_dim 32-bit floats each) those of the weights, whole:
+ * outputs (read), dq, dk receive those of q and k (may be q_out, k_out themselves), dq_weight, dk_weight (head_dim 32-bit floats each, 16-byte aligned) those of the weights, whole:
  * sums over all tokens and heads, in an order that depends on the sizes and the device alone.
  *   workspace : swz_qk_norm_rope_backward_workspace(args) bytes, 16-byte aligned, needed until the call has run. */
 int64_t swz_qk_norm_rope_backward_workspace(const swz_norm_args* args);

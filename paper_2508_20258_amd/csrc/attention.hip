@@ -73,23 +73,27 @@ int check_norm(const swz_norm_args* a) {
   return SWZ_OK;
 }
 
+swz::NormSide norm_side(const swz_heads& x, const swz_heads& z, const void* weight, int heads, int64_t tokens) {
+  const int blocks = (heads + swz::kNormHeads - 1) / swz::kNormHeads;
+  return {device_heads(x), device_heads(z), {}, static_cast<const uint16_t*>(weight), heads, blocks, (int)(tokens * blocks)};
+}
 swz::NormArgs norm_args(const swz_norm_args& a) {
   swz::NormArgs n{};
-  n.x[0] = device_heads(a.q), n.x[1] = device_heads(a.k);
-  n.z[0] = device_heads(a.q_out), n.z[1] = device_heads(a.k_out);
-  n.weight[0] = static_cast<const uint16_t*>(a.q_weight), n.weight[1] = static_cast<const uint16_t*>(a.k_weight);
+  n.q = norm_side(a.q, a.q_out, a.q_weight, a.q_heads, a.tokens);
+  n.k = norm_side(a.k, a.k_out, a.k_weight, a.k_heads, a.tokens);
   n.cos = a.cos, n.sin = a.sin, n.positions = a.positions;
-  n.heads[0] = a.q_heads, n.heads[1] = a.k_heads;
-  n.rows[0] = (int)(a.tokens * a.q_heads), n.rows[1] = (int)(a.tokens * a.k_heads);
   n.rotary = a.rotary_dim, n.table_rows = (int)a.table_rows, n.eps = a.eps;
   return n;
 }
-
-// Workgroups of the backward pass: as many as have rows, at most eight to a compute unit.
-int norm_backward_blocks(const swz_norm_args& a) {
-  const int64_t rows = a.tokens * (a.q_heads > a.k_heads ? a.q_heads : a.k_heads), per = 2 * swz::kNormThreads / (a.head_dim / 8);
-  const int64_t blocks = (rows + per - 1) / per, most = 8 * (int64_t)compute_units();
-  return (int)(blocks < 1 ? 1 : blocks < most ? blocks : most);
+// Workgroups that have an item for each of their D / 8 lanes.
+int norm_workgroups(int items, int head_dim) {
+  const int per = swz::kNormThreads / (head_dim / 8);
+  return items / per + (items % per != 0);
+}
+// Of the backward pass: as many as have items, at most four to a compute unit.
+int norm_backward_workgroups(const swz::NormArgs& n, int head_dim) {
+  const int most = 4 * compute_units(), some = norm_workgroups(n.q.items > n.k.items ? n.q.items : n.k.items, head_dim);
+  return some < 1 ? 1 : some < most ? some : most;
 }
 
 // ---------------------------------------------------------------- prompts
@@ -115,12 +119,6 @@ swz::PromptArgs prompt_args(const swz_attention_args& a) {
 
 // Workgroups for tiles of `rows` tokens (see find_slot) and `heads` heads; the launch refuses what is too many threads.
 int64_t slots_of(int64_t total, int sequences, int rows, int per = 1) { return total / rows + (int64_t)per * sequences; }
-
-template <class Kernel, class Args>
-int launch_slots(Kernel kernel, int64_t slots, int heads, int threads, hipStream_t stream, const Args& args) {
-  if (slots * heads >= kTokens) return SWZ_ERR_OVERFLOW;
-  return launch(kernel, dim3((unsigned)(slots * heads)), dim3((unsigned)threads), 0, stream, args);
-}
 
 // The launch of a kernel over prompts: `slots` turns, of `splits` workgroups each, `group` query heads of a key head apart or (1) together.
 template <auto KERNEL, class Args>
@@ -199,7 +197,11 @@ int store_or_read(const swz_cache4* cache, const swz_heads* k, const swz_heads* 
     a.cu = cu, a.before = before, a.total = (int)tokens, a.sequences = sequences;
     a.head_blocks = (cache->k_heads + swz::StoreShape<D>::kHeads - 1) / swz::StoreShape<D>::kHeads;
     auto kernel = READ ? swz::cache4_read_kernel<D> : swz::cache4_append_kernel<D>;
-    return launch_slots(kernel, slots_of(tokens, sequences, 8, 2), a.head_blocks, 256, stream, a);
+    // a workgroup for every block of heads where that does not fill the chip twice over, else one for all of them
+    const int64_t slots = slots_of(tokens, sequences, 8, 2);
+    a.splits = slots * a.head_blocks <= 4 * (int64_t)compute_units() ? a.head_blocks : 1;
+    if (slots * a.splits >= kTokens) return (int)SWZ_ERR_OVERFLOW;
+    return launch(kernel, dim3((unsigned)(slots * a.splits)), dim3(256), 0, stream, a);
   });
 }
 
@@ -239,17 +241,15 @@ int swz_qk_norm_rope(const swz_norm_args* args, hipStream_t stream) {
   return for_head_dim(args->head_dim, [&](auto dim) {
     return for_flag(args->interleaved != 0, [&](auto interleaved) {
       constexpr int D = decltype(dim)::value;
-      const int per = swz::kNormUnroll * swz::kNormThreads / (D / 8);
-      n.blocks_q = (n.rows[0] + per - 1) / per;
-      const int blocks_k = (n.rows[1] + per - 1) / per;
-      return launch(swz::qk_norm_kernel<D, decltype(interleaved)::value>, dim3((unsigned)(n.blocks_q + blocks_k)), dim3(swz::kNormThreads), 0, stream, n);
+      n.workgroups_q = norm_workgroups(n.q.items, D);
+      return launch(swz::qk_norm_kernel<D, decltype(interleaved)::value>, dim3((unsigned)(n.workgroups_q + norm_workgroups(n.k.items, D))), dim3(swz::kNormThreads), 0, stream, n);
     });
   });
 }
 
 int64_t swz_qk_norm_rope_backward_workspace(const swz_norm_args* args) {
   const int st = check_norm(args);
-  return st != SWZ_OK ? st : (int64_t)norm_backward_blocks(*args) * 2 * args->head_dim * 4;
+  return st != SWZ_OK ? st : (int64_t)norm_backward_workgroups(norm_args(*args), args->head_dim) * 2 * args->head_dim * 4;
 }
 
 int swz_qk_norm_rope_backward(const swz_norm_args* args, const swz_heads* dq, const swz_heads* dk, float* dq_weight, float* dk_weight,
@@ -259,19 +259,19 @@ int swz_qk_norm_rope_backward(const swz_norm_args* args, const swz_heads* dq, co
   if (dq == nullptr || dk == nullptr || dq_weight == nullptr || dk_weight == nullptr || workspace == nullptr) return SWZ_ERR_INVALID_ARG;
   st = check_heads(*dq, *dk);
   if (st != SWZ_OK) return st;
-  if (!aligned(dq_weight, 4) || !aligned(dk_weight, 4) || !aligned(workspace, 16)) return SWZ_ERR_UNSUPPORTED;
+  if (!aligned(dq_weight, 16) || !aligned(dk_weight, 16) || !aligned(workspace, 16)) return SWZ_ERR_UNSUPPORTED;
   if (workspace_bytes < swz_qk_norm_rope_backward_workspace(args)) return SWZ_ERR_INVALID_ARG;
   swz::NormArgs n = norm_args(*args);
-  n.dx[0] = device_heads(*dq), n.dx[1] = device_heads(*dk);
+  n.q.dx = device_heads(*dq), n.k.dx = device_heads(*dk);
   n.partial = static_cast<float*>(workspace);
-  const int blocks = norm_backward_blocks(*args);
+  const int blocks = norm_backward_workgroups(n, args->head_dim);
   st = for_head_dim(args->head_dim, [&](auto dim) {
     return for_flag(args->interleaved != 0, [&](auto interleaved) {
       return launch(swz::qk_norm_backward_kernel<decltype(dim)::value, decltype(interleaved)::value>, dim3((unsigned)blocks), dim3(swz::kNormThreads), 0, stream, n);
     });
   });
   if (st != SWZ_OK) return st;
-  return launch(swz::norm_weights_kernel, dim3((unsigned)(2 * args->head_dim / 16)), dim3(256), 0, stream, n.partial, blocks, args->head_dim, dq_weight, dk_weight);
+  return launch(swz::norm_weights_kernel, dim3((unsigned)(2 * args->head_dim / 4)), dim3(256), 0, stream, n.partial, blocks, args->head_dim, dq_weight, dk_weight);
 }
 
 int64_t swz_attention_workspace(const swz_attention_args* args) {

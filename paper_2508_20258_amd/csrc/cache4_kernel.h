@@ -37,41 +37,50 @@ __device__ __forceinline__ float over8(float x, Op op) {
   return op(x, dpp(x, std::integral_constant<int, 0x141>{}));
 }
 
-// Step and low (as a scale word) and the numbers of a group, 8 values in each of 8 lanes.
-__device__ __forceinline__ uint32_t quantise8(const u32x4& v, uint32_t (&number)[8]) {
+// Step and low (as a scale word) and the numbers (whole, as floats) of a group, 8 values in each of 8 lanes.  The number is that of the rounded quotient of x - low and step.  A product
+// with 1 / step, corrected by its residual, is that quotient: what is left of the error is 2^-45 of it, and a quotient of 24 bits by 8 is no nearer than 2^-33 to a boundary of
+// rounding.  A division instead is twice the instructions, and the vector unit is the bound.  Infinities, NaN and steps below the normal range come out as NaN and are
+// divided.
+__device__ __forceinline__ uint32_t quantise8(const u32x4& v, float (&number)[8]) {
   float x[8];
   unpack8(v, x);
-  float low = x[0], high = x[0], odd = 0.f;
+  float low = fminf(x[0], x[1]), high = fmaxf(x[0], x[1]);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    low = fminf(low, x[e]);
-    high = fmaxf(high, x[e]);
-    odd += x[e] * 0.f;                                       // NaN where an entry is no finite number
+  for (int e = 2; e < 8; e += 2) {
+    low = fminf(low, fminf(x[e], x[e + 1]));
+    high = fmaxf(high, fmaxf(x[e], x[e + 1]));
   }
   low = over8(low, [](float a, float b) { return fminf(a, b); });
   high = over8(high, [](float a, float b) { return fmaxf(a, b); });
-  odd = over8(odd, [](float a, float b) { return a + b; });
   const float range = high - low;
-  if (odd != 0.f || !(range < INFINITY)) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) number[e] = 0;
-    return 0x7fc07fc0u;                                      // NaN, NaN
-  }
   const uint32_t scale = pack_bf16(range / 15.f, low);
-  const float step = __uint_as_float(scale << 16);
+  const float step = __uint_as_float(scale << 16), inverse = step > 0.f ? __builtin_amdgcn_rcpf(step) : 0.f;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) number[e] = step > 0.f ? (uint32_t)fminf(rintf((x[e] - low) / step), 15.f) : 0u;
-  return scale;
+  for (int e = 0; e < 8; ++e) {
+    const float above = x[e] - low, quotient = above * inverse;
+    number[e] = rintf(__builtin_fmaf(__builtin_fmaf(-quotient, step, above), inverse, quotient));
+  }
+  const float all = ((number[0] + number[1]) + (number[2] + number[3])) + ((number[4] + number[5]) + (number[6] + number[7]));
+  if (!__any(!(all >= 0.f))) return scale;
+  float odd = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) odd += x[e] * 0.f;             // NaN where an entry is no finite number
+  odd = over8(odd, [](float a, float b) { return a + b; });
+  const bool bad = odd != 0.f || !(range < INFINITY);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) number[e] = !bad && step > 0.f ? fminf(rintf((x[e] - low) / step), 15.f) : 0.f;
+  return bad ? 0x7fc07fc0u : scale;                          // NaN, NaN
 }
 
 struct StoreArgs {
   CacheArgs c;
   Heads k, v;
   const int32_t *cu, *before;
-  int total, sequences, head_blocks;
+  int total, sequences, head_blocks, splits;         // workgroup i of `splits` for a word takes head blocks i, i + splits, ..
 };
 
-// Eight neighbouring positions of a sequence (a word of values) and 2048 / D heads a workgroup.  The slots of a sequence start at its tokens / 8 + 2 * b,
+// Eight neighbouring positions of a sequence (a word of values) a workgroup, 256 / D heads at a time: finding the place takes four loads one after another, longer than the
+// loads of the heads, which are then on their way a turn ahead.  The slots of a sequence start at its tokens / 8 + 2 * b,
 // as its positions start anywhere in a word.
 template <int D>
 struct StoreShape {
@@ -102,80 +111,103 @@ __device__ __forceinline__ StorePlace store_place(const StoreArgs& a, int slot) 
 template <int D>
 __global__ void __launch_bounds__(256) cache4_append_kernel(StoreArgs a) {
   using S = StoreShape<D>;
-  __shared__ __attribute__((aligned(16))) unsigned char numbers[S::kHeads][8][D];
-  const int slot = (int)blockIdx.x / a.head_blocks, head0 = ((int)blockIdx.x - slot * a.head_blocks) * S::kHeads;
+  __shared__ __attribute__((aligned(16))) unsigned char numbers[2][S::kHeads][8][D];
+  const int slot = (int)blockIdx.x / a.splits, split = (int)blockIdx.x - slot * a.splits;
   const StorePlace p = store_place(a, slot);
   if (p.from >= p.to || p.page < 0) return;
-  const int lane = (int)threadIdx.x % S::kLanes, e = ((int)threadIdx.x / S::kLanes) % 8, mine = (int)threadIdx.x / (8 * S::kLanes), head = head0 + mine;
-  const bool real = head < a.c.k_heads && e >= p.from && e < p.to;
-  u32x4 k = u32x4{}, v = u32x4{};
-  if (real) {
-    k = *reinterpret_cast<const u32x4*>(a.k.at(p.token + e, head) + lane * 8);
-    v = *reinterpret_cast<const u32x4*>(a.v.at(p.token + e, head) + lane * 8);
-  }
-  const int64_t at = a.c.token_at(p.page, min(head, a.c.k_heads - 1), p.position + e);
-  uint32_t n[8];
-  uint32_t scale = quantise8(k, n);
-  if (real) {
-    uint32_t word = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) word |= n[i] << number_shift(i);
-    a.c.k_words[at * (D / 8) + (D / 32) * (lane & 3) + (lane >> 2)] = word;
-    if ((lane & 7) == 0) a.c.k_scales[at * (D / 64) + (lane >> 3)] = scale;
-  }
-  scale = quantise8(v, n);
-  if (real && (lane & 7) == 0) a.c.v_scales[at * (D / 64) + (lane >> 3)] = scale;
-  *reinterpret_cast<u32x2*>(&numbers[mine][e][lane * 8]) =
-      u32x2{n[0] | n[1] << 8 | n[2] << 16 | n[3] << 24, n[4] | n[5] << 8 | n[6] << 16 | n[7] << 24};
-  __syncthreads();
+  const int lane = (int)threadIdx.x % S::kLanes, place = ((int)threadIdx.x / S::kLanes) % 8, mine = (int)threadIdx.x / (8 * S::kLanes);
   const int d = (int)threadIdx.x % D, h = (int)threadIdx.x / D;
-  if (head0 + h >= a.c.k_heads) return;
-  uint32_t word = 0, mask = 0;
+  const bool token = place >= p.from && place < p.to;
+  uint32_t mask = 0;                                         // numbers of a word that are written
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (i >= p.from && i < p.to) {
-      word |= (uint32_t)numbers[h][i][d] << number_shift(i);
-      mask |= 15u << number_shift(i);
+  for (int i = 0; i < 8; ++i) mask |= i >= p.from && i < p.to ? 15u << number_shift(i) : 0u;
+  u32x4 k = u32x4{}, v = u32x4{};
+  auto load = [&](int block) {
+    const int head = block * S::kHeads + mine;
+    if (!token || head >= a.c.k_heads) return;
+    k = *reinterpret_cast<const u32x4*>(a.k.at(p.token + place, head) + lane * 8);
+    v = *reinterpret_cast<const u32x4*>(a.v.at(p.token + place, head) + lane * 8);
+  };
+  load(split);
+  for (int block = split, turn = 0; block < a.head_blocks; block += a.splits, turn ^= 1) {
+    const int head = block * S::kHeads + mine;
+    const bool real = token && head < a.c.k_heads;
+    const int64_t at = a.c.token_at(p.page, min(head, a.c.k_heads - 1), p.position + place);
+    const u32x4 keys = k, values = v;
+    if (block + a.splits < a.head_blocks) load(block + a.splits);
+    float n[8];
+    uint32_t scale = quantise8(keys, n);
+    if (real) {
+      // number 2 i + h in bits 4 (i + 4 h)
+      const float even = __builtin_fmaf(__builtin_fmaf(n[6], 16.f, n[4]), 256.f, __builtin_fmaf(n[2], 16.f, n[0]));
+      const float odd = __builtin_fmaf(__builtin_fmaf(n[7], 16.f, n[5]), 256.f, __builtin_fmaf(n[3], 16.f, n[1]));
+      a.c.k_words[at * (D / 8) + (D / 32) * (lane & 3) + (lane >> 2)] = (uint32_t)odd << 16 | (uint32_t)even;
+      if ((lane & 7) == 0) a.c.k_scales[at * (D / 64) + (lane >> 3)] = scale;
     }
-  uint32_t* to = a.c.v_words + (a.c.token_at(p.page, head0 + h, p.position) >> 3) * D + d;
-  if (mask != 0xffffffffu) word |= *to & ~mask;              // tokens that were there before
-  *to = word;
+    scale = quantise8(values, n);
+    if (real && (lane & 7) == 0) a.c.v_scales[at * (D / 64) + (lane >> 3)] = scale;
+    u32x2 bytes = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bytes[e / 4] |= (uint32_t)n[e] << (8 * (e % 4));
+    *reinterpret_cast<u32x2*>(&numbers[turn][mine][place][lane * 8]) = bytes;
+    __syncthreads();
+    if (block * S::kHeads + h < a.c.k_heads) {
+      uint32_t word = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) word |= (uint32_t)numbers[turn][h][i][d] << number_shift(i);
+      word &= mask;
+      uint32_t* to = a.c.v_words + (a.c.token_at(p.page, block * S::kHeads + h, p.position) >> 3) * D + d;
+      if (mask != 0xffffffffu) word |= *to & ~mask;          // tokens that were there before
+      *to = word;
+    }
+  }
 }
 
 template <int D>
 __global__ void __launch_bounds__(256) cache4_read_kernel(StoreArgs a) {
   using S = StoreShape<D>;
-  __shared__ __attribute__((aligned(16))) uint16_t values[S::kHeads][8][D];
-  const int slot = (int)blockIdx.x / a.head_blocks, head0 = ((int)blockIdx.x - slot * a.head_blocks) * S::kHeads;
+  __shared__ __attribute__((aligned(16))) uint16_t values[2][S::kHeads][8][D];
+  const int slot = (int)blockIdx.x / a.splits, split = (int)blockIdx.x - slot * a.splits;
   const StorePlace p = store_place(a, slot);
   if (p.from >= p.to) return;
-  const int lane = (int)threadIdx.x % S::kLanes, e = ((int)threadIdx.x / S::kLanes) % 8, mine = (int)threadIdx.x / (8 * S::kLanes), head = head0 + mine;
-  const bool real = head < a.c.k_heads && e >= p.from && e < p.to;
+  const int lane = (int)threadIdx.x % S::kLanes, place = ((int)threadIdx.x / S::kLanes) % 8, mine = (int)threadIdx.x / (8 * S::kLanes);
+  const int d = (int)threadIdx.x % D, h = (int)threadIdx.x / D;
+  const bool token = place >= p.from && place < p.to;
   auto value = [](uint32_t scale, uint32_t n) { return __builtin_fmaf(__uint_as_float(scale << 16), (float)n, __uint_as_float(scale & 0xffff0000u)); };
-  if (real) {
-    uint32_t word = 0, scale = 0x7fc07fc0u;
-    if (p.page >= 0) {
-      const int64_t at = a.c.token_at(p.page, head, p.position + e);
-      word = a.c.k_words[at * (D / 8) + (D / 32) * (lane & 3) + (lane >> 2)];
-      scale = a.c.k_scales[at * (D / 64) + (lane >> 3)];
+  constexpr uint32_t kNan = 0x7fc07fc0u;
+  uint32_t k_word = 0, k_scale = kNan, v_word = 0, v_scale[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v_scale[i] = kNan;
+  auto load = [&](int block) {
+    if (p.page < 0) return;
+    const int head = block * S::kHeads + mine, v_head = block * S::kHeads + h;
+    if (token && head < a.c.k_heads) {
+      const int64_t at = a.c.token_at(p.page, head, p.position + place);
+      k_word = a.c.k_words[at * (D / 8) + (D / 32) * (lane & 3) + (lane >> 2)];
+      k_scale = a.c.k_scales[at * (D / 64) + (lane >> 3)];
     }
+    if (v_head < a.c.k_heads) {
+      const int64_t at = a.c.token_at(p.page, v_head, p.position);
+      v_word = a.c.v_words[(at >> 3) * D + d];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v_scale[i] = a.c.v_scales[(at + i) * (D / 64) + d / 64];
+    }
+  };
+  load(split);
+  for (int block = split, turn = 0; block < a.head_blocks; block += a.splits, turn ^= 1) {
     float x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = value(scale, word >> number_shift(i) & 15u);
-    *reinterpret_cast<u32x4*>(a.k.at(p.token + e, head) + lane * 8) = pack8(x);
-  }
-  const int d = (int)threadIdx.x % D, h = (int)threadIdx.x / D;
-  if (head0 + h < a.c.k_heads) {
-    const int64_t at = p.page < 0 ? 0 : a.c.token_at(p.page, head0 + h, p.position);
-    const uint32_t word = p.page < 0 ? 0u : a.c.v_words[(at >> 3) * D + d];
-#pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const uint32_t scale = p.page < 0 ? 0x7fc07fc0u : a.c.v_scales[(at + i) * (D / 64) + d / 64];
-      values[h][i][d] = __builtin_bit_cast(uint16_t, (__bf16)value(scale, word >> number_shift(i) & 15u));
+      x[i] = value(k_scale, k_word >> number_shift(i) & 15u);
+      values[turn][h][i][d] = __builtin_bit_cast(uint16_t, (__bf16)value(v_scale[i], v_word >> number_shift(i) & 15u));
     }
+    if (block + a.splits < a.head_blocks) load(block + a.splits);
+    const int head = block * S::kHeads + mine;
+    const bool real = token && head < a.c.k_heads;
+    if (real) *reinterpret_cast<u32x4*>(a.k.at(p.token + place, head) + lane * 8) = pack8(x);
+    __syncthreads();
+    if (real) *reinterpret_cast<u32x4*>(a.v.at(p.token + place, head) + lane * 8) = *reinterpret_cast<const u32x4*>(&values[turn][mine][place][lane * 8]);
   }
-  __syncthreads();
-  if (real) *reinterpret_cast<u32x4*>(a.v.at(p.token + e, head) + lane * 8) = *reinterpret_cast<const u32x4*>(&values[mine][e][lane * 8]);
 }
 
 // ---------------------------------------------------------------- attention of one token of each sequence
