@@ -10,7 +10,7 @@ from __future__ import annotations
 import ctypes
 from typing import NamedTuple
 
-from .binding import _check, _launch_stream, lib, torch
+from .binding import _NoFast, _check, _fast, _launch_stream, lib, torch
 
 EXPORTS = ("swz_qk_norm_rope", "swz_qk_norm_rope_backward_workspace", "swz_qk_norm_rope_backward", "swz_attention_workspace", "swz_attention", "swz_attention_backward_workspace",
            "swz_attention_backward", "swz_cache4_append", "swz_cache4_read", "swz_cache4_attention_workspace", "swz_cache4_attention")
@@ -56,6 +56,17 @@ def _declare() -> None:
 
 
 _declare()
+if _fast is not _NoFast:
+    _fast.bind_attention(*(ctypes.cast(getattr(lib, "swz_" + name), ctypes.c_void_p).value for name in (
+        "qk_norm_rope", "qk_norm_rope_backward_workspace", "qk_norm_rope_backward", "attention_workspace", "attention", "attention_backward_workspace",
+        "attention_backward", "cache4_append", "cache4_read", "cache4_attention_workspace", "cache4_attention")))
+
+
+def _done(result, where: str):
+    """What the ordinary call returned: its result, or the status it failed with."""
+    if result.__class__ is int:
+        _check(result, where)
+    return result
 
 
 def _heads(t) -> _Heads:
@@ -110,6 +121,10 @@ def qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions, q_out=None, k_ou
     q (tokens, q_heads, head_dim), k (tokens, k_heads, head_dim); weights (head_dim,) bfloat16; cos, sin (positions, rotary_dim / 2) float32 tables; positions
     (tokens,) int32.  Pairs are (i, i + rotary_dim / 2), or neighbours with `interleaved`; dimensions from rotary_dim on are not turned.  The outputs may be q and
     k themselves.  A position outside the tables gives NaN."""
+    if stream is None and q_out is None and k_out is None:
+        done = _fast.qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
+        if done is not None:
+            return _done(done, "swz_qk_norm_rope")
     q_out, k_out = _out(q_out, q), _out(k_out, k)
     a = _norm_args(q, k, q_out, k_out, q_weight, k_weight, cos, sin, positions, eps, interleaved)
     h = _launch_stream(stream, q, k, q_out, k_out, q_weight, k_weight, cos, sin, positions)
@@ -121,6 +136,10 @@ def qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions, q_out=None, k_ou
 def qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, positions, dq=None, dk=None, eps: float = 1e-6, interleaved: bool = False, stream=None):
     """(dq, dk, dq_weight, dk_weight) from the gradients of qk_norm_rope's outputs and its inputs; the weights' gradients are float32 sums over all tokens and
     heads.  dq, dk may be dq_out, dk_out themselves."""
+    if stream is None and dq is None and dk is None:
+        done = _fast.qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
+        if done is not None:
+            return _done(done, "swz_qk_norm_rope_backward")
     assert _is_heads(dq_out, *q.shape) and _is_heads(dk_out, *k.shape)
     dq, dk = _out(dq, q), _out(dk, k)
     a = _norm_args(q, k, dq_out, dk_out, q_weight, k_weight, cos, sin, positions, eps, interleaved)
@@ -160,6 +179,10 @@ def attention(q, k, v, cu_q, cu_k=None, out=None, lse=None, causal: bool = True,
 
     q (tokens, q_heads, head_dim), k and v (key tokens, k_heads, head_dim), q_heads a multiple of k_heads; cu_k where keys belong to other tokens than queries.
     causal: the last query of a sequence looks at all its keys, each before at one fewer.  scale: head_dim ** -0.5 by default."""
+    if stream is None and out is None and lse is None:
+        done = _fast.attention(q, k, v, cu_q, cu_k, causal, scale)
+        if done is not None:
+            return _done(done, "swz_attention")
     cu_k = _check_prompt(q, k, v, cu_q, cu_k)
     out = _out(out, q)
     if lse is None:
@@ -179,6 +202,10 @@ def attention(q, k, v, cu_q, cu_k=None, out=None, lse=None, causal: bool = True,
 
 def attention_backward(dout, q, k, v, out, lse, cu_q, cu_k=None, dq=None, dk=None, dv=None, causal: bool = True, scale: float | None = None, stream=None):
     """(dq, dk, dv) from the gradient of attention's out, its arguments and what it returned."""
+    if stream is None and dq is None and dk is None and dv is None:
+        done = _fast.attention_backward(dout, q, k, v, out, lse, cu_q, cu_k, causal, scale)
+        if done is not None:
+            return _done(done, "swz_attention_backward")
     cu_k = _check_prompt(q, k, v, cu_q, cu_k)
     assert _is_heads(dout, *q.shape) and _is_heads(out, *q.shape)
     assert lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (q.shape[1], q.shape[0])
@@ -237,6 +264,10 @@ def cache4_append(cache: Cache4, k, v, cu, before, block_table, stream=None) -> 
 
     k, v (tokens, k_heads, head_dim); before (sequences,) int32, the tokens already there; block_table (sequences, width) int32, the page of positions page_tokens * j ..
     at [b, j].  Positions beyond the table and entries that name no page (-1) are not written.  A page belongs to one sequence of a call."""
+    if stream is None:
+        status = _fast.cache4_append(cache, k, v, cu, before, block_table)
+        if status is not None:
+            return _check(status, "swz_cache4_append")
     c = _cache(cache)
     assert _is_heads(k, None, c.k_heads, c.head_dim) and _is_heads(v, *k.shape)
     n = before.shape[0]
@@ -249,6 +280,10 @@ def cache4_append(cache: Cache4, k, v, cu, before, block_table, stream=None) -> 
 
 def cache4_read(cache: Cache4, cu, first, block_table, tokens: int, k=None, v=None, stream=None):
     """(k, v): positions first[b] .. of every sequence, cu[b + 1] - cu[b] of them, as bfloat16 (tokens, k_heads, head_dim); tokens is cu's last entry."""
+    if stream is None and k is None and v is None:
+        done = _fast.cache4_read(cache, cu, first, block_table, tokens)
+        if done is not None:
+            return _done(done, "swz_cache4_read")
     c = _cache(cache)
     n = first.shape[0]
     assert _is_ints(first, n) and _is_ints(cu, n + 1) and block_table.dim() == 2 and _is_ints(block_table, n, block_table.shape[1])
@@ -267,6 +302,10 @@ def cache4_read(cache: Cache4, cu, first, block_table, tokens: int, k=None, v=No
 def cache4_attention(q, cache: Cache4, lengths, block_table, max_length: int = 0, out=None, scale: float | None = None, stream=None):
     """Attention of one token of each sequence (q: (sequences, q_heads, head_dim)) over the first lengths[b] positions of the cache, its own appended before.
     A sequence of length 0 gets 0.  max_length: the longest length if the program knows it; it decides how sequences are split over the device."""
+    if stream is None and out is None:
+        done = _fast.cache4_attention(q, cache, lengths, block_table, max_length, scale)
+        if done is not None:
+            return _done(done, "swz_cache4_attention")
     c = _cache(cache)
     assert _is_heads(q, None, None, c.head_dim)
     n, q_heads, dim = q.shape

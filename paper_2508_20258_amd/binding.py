@@ -95,6 +95,7 @@ lib = _load()
 class _NoFast:
     """In the place of _fastcall.so: nothing is an ordinary call."""
     gemm = transpose = softmax = layernorm = staticmethod(lambda *args: None)
+    qk_norm_rope = qk_norm_rope_backward = attention = attention_backward = cache4_append = cache4_read = cache4_attention = gemm
 
 
 def _load_fast():

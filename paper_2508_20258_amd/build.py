@@ -32,7 +32,7 @@ FLAGS = [
 ]
 
 
-FAST_DEPS = [FAST_SOURCE, os.path.join(HERE, "..", "include", "swz.h")]
+FAST_DEPS = [FAST_SOURCE, os.path.join(HERE, "..", "include", "swz.h"), os.path.join(HERE, "..", "include", "swz_attention.h")]
 
 
 def rocm_include() -> str:
