@@ -63,7 +63,7 @@ int swz_qk_norm_rope_backward(const swz_norm_args* args, const swz_heads* dq, co
  *   causal not 0: the last query of a sequence looks at all its keys, each query before at one key fewer; with fewer keys than queries the
  *   first queries look at nothing.  A query that looks at nothing gets out = 0, lse = -inf.
  *   The weights are rounded to bfloat16 for their product with v, their sum is not.  Infinities and NaN in keys and values that a query does not look
- *   at do not reach its output. */
+ *   at do not reach its output.   The distances of tokens of q, k, v (and dout below) are less than 2^28 elements. */
 typedef struct {
   swz_heads q, k, v, out;
   float* lse;                        /* q_heads x total_q, dense */
@@ -115,9 +115,10 @@ int swz_cache4_read(const swz_cache4* cache, const swz_heads* k, const swz_heads
 
 /* Attention of one token of each sequence over the first lengths[b] positions of the cache, its own among them.  A sequence of length 0 gets 0; one longer
  * than its table is cut to it; pages that the cache has not give NaN.
- *   q, out : sequences tokens of q_heads heads.   max_length : the longest length, or more (0: the table's); it decides how sequences are split, not the result's meaning.
+ *   q, out : sequences tokens of q_heads heads.   max_length : the longest length, or more (0: the table's); it decides how many waves share the work, no
+ *   more: longer lengths are right too, and slower.
  *   The weights times the steps of v are rounded to bfloat16 for their product with v's numbers.
- *   workspace : swz_cache4_attention_workspace(...) bytes, 16-byte aligned; may be null where that is 0. */
+ *   workspace : swz_cache4_attention_workspace(...) bytes, 16-byte aligned. */
 int64_t swz_cache4_attention_workspace(const swz_cache4* cache, int32_t sequences, int32_t q_heads, int32_t table_width, int32_t max_length);
 int swz_cache4_attention(const swz_cache4* cache, const swz_heads* q, const swz_heads* out, const int32_t* lengths, const int32_t* block_table,
                          int32_t table_width, int32_t sequences, int32_t q_heads, int32_t max_length, float scale, void* workspace, int64_t workspace_bytes,

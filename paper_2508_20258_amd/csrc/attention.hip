@@ -20,6 +20,7 @@ using swz::launch;
 using swz::query_device;
 
 constexpr int64_t kTokens = (int64_t)1 << 31;      // fewer than these
+constexpr int64_t kRowDistance = (int64_t)1 << 28;      // less than this from one token to the next, where tiles of tokens are loaded (RowLoader)
 
 swz::Heads device_heads(const swz_heads& h) { return {static_cast<uint16_t*>(h.data), h.token, h.head}; }
 
@@ -104,6 +105,7 @@ int check_prompt(const swz_attention_args* a) {
   if (!(a->scale > 0.f) || !isfinite(a->scale)) return SWZ_ERR_INVALID_ARG;
   const int st = check_heads(a->q, a->k, a->v, a->out);
   if (st != SWZ_OK) return st;
+  if (a->q.token >= kRowDistance || a->k.token >= kRowDistance || a->v.token >= kRowDistance) return SWZ_ERR_UNSUPPORTED;
   if (!head_dim_ok(a->head_dim) || !aligned(a->lse, 4) || !aligned(a->cu_q, 4) || !aligned(a->cu_k, 4)) return SWZ_ERR_UNSUPPORTED;
   return a->total_q >= kTokens || a->total_k >= kTokens ? SWZ_ERR_OVERFLOW : SWZ_OK;
 }
@@ -157,9 +159,28 @@ constexpr int kDqWaves = 4;
 
 template <int D>
 struct DkvShape {
-  static constexpr int kKeyWaves = D == 128 ? 4 : 2, kBlocks = 1, kParts = 2;
-  static constexpr int kKeys = 32 * kKeyWaves * kBlocks, kThreads = 64 * kKeyWaves * kParts;
+  static constexpr int kKeyWaves = D == 128 ? 4 : 2, kParts = 2;
+  static constexpr int kKeys = 32 * kKeyWaves, kThreads = 64 * kKeyWaves * kParts;
 };
+
+// How many workgroups share the queries of a tile of keys and leave their sums to another kernel: where tiles and key heads give less than a workgroup for half of the
+// compute units (a compute unit holds one of 512 threads, or three of 256), as many as give two (four of 256 threads) to each, or one for every eight rounds of the
+// queries of an average sequence, if that is fewer, as writing and reading the sums takes about as long as ten rounds.  8 query heads of one key head, 4096 causal tokens, the
+// whole gradient: 928 us whole, 268 with 15 splits; 32 heads of 8, 2048 tokens: 312 whole, 210 with 3; 16 of 2, 2007 tokens of four sequences: 263 whole, 103 with 7, 113 with 15.
+int dkv_splits(const swz_attention_args& a) {
+  auto splits = [&](auto shape) {
+    using K = decltype(shape);
+    const int64_t room = (K::kThreads == 512 ? 2 : 4) * (int64_t)compute_units() / (slots_of(a.total_k, 1, K::kKeys) * a.k_heads);
+    const int64_t rounds = (a.total_q / a.sequences / swz::kBackRows + 1) * (a.q_heads / a.k_heads) / K::kParts, most = room < rounds / 8 ? room : rounds / 8;
+    return (int)(most < 1 ? 1 : most < 16 ? most : 16);
+  };
+  return a.head_dim == 128 ? splits(DkvShape<128>{}) : splits(DkvShape<64>{});
+}
+// Statistics of queries, then the splits' sums.
+int64_t backward_floats(const swz_attention_args& a, int splits) {
+  const int64_t stats = (2 * a.total_q * a.q_heads + 3) / 4 * 4;
+  return stats + (splits == 1 ? 0 : (int64_t)splits * a.total_k * a.k_heads * 2 * a.head_dim);
+}
 
 // ---------------------------------------------------------------- the cache
 
@@ -314,8 +335,7 @@ int swz_attention(const swz_attention_args* args, void* workspace, int64_t works
 
 int64_t swz_attention_backward_workspace(const swz_attention_args* args) {
   const int st = check_prompt(args);
-  if (st != SWZ_OK) return st;
-  return 2 * args->total_q * args->q_heads * 4;
+  return st != SWZ_OK ? st : 4 * backward_floats(*args, dkv_splits(*args));
 }
 
 int swz_attention_backward(const swz_attention_args* args, const swz_heads* dout, const swz_heads* dq, const swz_heads* dk, const swz_heads* dv,
@@ -325,25 +345,34 @@ int swz_attention_backward(const swz_attention_args* args, const swz_heads* dout
   if (dout == nullptr || dq == nullptr || dk == nullptr || dv == nullptr || workspace == nullptr) return SWZ_ERR_INVALID_ARG;
   st = check_heads(*dout, *dq, *dk, *dv);
   if (st != SWZ_OK) return st;
-  if (!aligned(workspace, 16)) return SWZ_ERR_UNSUPPORTED;
+  if (!aligned(workspace, 16) || dout->token >= kRowDistance) return SWZ_ERR_UNSUPPORTED;
   if (workspace_bytes < swz_attention_backward_workspace(args)) return SWZ_ERR_INVALID_ARG;
   swz::PromptBackArgs p{};
   p.f = prompt_args(*args);
   p.dout = device_heads(*dout), p.dq = device_heads(*dq), p.dk = device_heads(*dk), p.dv = device_heads(*dv);
   p.log_sums = static_cast<float*>(workspace);
   p.deltas = p.log_sums + args->total_q * args->q_heads;
+  const int splits = dkv_splits(*args);
+  p.f.part_sums = p.log_sums + backward_floats(*args, 1);
   return for_head_dim(args->head_dim, [&](auto dim) {
     return for_flag(args->causal != 0, [&](auto causal) {
       constexpr int D = decltype(dim)::value;
       constexpr bool kCausal = decltype(causal)::value;
       using K = DkvShape<D>;
       const int64_t q_slots = slots_of(args->total_q, args->sequences, 32 * kDqWaves), k_slots = slots_of(args->total_k, args->sequences, K::kKeys);
+      const int64_t sum_slots = slots_of(args->total_k, args->sequences, swz::SumShape<D>::kKeys);
       const int group = args->q_heads / args->k_heads;
-      if (too_many_threads(q_slots, args->k_heads, group, p.f.num_xcd, 64 * kDqWaves) || too_many_threads(k_slots, args->k_heads, 1, p.f.num_xcd, K::kThreads)) return (int)SWZ_ERR_OVERFLOW;
+      if (too_many_threads(q_slots, args->k_heads, group, p.f.num_xcd, 64 * kDqWaves) || too_many_threads(k_slots * splits, args->k_heads, 1, p.f.num_xcd, K::kThreads) ||
+          (splits > 1 && too_many_threads(sum_slots, args->k_heads, 1, p.f.num_xcd, swz::kSumThreads))) {
+        return (int)SWZ_ERR_OVERFLOW;
+      }
       int status = SWZ_OK;
       if (args->total_q > 0) status = launch_prompt<swz::attention_dq_kernel<D, kDqWaves, kCausal>>(p, p.f, q_slots, 1, group, 64 * kDqWaves, stream);
       if (status != SWZ_OK || args->total_k == 0) return status;
-      return launch_prompt<swz::attention_dkv_kernel<D, K::kKeyWaves, K::kBlocks, K::kParts, kCausal>>(p, p.f, k_slots, 1, 1, K::kThreads, stream);
+      status = launch_prompt<swz::attention_dkv_kernel<D, K::kKeyWaves, K::kParts, kCausal>>(p, p.f, k_slots, splits, 1, K::kThreads, stream);
+      if (status != SWZ_OK || splits == 1) return status;
+      p.f.slots = (int)sum_slots;
+      return launch(swz::attention_dkv_sum_kernel<D>, dim3((unsigned)swz::prompt_workgroups(sum_slots, args->k_heads, 1, p.f.num_xcd)), dim3(swz::kSumThreads), 0, stream, p);
     });
   });
 }

@@ -68,34 +68,48 @@ __global__ void __launch_bounds__(NW * 64, 2) attention_dq_kernel(PromptBackArgs
   for (int i = 0; i < D / 32; ++i) acc[i] = f32x16{};
   const float c = a.scale * kLog2E;
 
-  for (int t = 0; t < tiles; ++t) {
-    publish();
-    if (t + 1 < tiles) fetch(t + 1);
-    const int k0 = t * kPromptKeys;
-    if (k0 >= wave_keys) continue;
-    const uint32_t at = lds + (uint32_t)((t & 1) * S::kTileBytes);
-    const uint32_t k_lane = row_address<D>(at, lane), v_lane = row_address<D>(at + 2 * S::kTileBytes, lane), kt_lane = column_address<D>(at, lane);
-    const bool masked = k0 + kPromptKeys > all_keys;
+  auto pass = [&](auto careful) __attribute__((always_inline)) {
+    for (int t = 0; t < tiles; ++t) {
+      publish();
+      if (t + 1 < tiles) fetch(t + 1);
+      const int k0 = t * kPromptKeys;
+      if (k0 >= wave_keys) continue;
+      const uint32_t at = lds + (uint32_t)((t & 1) * S::kTileBytes);
+      const uint32_t k_lane = row_address<D>(at, lane), v_lane = row_address<D>(at + 2 * S::kTileBytes, lane), kt_lane = column_address<D>(at, lane);
+      const bool masked = k0 + kPromptKeys > all_keys;
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      f32x16 s = f32x16{}, dp = f32x16{};
+      for (int b = 0; b < 2; ++b) {
+        f32x16 s = f32x16{}, dp = f32x16{};
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) s = mfma32(read_rows<D>(k_lane, b, i), qf[i], s);
+        for (int i = 0; i < D / 16; ++i) s = mfma32(read_rows<D>(k_lane, b, i), qf[i], s);
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) dp = mfma32(read_rows<D>(v_lane, b, i), gf[i], dp);
+        for (int i = 0; i < D / 16; ++i) dp = mfma32(read_rows<D>(v_lane, b, i), gf[i], dp);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -lse)) * (dp[r] - delta);
-      if (masked) {
-        const int last = last_key - k0 - 32 * b - 4 * h;
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -lse)) * (dp[r] - delta);
+        const int last = last_key - k0 - 32 * b;
+        if (masked) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = 8 * (r / 4) + r % 4 <= last ? s[r] : 0.f;
+          for (int r = 0; r < 16; ++r) s[r] = 8 * (r / 4) + 4 * h + r % 4 <= last ? s[r] : 0.f;
+        }
+        const u32x4 ds[2] = {as_words(s, 0), as_words(s, 1)};
+        if (decltype(careful)::value && masked) {
+          add_by_row<D, 32>(acc, ds, smem + (t & 1) * S::kTileBytes + b * 64 * D, 0, last, lane);
+          continue;
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int i = 0; i < D / 32; ++i) acc[i] = mfma32(read_columns<D>(kt_lane, 2 * b + j, i), __builtin_bit_cast(bf16x8, ds[j]), acc[i]);
       }
+    }
+  };
+  pass(std::false_type{});
+  if constexpr (CAUSAL) {            // a key that is no finite number and only some rows of a tile look at: as in the forward kernel
+    if (__builtin_expect(any_wave<NW>(__any(odd_sums(acc) != 0.f), smem, wave, lane), 0)) {
+      if (tiles > 0) fetch(0);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const bf16x8 ds = as_operand(s, j);
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) acc[i] = mfma32(read_columns<D>(kt_lane, 2 * b + j, i), ds, acc[i]);
-      }
+      for (int i = 0; i < D / 32; ++i) acc[i] = f32x16{};
+      pass(std::true_type{});
     }
   }
   store_columns<D>(acc, a.scale, args.dq.at(token, head), real, lane);
@@ -108,49 +122,55 @@ __global__ void __launch_bounds__(NW * 64, 2) attention_dq_kernel(PromptBackArgs
 constexpr int kBackRows = 32;      // queries of a tile
 __device__ const float kMinusInfinity = -INFINITY;
 
-template <int D, int KW, int KB, int QP>
+template <int D, int KW, int QP>
 struct BackShape {
-  static constexpr int kKeys = 32 * KW * KB, kThreads = 64 * KW * QP;
+  static constexpr int kKeys = 32 * KW, kThreads = 64 * KW * QP;
   static constexpr int kTileBytes = kBackRows * 2 * D;       // of q, or of dout
   static constexpr int kGroupBytes = 4 * kTileBytes;         // q and dout of one tile, then of the next
   static constexpr int kKeyBytes = kKeys * 2 * D, kKeysAt = QP * kGroupBytes, kStatsAt = kKeysAt + 2 * kKeyBytes;      // keys, values, statistics
   static constexpr int kLdsBytes = kStatsAt + QP * 2 * 2 * kBackRows * 4;
-  static constexpr int kAccBytes = KB * (D / 32) * 4096;     // of a wave: dk or dv
-  static_assert(kLdsBytes <= 160 * 1024 && (QP == 1 || QP / 2 * KW * kAccBytes <= kLdsBytes), "LDS");
+  static constexpr int kAccBytes = (D / 32) * 4096;     // of a wave: dk or dv
+  static_assert(kLdsBytes <= 160 * 1024 && QP / 2 * KW * kAccBytes <= kLdsBytes, "LDS");
 };
 
-template <int D, int KW, int KB, int QP, bool CAUSAL>
-__global__ void __launch_bounds__(64 * KW * QP, D == 64 ? (KB == 2 ? 2 : 3) : (KB == 2 ? 1 : 2)) attention_dkv_kernel(PromptBackArgs args) {
+template <int D, int KW, int QP, bool CAUSAL>
+__global__ void __launch_bounds__(64 * KW * QP, D == 64 ? 3 : 2) attention_dkv_kernel(PromptBackArgs args) {
   const PromptArgs& a = args.f;
-  using S = BackShape<D, KW, KB, QP>;
+  using S = BackShape<D, KW, QP>;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[S::kLdsBytes];
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
   const int lane = threadIdx.x & 63, h = lane >> 5, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int wave = w % KW, part = QP == 1 ? 0 : w / KW;
+  const int wave = w % KW, part = w / KW;
 
   const int group = a.q_heads / a.k_heads;
-  const PromptPiece piece = prompt_piece((int)blockIdx.x, a.slots, a.k_heads, 1, a.num_xcd, a.sets);
+  const PromptPiece piece = prompt_piece((int)blockIdx.x, a.slots * a.splits, a.k_heads, 1, a.num_xcd, a.sets);
   if (piece.turn < 0) return;
-  const int k_head = piece.k_head;
-  const TurnPlace place = find_turn(a.cu_k, a.total_k, a.cu_q, a.total_q, a.sequences, S::kKeys, piece.turn);
+  const int k_head = piece.k_head, split = a.splits == 1 ? 0 : piece.turn % a.splits;
+  const TurnPlace place = find_turn(a.cu_k, a.total_k, a.cu_q, a.total_q, a.sequences, S::kKeys, a.splits == 1 ? piece.turn : piece.turn / a.splits);
   const Span q = place.other, k = place.mine;
   const int first = place.tile * S::kKeys;
   if (place.tile < 0 || first >= k.length) return;
 
-  const int key0 = first + wave * 32 * KB, key = key0 + (lane & 31);       // and with KB = 2 the key 32 behind it
+  const int key0 = first + wave * 32, key = key0 + (lane & 31);
   const int ahead = k.length - q.length;
   const int from = CAUSAL ? clamp_to(first - ahead, 0, q.length) / kBackRows : 0;      // the first tile of queries that looks at a key of the workgroup
-  const int tiles = (q.length + kBackRows - 1) / kBackRows - from, steps = tiles > 0 ? tiles * group : 0, rounds = (steps + QP - 1) / QP;
+  const int tiles = (q.length + kBackRows - 1) / kBackRows - from, steps = tiles > 0 ? tiles * group : 0;
+  const int stride = QP * a.splits, rounds = max(0, (steps - QP * split + stride - 1) / stride);        // of this split's groups
 
   const RowLoader<D, S::kKeys, KW * QP> load_k(a.k.at(k.first, k_head), a.k.token, k.length, w, lane), load_v(a.v.at(k.first, k_head), a.v.token, k.length, w, lane);
   if (rounds > 0) load_k(first, lds + S::kKeysAt), load_v(first, lds + S::kKeysAt + S::kKeyBytes);
 
-  // this group's steps: query head k_head * group + member, tile `tile` of it, QP further each round
+  // this group's steps: query head k_head * group + member, tile `tile` of it, `stride` further each round
   RowLoader<D, kBackRows, KW> load_q(a.q.data, a.q.token, q.length, wave, lane), load_g(args.dout.data, args.dout.token, q.length, wave, lane);
   const uint32_t tile_lds = lds + (uint32_t)(part * S::kGroupBytes), stats_lds = lds + (uint32_t)(S::kStatsAt + part * 4 * kBackRows * 4);
-  int member = tiles > 0 ? part / tiles : 0, tile = part - member * tiles;
+  int member, tile;
+  auto begin = [&]() {
+    member = tiles > 0 ? (QP * split + part) / tiles : 0;
+    tile = QP * split + part - member * tiles;
+  };
+  begin();
   auto advance = [&]() {
-    tile += QP;
+    tile += stride;
     while (tile >= tiles) tile -= tiles, ++member;
   };
   auto fetch = [&](int round) __attribute__((always_inline)) {         // of (member, tile), the round's
@@ -170,11 +190,9 @@ __global__ void __launch_bounds__(64 * KW * QP, D == 64 ? (KB == 2 ? 2 : 3) : (K
   if (rounds > 0) fetch(0);
 
   constexpr int kSteps = D / 16, kParts = D / 32;
-  f32x16 dk[KB][kParts], dv[KB][kParts];
+  f32x16 dk[kParts], dv[kParts];
 #pragma unroll
-  for (int b = 0; b < KB; ++b)
-#pragma unroll
-    for (int i = 0; i < kParts; ++i) dk[b][i] = dv[b][i] = f32x16{};
+  for (int i = 0; i < kParts; ++i) dk[i] = dv[i] = f32x16{};
   const float c = a.scale * kLog2E;
   uint32_t q_at = row_address<D>(tile_lds, lane), g_at = q_at + S::kTileBytes, column_at[kParts][2];
   keep(g_at);                        // or the compiler shares their steps' addresses, and has no registers for them
@@ -183,31 +201,40 @@ __global__ void __launch_bounds__(64 * KW * QP, D == 64 ? (KB == 2 ? 2 : 3) : (K
     keep(column_at[i][0] = column_address<D>(tile_lds, lane) ^ (uint32_t)(i << 6));
     keep(column_at[i][1] = (column_address<D>(tile_lds, lane) ^ (uint32_t)(i << 6) ^ 32u) + 16u * D);
   }
-  const uint32_t key_at = row_address<D>(lds + (uint32_t)(S::kKeysAt + wave * KB * 64 * D), lane);
+  const uint32_t key_at = row_address<D>(lds + (uint32_t)(S::kKeysAt + wave * 64 * D), lane);
   uint32_t value_at = key_at + S::kKeyBytes;
   keep(value_at);
   typedef __attribute__((address_space(3))) const f32x4* stat_ptr;
   uint32_t stat_at = stats_lds + (uint32_t)(16 * h);
 
+  auto start = [&](f32x16& s, f32x16& dp) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x4 x = *(stat_ptr)(uintptr_t)(stat_at + (uint32_t)(32 * i)), y = *(stat_ptr)(uintptr_t)(stat_at + (uint32_t)(32 * i + kBackRows * 4));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[4 * i + e] = x[e], dp[4 * i + e] = y[e];
+    }
+  };
+  auto looks = [&](int r0) { return member < group && !(CAUSAL && r0 + kBackRows - 1 + ahead < key0); };      // some of these rows do, at a key of this wave
+  auto masked = [&](int r0) { return (CAUSAL && r0 + ahead < key0 + 31) || key0 + 32 > k.length; };
+  auto first_row = [&](int r0) { return key < k.length ? (CAUSAL ? key - ahead - r0 : 0) : kBackRows; };     // of those that look at the lane's key
+  auto mask = [&](f32x16& s, int r0) __attribute__((always_inline)) {
+    const int from_row = first_row(r0) - 4 * h;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = 8 * (r / 4) + r % 4 >= from_row ? s[r] : -INFINITY;
+  };
   for (int round = 0; round < rounds; ++round) {
     publish();
     const int r0 = (from + tile) * kBackRows;
-    const bool mine = member < group && !(CAUSAL && r0 + kBackRows - 1 + ahead < key0);       // some of these rows look at a key of this wave
+    const bool mine = looks(r0);
     advance();
     if (round + 1 < rounds) fetch(round + 1);
     if (mine) {
-      f32x16 s[KB], dp[KB];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f32x4 x = *(stat_ptr)(uintptr_t)(stat_at + (uint32_t)(32 * i)), y = *(stat_ptr)(uintptr_t)(stat_at + (uint32_t)(32 * i + kBackRows * 4));
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-          for (int b = 0; b < KB; ++b) s[b][4 * i + e] = x[e], dp[b][4 * i + e] = y[e];
-      }
-      // Slots of KB products with one A: S, dP, dv, dk.
+      f32x16 s, dp;
+      start(s, dp);
+      // Slots of one product each: S, dP, dv, dk.
       constexpr int kAhead = 2, kRing = kAhead + 1;
-      bf16x8 f[kRing], kf[kRing][KB];
+      bf16x8 f[kRing], kf[kRing];
       auto read_a = [&](auto slot) __attribute__((always_inline)) {
         constexpr int i = decltype(slot)::value, j = i - 2 * kSteps;
         if constexpr (i < 2 * kSteps) return read_rows<D>(i < kSteps ? q_at : g_at, 0, i % kSteps);
@@ -215,10 +242,9 @@ __global__ void __launch_bounds__(64 * KW * QP, D == 64 ? (KB == 2 ? 2 : 3) : (K
       };
       auto read_k = [&](auto slot) __attribute__((always_inline)) {
         constexpr int i = decltype(slot)::value;
-#pragma unroll
-        for (int b = 0; b < KB; ++b) kf[i % kRing][b] = read_rows<D>(i < kSteps ? key_at : value_at, b, i % kSteps);
+        kf[i % kRing] = read_rows<D>(i < kSteps ? key_at : value_at, 0, i % kSteps);
       };
-      constexpr int kSlots = 2 * kSteps + 4 * kParts, kPairs = 8 * KB;       // pairs of weights, of blocks 0 and 1 in turn
+      constexpr int kSlots = 2 * kSteps + 4 * kParts, kPairs = 8;       // pairs of weights
       for_each_index([&](auto slot) __attribute__((always_inline)) {
         f[decltype(slot)::value] = read_a(slot);
         read_k(slot);
@@ -228,29 +254,18 @@ __global__ void __launch_bounds__(64 * KW * QP, D == 64 ? (KB == 2 ? 2 : 3) : (K
         constexpr int i = decltype(slot)::value;
         f[(i + kAhead) % kRing] = read_a(std::integral_constant<int, i + kAhead>{});
         read_k(std::integral_constant<int, i + kAhead>{});
-#pragma unroll
-        for (int b = 0; b < KB; ++b) s[b] = mfma32(f[i % kRing], kf[i % kRing][b], s[b]);
+        s = mfma32(f[i % kRing], kf[i % kRing], s);
         __builtin_amdgcn_sched_barrier(0);
       }, std::make_integer_sequence<int, kSteps>{});
-      if ((CAUSAL && r0 + ahead < key0 + 32 * KB - 1) || key0 + 32 * KB > k.length) {
-#pragma unroll
-        for (int b = 0; b < KB; ++b) {
-          const int at = key + 32 * b, first_row = (at < k.length ? (CAUSAL ? at - ahead - r0 : 0) : 64) - 4 * h;          // of those that look at this key
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[b][r] = 8 * (r / 4) + r % 4 >= first_row ? s[b][r] : -INFINITY;
-        }
-      }
-      u32x4 p[KB][2], ds[KB][2];
+      if (masked(r0)) mask(s, r0);
+      u32x4 p[2], ds[2];
       for_each_index([&](auto slot) __attribute__((always_inline)) {
         constexpr int u = decltype(slot)::value, i = kSteps + u, j = i - 2 * kSteps;
         if constexpr (i + kAhead < kSlots) f[(i + kAhead) % kRing] = read_a(std::integral_constant<int, i + kAhead>{});
         if constexpr (i + kAhead < 2 * kSteps) read_k(std::integral_constant<int, i + kAhead>{});
-#pragma unroll
-        for (int b = 0; b < KB; ++b) {
-          if constexpr (i < 2 * kSteps) dp[b] = mfma32(f[i % kRing], kf[i % kRing][b], dp[b]);
-          else if constexpr (j < 2 * kParts) dv[b][j % kParts] = mfma32(f[i % kRing], __builtin_bit_cast(bf16x8, p[b][j / kParts]), dv[b][j % kParts]);
-          else dk[b][j % kParts] = mfma32(f[i % kRing], __builtin_bit_cast(bf16x8, ds[b][j / kParts - 2]), dk[b][j % kParts]);
-        }
+        if constexpr (i < 2 * kSteps) dp = mfma32(f[i % kRing], kf[i % kRing], dp);
+        else if constexpr (j < 2 * kParts) dv[j % kParts] = mfma32(f[i % kRing], __builtin_bit_cast(bf16x8, p[j / kParts]), dv[j % kParts]);
+        else dk[j % kParts] = mfma32(f[i % kRing], __builtin_bit_cast(bf16x8, ds[j / kParts - 2]), dk[j % kParts]);
         // weights while dP and the first half of dv are multiplied (half of them before any of dv, all before its second half), then the gradients of
         // the scores, half of them before any of dk
         constexpr int kW = kSteps + kParts, kD = 3 * kParts;
@@ -258,15 +273,15 @@ __global__ void __launch_bounds__(64 * KW * QP, D == 64 ? (KB == 2 ? 2 : 3) : (K
         constexpr auto slopes_before = [](int n) constexpr { return n >= kD ? kPairs : n <= 0 ? 0 : (n * kPairs + kD - 1) / kD; };
 #pragma unroll
         for (int n = weights_before(u); n < weights_before(u + 1); ++n) {
-          const int b = n % KB, e = n / KB * 2;
-          s[b][e] = __builtin_amdgcn_exp2f(s[b][e] * c);
-          s[b][e + 1] = __builtin_amdgcn_exp2f(s[b][e + 1] * c);
-          p[b][e / 8][e % 8 / 2] = pack_bf16(s[b][e], s[b][e + 1]);
+          const int e = 2 * n;
+          s[e] = __builtin_amdgcn_exp2f(s[e] * c);
+          s[e + 1] = __builtin_amdgcn_exp2f(s[e + 1] * c);
+          p[e / 8][e % 8 / 2] = pack_bf16(s[e], s[e + 1]);
         }
 #pragma unroll
         for (int n = slopes_before(j); n < slopes_before(j + 1); ++n) {
-          const int b = n % KB, e = n / KB * 2;
-          ds[b][e / 8][e % 8 / 2] = pack_bf16(s[b][e] * dp[b][e], s[b][e + 1] * dp[b][e + 1]);
+          const int e = 2 * n;
+          ds[e / 8][e % 8 / 2] = pack_bf16(s[e] * dp[e], s[e + 1] * dp[e + 1]);
         }
         __builtin_amdgcn_sched_barrier(0);
       }, std::make_integer_sequence<int, kSlots - kSteps>{});
@@ -282,46 +297,132 @@ __global__ void __launch_bounds__(64 * KW * QP, D == 64 ? (KB == 2 ? 2 : 3) : (K
     stat_at ^= 2 * kBackRows * 4;
   }
 
+  if constexpr (CAUSAL) {            // queries and gradients that are no finite numbers and look at some keys of a tile only: as in the forward kernel
+    if (__builtin_expect(any_wave<KW * QP>(__any(odd_sums(dv, odd_sums(dk)) != 0.f), smem, w, lane), 0)) {
+      begin();
+      if (rounds > 0) fetch(0);
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) dk[i] = dv[i] = f32x16{};
+      for (int round = 0; round < rounds; ++round) {
+        publish();
+        const int r0 = (from + tile) * kBackRows;
+        const bool mine = looks(r0);
+        advance();
+        if (round + 1 < rounds) fetch(round + 1);
+        if (!mine) continue;
+        const int tiles_at = part * S::kGroupBytes + (round & 1) * 2 * S::kTileBytes;
+        uint32_t l = (uint32_t)lane;
+        keep(l);                     // or these addresses have registers all along
+        const uint32_t q_lane = row_address<D>(lds + (uint32_t)tiles_at, (int)l), q_column = column_address<D>(lds + (uint32_t)tiles_at, (int)l);
+        stat_at = stats_lds + (uint32_t)(16 * h + (round & 1) * 2 * kBackRows * 4);
+        f32x16 s, dp;
+        start(s, dp);
+        // (one read at a time: few registers)
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+          s = mfma32(read_rows<D>(q_lane, 0, i), read_rows<D>(key_at, 0, i), s);
+          __builtin_amdgcn_sched_barrier(0);
+          dp = mfma32(read_rows<D>(q_lane + S::kTileBytes, 0, i), read_rows<D>(value_at, 0, i), dp);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        mask(s, r0);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r] * c);
+        const u32x4 weights[2] = {as_words(s, 0), as_words(s, 1)};
+        s *= dp;
+        const u32x4 ds[2] = {as_words(s, 0), as_words(s, 1)};
+        auto add = [&](f32x16 (&sum)[kParts], const u32x4 (&words)[2], int at) __attribute__((always_inline)) {
+          if (masked(r0)) {
+            add_by_row<D, kBackRows>(sum, words, smem + tiles_at + at, first_row(r0), kBackRows, lane);
+            return;
+          }
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < kParts; ++i) {
+              sum[i] = mfma32(read_columns<D>(q_column + (uint32_t)at, j, i), __builtin_bit_cast(bf16x8, words[j]), sum[i]);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        add(dv, weights, S::kTileBytes);
+        add(dk, ds, 0);
+      }
+    }
+  }
+
   // the groups in halves, first dk, then dv: the upper one's sums go to the lower one
-  auto join = [&](f32x16 (&x)[KB][kParts]) __attribute__((always_inline)) {
+  auto join = [&](f32x16 (&x)[kParts]) __attribute__((always_inline)) {
 #pragma unroll
     for (int half = QP / 2; half > 0; half /= 2) {
       publish();
       f32x4* held = reinterpret_cast<f32x4*>(smem) + lane;
-      auto at = [&](int p, int b, int i, int r) { return ((((p * KW + wave) * KB + b) * kParts + i) * 4 + r) * 64; };
+      auto at = [&](int p, int i, int r) { return (((p * KW + wave) * kParts + i) * 4 + r) * 64; };
       if (part >= half && part < 2 * half) {
 #pragma unroll
-        for (int b = 0; b < KB; ++b)
+        for (int i = 0; i < kParts; ++i)
 #pragma unroll
-          for (int i = 0; i < kParts; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) held[at(part - half, b, i, r)] = f32x4{x[b][i][4 * r], x[b][i][4 * r + 1], x[b][i][4 * r + 2], x[b][i][4 * r + 3]};
+          for (int r = 0; r < 4; ++r) held[at(part - half, i, r)] = f32x4{x[i][4 * r], x[i][4 * r + 1], x[i][4 * r + 2], x[i][4 * r + 3]};
       }
       publish();
       if (part < half) {
 #pragma unroll
-        for (int b = 0; b < KB; ++b)
+        for (int i = 0; i < kParts; ++i)
 #pragma unroll
-          for (int i = 0; i < kParts; ++i)
+          for (int r = 0; r < 4; ++r) {
+            const f32x4 y = held[at(part, i, r)];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const f32x4 y = held[at(part, b, i, r)];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) x[b][i][4 * r + e] += y[e];
-            }
+            for (int e = 0; e < 4; ++e) x[i][4 * r + e] += y[e];
+          }
       }
     }
   };
   join(dk);
   join(dv);
   if (part > 0) return;
+  const bool real = key < k.length;
+  if (a.splits > 1) {                // splits x total_k x k_heads x (dk, dv) x D
+    if (!real) return;
+    float* to = a.part_sums + (((int64_t)split * a.total_k + k.first + key) * a.k_heads + k_head) * 2 * D + 4 * h;
 #pragma unroll
-  for (int b = 0; b < KB; ++b) {
-    const bool real = key + 32 * b < k.length;
-    const int64_t token = k.first + min(key + 32 * b, k.length - 1);
-    store_columns<D>(dk[b], a.scale, args.dk.at(token, k_head), real, lane);
-    store_columns<D>(dv[b], 1.f, args.dv.at(token, k_head), real, lane);
+    for (int i = 0; i < kParts; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        *reinterpret_cast<f32x4*>(to + 32 * i + 2 * r) = f32x4{dk[i][r], dk[i][r + 1], dk[i][r + 2], dk[i][r + 3]};
+        *reinterpret_cast<f32x4*>(to + D + 32 * i + 2 * r) = f32x4{dv[i][r], dv[i][r + 1], dv[i][r + 2], dv[i][r + 3]};
+      }
+    return;
   }
+  const int64_t token = k.first + min(key, k.length - 1);
+  store_columns<D>(dk, a.scale, args.dk.at(token, k_head), real, lane);
+  store_columns<D>(dv, 1.f, args.dv.at(token, k_head), real, lane);
+}
+
+// The splits' sums of a key, dk and dv, added up in their order: D / 4 lanes for a key, four dimensions of both a lane.
+constexpr int kSumThreads = 256;
+template <int D>
+struct SumShape {
+  static constexpr int kLanes = D / 4, kKeys = kSumThreads / kLanes;
+};
+template <int D>
+__global__ void __launch_bounds__(kSumThreads) attention_dkv_sum_kernel(PromptBackArgs args) {
+  const PromptArgs& a = args.f;
+  using S = SumShape<D>;
+  const PromptPiece piece = prompt_piece((int)blockIdx.x, a.slots, a.k_heads, 1, a.num_xcd, a.sets);
+  if (piece.turn < 0) return;
+  const TurnPlace place = find_turn(a.cu_k, a.total_k, a.cu_q, a.total_q, a.sequences, S::kKeys, piece.turn);
+  const int key = place.tile * S::kKeys + (int)threadIdx.x / S::kLanes, d = (int)threadIdx.x % S::kLanes * 4;
+  if (place.tile < 0 || key >= place.mine.length) return;
+  const int64_t token = place.mine.first + key, step = (int64_t)a.total_k * a.k_heads * 2 * D;
+  const float* from = a.part_sums + (token * a.k_heads + piece.k_head) * 2 * D + d;
+  f32x4 dk = f32x4{}, dv = f32x4{};
+#pragma unroll 4
+  for (int s = 0; s < a.splits; ++s) {
+    dk += *reinterpret_cast<const f32x4*>(from + s * step);
+    dv += *reinterpret_cast<const f32x4*>(from + s * step + D);
+  }
+  dk *= a.scale;
+  *reinterpret_cast<u32x2*>(args.dk.at(token, piece.k_head) + d) = u32x2{pack_bf16(dk[0], dk[1]), pack_bf16(dk[2], dk[3])};
+  *reinterpret_cast<u32x2*>(args.dv.at(token, piece.k_head) + d) = u32x2{pack_bf16(dv[0], dv[1]), pack_bf16(dv[2], dv[3])};
 }
 
 }  // namespace swz

@@ -14,33 +14,58 @@ struct PromptShape {                   // a workgroup: QW waves of 32 rows each
   static constexpr int kTileBytes = kPromptKeys * 2 * D, kLdsBytes = 4 * kTileBytes;      // two tiles of keys, two of values
 };
 
-// o += p v for the 64 keys of a tile that the lane's row looks at (up to `last` of the tile), one at a time; p as the product with the values takes it.
-template <int D>
-__device__ __forceinline__ void add_by_key(f32x16 (&o)[D / 32], const u32x4 (&p)[4], const unsigned char* v_tile, int last, int lane) {
-  const int h = lane >> 5;
+// o += p x for rows `from` .. `to` (the lane's own) of ROWS of a tile, one at a time; p as the product with the tile's columns takes it.
+template <int D, int ROWS>
+__device__ __forceinline__ void add_by_row(f32x16 (&o)[D / 32], const u32x4 (&p)[ROWS / 16], const unsigned char* tile, int from, int to, int lane) {
 #pragma unroll 1
-  for (int key = 0; key < kPromptKeys; ++key) {
-    // key 16 j + 8 a + 4 h + e is number 4 a + e of operand j in lane half h
+  for (int row = 0; row < ROWS; ++row) {
+    uint32_t l = (uint32_t)lane;
+    keep(l);                         // or the loop has registers for its addresses, which are the kernel's
+    const int h = (int)l >> 5;
+    // row 16 j + 8 a + 4 h + e is number 4 a + e of operand j in lane half h
     uint32_t word = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < ROWS / 16; ++j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) word = j == key >> 4 && e == 2 * (key >> 3 & 1) + (key >> 1 & 1) ? p[j][e] : word;
-    const float mine = (key >> 2 & 1) == h ? __uint_as_float(key & 1 ? word & 0xffff0000u : word << 16) : 0.f;
+      for (int e = 0; e < 4; ++e) word = j == row >> 4 && e == 2 * (row >> 3 & 1) + (row >> 1 & 1) ? p[j][e] : word;
+    const float mine = (row >> 2 & 1) == h ? __uint_as_float(row & 1 ? word & 0xffff0000u : word << 16) : 0.f;
     const float w = across_halves(mine, [](float x, float y) { return x + y; });
-    const bool seen = key <= last;
+    const bool seen = row >= from && row <= to;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i)
 #pragma unroll
       for (int part = 0; part < 4; ++part) {
         typedef __attribute__((ext_vector_type(4))) uint16_t u16x4;
         const int d = 32 * i + 8 * part + 4 * h;
-        const u16x4 v = *reinterpret_cast<const u16x4*>(v_tile + key * 2 * D + (((d >> 3) ^ tile_key<D>(key)) << 4) + (d & 7) * 2);
+        const u16x4 x = *reinterpret_cast<const u16x4*>(tile + row * 2 * D + (((d >> 3) ^ tile_key<D>(row)) << 4) + (d & 7) * 2);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[i][4 * part + e] += seen ? w * __uint_as_float((uint32_t)v[e] << 16) : 0.f;
-        __builtin_amdgcn_sched_barrier(0);                  // few registers at a time: this path is rare, and they are the kernel's
+        for (int e = 0; e < 4; ++e) o[i][4 * part + e] += seen ? w * __uint_as_float((uint32_t)x[e] << 16) : 0.f;
+        __builtin_amdgcn_sched_barrier(0);                  // few registers at a time: this path is rare
       }
   }
+}
+
+// 0, or NaN where one of the sums is no finite number.
+template <int N>
+__device__ __forceinline__ float odd_sums(const f32x16 (&x)[N], float odd = 0.f) {
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) odd = __builtin_fmaf(x[i][r], 0.f, odd);
+  return odd;
+}
+// Whether `mine` is true in any of the workgroup's WAVES waves.  Takes the start of LDS, which no wave reads any more.
+template <int WAVES>
+__device__ __forceinline__ bool any_wave(bool mine, unsigned char* smem, int wave, int lane) {
+  publish();
+  uint32_t* flags = reinterpret_cast<uint32_t*>(smem);
+  if (lane == 0) flags[wave] = mine;
+  publish();
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i) any |= flags[i];
+  publish();
+  return __builtin_amdgcn_readfirstlane((int)any) != 0;
 }
 
 template <int D, int QW, bool CAUSAL>
@@ -228,21 +253,7 @@ __global__ void __launch_bounds__(64 * QW, D == 64 ? 3 : 2) attention_kernel(Pro
   // A weight of 0 times an infinity or NaN is NaN: where a value that only some rows of a tile look at is no finite number, the products carry it into the others.
   // The result shows it, and the tiles are then taken a second time, the masked ones key by key.
   if constexpr (CAUSAL) {
-    float odd = 0.f;
-#pragma unroll
-    for (int i = 0; i < kParts; ++i)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) odd = __builtin_fmaf(o[i][r], 0.f, odd);
-    const bool mine = __any(odd != 0.f);
-    publish();
-    uint32_t* flags = reinterpret_cast<uint32_t*>(smem);
-    if (lane == 0) flags[wave] = mine;
-    publish();
-    uint32_t again = 0;
-#pragma unroll
-    for (int i = 0; i < QW; ++i) again |= flags[i];
-    publish();
-    if (__builtin_expect(__builtin_amdgcn_readfirstlane((int)again) != 0, 0)) {
+    if (__builtin_expect(any_wave<QW>(__any(odd_sums(o) != 0.f), smem, wave, lane), 0)) {
       if (tiles > 0) fetch_k(0), fetch_v(0);
       top = -FLT_MAX;
       sum = 0.f;
@@ -263,7 +274,7 @@ __global__ void __launch_bounds__(64 * QW, D == 64 ? 3 : 2) attention_kernel(Pro
           p[n / 4][n % 4] = pack_bf16(w0, w1);
         }
         if (t >= whole) {
-          add_by_key<D>(o, p, smem + (2 + (t & 1)) * S::kTileBytes, last_key - first_key(t), lane);
+          add_by_row<D, kPromptKeys>(o, p, smem + (2 + (t & 1)) * S::kTileBytes, 0, last_key - first_key(t), lane);
         } else {
           const uint32_t v_lane = column_address<D>(lds + (uint32_t)((2 + (t & 1)) * S::kTileBytes), lane);
 #pragma unroll

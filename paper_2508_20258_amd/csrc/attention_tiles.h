@@ -40,7 +40,7 @@ struct PromptArgs {
   const int32_t *cu_q, *cu_k;
   int total_q, total_k, sequences, slots, q_heads, k_heads, num_xcd, sets;
   float scale;
-  int splits;                        // of a row's keys, in the forward pass: each writes what it has (splits x total_q x q_heads x head_dim, and maximum and sum)
+  int splits;                        // of a row's keys, forward, or of a tile's queries, backward: each writes what it has to the parts
   float *part_sums, *part_stats;
 };
 
@@ -240,11 +240,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 }
 
 // Registers 8 j .. 8 j + 7 of a product, rounded, as B of the next one.
-__device__ __forceinline__ bf16x8 as_operand(const f32x16& x, int j) {
+__device__ __forceinline__ u32x4 as_words(const f32x16& x, int j) {
   u32x4 w;
 #pragma unroll
   for (int e = 0; e < 4; ++e) w[e] = pack_bf16(x[8 * j + 2 * e], x[8 * j + 2 * e + 1]);
-  return __builtin_bit_cast(bf16x8, w);
+  return w;
 }
 
 // x of both halves of the wave: op over lanes l and l + 32.

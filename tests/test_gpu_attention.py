@@ -169,6 +169,77 @@ def test_what_is_not_looked_at_does_not_matter(swz, dim, bad):
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("q_lens,k_lens,q_heads,k_heads", [
+    ([600], [600], 8, 1), ([333], [333], 24, 2), ([200, 0, 301, 1], [200, 0, 301, 1], 20, 1), ([500], [170], 6, 1), ([150, 250], [700, 0], 16, 1)])
+def test_gradient_of_few_key_heads(swz, q_lens, k_lens, q_heads, k_heads, dim, causal):
+    """A tile of keys whose queries several workgroups share: their sums are added up by another kernel."""
+    nq, nk = sum(q_lens), sum(k_lens)
+    q, k, v, dout = randn(nq, nq, q_heads, dim, scale=2.0), randn(nq + 1, nk, k_heads, dim), randn(nq + 2, nk, k_heads, dim), randn(nq + 3, nq, q_heads, dim)
+    cu_q, cu_k = cu_of(q_lens), cu_of(k_lens)
+    out, lse = swz.attention(q, k, v, cu_q, cu_k, causal=causal)
+    grads = swz.attention_backward(dout, q, k, v, out, lse, cu_q, cu_k, causal=causal)
+    check_backward(q, k, v, dout, grads, q_lens, k_lens, causal, dim ** -0.5)
+    again = swz.attention_backward(dout, q, k, v, out, lse, cu_q, cu_k, causal=causal)
+    assert all(torch.equal(a, b) for a, b in zip(again, grads))
+
+
+@pytest.mark.parametrize("q_heads", [2, 16])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_gradients_of_what_is_not_looked_at(swz, dim, bad, q_heads):
+    """Infinities and NaN in keys, values, queries and gradients reach the gradients of what looks at them or is looked at by them, no others."""
+    lens, n, group = [300, 77], 377, q_heads // 2
+    q, k, v, dout = randn(7, n, q_heads, dim), randn(8, n, 2, dim), randn(9, n, 2, dim), randn(10, n, q_heads, dim)
+    cu = cu_of(lens)
+
+    def gradients(q, k, v, dout):
+        return swz.attention_backward(dout, q, k, v, *swz.attention(q, k, v, cu), cu)
+
+    clean = gradients(q, k, v, dout)
+
+    def near(got, want):                                  # the same numbers but for the order and rounding of their sums
+        return torch.isfinite(got).all() and (got.float() - want.float()).abs().max() <= 2 ** -6 * want.float().abs().max()
+
+    for at in (40, 100, 211):
+        k2, v2, q2, d2 = k.clone(), v.clone(), q.clone(), dout.clone()
+        k2[at, 0] = v2[at, 0] = bad
+        q2[at, 0] = bad
+        d2[at, 0] = bad
+        for dq, dk, dv in (gradients(q, k2, v, dout), gradients(q, k, v2, dout)):
+            # queries before the key, other key heads and sequences
+            assert near(dq[:at, :group], clean[0][:at, :group]) and torch.equal(dq[:, group:], clean[0][:, group:]) and torch.equal(dq[300:], clean[0][300:])
+            assert not torch.isfinite(dq[at:300, :group]).any()
+            assert torch.equal(dk[:, 1], clean[1][:, 1]) and torch.equal(dv[:, 1], clean[2][:, 1]) and torch.equal(dk[300:], clean[1][300:])
+        for dq, dk, dv in (gradients(q2, k, v, dout), gradients(q, k, v, d2)):
+            # keys behind the query, other heads and sequences
+            assert near(dk[at + 1:300, 0], clean[1][at + 1:300, 0]) and near(dv[at + 1:300, 0], clean[2][at + 1:300, 0])
+            assert not torch.isfinite(dk[:at + 1, 0]).any() and torch.equal(dk[:, 1], clean[1][:, 1]) and torch.equal(dv[300:], clean[2][300:])
+            assert near(dq[:at, 0], clean[0][:at, 0]) and torch.equal(dq[:, 1:], clean[0][:, 1:]) and not torch.isfinite(dq[at, 0]).any()
+
+
+def test_distances_between_tokens(swz):
+    # tiles are loaded with 32-bit offsets from their first row: longer distances are refused, not wrapped
+    memory, cu = torch.zeros((1 << 28) + 64, dtype=torch.bfloat16, device="cuda"), cu_of([2])
+    far, near = memory.as_strided((2, 1, 64), (1 << 28, 64, 1)), memory.as_strided((2, 1, 64), ((1 << 28) - 8, 64, 1))
+    near.copy_(randn(1, 2, 1, 64))
+    dense = near.contiguous()
+    out, lse = swz.attention(near, near, near, cu)
+    want = swz.attention(dense, dense, dense, cu)
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+    assert all(torch.equal(a, b) for a, b in zip(swz.attention_backward(near, near, near, near, out, lse, cu), swz.attention_backward(dense, dense, dense, dense, out, lse, cu)))
+    for which in range(3):
+        args = [dense] * 3
+        args[which] = far
+        with pytest.raises(swz.SwzError):
+            swz.attention(*args, cu)
+        with pytest.raises(swz.SwzError):
+            swz.attention_backward(dense, *args, out, lse, cu)
+    with pytest.raises(swz.SwzError):
+        swz.attention_backward(far, dense, dense, dense, out, lse, cu)
+
+
 def test_tokens_of_no_sequence_are_left_alone(swz):
     cu = torch.tensor([10, 50, 50, 90], dtype=torch.int32, device="cuda")
     q, k, v, dout = randn(1, 120, 2, 64), randn(2, 120, 1, 64), randn(3, 120, 1, 64), randn(4, 120, 2, 64)
