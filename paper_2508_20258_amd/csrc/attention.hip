@@ -122,7 +122,7 @@ swz::PromptArgs prompt_args(const swz_attention_args& a) {
 // Workgroups for tiles of `rows` tokens (see find_slot) and `heads` heads; the launch refuses what is too many threads.
 int64_t slots_of(int64_t total, int sequences, int rows, int per = 1) { return total / rows + (int64_t)per * sequences; }
 
-// The launch of a kernel over prompts: `slots` turns, of `splits` workgroups each, `group` query heads of a key head apart or (1) together.
+// The launch of a kernel over prompts: `slots` turns, of `splits` workgroups each, for each of `group` parts of a key head's query heads.
 template <auto KERNEL, class Args>
 int launch_prompt(Args& args, swz::PromptArgs& p, int64_t slots, int splits, int group, int threads, hipStream_t stream) {
   const int64_t workgroups = slots * splits < kTokens ? swz::prompt_workgroups(slots * splits, p.k_heads, group, p.num_xcd) : kTokens;
@@ -135,25 +135,30 @@ bool too_many_threads(int64_t slots, int heads_k, int group, int num_xcd, int th
   return slots >= kTokens || swz::prompt_workgroups(slots, heads_k, group, num_xcd) * threads > swz::kLaunchThreads;
 }
 
-// Forward: rows of a workgroup, and into how many pieces the keys of a row are cut.
-struct ForwardPlan {
-  int waves, splits;
-};
-ForwardPlan forward_plan(const swz_attention_args& a) {
-  const int64_t cus = compute_units(), group = a.q_heads / a.k_heads;
-  const int xcd = xcds();
-  const int64_t few = swz::prompt_workgroups(slots_of(a.total_q, 1, 128), a.k_heads, (int)group, xcd);       // workgroups of 128 rows, if the sequences were one
-  ForwardPlan p{4, 1};
-  if (a.head_dim == 128 && few >= 16 * cus) p.waves = 8;
-  const int64_t tiles = a.total_k / a.sequences / swz::kPromptKeys;                                      // of an average sequence
-  if (few < cus && tiles >= 16) {
-    int64_t splits = 2 * cus / few;
-    if (splits > tiles / 8) splits = tiles / 8;
-    p.splits = (int)(splits < 32 ? splits : 32);
-  }
-  return p;
+// Waves of a workgroup that share its tiles, 32 rows each (8 instead of 4: 0.7% less time at 32768 tokens, more at short ones).  As many of them as the sharing of key heads
+// allows have the same rows of another query head: a tile is then loaded once for all of them, and short sequences fill their workgroups.  Causal, 32 heads of 128 sharing 8,
+// with four query heads together and with the 128 rows of one: 32 sequences of 16 tokens 6.6 us and 11.8, of 200 37.6 and 44.8, of 512 124 and 139, one of 8192 499 and 501.
+constexpr int kPromptWaves = 4;
+int heads_together(const swz_attention_args& a) {
+  const int group = a.q_heads / a.k_heads;
+  return group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1;
 }
-int64_t forward_floats(const swz_attention_args& a, const ForwardPlan& p) { return p.splits == 1 ? 0 : (int64_t)p.splits * a.total_q * a.q_heads * (a.head_dim + 2); }
+template <class F>
+int for_heads_together(int heads, F&& f) {
+  return heads == 4 ? f(std::integral_constant<int, 4>{}) : heads == 2 ? f(std::integral_constant<int, 2>{}) : f(std::integral_constant<int, 1>{});
+}
+
+// Forward: into how many pieces the keys of a row are cut.
+int forward_splits(const swz_attention_args& a) {
+  const int64_t cus = compute_units();
+  const int heads = heads_together(a), group = a.q_heads / a.k_heads;
+  const int64_t few = swz::prompt_workgroups(slots_of(a.total_q, 1, 32 * kPromptWaves / heads), a.k_heads, group / heads, xcds());       // workgroups, if the sequences were one
+  const int64_t tiles = a.total_k / a.sequences / swz::kPromptKeys;                                      // of an average sequence
+  if (few >= cus || tiles < 16) return 1;
+  const int64_t splits = 2 * cus / few < tiles / 8 ? 2 * cus / few : tiles / 8;
+  return (int)(splits < 32 ? splits : 32);
+}
+int64_t forward_floats(const swz_attention_args& a, int splits) { return splits == 1 ? 0 : (int64_t)splits * a.total_q * a.q_heads * (a.head_dim + 2); }
 
 constexpr int kDqWaves = 4;
 
@@ -297,33 +302,29 @@ int swz_qk_norm_rope_backward(const swz_norm_args* args, const swz_heads* dq, co
 
 int64_t swz_attention_workspace(const swz_attention_args* args) {
   const int st = check_prompt(args);
-  return st != SWZ_OK ? st : 4 * forward_floats(*args, forward_plan(*args));
+  return st != SWZ_OK ? st : 4 * forward_floats(*args, forward_splits(*args));
 }
 
 int swz_attention(const swz_attention_args* args, void* workspace, int64_t workspace_bytes, hipStream_t stream) {
   const int st = check_prompt(args);
   if (st != SWZ_OK || args->total_q == 0) return st;
-  const ForwardPlan plan = forward_plan(*args);
-  const int64_t floats = forward_floats(*args, plan);
+  const int splits = forward_splits(*args);
+  const int64_t floats = forward_floats(*args, splits);
   if (floats > 0 && (workspace == nullptr || workspace_bytes < 4 * floats)) return SWZ_ERR_INVALID_ARG;
   if (!aligned(workspace, 16)) return SWZ_ERR_UNSUPPORTED;
   swz::PromptArgs p = prompt_args(*args);
-  p.splits = plan.splits;
   p.part_sums = static_cast<float*>(workspace);
   p.part_stats = p.part_sums + (floats > 0 ? floats / (args->head_dim + 2) * args->head_dim : 0);
   return for_head_dim(args->head_dim, [&](auto dim) {
     return for_flag(args->causal != 0, [&](auto causal) {
       constexpr int D = decltype(dim)::value;
       constexpr bool kCausal = decltype(causal)::value;
-      const int group = args->q_heads / args->k_heads;
-      auto go = [&](auto waves) {
-        constexpr int W = decltype(waves)::value;
-        return launch_prompt<swz::attention_kernel<D, W, kCausal>>(p, p, slots_of(args->total_q, args->sequences, 32 * W), plan.splits, group, 64 * W, stream);
-      };
-      int status = SWZ_ERR_UNSUPPORTED;
-      if constexpr (D == 128) status = plan.waves == 8 ? go(std::integral_constant<int, 8>{}) : go(std::integral_constant<int, 4>{});
-      else status = go(std::integral_constant<int, 4>{});
-      if (status != SWZ_OK || plan.splits == 1) return status;
+      const int status = for_heads_together(heads_together(*args), [&](auto heads) {
+        constexpr int H = decltype(heads)::value;
+        return launch_prompt<swz::attention_kernel<D, kPromptWaves, H, kCausal>>(p, p, slots_of(args->total_q, args->sequences, 32 * kPromptWaves / H), splits, args->q_heads / args->k_heads / H,
+                                                                                 64 * kPromptWaves, stream);
+      });
+      if (status != SWZ_OK || splits == 1) return status;
       p.sets = swz::prompt_sets(args->q_heads, p.num_xcd);
       const int64_t slots = slots_of(args->total_q, args->sequences, swz::kJoinRows);
       if (slots >= kTokens || swz::prompt_workgroups(slots, args->q_heads, 1, p.num_xcd) >= kTokens) return (int)SWZ_ERR_OVERFLOW;

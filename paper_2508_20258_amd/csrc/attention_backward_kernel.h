@@ -68,12 +68,12 @@ __global__ void __launch_bounds__(NW * 64, 2) attention_dq_kernel(PromptBackArgs
   for (int i = 0; i < D / 32; ++i) acc[i] = f32x16{};
   const float c = a.scale * kLog2E;
 
-  auto pass = [&](auto careful) __attribute__((always_inline)) {
+  auto pass = [&](auto careful, bool mine) __attribute__((always_inline)) {
     for (int t = 0; t < tiles; ++t) {
       publish();
       if (t + 1 < tiles) fetch(t + 1);
       const int k0 = t * kPromptKeys;
-      if (k0 >= wave_keys) continue;
+      if ((decltype(careful)::value && !mine) || k0 >= wave_keys) continue;
       const uint32_t at = lds + (uint32_t)((t & 1) * S::kTileBytes);
       const uint32_t k_lane = row_address<D>(at, lane), v_lane = row_address<D>(at + 2 * S::kTileBytes, lane), kt_lane = column_address<D>(at, lane);
       const bool masked = k0 + kPromptKeys > all_keys;
@@ -103,13 +103,16 @@ __global__ void __launch_bounds__(NW * 64, 2) attention_dq_kernel(PromptBackArgs
       }
     }
   };
-  pass(std::false_type{});
+  pass(std::false_type{}, true);
   if constexpr (CAUSAL) {            // a key that is no finite number and only some rows of a tile look at: as in the forward kernel
-    if (__builtin_expect(any_wave<NW>(__any(odd_sums(acc) != 0.f), smem, wave, lane), 0)) {
+    const bool mine = __any(odd_sums(acc) != 0.f);
+    if (__builtin_expect(any_wave<NW>(mine, smem, wave, lane), 0)) {
       if (tiles > 0) fetch(0);
+      if (mine) {
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i) acc[i] = f32x16{};
-      pass(std::true_type{});
+        for (int i = 0; i < D / 32; ++i) acc[i] = f32x16{};
+      }
+      pass(std::true_type{}, mine);
     }
   }
   store_columns<D>(acc, a.scale, args.dq.at(token, head), real, lane);
@@ -298,15 +301,18 @@ __global__ void __launch_bounds__(64 * KW * QP, D == 64 ? 3 : 2) attention_dkv_k
   }
 
   if constexpr (CAUSAL) {            // queries and gradients that are no finite numbers and look at some keys of a tile only: as in the forward kernel
-    if (__builtin_expect(any_wave<KW * QP>(__any(odd_sums(dv, odd_sums(dk)) != 0.f), smem, w, lane), 0)) {
+    const bool odd = __any(odd_sums(dv, odd_sums(dk)) != 0.f);
+    if (__builtin_expect(any_wave<KW * QP>(odd, smem, w, lane), 0)) {
       begin();
       if (rounds > 0) fetch(0);
+      if (odd) {
 #pragma unroll
-      for (int i = 0; i < kParts; ++i) dk[i] = dv[i] = f32x16{};
+        for (int i = 0; i < kParts; ++i) dk[i] = dv[i] = f32x16{};
+      }
       for (int round = 0; round < rounds; ++round) {
         publish();
         const int r0 = (from + tile) * kBackRows;
-        const bool mine = looks(r0);
+        const bool mine = odd && looks(r0);
         advance();
         if (round + 1 < rounds) fetch(round + 1);
         if (!mine) continue;

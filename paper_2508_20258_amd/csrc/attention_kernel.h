@@ -8,9 +8,9 @@ namespace swz {
 constexpr int kPromptKeys = 64;        // keys of a tile
 constexpr float kLazyRise = 8.f;       // a maximum that rises by less than 2^8 does not rescale what has been summed
 
-template <int D, int QW>
-struct PromptShape {                   // a workgroup: QW waves of 32 rows each
-  static constexpr int kRows = 32 * QW;
+template <int D, int QW, int HW = 1>
+struct PromptShape {                   // a workgroup: QW waves of 32 rows each, of HW query heads of a key head
+  static constexpr int kRows = 32 * QW / HW;
   static constexpr int kTileBytes = kPromptKeys * 2 * D, kLdsBytes = 4 * kTileBytes;      // two tiles of keys, two of values
 };
 
@@ -54,12 +54,12 @@ __device__ __forceinline__ float odd_sums(const f32x16 (&x)[N], float odd = 0.f)
     for (int r = 0; r < 16; ++r) odd = __builtin_fmaf(x[i][r], 0.f, odd);
   return odd;
 }
-// Whether `mine` is true in any of the workgroup's WAVES waves.  Takes the start of LDS, which no wave reads any more.
+// Whether x is true in any of the workgroup's WAVES waves.  Takes the start of LDS, which no wave reads any more.
 template <int WAVES>
-__device__ __forceinline__ bool any_wave(bool mine, unsigned char* smem, int wave, int lane) {
+__device__ __forceinline__ bool any_wave(bool x, unsigned char* smem, int wave, int lane) {
   publish();
   uint32_t* flags = reinterpret_cast<uint32_t*>(smem);
-  if (lane == 0) flags[wave] = mine;
+  if (lane == 0) flags[wave] = x;
   publish();
   uint32_t any = 0;
 #pragma unroll
@@ -68,23 +68,23 @@ __device__ __forceinline__ bool any_wave(bool mine, unsigned char* smem, int wav
   return __builtin_amdgcn_readfirstlane((int)any) != 0;
 }
 
-template <int D, int QW, bool CAUSAL>
+template <int D, int QW, int HW, bool CAUSAL>
 __global__ void __launch_bounds__(64 * QW, D == 64 ? 3 : 2) attention_kernel(PromptArgs a) {
-  using S = PromptShape<D, QW>;
+  using S = PromptShape<D, QW, HW>;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[S::kLdsBytes];
   const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
 
   const int group = a.q_heads / a.k_heads;
-  const PromptPiece piece = prompt_piece((int)blockIdx.x, a.slots * a.splits, a.k_heads, group, a.num_xcd, a.sets);
+  const PromptPiece piece = prompt_piece((int)blockIdx.x, a.slots * a.splits, a.k_heads, group / HW, a.num_xcd, a.sets);
   if (piece.turn < 0) return;
-  const int k_head = piece.k_head, head = k_head * group + piece.member, split = a.splits == 1 ? 0 : piece.turn % a.splits;
+  const int k_head = piece.k_head, head = k_head * group + piece.member * HW + wave % HW, split = a.splits == 1 ? 0 : piece.turn % a.splits;
   const TurnPlace place = find_turn(a.cu_q, a.total_q, a.cu_k, a.total_k, a.sequences, S::kRows, a.splits == 1 ? piece.turn : piece.turn / a.splits);
   const Span q = place.mine, k = place.other;
   const int first = ((q.length + S::kRows - 1) / S::kRows - 1 - place.tile) * S::kRows;      // a sequence's last rows look at the most keys
   if (place.tile < 0 || first < 0) return;
 
-  const int row0 = first + wave * 32, row = row0 + (lane & 31);
+  const int row0 = first + wave / HW * 32, row = row0 + (lane & 31);
   const int ahead = k.length - q.length;                    // causal: query i looks at keys 0 .. i + ahead
   auto keys_of = [&](int last_row) { return CAUSAL ? clamp_to(last_row + ahead + 1, 0, k.length) : k.length; };
   const int keys = keys_of(min(first + S::kRows, q.length) - 1);              // of any row of the workgroup,
@@ -253,16 +253,19 @@ __global__ void __launch_bounds__(64 * QW, D == 64 ? 3 : 2) attention_kernel(Pro
   // A weight of 0 times an infinity or NaN is NaN: where a value that only some rows of a tile look at is no finite number, the products carry it into the others.
   // The result shows it, and the tiles are then taken a second time, the masked ones key by key.
   if constexpr (CAUSAL) {
-    if (__builtin_expect(any_wave<QW>(__any(odd_sums(o) != 0.f), smem, wave, lane), 0)) {
+    const bool mine = __any(odd_sums(o) != 0.f);            // (the other waves keep what they have)
+    if (__builtin_expect(any_wave<QW>(mine, smem, wave, lane), 0)) {
       if (tiles > 0) fetch_k(0), fetch_v(0);
-      top = -FLT_MAX;
-      sum = 0.f;
+      if (mine) {
+        top = -FLT_MAX;
+        sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < kParts; ++i) o[i] = f32x16{};
+        for (int i = 0; i < kParts; ++i) o[i] = f32x16{};
+      }
       for (t = 0; t < tiles; ++t) {
         publish();
         if (t + 1 < tiles) fetch_k(t + 1), fetch_v(t + 1);
-        if (t >= wave_tiles) continue;
+        if (!mine || t >= wave_tiles) continue;
         score(s, t);
         mask(s, t);
         raise(highest(s));
