@@ -160,8 +160,6 @@ int forward_splits(const swz_attention_args& a) {
 }
 int64_t forward_floats(const swz_attention_args& a, int splits) { return splits == 1 ? 0 : (int64_t)splits * a.total_q * a.q_heads * (a.head_dim + 2); }
 
-constexpr int kDqWaves = 4;
-
 template <int D>
 struct DkvShape {
   static constexpr int kKeyWaves = D == 128 ? 4 : 2, kParts = 2;
@@ -360,15 +358,20 @@ int swz_attention_backward(const swz_attention_args* args, const swz_heads* dout
       constexpr int D = decltype(dim)::value;
       constexpr bool kCausal = decltype(causal)::value;
       using K = DkvShape<D>;
-      const int64_t q_slots = slots_of(args->total_q, args->sequences, 32 * kDqWaves), k_slots = slots_of(args->total_k, args->sequences, K::kKeys);
+      const int heads = heads_together(*args);
+      const int64_t q_slots = slots_of(args->total_q, args->sequences, 32 * kPromptWaves / heads), k_slots = slots_of(args->total_k, args->sequences, K::kKeys);
       const int64_t sum_slots = slots_of(args->total_k, args->sequences, swz::SumShape<D>::kKeys);
-      const int group = args->q_heads / args->k_heads;
-      if (too_many_threads(q_slots, args->k_heads, group, p.f.num_xcd, 64 * kDqWaves) || too_many_threads(k_slots * splits, args->k_heads, 1, p.f.num_xcd, K::kThreads) ||
+      const int group = args->q_heads / args->k_heads / heads;
+      if (too_many_threads(q_slots, args->k_heads, group, p.f.num_xcd, 64 * kPromptWaves) || too_many_threads(k_slots * splits, args->k_heads, 1, p.f.num_xcd, K::kThreads) ||
           (splits > 1 && too_many_threads(sum_slots, args->k_heads, 1, p.f.num_xcd, swz::kSumThreads))) {
         return (int)SWZ_ERR_OVERFLOW;
       }
       int status = SWZ_OK;
-      if (args->total_q > 0) status = launch_prompt<swz::attention_dq_kernel<D, kDqWaves, kCausal>>(p, p.f, q_slots, 1, group, 64 * kDqWaves, stream);
+      if (args->total_q > 0) {
+        status = for_heads_together(heads, [&](auto together) {
+          return launch_prompt<swz::attention_dq_kernel<D, kPromptWaves, decltype(together)::value, kCausal>>(p, p.f, q_slots, 1, group, 64 * kPromptWaves, stream);
+        });
+      }
       if (status != SWZ_OK || args->total_k == 0) return status;
       status = launch_prompt<swz::attention_dkv_kernel<D, K::kKeyWaves, K::kParts, kCausal>>(p, p.f, k_slots, splits, 1, K::kThreads, stream);
       if (status != SWZ_OK || splits == 1) return status;

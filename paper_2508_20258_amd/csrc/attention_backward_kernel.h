@@ -12,24 +12,24 @@ struct PromptBackArgs {
 };
 
 // dq, and delta for the other kernel.  As the forward kernel, with a third product: dq^T += k^T dS^T.
-template <int D, int NW, bool CAUSAL>
-__global__ void __launch_bounds__(NW * 64, 2) attention_dq_kernel(PromptBackArgs args) {
+template <int D, int NW, int HW, bool CAUSAL>
+__global__ void __launch_bounds__(NW * 64, D == 64 ? 3 : 2) attention_dq_kernel(PromptBackArgs args) {
   const PromptArgs& a = args.f;
-  using S = PromptShape<D, NW>;
+  using S = PromptShape<D, NW, HW>;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[S::kLdsBytes];
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5;
 
   const int group = a.q_heads / a.k_heads;
-  const PromptPiece piece = prompt_piece((int)blockIdx.x, a.slots, a.k_heads, group, a.num_xcd, a.sets);
+  const PromptPiece piece = prompt_piece((int)blockIdx.x, a.slots, a.k_heads, group / HW, a.num_xcd, a.sets);
   if (piece.turn < 0) return;
-  const int k_head = piece.k_head, head = k_head * group + piece.member;
+  const int k_head = piece.k_head, head = k_head * group + piece.member * HW + wave % HW;
   const TurnPlace place = find_turn(a.cu_q, a.total_q, a.cu_k, a.total_k, a.sequences, S::kRows, piece.turn);
   const Span q = place.mine, k = place.other;
   const int first = ((q.length + S::kRows - 1) / S::kRows - 1 - place.tile) * S::kRows;
   if (place.tile < 0 || first < 0) return;
 
-  const int row0 = first + wave * 32, row = row0 + (lane & 31);
+  const int row0 = first + wave / HW * 32, row = row0 + (lane & 31);
   const bool real = row < q.length;
   const int ahead = k.length - q.length;
   auto keys_of = [&](int last_row) { return CAUSAL ? clamp_to(last_row + ahead + 1, 0, k.length) : k.length; };
@@ -68,42 +68,78 @@ __global__ void __launch_bounds__(NW * 64, 2) attention_dq_kernel(PromptBackArgs
   for (int i = 0; i < D / 32; ++i) acc[i] = f32x16{};
   const float c = a.scale * kLog2E;
 
-  auto pass = [&](auto careful, bool mine) __attribute__((always_inline)) {
-    for (int t = 0; t < tiles; ++t) {
-      publish();
-      if (t + 1 < tiles) fetch(t + 1);
-      const int k0 = t * kPromptKeys;
-      if ((decltype(careful)::value && !mine) || k0 >= wave_keys) continue;
-      const uint32_t at = lds + (uint32_t)((t & 1) * S::kTileBytes);
-      const uint32_t k_lane = row_address<D>(at, lane), v_lane = row_address<D>(at + 2 * S::kTileBytes, lane), kt_lane = column_address<D>(at, lane);
-      const bool masked = k0 + kPromptKeys > all_keys;
+  auto mask = [&](f32x16& s, int first_key) __attribute__((always_inline)) {
+    const int last = last_key - first_key - 4 * h;
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        f32x16 s = f32x16{}, dp = f32x16{};
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) s = mfma32(read_rows<D>(k_lane, b, i), qf[i], s);
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) dp = mfma32(read_rows<D>(v_lane, b, i), gf[i], dp);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -lse)) * (dp[r] - delta);
-        const int last = last_key - k0 - 32 * b;
-        if (masked) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = 8 * (r / 4) + 4 * h + r % 4 <= last ? s[r] : 0.f;
-        }
-        const u32x4 ds[2] = {as_words(s, 0), as_words(s, 1)};
-        if (decltype(careful)::value && masked) {
-          add_by_row<D, 32>(acc, ds, smem + (t & 1) * S::kTileBytes + b * 64 * D, 0, last, lane);
-          continue;
-        }
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int i = 0; i < D / 32; ++i) acc[i] = mfma32(read_columns<D>(kt_lane, 2 * b + j, i), __builtin_bit_cast(bf16x8, ds[j]), acc[i]);
-      }
-    }
+    for (int r = 0; r < 16; ++r) s[r] = 8 * (r / 4) + r % 4 <= last ? s[r] : -INFINITY;
   };
-  pass(std::false_type{}, true);
+  constexpr int kSteps = D / 16, kParts = D / 32, kSlots = 4 * kSteps + 4 * kParts;
+  uint32_t k_at[kSteps], t_at[kParts][2];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) keep(k_at[i] = row_address<D>(lds, lane) ^ (uint32_t)(i << 5));
+#pragma unroll
+  for (int i = 0; i < kParts; ++i) {
+    keep(t_at[i][0] = column_address<D>(lds, lane) ^ (uint32_t)(i << 6));
+    keep(t_at[i][1] = (column_address<D>(lds, lane) ^ (uint32_t)(i << 6) ^ 32u) + 16u * D);
+  }
+  // One tile in slots of one product each, with their share of the vector unit's work, blocks 0 and 1 of 32 keys: S0; dP0 and the weights of 0; S1 and the
+  // gradients of the scores of 0; dP1 and the weights of 1; dq from 0 and the gradients of 1; dq from 1.
+  auto tile_pass = [&](int t, auto parity, auto with_mask) __attribute__((always_inline)) {
+    constexpr uint32_t kAt = (uint32_t)(decltype(parity)::value * S::kTileBytes);
+    auto read = [&](auto slot) __attribute__((always_inline)) {
+      constexpr int i = decltype(slot)::value, j = i - 4 * kSteps;
+      if constexpr (j < 0) return read_rows_at<D>(k_at[i % kSteps], kAt + (uint32_t)((i / kSteps % 2 ? 2 * S::kTileBytes : 0) + i / (2 * kSteps) * 64 * D));
+      else return read_columns_at<D>(t_at[j % kParts][0], t_at[j % kParts][1], kAt + (uint32_t)(j / kParts * 32 * D));
+    };
+    constexpr int kAhead = 2, kRing = kAhead + 1;
+    bf16x8 f[kRing];
+    for_each_index([&](auto slot) __attribute__((always_inline)) { f[decltype(slot)::value] = read(slot); }, std::make_integer_sequence<int, kAhead>{});
+    f32x16 s[2], dp[2];
+    u32x4 ds[4];
+    __builtin_amdgcn_sched_barrier(0);
+    for_each_index([&](auto slot) __attribute__((always_inline)) {
+      constexpr int i = decltype(slot)::value, j = i - 4 * kSteps, b = i / (2 * kSteps);
+      if constexpr (i + kAhead < kSlots) f[(i + kAhead) % kRing] = read(std::integral_constant<int, i + kAhead>{});
+      if constexpr (j < 0 && i / kSteps % 2 == 0) s[b] = mfma32(f[i % kRing], qf[i % kSteps], i % kSteps ? s[b] : f32x16{});
+      if constexpr (j < 0 && i / kSteps % 2 == 1) dp[b] = mfma32(f[i % kRing], gf[i % kSteps], i % kSteps ? dp[b] : f32x16{});
+      if constexpr (j >= 0) acc[j % kParts] = mfma32(f[i % kRing], __builtin_bit_cast(bf16x8, ds[j / kParts]), acc[j % kParts]);
+      if constexpr (decltype(with_mask)::value && j < 0 && i % (2 * kSteps) == kSteps - 1) mask(s[b], t * kPromptKeys + 32 * b);
+      // pairs taken before a slot: weights of block 0 from slot kSteps on, ..
+      constexpr auto pairs = [](int n, int slots) constexpr { return n <= 0 ? 0 : n >= slots ? 8 : (n * 8 + slots - 1) / slots; };
+#pragma unroll
+      for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int n = pairs(i - (1 + 2 * w) * kSteps, kSteps); n < pairs(i + 1 - (1 + 2 * w) * kSteps, kSteps); ++n)
+#pragma unroll
+          for (int e = 2 * n; e < 2 * n + 2; ++e) s[w][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[w][e], c, -lse));
+#pragma unroll
+      for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int n = pairs(i - (2 + 2 * w) * kSteps, w ? 2 * kParts : kSteps); n < pairs(i + 1 - (2 + 2 * w) * kSteps, w ? 2 * kParts : kSteps); ++n)
+          ds[2 * w + n / 4][n % 4] = pack_bf16(s[w][2 * n] * (dp[w][2 * n] - delta), s[w][2 * n + 1] * (dp[w][2 * n + 1] - delta));
+      __builtin_amdgcn_sched_barrier(0);
+    }, std::make_integer_sequence<int, kSlots>{});
+  };
+  constexpr std::integral_constant<int, 0> kEven{};
+  constexpr std::integral_constant<int, 1> kOdd{};
+  auto turn = [&](int t) __attribute__((always_inline)) {
+    publish();
+    if (t + 1 < tiles) fetch(t + 1);
+  };
+  const int wave_tiles = (wave_keys + kPromptKeys - 1) / kPromptKeys, whole = min(all_keys / kPromptKeys, wave_tiles);       // tiles that this wave has, and without a mask
+  int t = 0;
+  for (; t + 1 < whole; t += 2) {
+    turn(t);
+    tile_pass(t, kEven, std::false_type{});
+    turn(t + 1);
+    tile_pass(t + 1, kOdd, std::false_type{});
+  }
+  for (; t < tiles; ++t) {
+    turn(t);
+    if (t >= wave_tiles) continue;
+    if (t & 1) tile_pass(t, kOdd, std::true_type{});
+    else tile_pass(t, kEven, std::true_type{});
+  }
   if constexpr (CAUSAL) {            // a key that is no finite number and only some rows of a tile look at: as in the forward kernel
     const bool mine = __any(odd_sums(acc) != 0.f);
     if (__builtin_expect(any_wave<NW>(mine, smem, wave, lane), 0)) {
@@ -112,7 +148,39 @@ __global__ void __launch_bounds__(NW * 64, 2) attention_dq_kernel(PromptBackArgs
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) acc[i] = f32x16{};
       }
-      pass(std::true_type{}, mine);
+      for (t = 0; t < tiles; ++t) {
+        turn(t);
+        if (!mine || t >= wave_tiles) continue;
+        const uint32_t at = lds + (uint32_t)((t & 1) * S::kTileBytes);
+        uint32_t l = (uint32_t)lane;
+        keep(l);                     // or these addresses have registers all along
+        const uint32_t k_lane = row_address<D>(at, (int)l), t_lane = column_address<D>(at, (int)l);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          f32x16 s = f32x16{}, dp = f32x16{};
+#pragma unroll
+          for (int i = 0; i < kSteps; ++i) {
+            s = mfma32(read_rows<D>(k_lane, b, i), qf[i], s);
+            dp = mfma32(read_rows<D>(k_lane + 2 * S::kTileBytes, b, i), gf[i], dp);
+            __builtin_amdgcn_sched_barrier(0);              // one read at a time: few registers
+          }
+          mask(s, t * kPromptKeys + 32 * b);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -lse)) * (dp[r] - delta);
+          const u32x4 ds[2] = {as_words(s, 0), as_words(s, 1)};
+          if (t >= whole) {
+            add_by_row<D, 32>(acc, ds, smem + (t & 1) * S::kTileBytes + b * 64 * D, 0, last_key - t * kPromptKeys - 32 * b, lane);
+            continue;
+          }
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < kParts; ++i) {
+              acc[i] = mfma32(read_columns<D>(t_lane, 2 * b + j, i), __builtin_bit_cast(bf16x8, ds[j]), acc[i]);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+      }
     }
   }
   store_columns<D>(acc, a.scale, args.dq.at(token, head), real, lane);
