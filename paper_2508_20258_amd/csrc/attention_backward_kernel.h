@@ -278,14 +278,20 @@ __global__ void __launch_bounds__(64 * KW * QP, D == 64 ? 3 : 2) attention_dkv_k
   typedef __attribute__((address_space(3))) const f32x4* stat_ptr;
   uint32_t stat_at = stats_lds + (uint32_t)(16 * h);
 
-  auto start = [&](f32x16& s, f32x16& dp) __attribute__((always_inline)) {
+  auto start = [&](f32x16& x, uint32_t at) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const f32x4 x = *(stat_ptr)(uintptr_t)(stat_at + (uint32_t)(32 * i)), y = *(stat_ptr)(uintptr_t)(stat_at + (uint32_t)(32 * i + kBackRows * 4));
+      const f32x4 y = *(stat_ptr)(uintptr_t)(at + (uint32_t)(32 * i));
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[4 * i + e] = x[e], dp[4 * i + e] = y[e];
+      for (int e = 0; e < 4; ++e) x[4 * i + e] = y[e];
     }
   };
+  constexpr bool kHold = D == 128;   // the wave's keys stay in registers (1% less time than reading them from LDS for every tile); with heads of 64 that would cost a wave of three
+  bf16x8 held[kHold ? kSteps : 1];
+  if constexpr (kHold) {
+    publish();
+    for_each_index([&](auto i) __attribute__((always_inline)) { held[decltype(i)::value] = read_rows<D>(key_at, 0, decltype(i)::value); }, std::make_integer_sequence<int, kSteps>{});
+  }
   auto looks = [&](int r0) { return member < group && !(CAUSAL && r0 + kBackRows - 1 + ahead < key0); };      // some of these rows do, at a key of this wave
   auto masked = [&](int r0) { return (CAUSAL && r0 + ahead < key0 + 31) || key0 + 32 > k.length; };
   auto first_row = [&](int r0) { return key < k.length ? (CAUSAL ? key - ahead - r0 : 0) : kBackRows; };     // of those that look at the lane's key
@@ -302,7 +308,7 @@ __global__ void __launch_bounds__(64 * KW * QP, D == 64 ? 3 : 2) attention_dkv_k
     if (round + 1 < rounds) fetch(round + 1);
     if (mine) {
       f32x16 s, dp;
-      start(s, dp);
+      start(s, stat_at);
       // Slots of one product each: S, dP, dv, dk.
       constexpr int kAhead = 2, kRing = kAhead + 1;
       bf16x8 f[kRing], kf[kRing];
@@ -313,7 +319,7 @@ __global__ void __launch_bounds__(64 * KW * QP, D == 64 ? 3 : 2) attention_dkv_k
       };
       auto read_k = [&](auto slot) __attribute__((always_inline)) {
         constexpr int i = decltype(slot)::value;
-        kf[i % kRing] = read_rows<D>(i < kSteps ? key_at : value_at, 0, i % kSteps);
+        if constexpr (!kHold || i >= kSteps) kf[i % kRing] = read_rows<D>(i < kSteps ? key_at : value_at, 0, i % kSteps);
       };
       constexpr int kSlots = 2 * kSteps + 4 * kParts, kPairs = 8;       // pairs of weights
       for_each_index([&](auto slot) __attribute__((always_inline)) {
@@ -325,7 +331,8 @@ __global__ void __launch_bounds__(64 * KW * QP, D == 64 ? 3 : 2) attention_dkv_k
         constexpr int i = decltype(slot)::value;
         f[(i + kAhead) % kRing] = read_a(std::integral_constant<int, i + kAhead>{});
         read_k(std::integral_constant<int, i + kAhead>{});
-        s = mfma32(f[i % kRing], kf[i % kRing], s);
+        s = mfma32(f[i % kRing], kHold ? held[kHold ? i : 0] : kf[i % kRing], s);
+        if constexpr (i == kSteps - 2) start(dp, stat_at + kBackRows * 4);
         __builtin_amdgcn_sched_barrier(0);
       }, std::make_integer_sequence<int, kSteps>{});
       if (masked(r0)) mask(s, r0);
@@ -390,7 +397,8 @@ __global__ void __launch_bounds__(64 * KW * QP, D == 64 ? 3 : 2) attention_dkv_k
         const uint32_t q_lane = row_address<D>(lds + (uint32_t)tiles_at, (int)l), q_column = column_address<D>(lds + (uint32_t)tiles_at, (int)l);
         stat_at = stats_lds + (uint32_t)(16 * h + (round & 1) * 2 * kBackRows * 4);
         f32x16 s, dp;
-        start(s, dp);
+        start(s, stat_at);
+        start(dp, stat_at + kBackRows * 4);
         // (one read at a time: few registers)
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
