@@ -118,7 +118,7 @@ int swz_cache4_read(const swz_cache4* cache, const swz_heads* k, const swz_heads
  *   q, out : sequences tokens of q_heads heads.   max_length : the longest length, or more (0: the table's); it decides how many waves share the work, no
  *   more: longer lengths are right too, and slower.
  *   The weights times the steps of v are rounded to bfloat16 for their product with v's numbers.
- *   workspace : swz_cache4_attention_workspace(...) bytes, 16-byte aligned. */
+ *   workspace : swz_cache4_attention_workspace(...) bytes, 16-byte aligned; may be null where that is 0 (it is where the longest length is short). */
 int64_t swz_cache4_attention_workspace(const swz_cache4* cache, int32_t sequences, int32_t q_heads, int32_t table_width, int32_t max_length);
 int swz_cache4_attention(const swz_cache4* cache, const swz_heads* q, const swz_heads* out, const int32_t* lengths, const int32_t* block_table,
                          int32_t table_width, int32_t sequences, int32_t q_heads, int32_t max_length, float scale, void* workspace, int64_t workspace_bytes,

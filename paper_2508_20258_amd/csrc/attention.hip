@@ -231,11 +231,15 @@ int store_or_read(const swz_cache4* cache, const swz_heads* k, const swz_heads* 
 
 // A decoding step: waves that share the steps of a key head (of each block of 16 of its query heads), rows that a product has for queries.
 struct DecodePlan {
-  int columns, rows, shares;
+  int columns, rows, shares;         // shares 0: a workgroup for each sequence and key head
 };
 DecodePlan decode_plan(const swz_cache4& c, int sequences, int q_heads, int table_width, int max_length) {
   const int group = q_heads / c.k_heads, columns = (group + 15) / 16, rows = group <= 4 ? 4 : group <= 8 ? 8 : 16;
   const int64_t cut = (int64_t)table_width * c.page_tokens, longest = max_length > 0 && max_length < cut ? max_length : cut;
+  // Few tokens: one launch, a workgroup of 8 waves for each sequence and key head, not waves that share all steps and a second launch that joins them.  4 heads of 128 for each of 8 key
+  // heads: 16 sequences of 256 tokens 8.1 us and 10.8, of 1000 11.5 and 15.0, of 2000 18.3 and 19.8, of 4000 28.8 and 26.0; one of 1000 10.8 and 10.9, of 2000 15.1 and 12.5; 64 of
+  // 1000 25.8 and 25.7.  16 heads of one key head, 8 of 1000: 13.6 and 12.9.  Heads of 64: 8 of 2000 10.1 and 13.5, of 4000 18.4 and 17.1.
+  if (longest * c.head_dim <= 1 << 17) return {columns, rows, 0};
   // as many as run together; fewer where there are fewer steps
   const int64_t together = (int64_t)compute_units() * 4 * (c.head_dim == 64 ? 3 : rows >= 8 ? 2 : 3) / ((int64_t)c.k_heads * columns);
   const int64_t steps = (longest + swz::kDecodeStep - 1) / swz::kDecodeStep * sequences;
@@ -252,7 +256,7 @@ int check_decode(const swz_cache4* c, int sequences, int q_heads, int table_widt
 
 // The parts' sums, their statistics, and where they are.
 int64_t decode_parts(const swz_cache4& c, const DecodePlan& p) { return (int64_t)p.shares * c.k_heads * p.columns * 2 * p.rows; }
-int64_t decode_bytes(const swz_cache4& c, const DecodePlan& p, int sequences) { return 4 * decode_parts(c, p) * (c.head_dim + 2) + (int64_t)8 * sequences * c.k_heads * p.columns; }
+int64_t decode_bytes(const swz_cache4& c, const DecodePlan& p, int sequences) { return p.shares == 0 ? 0 : 4 * decode_parts(c, p) * (c.head_dim + 2) + (int64_t)8 * sequences * c.k_heads * p.columns; }
 
 }  // namespace
 
@@ -406,7 +410,8 @@ int swz_cache4_attention(const swz_cache4* cache, const swz_heads* q, const swz_
   st = check_heads(*q, *out);
   if (st != SWZ_OK) return st;
   const DecodePlan p = decode_plan(*cache, sequences, q_heads, table_width, max_length);
-  if (workspace == nullptr || workspace_bytes < decode_bytes(*cache, p, sequences)) return SWZ_ERR_INVALID_ARG;
+  const int64_t bytes = decode_bytes(*cache, p, sequences);
+  if (bytes > 0 && (workspace == nullptr || workspace_bytes < bytes)) return SWZ_ERR_INVALID_ARG;
   if (!aligned(lengths, 4) || !aligned(block_table, 4) || !aligned(workspace, 16)) return SWZ_ERR_UNSUPPORTED;
   swz::DecodeArgs a{};
   a.c = cache_args(*cache, block_table, table_width);
@@ -418,10 +423,16 @@ int swz_cache4_attention(const swz_cache4* cache, const swz_heads* q, const swz_
   a.parts = reinterpret_cast<int2*>(a.stats + decode_parts(*cache, p) * 2);
   return for_head_dim(cache->head_dim, [&](auto dim) {
     constexpr int D = decltype(dim)::value;
-    const int64_t waves = (int64_t)p.shares * cache->k_heads * p.columns;
+    const int64_t heads = (int64_t)cache->k_heads * p.columns, waves = p.shares * heads;
+    if (2 * waves >= kTokens || sequences * heads >= kTokens || (int64_t)sequences * q_heads * 64 * swz::kJoinWaves > swz::kLaunchThreads || sequences * heads * 64 * swz::kOwnWaves > swz::kLaunchThreads) {
+      return (int)SWZ_ERR_OVERFLOW;
+    }
+    if (p.shares == 0) {
+      auto kernel = p.rows == 4 ? swz::cache4_attention_kernel<D, 4, true> : p.rows == 8 ? swz::cache4_attention_kernel<D, 8, true> : swz::cache4_attention_kernel<D, 16, true>;
+      return launch(kernel, dim3((unsigned)(sequences * heads)), dim3(64 * swz::kOwnWaves), 0, stream, a);
+    }
     const dim3 grid((unsigned)((waves + swz::kDecodeWaves - 1) / swz::kDecodeWaves)), block(64 * swz::kDecodeWaves);
-    if (2 * waves >= kTokens || (int64_t)sequences * cache->k_heads * p.columns >= kTokens || (int64_t)sequences * q_heads * 64 * swz::kJoinWaves > swz::kLaunchThreads) return (int)SWZ_ERR_OVERFLOW;
-    auto kernel = p.rows == 4 ? swz::cache4_attention_kernel<D, 4> : p.rows == 8 ? swz::cache4_attention_kernel<D, 8> : swz::cache4_attention_kernel<D, 16>;
+    auto kernel = p.rows == 4 ? swz::cache4_attention_kernel<D, 4, false> : p.rows == 8 ? swz::cache4_attention_kernel<D, 8, false> : swz::cache4_attention_kernel<D, 16, false>;
     const int status = launch(kernel, grid, block, 0, stream, a);
     if (status != SWZ_OK) return status;
     return launch(swz::cache4_join_kernel<D>, dim3((unsigned)((int64_t)sequences * q_heads)), dim3(64 * swz::kJoinWaves), 0, stream, a, p.rows);

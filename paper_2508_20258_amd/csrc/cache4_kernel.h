@@ -235,7 +235,7 @@ struct DecodeArgs {
   float scale;
 };
 
-constexpr int kDecodeStep = 64, kDecodeWaves = 4;
+constexpr int kDecodeStep = 64, kDecodeWaves = 4, kOwnWaves = 8;
 
 __device__ __forceinline__ int cached_length(const DecodeArgs& a, int sequence) {
   return (int)min((int64_t)max(a.lengths[sequence], 0), (int64_t)a.c.table_width << a.c.page_shift);
@@ -289,35 +289,47 @@ __device__ __forceinline__ float over_tokens(float x, Op op) {
   return x;
 }
 
-template <int D, int R>
-__global__ void __launch_bounds__(64 * kDecodeWaves, D == 128 && R >= 8 ? 2 : 3) cache4_attention_kernel(DecodeArgs a) {
+// OWN: a workgroup of kOwnWaves for each sequence and key head instead, whose waves share its steps and join what they have in LDS.
+template <int D, int R, bool OWN>
+__global__ void __launch_bounds__(64 * (OWN ? kOwnWaves : kDecodeWaves), D == 128 && R >= 8 ? 2 : 3) cache4_attention_kernel(DecodeArgs a) {
   constexpr int kGroups = D / 64, kSteps = D / 32;
   constexpr int kQuads = R / 4, kSets = R / 4, kBlocks = 16 / R;      // row groups that a query's four rows take part in; sets of 4 weights a lane; blocks of 16 tokens of a set
-  __shared__ __attribute__((aligned(16))) uint16_t weights[kDecodeWaves][kGroups][kDecodeStep][R];
+  constexpr int kWaves = OWN ? kOwnWaves : kDecodeWaves;
+  __shared__ __attribute__((aligned(16))) uint16_t weights[kWaves][kGroups][kDecodeStep][R];
+  __shared__ __attribute__((aligned(16))) float own_sums[OWN ? kWaves : 1][OWN ? R : 1][D], own_stats[OWN ? kWaves : 1][OWN ? R : 1][2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   const int heads = a.c.k_heads * a.columns, group = a.q_heads / a.c.k_heads;
-  const int id = (int)blockIdx.x * kDecodeWaves + wave, share = id / heads, pair = id - share * heads;
-  int64_t total = 0;
-  over_sequences(a, [&](int, int, int sum) {
-    total += __builtin_amdgcn_readlane(sum, 63);
-    return true;
-  });
-  const int shares = (int)min((int64_t)a.shares, total);
-  if (share >= shares) return;
-  const int64_t my_start = total * share / shares, my_end = total * (share + 1) / shares;
+  const int id = OWN ? (int)blockIdx.x : (int)blockIdx.x * kDecodeWaves + wave, share = id / heads, pair = id - share * heads;
   int sequence = 0;
-  int64_t before = 0;                                        // steps of the sequences before it
-  over_sequences(a, [&](int first, int n, int sum) {
-    const uint64_t found = __ballot(my_start < before + sum);
-    if (found == 0) {
-      before += __builtin_amdgcn_readlane(sum, 63);
+  int64_t before = 0, my_start = 0, my_end = 0;              // before: steps of the sequences before it
+  if constexpr (OWN) {
+    sequence = share;
+    const int all = steps_of(__builtin_amdgcn_readfirstlane(cached_length(a, sequence)));
+    my_start = (int64_t)all * wave / kWaves;
+    my_end = (int64_t)all * (wave + 1) / kWaves;
+    if (lane < R) own_stats[wave][lane][0] = -FLT_MAX, own_stats[wave][lane][1] = 0.f;
+  } else {
+    int64_t total = 0;
+    over_sequences(a, [&](int, int, int sum) {
+      total += __builtin_amdgcn_readlane(sum, 63);
       return true;
-    }
-    const int s = __ffsll((unsigned long long)found) - 1;
-    sequence = first + s;
-    before += __builtin_amdgcn_readlane(sum - n, s);
-    return false;
-  });
+    });
+    const int shares = (int)min((int64_t)a.shares, total);
+    if (share >= shares) return;
+    my_start = total * share / shares;
+    my_end = total * (share + 1) / shares;
+    over_sequences(a, [&](int first, int n, int sum) {
+      const uint64_t found = __ballot(my_start < before + sum);
+      if (found == 0) {
+        before += __builtin_amdgcn_readlane(sum, 63);
+        return true;
+      }
+      const int s = __ffsll((unsigned long long)found) - 1;
+      sequence = first + s;
+      before += __builtin_amdgcn_readlane(sum - n, s);
+      return false;
+    });
+  }
   const int k_head = pair / a.columns, column = pair - k_head * a.columns;
   const int head0 = k_head * group + column * 16, queries = min(16, group - column * 16);
 
@@ -531,7 +543,7 @@ __global__ void __launch_bounds__(64 * kDecodeWaves, D == 128 && R >= 8 ? 2 : 3)
       for (int i = 0; i < kGroups; ++i) mids[i][r] = over_tokens<R>(mids[i][r], [](float x, float y) { return x + y; });
     }
     const float my_sum = of_query(sum), my_top = of_query(top);
-    const bool whole = count == all;
+    const bool whole = !OWN && count == all;
     const float f = !whole ? 1.f : my_sum == 0.f ? 0.f : 1.f / my_sum;
 #pragma unroll
     for (int i = 0; i < kGroups; ++i) {
@@ -553,6 +565,12 @@ __global__ void __launch_bounds__(64 * kDecodeWaves, D == 128 && R >= 8 ? 2 : 3)
             for (int z = 0; z < 8; ++z) y[z] = o[i][z % 4][2 * half + z / 4];
             *reinterpret_cast<u32x4*>(a.out.at(sequence, head0 + n) + 64 * i + 16 * g + 8 * half) = pack8(y);
           }
+      } else if constexpr (OWN) {
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) *reinterpret_cast<f32x4*>(&own_sums[wave][n][64 * i + 16 * g + 4 * e]) = f32x4{o[i][0][e], o[i][1][e], o[i][2][e], o[i][3][e]};
+        if (g == 0) own_stats[wave][n][0] = my_top, own_stats[wave][n][1] = my_sum;
       } else {
         const int part = id * 2 + (step == my_start ? 0 : 1);
         const int64_t to = (int64_t)part * R + n;
@@ -565,9 +583,28 @@ __global__ void __launch_bounds__(64 * kDecodeWaves, D == 128 && R >= 8 ? 2 : 3)
         if (lane == 0 && from == 0) a.parts[sequence * heads + pair].x = part;
       }
     }
-    if (lane == 0 && from + count == all) a.parts[sequence * heads + pair].y = whole ? -1 : share;
+    if (!OWN && lane == 0 && from + count == all) a.parts[sequence * heads + pair].y = whole ? -1 : share;
     step += count;
     before += all;
+  }
+  if constexpr (OWN) {
+    __syncthreads();
+    for (int i = (int)threadIdx.x; i < queries * (D / 2); i += 64 * kWaves) {
+      const int query = i / (D / 2), d = i % (D / 2) * 2;
+      float top = -FLT_MAX, sum = 0.f, x = 0.f, y = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, own_stats[w][query][0]);
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float its = own_stats[w][query][1], f = __builtin_amdgcn_exp2f(own_stats[w][query][0] - top);
+        if (its == 0.f) continue;                            // no steps, and nothing written
+        sum = __builtin_fmaf(its, f, sum);
+        x = __builtin_fmaf(own_sums[w][query][d], f, x);
+        y = __builtin_fmaf(own_sums[w][query][d + 1], f, y);
+      }
+      const float f = sum == 0.f ? 0.f : 1.f / sum;
+      *reinterpret_cast<uint32_t*>(a.out.at(share, head0 + query) + d) = pack_bf16(x * f, y * f);
+    }
   }
 }
 

@@ -9,6 +9,7 @@ candidate search of the paper's optimisation loop without the LLM.
     python -m paper_2508_20258_amd.harness copy --mib 1024 --launches 3
     python -m paper_2508_20258_amd.harness transpose --m 16384 --n 16384 --tile 32 --mode rr
     python -m paper_2508_20258_amd.harness rows --op softmax --m 8192 --n 8192 --chunks 8 --mode xcd
+    python -m paper_2508_20258_amd.harness attention --case train_packed
     python -m paper_2508_20258_amd.harness peak
     python -m paper_2508_20258_amd.harness summarize <rocprofv3 output dir>
 
@@ -582,6 +583,74 @@ def cmd_profile_rows(args):
         f.write(text)
 
 
+def _operators():
+    """perf/operators.py, whose cases the attention layers are measured on."""
+    import importlib.util
+    spec = importlib.util.spec_from_file_location("swz_operators", os.path.join(os.path.dirname(HERE), "perf", "operators.py"))
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    module.own = True
+    return module
+
+
+def cmd_attention(args):
+    import torch
+
+    ops = _operators()
+    case = next(c for c in ops.listed() if c["name"] == args.case)
+    state = ops.prepare(case, 1)
+    for _ in range(args.launches):
+        ops.run(state)
+    torch.cuda.synchronize()
+    print(f"ran {args.launches} x {args.case}", flush=True)
+
+
+ATTENTION_COUNTERS = ["SQ_BUSY_CU_CYCLES", "SQ_VALU_MFMA_BUSY_CYCLES", "SQ_LDS_IDX_ACTIVE", "SQ_LDS_BANK_CONFLICT", "SQ_ACTIVE_INST_VALU"]
+
+
+def cmd_profile_attention(args):
+    """rocprofv3 passes for every listed case of perf/operators.py, as child processes; prints the summary table."""
+    out = os.path.abspath(args.out)
+    os.makedirs(out, exist_ok=True)
+    ops = _operators()
+    names = [c["name"] for c in ops.listed()]
+    passes = (("sq", ATTENTION_COUNTERS), ("fetch", ["FETCH_SIZE"]), ("write", ["WRITE_SIZE"]))
+    if not args.table_only:
+        for c, tag in (("FETCH_SIZE", "copy_fetch"), ("WRITE_SIZE", "copy_write")):
+            _rocprof(out, tag, "csv", ["--pmc", c], ["copy", "--mib", "1024", "--launches", "3"])
+        for name in names:
+            prog = ["attention", "--case", name]
+            _rocprof(out, name + "_kt", "csv", ["--kernel-trace", "--stats"], prog + ["--launches", str(args.launches + 10)])
+            for tag, counters in passes:
+                _rocprof(out, f"{name}_{tag}", "csv", ["--pmc", *counters], prog + ["--launches", "3"], 90)
+    fs = 1024 * 1024 / _one(f"{out}/copy_fetch", "copy")["counters"]["FETCH_SIZE"]
+    ws = 1024 * 1024 / _one(f"{out}/copy_write", "copy")["counters"]["WRITE_SIZE"]
+    H = "python3 -m paper_2508_20258_amd.harness"
+    lines = ["rocprofv3 summary: the kernels of the attention layers on the listed cases of perf/operators.py, MI355X, one GPU.",
+             "Written by (repository root, TMPDIR=/tmp):",
+             f"  {H} profile-attention --out <dir>",
+             "which runs, for CASE as in the table:",
+             f"  rocprofv3 --kernel-trace --stats --output-format csv -d <out> -- {H} attention --case CASE --launches {args.launches + 10}",
+             f"  rocprofv3 --pmc {' '.join(ATTENTION_COUNTERS)} (then FETCH_SIZE, then WRITE_SIZE) --output-format csv -d <out> -- {H} attention --case CASE --launches 3",
+             f"  and FETCH_SIZE, WRITE_SIZE on `{H} copy --mib 1024` (calibration: FETCH_SIZE x {fs:.3f}, WRITE_SIZE x {ws:.3f}).",
+             f"us = kernel duration in the trace, average over its last {args.launches} launches, over the same data.  MFMA: share of the matrix units' cycles, of busy compute units, in which one works;",
+             "LDS: share of these compute units' cycles in which LDS serves a read or write, conflicts among them; VALU: instructions of the vector unit issued a cycle and SIMD.",
+             "", f"{'case':14s} {'us':>8s} {'MFMA %':>7s} {'LDS %':>6s} {'conflict %':>10s} {'VALU':>5s} {'fetch MiB':>10s} {'write MiB':>10s}  kernel"]
+    for name in names:
+        t = f"{out}/{name}"
+        trace, sq, fetch, write = summarize(t + "_kt", "swz", args.launches), summarize(t + "_sq", "swz"), summarize(t + "_fetch", "swz"), summarize(t + "_write", "swz")
+        for kernel, d in trace.items():
+            c = sq[kernel]["counters"]
+            busy = c["SQ_BUSY_CU_CYCLES"]
+            lines.append(f"{name:14s} {d['warm_avg_ns'] / 1e3:8.2f} {100 * c['SQ_VALU_MFMA_BUSY_CYCLES'] / (4 * busy):7.1f} {100 * c['SQ_LDS_IDX_ACTIVE'] / busy:6.1f} "
+                         f"{100 * c['SQ_LDS_BANK_CONFLICT'] / busy:10.2f} {c['SQ_ACTIVE_INST_VALU'] / (4 * busy):5.2f} {fetch[kernel]['counters']['FETCH_SIZE'] * fs / 1024:10.1f} "
+                         f"{write[kernel]['counters']['WRITE_SIZE'] * ws / 1024:10.1f}  {kernel.split('(')[0].replace('void ', '').replace('swz::', '')}")
+    text = "\n".join(lines) + "\n"
+    print(text, flush=True)
+    with open(os.path.join(out, "attention_layers.txt"), "w") as f:
+        f.write(text)
+
+
 def cmd_profile(args):
     """Every rocprofv3 pass for the three mappings of one workload, as child processes; prints the summary table."""
     import json
@@ -939,6 +1008,15 @@ def main(argv=None):
     pr.add_argument("--launches", type=int, default=10)
     pr.add_argument("--table-only", action="store_true")
     pr.set_defaults(fn=cmd_profile_rows)
+    at = sub.add_parser("attention")
+    at.add_argument("--case", required=True)
+    at.add_argument("--launches", type=int, default=20)
+    at.set_defaults(fn=cmd_attention)
+    pa = sub.add_parser("profile-attention")
+    pa.add_argument("--out", required=True)
+    pa.add_argument("--launches", type=int, default=10)
+    pa.add_argument("--table-only", action="store_true")
+    pa.set_defaults(fn=cmd_profile_attention)
     ck = sub.add_parser("clocks")
     ck.add_argument("--workload", default="cfg2_4096")
     ck.add_argument("--mode", default="xcd_groupm", choices=MODE_NAMES)

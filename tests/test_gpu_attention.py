@@ -561,6 +561,22 @@ def test_cache_attention_split_over_a_long_table(swz):
         check_decode(swz.cache4_attention(q, cache, lengths, wide, longest), q, held, lens, 2, dim ** -0.5)
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("q_heads,k_heads", [(1, 1), (8, 2), (15, 3), (16, 2), (40, 2)])
+@pytest.mark.parametrize("lens", [[1], [64], [65, 0, 127], [700, 3], [1025, 2049, 0, 0, 130], [5] * 70])
+def test_cache_attention_by_workgroups_and_by_waves(swz, lens, q_heads, k_heads, dim):
+    """Short sequences have a workgroup each, where the longest length says so; else waves share the steps of all sequences.  Both on the same cache."""
+    page = 64
+    cache, table, q = decode_case(swz, lens, q_heads, k_heads, dim, page, seed=sum(lens) + q_heads)
+    lengths = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    held = numbers_of(cache, table, lens, page)
+    for longest in (64, 1 << 20):
+        wide = torch.full((len(lens), max(table.shape[1], 40)), -1, dtype=torch.int32, device="cuda")
+        wide[:, :table.shape[1]] = table
+        got = swz.cache4_attention(q, cache, lengths, wide, longest)
+        check_decode(got, q, held, lens, k_heads, dim ** -0.5)
+
+
 def test_cache_attention_sees_nothing_else(swz):
     lens, dim, page = [70, 33], 64, 32
     cache, table, q = decode_case(swz, lens, 2, 1, dim, page)
