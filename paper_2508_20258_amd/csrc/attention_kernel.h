@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(64 * QW, D == 64 ? 3 : 2) attention_kernel(Pro
       if constexpr (MORE && i >= kScoreSlots) {
 #pragma unroll
         for (int e = v * 32 / (4 * kParts); e < (v + 1) * 32 / (4 * kParts); e += 2)
-          high[e / 2 % 2] = fmaxf(high[e / 2 % 2], fmaxf(then[e / 16][e % 16], then[e / 16][e % 16 + 1]));
+          high[e / 2 % 2] = __builtin_elementwise_maximum(high[e / 2 % 2], __builtin_elementwise_maximum(then[e / 16][e % 16], then[e / 16][e % 16 + 1]));
       }
       __builtin_amdgcn_sched_barrier(0);
     }, std::make_integer_sequence<int, kSlots - kFirst>{});

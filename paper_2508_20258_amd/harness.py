@@ -634,8 +634,8 @@ def cmd_profile_attention(args):
              f"  rocprofv3 --pmc {' '.join(ATTENTION_COUNTERS)} (then FETCH_SIZE, then WRITE_SIZE) --output-format csv -d <out> -- {H} attention --case CASE --launches 3",
              f"  and FETCH_SIZE, WRITE_SIZE on `{H} copy --mib 1024` (calibration: FETCH_SIZE x {fs:.3f}, WRITE_SIZE x {ws:.3f}).",
              f"us = kernel duration in the trace, average over its last {args.launches} launches, over the same data.  MFMA: share of the matrix units' cycles, of busy compute units, in which one works;",
-             "LDS: share of these compute units' cycles in which LDS serves a read or write, conflicts among them; VALU: instructions of the vector unit issued a cycle and SIMD.",
-             "", f"{'case':14s} {'us':>8s} {'MFMA %':>7s} {'LDS %':>6s} {'conflict %':>10s} {'VALU':>5s} {'fetch MiB':>10s} {'write MiB':>10s}  kernel"]
+             "LDS: share of these compute units' cycles in which LDS serves a read or write, conflicts among them; VALU: share of them in which vector instructions are issued.",
+             "", f"{'case':14s} {'us':>8s} {'MFMA %':>7s} {'LDS %':>6s} {'conflict %':>10s} {'VALU %':>6s} {'fetch MiB':>10s} {'write MiB':>10s}  kernel"]
     for name in names:
         t = f"{out}/{name}"
         trace, sq, fetch, write = summarize(t + "_kt", "swz", args.launches), summarize(t + "_sq", "swz"), summarize(t + "_fetch", "swz"), summarize(t + "_write", "swz")
@@ -643,7 +643,7 @@ def cmd_profile_attention(args):
             c = sq[kernel]["counters"]
             busy = c["SQ_BUSY_CU_CYCLES"]
             lines.append(f"{name:14s} {d['warm_avg_ns'] / 1e3:8.2f} {100 * c['SQ_VALU_MFMA_BUSY_CYCLES'] / (4 * busy):7.1f} {100 * c['SQ_LDS_IDX_ACTIVE'] / busy:6.1f} "
-                         f"{100 * c['SQ_LDS_BANK_CONFLICT'] / busy:10.2f} {c['SQ_ACTIVE_INST_VALU'] / (4 * busy):5.2f} {fetch[kernel]['counters']['FETCH_SIZE'] * fs / 1024:10.1f} "
+                         f"{100 * c['SQ_LDS_BANK_CONFLICT'] / busy:10.2f} {100 * c['SQ_ACTIVE_INST_VALU'] / busy:6.1f} {fetch[kernel]['counters']['FETCH_SIZE'] * fs / 1024:10.1f} "
                          f"{write[kernel]['counters']['WRITE_SIZE'] * ws / 1024:10.1f}  {kernel.split('(')[0].replace('void ', '').replace('swz::', '')}")
     text = "\n".join(lines) + "\n"
     print(text, flush=True)
