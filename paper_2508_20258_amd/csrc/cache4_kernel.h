@@ -44,17 +44,23 @@ __device__ __forceinline__ float over8(float x, Op op) {
 __device__ __forceinline__ uint32_t quantise8(const u32x4& v, float (&number)[8]) {
   float x[8];
   unpack8(v, x);
-  float low = fminf(x[0], x[1]), high = fmaxf(x[0], x[1]);
+  // (minimum, maximum: those that keep a NaN, which is found below; fminf and fmaxf would quiet every value first)
+  auto lower = [](float a, float b) { return __builtin_elementwise_minimum(a, b); };
+  auto higher = [](float a, float b) { return __builtin_elementwise_maximum(a, b); };
+  float low = lower(x[0], x[1]), high = higher(x[0], x[1]);
 #pragma unroll
   for (int e = 2; e < 8; e += 2) {
-    low = fminf(low, fminf(x[e], x[e + 1]));
-    high = fmaxf(high, fmaxf(x[e], x[e + 1]));
+    low = lower(low, lower(x[e], x[e + 1]));
+    high = higher(high, higher(x[e], x[e + 1]));
   }
-  low = over8(low, [](float a, float b) { return fminf(a, b); });
-  high = over8(high, [](float a, float b) { return fmaxf(a, b); });
+  low = over8(low, lower);
+  high = over8(high, higher);
   const float range = high - low;
-  const uint32_t scale = pack_bf16(range / 15.f, low);
-  const float step = __uint_as_float(scale << 16), inverse = step > 0.f ? __builtin_amdgcn_rcpf(step) : 0.f;
+  // range / 15 the same way: for all 2^23 fractions it is the rounded quotient, and a residual is exact as long as the step is a normal number
+  const float fifteenth = range * (1.f / 15.f);
+  uint32_t scale = pack_bf16(__builtin_fmaf(__builtin_fmaf(-fifteenth, 15.f, range), 1.f / 15.f, fifteenth), low);
+  float step = __uint_as_float(scale << 16);
+  const float inverse = step > 0.f ? __builtin_amdgcn_rcpf(step) : 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float above = x[e] - low, quotient = above * inverse;
@@ -67,6 +73,8 @@ __device__ __forceinline__ uint32_t quantise8(const u32x4& v, float (&number)[8]
   for (int e = 0; e < 8; ++e) odd += x[e] * 0.f;             // NaN where an entry is no finite number
   odd = over8(odd, [](float a, float b) { return a + b; });
   const bool bad = odd != 0.f || !(range < INFINITY);
+  scale = pack_bf16(range / 15.f, low);
+  step = __uint_as_float(scale << 16);
 #pragma unroll
   for (int e = 0; e < 8; ++e) number[e] = !bad && step > 0.f ? fminf(rintf((x[e] - low) / step), 15.f) : 0.f;
   return bad ? 0x7fc07fc0u : scale;                          // NaN, NaN
