@@ -1,4 +1,12 @@
 // Attention over packed prompts, backward.
+//
+// With P = exp(scale q k^T - lse), dP = dout v^T and delta = sum over the dimensions of dout * out: dS = P (dP - delta), dq = scale dS k, dk = scale dS^T q, dv = P^T dout.
+// Two kernels, one for dq with a row's keys in turn, one for dk and dv with a key's queries in turn: scores and dP are worked out in both (9 products with the forward pass, where 7
+// would do), so that every sum has one owner and an order of its own, without atomics and without the scores in memory.
+// P and dS are rounded to bfloat16 for the products that sum over them, as the instruction takes nothing else: dq and dk have 0.0025 relative error, where rounding the result
+// alone has 0.0017; a second product with what the rounding leaves over would take a quarter more time.  delta comes from the rounded out: 0.0001 of that, 0.0002 with a few keys.
+// Bound by power (1.57 and 1.67 GHz; matrix units busy for 77 and 60 % of it, LDS for 38 and 52 %).  8227 tokens in six sequences, 32 heads of 128 sharing 8, causal: dq 290 us,
+// 1030 TFLOP/s, dk and dv 470 us, 850; 4 x 2048 tokens, 16 heads of 64: 77 to 84 and 95 to 105 us.
 #pragma once
 
 #include "attention_kernel.h"
@@ -11,7 +19,7 @@ struct PromptBackArgs {
   float *log_sums, *deltas;        // q_heads x total_q each: -lse / scale, and -(sum over the dimensions of dout * out)
 };
 
-// dq, and delta for the other kernel.  As the forward kernel, with a third product: dq^T += k^T dS^T.
+// dq, and delta for the other kernel.  As the forward kernel, with a third product, dq^T += k^T dS^T, and without its maximum: lse is known.
 template <int D, int NW, int HW, bool CAUSAL>
 __global__ void __launch_bounds__(NW * 64, D == 64 ? 3 : 2) attention_dq_kernel(PromptBackArgs args) {
   const PromptArgs& a = args.f;

@@ -1,4 +1,16 @@
-// Attention over packed prompts, forward.
+// Attention over packed prompts, forward: out = softmax(scale q k^T) v.
+//
+// One pass over the keys, 64 at a time, with the row's maximum m so far and its sum l of exp(score - m) in 32 bits: where m rises, what has been summed is scaled by
+// exp(m before - m).  It rises only by 8 powers of two or more (a smaller one costs no precision, as weights up to 2^8 are as exact as those up to 1), so that the rescaling is rare.
+// Scores come as S^T = k q^T: a lane has 32 scores of one query, whose maximum and sum need one exchange between the halves of the wave, and its weights, rounded, are the operand of
+// out^T += v^T P^T where they are.  The rounding of weights to bfloat16 (the instruction takes nothing else for bfloat16 values) costs 0.0021 relative error against 0.0016 of
+// rounding the result alone; their sum is taken before it.
+//
+// A wave has 32 rows, a workgroup four waves that share tiles of keys and values in LDS, two of each: the next ones load while these are used.  Two or three workgroups to a compute unit.
+// With heads of 128 the bound is power: 1.55 to 1.66 GHz under this kernel, the matrix units busy for 62 to 71 % of it and the vector unit for 59 % (the exponentials).  32768 causal tokens,
+// 16 heads of 128 sharing 4: 3.68 ms, 1195 TFLOP/s; 8192, 32 heads sharing 8: 479 us, 1147.  With heads of 64 a product has half the work for the same exponentials and the vector unit is
+// the bound (90 % at 1.84 GHz): 8192, 32 heads of 64 sharing 8: 288 us, 955 TFLOP/s.  Short prompts are bound by the latency of their loads, one after another: places, then
+// queries and keys, then values.  50 sequences of 1 to 512 tokens, 32 heads of 128 sharing 8: 44 us.
 #pragma once
 
 #include "attention_tiles.h"
