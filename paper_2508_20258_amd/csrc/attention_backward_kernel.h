@@ -65,11 +65,12 @@ __global__ void __launch_bounds__(NW * 64, D == 64 ? 3 : 2) attention_dq_kernel(
     for (int e = 0; e < 8; ++e) delta = __builtin_fmaf((float)gf[i][e], (float)qf[i][e], delta);
   delta = across_halves(delta, [](float x, float y) { return x + y; });
   const int64_t stat = (int64_t)head * a.total_q + token;
-  const float lse = a.lse[stat] * kLog2E;                   // -inf where a row looks at nothing: all of it is masked below
+  float lse = a.lse[stat] * kLog2E;
   if (real && h == 0) {
     args.log_sums[stat] = lse == -INFINITY ? -INFINITY : -lse / (a.scale * kLog2E);
     args.deltas[stat] = -delta;
   }
+  lse = lse == -INFINITY ? 0.f : lse;                       // a row that looks at nothing: its scores are -inf, and so its weights 0
   load_fragments<D>(qf, a.q.at(token, head), lane);
   f32x16 acc[D / 32];
 #pragma unroll
