@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libswz.so")
 SOURCES = ["swz.hip", "attention.hip"]
 HEADERS = ["gemm_kernel.h", "gemm_subtile_kernel.h", "gemm_pair_kernel.h", "gemm_dispatch.h", "aux_kernels.h", "transpose_kernel.h", "transpose_dispatch.h", "tile_sweep.h", "rowwise_kernel.h", "row_dispatch.h", "mfma_peak_kernel.h", "pid_decode.h", "launch.h",
-           "attention_tiles.h", "prompt_order.h", "attention_kernel.h", "attention_backward_kernel.h", "qk_norm_kernel.h", "cache4_kernel.h", os.path.join("..", "..", "include", "swz.h"),
+           "attention_tiles.h", "prompt_order.h", "attention_kernel.h", "attention_backward_kernel.h", "norm_place.h", "qk_norm_kernel.h", "cache4_kernel.h", os.path.join("..", "..", "include", "swz.h"),
            os.path.join("..", "..", "include", "swz_attention.h")]
 
 FAST_SOURCE = os.path.join(CSRC, "fastcall.cpp")

@@ -75,7 +75,7 @@ int check_norm(const swz_norm_args* a) {
 }
 
 swz::NormSide norm_side(const swz_heads& x, const swz_heads& z, const void* weight, int heads, int64_t tokens) {
-  const int blocks = (heads + swz::kNormHeads - 1) / swz::kNormHeads;
+  const int blocks = swz::norm_blocks(heads);
   return {device_heads(x), device_heads(z), {}, static_cast<const uint16_t*>(weight), heads, blocks, (int)(tokens * blocks)};
 }
 swz::NormArgs norm_args(const swz_norm_args& a) {
@@ -86,14 +86,9 @@ swz::NormArgs norm_args(const swz_norm_args& a) {
   n.rotary = a.rotary_dim, n.table_rows = (int)a.table_rows, n.eps = a.eps;
   return n;
 }
-// Workgroups that have an item for each of their D / 8 lanes.
-int norm_workgroups(int items, int head_dim) {
-  const int per = swz::kNormThreads / (head_dim / 8);
-  return items / per + (items % per != 0);
-}
 // Of the backward pass: as many as have items, at most four to a compute unit.
 int norm_backward_workgroups(const swz::NormArgs& n, int head_dim) {
-  const int most = 4 * compute_units(), some = norm_workgroups(n.q.items > n.k.items ? n.q.items : n.k.items, head_dim);
+  const int most = 4 * compute_units(), some = swz::norm_workgroups(n.q.items > n.k.items ? n.q.items : n.k.items, head_dim);
   return some < 1 ? 1 : some < most ? some : most;
 }
 
@@ -269,8 +264,8 @@ int swz_qk_norm_rope(const swz_norm_args* args, hipStream_t stream) {
   return for_head_dim(args->head_dim, [&](auto dim) {
     return for_flag(args->interleaved != 0, [&](auto interleaved) {
       constexpr int D = decltype(dim)::value;
-      n.workgroups_q = norm_workgroups(n.q.items, D);
-      return launch(swz::qk_norm_kernel<D, decltype(interleaved)::value>, dim3((unsigned)(n.workgroups_q + norm_workgroups(n.k.items, D))), dim3(swz::kNormThreads), 0, stream, n);
+      n.workgroups_q = swz::norm_workgroups(n.q.items, D);
+      return launch(swz::qk_norm_kernel<D, decltype(interleaved)::value>, dim3((unsigned)(n.workgroups_q + swz::norm_workgroups(n.k.items, D))), dim3(swz::kNormThreads), 0, stream, n);
     });
   });
 }

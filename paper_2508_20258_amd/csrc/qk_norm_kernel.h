@@ -7,6 +7,7 @@
 #pragma once
 
 #include "attention_tiles.h"
+#include "norm_place.h"
 
 namespace swz {
 
@@ -25,11 +26,6 @@ struct NormArgs {
   int rotary, table_rows;
   float eps;
 };
-
-// D / 8 lanes take kNormHeads heads of a token, 8 dimensions each: the token's angles are loaded once for them, and their product with the weight is
-// taken once.  What turns is exchanged among lanes as it was loaded.
-constexpr int kNormThreads = 256;
-constexpr int kNormHeads = 4;
 
 // Sum over the 8 or 16 neighbouring lanes that hold a row.
 template <int LANES>
@@ -108,12 +104,11 @@ __global__ void __launch_bounds__(kNormThreads) qk_norm_kernel(NormArgs n) {
   const bool keys = (int)blockIdx.x >= n.workgroups_q;
   const NormSide side = keys ? n.k : n.q;
   const int lane = threadIdx.x & 63, d = ((int)threadIdx.x % kLanes) * 8;
-  const int item = min(((int)blockIdx.x - (keys ? n.workgroups_q : 0)) * kItems + (int)threadIdx.x / kLanes, side.items - 1);      // past the end: the last once more
-  const int token = item / side.blocks, head0 = (item - token * side.blocks) * kNormHeads;
-  const int position = n.positions[token];
+  const NormPlace p = norm_place((int64_t)((int)blockIdx.x - (keys ? n.workgroups_q : 0)) * kItems + (int)threadIdx.x / kLanes, side.items, side.blocks);
+  const int position = n.positions[p.token];
   u32x4 x[kNormHeads];
 #pragma unroll
-  for (int i = 0; i < kNormHeads; ++i) x[i] = *reinterpret_cast<const u32x4*>(side.x.at(token, min(head0 + i, side.heads - 1)) + d);
+  for (int i = 0; i < kNormHeads; ++i) x[i] = *reinterpret_cast<const u32x4*>(side.x.at(p.token, min(p.head0 + i, side.heads - 1)) + d);
   const u32x4 weight = *reinterpret_cast<const u32x4*>(side.weight + d);
   const int partner = partner_lane<D, INTERLEAVED>(n.rotary, lane);
   Angles a;
@@ -136,7 +131,7 @@ __global__ void __launch_bounds__(kNormThreads) qk_norm_kernel(NormArgs n) {
     const float r = __builtin_amdgcn_rsqf(row_sum<kLanes>(squares) * (1.f / D) + n.eps);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(v[e], a.c[e], other[e] * a.s[e]) * r;
-    if (head0 + i < side.heads) *reinterpret_cast<u32x4*>(side.z.at(token, head0 + i) + d) = pack8(v);
+    if (norm_stores(p, i, side.heads)) *reinterpret_cast<u32x4*>(side.z.at(p.token, p.head0 + i) + d) = pack8(v);
   }
 }
 
@@ -154,23 +149,22 @@ __global__ void __launch_bounds__(kNormThreads, 4) qk_norm_backward_kernel(NormA
     unpack8(*reinterpret_cast<const u32x4*>(side.weight + d), w);
 #pragma unroll
     for (int e = 0; e < 8; ++e) dw[e] = 0.f;
-    // the last turn of a wave may be partly past the end: those lanes take the last item once more, for the exchanges among lanes, and keep nothing
+    // the last turn of a wave may be partly past the end: those lanes keep nothing
     for (int64_t first = (int64_t)blockIdx.x * kItems; first < side.items; first += (int64_t)gridDim.x * kItems) {
-      const int item = (int)min(first + mine, (int64_t)side.items - 1), token = item / side.blocks, head0 = (item - token * side.blocks) * kNormHeads;
-      const bool there = first + mine < side.items;
-      const int position = n.positions[token];
+      const NormPlace p = norm_place(first + mine, side.items, side.blocks);
+      const int position = n.positions[p.token];
       u32x4 x[kNormHeads], g[kNormHeads];
 #pragma unroll
       for (int i = 0; i < kNormHeads; ++i) {
-        const int head = min(head0 + i, side.heads - 1);
-        x[i] = *reinterpret_cast<const u32x4*>(side.x.at(token, head) + d);
-        g[i] = *reinterpret_cast<const u32x4*>(side.z.at(token, head) + d);
+        const int head = min(p.head0 + i, side.heads - 1);
+        x[i] = *reinterpret_cast<const u32x4*>(side.x.at(p.token, head) + d);
+        g[i] = *reinterpret_cast<const u32x4*>(side.z.at(p.token, head) + d);
       }
       Angles a;
       load_angles<D, INTERLEAVED>(a, n, position, lane, true);
 #pragma unroll
       for (int i = 0; i < kNormHeads; ++i) {
-        const bool real = there && head0 + i < side.heads;
+        const bool real = norm_stores(p, i, side.heads);
         float u[8], dy[8], other[8], squares = 0.f, along = 0.f;
         unpack8(x[i], u);
         unpack8(g[i], dy);
@@ -191,7 +185,7 @@ __global__ void __launch_bounds__(kNormThreads, 4) qk_norm_backward_kernel(NormA
         along = row_sum<kLanes>(along) * (1.f / D);
 #pragma unroll
         for (int e = 0; e < 8; ++e) dy[e] = r * __builtin_fmaf(-u[e], along, dy[e]);
-        if (real) *reinterpret_cast<u32x4*>(side.dx.at(token, head0 + i) + d) = pack8(dy);
+        if (real) *reinterpret_cast<u32x4*>(side.dx.at(p.token, p.head0 + i) + d) = pack8(dy);
       }
     }
     __syncthreads();

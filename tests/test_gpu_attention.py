@@ -356,6 +356,18 @@ def test_norm_rope_and_gradient(swz, tokens, q_heads, k_heads, dim, r, interleav
     assert torch.equal(vq, outs[0]) and torch.equal(vk, outs[1])
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("tokens,q_heads,k_heads", [(1, 8, 1), (1, 32, 8), (37, 8, 2), (74, 4, 1), (129, 32, 8), (1234, 8, 3)])
+def test_norm_in_place_where_the_last_workgroup_is_not_full(swz, tokens, q_heads, k_heads, dim):
+    """Waves past the last head have nothing to store: one that stored what it had loaded from an output would norm it twice."""
+    q, k, wq, wk = randn(tokens, tokens, q_heads, dim, scale=3.0), randn(tokens + 1, tokens, k_heads, dim), randn(2, dim), randn(3, dim)
+    cos, sin = tables(50, dim)
+    p = (torch.arange(tokens, device="cuda") % 50).to(torch.int32)
+    want = swz.qk_norm_rope(q, k, wq, wk, cos, sin, p)
+    got = swz.qk_norm_rope(q, k, wq, wk, cos, sin, p, q, k)
+    assert got[0] is q and got[1] is k and torch.equal(q, want[0]) and torch.equal(k, want[1])
+
+
 def test_norm_positions_outside_the_tables(swz):
     q, w = randn(1, 6, 2, 64), randn(2, 64)
     cos, sin = tables(4, 64)
