@@ -4,13 +4,16 @@ marshalling only, as in binding.py.
 
 Tensors of heads are bfloat16, (tokens, heads, head_dim) with dense head_dim and any distances that are multiples of 8 elements, so that queries, keys and
 values may be views of the rows that one projection wrote.  Sequences are packed: `cu` (int32, sequences + 1) holds the first token of each, and the end.
+
+`stream`: what works, with its outputs and workspaces, instead of the current stream.  As for the library's other functions, the caller orders it with the streams that make
+the inputs and use the outputs.
 """
 from __future__ import annotations
 
 import ctypes
 from typing import NamedTuple
 
-from .binding import _NoFast, _check, _fast, _launch_stream, lib, torch
+from .binding import _NoFast, _check, _empty, _fast, _launch_stream, _on, lib, torch
 
 EXPORTS = ("swz_qk_norm_rope", "swz_qk_norm_rope_backward_workspace", "swz_qk_norm_rope_backward", "swz_attention_workspace", "swz_attention", "swz_attention_backward_workspace",
            "swz_attention_backward", "swz_cache4_append", "swz_cache4_read", "swz_cache4_attention_workspace", "swz_cache4_attention")
@@ -83,20 +86,20 @@ def _is_ints(t, *shape) -> bool:
     return t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == shape
 
 
-def _out(t, like):
+def _out(t, like, stream):
     """An output: `t`, or a new dense tensor; its tokens and heads must not share memory."""
     if t is None:
-        return torch.empty(like.shape, dtype=like.dtype, device=like.device)
+        return _empty(stream, like.shape, like.dtype, like.device)
     assert _is_heads(t, *like.shape)
     (n, h, d), (token, head, _) = t.shape, t.stride()
     assert (n < 2 or h < 2 or token >= h * head >= h * d or head >= n * token >= n * d) and (n < 2 or token >= d) and (h < 2 or head >= d), "tokens or heads of an output overlap"
     return t
 
 
-def _workspace(size: int, where: str, like):
+def _workspace(size: int, where: str, like, stream):
     if size < 0:
         _check(size, where)
-    return torch.empty(size, dtype=torch.uint8, device=like.device) if size else None
+    return _empty(stream, size, torch.uint8, like.device, result=False) if size else None
 
 
 def _pointer(t):
@@ -125,7 +128,7 @@ def qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions, q_out=None, k_ou
         done = _fast.qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
         if done is not None:
             return _done(done, "swz_qk_norm_rope")
-    q_out, k_out = _out(q_out, q), _out(k_out, k)
+    q_out, k_out = _out(q_out, q, stream), _out(k_out, k, stream)
     a = _norm_args(q, k, q_out, k_out, q_weight, k_weight, cos, sin, positions, eps, interleaved)
     h = _launch_stream(stream, q, k, q_out, k_out, q_weight, k_weight, cos, sin, positions)
     if q.shape[0] > 0:
@@ -141,25 +144,17 @@ def qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, po
         if done is not None:
             return _done(done, "swz_qk_norm_rope_backward")
     assert _is_heads(dq_out, *q.shape) and _is_heads(dk_out, *k.shape)
-    dq, dk = _out(dq, q), _out(dk, k)
+    dq, dk = _out(dq, q, stream), _out(dk, k, stream)
     a = _norm_args(q, k, dq_out, dk_out, q_weight, k_weight, cos, sin, positions, eps, interleaved)
-    weights = torch.empty((2, q.shape[2]), dtype=torch.float32, device=q.device)
+    weights = _empty(stream, (2, q.shape[2]), torch.float32, q.device)
     h = _launch_stream(stream, q, k, dq_out, dk_out, dq, dk, q_weight, k_weight, cos, sin, positions)
     if q.shape[0] == 0:
-        return dq, dk, *weights.zero_()
-    work = _workspace(lib.swz_qk_norm_rope_backward_workspace(ctypes.byref(a)), "swz_qk_norm_rope_backward", q)
+        _fill_zero(weights, stream)
+        return dq, dk, *weights
+    work = _workspace(lib.swz_qk_norm_rope_backward_workspace(ctypes.byref(a)), "swz_qk_norm_rope_backward", q, stream)
     _check(lib.swz_qk_norm_rope_backward(ctypes.byref(a), ctypes.byref(_heads(dq)), ctypes.byref(_heads(dk)), weights[0].data_ptr(), weights[1].data_ptr(),
                                          work.data_ptr(), work.numel(), h), "swz_qk_norm_rope_backward")
-    _keep(stream, work, weights)
     return dq, dk, weights[0], weights[1]
-
-
-def _keep(stream, *tensors) -> None:
-    """Memory made here is used on `stream`, not the one that torch hands it out for again."""
-    if stream is not None:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
 
 
 def _attention_args(q, k, v, out, lse, cu_q, cu_k, causal, scale) -> _AttentionArgs:
@@ -184,9 +179,9 @@ def attention(q, k, v, cu_q, cu_k=None, out=None, lse=None, causal: bool = True,
         if done is not None:
             return _done(done, "swz_attention")
     cu_k = _check_prompt(q, k, v, cu_q, cu_k)
-    out = _out(out, q)
+    out = _out(out, q, stream)
     if lse is None:
-        lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
+        lse = _empty(stream, (q.shape[1], q.shape[0]), torch.float32, q.device)
     assert lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (q.shape[1], q.shape[0])
     h = _launch_stream(stream, q, k, v, out, lse, cu_q, cu_k)
     if q.shape[0] == 0:
@@ -194,9 +189,8 @@ def attention(q, k, v, cu_q, cu_k=None, out=None, lse=None, causal: bool = True,
     if k.shape[0] == 0:                                   # nothing to look at: no memory that a pointer could name either
         k = v = q[:1, :1].expand(1, k.shape[1], -1)
     a = _attention_args(q, k, v, out, lse, cu_q, cu_k, causal, scale)
-    work = _workspace(lib.swz_attention_workspace(ctypes.byref(a)), "swz_attention", q)
+    work = _workspace(lib.swz_attention_workspace(ctypes.byref(a)), "swz_attention", q, stream)
     _check(lib.swz_attention(ctypes.byref(a), _pointer(work), 0 if work is None else work.numel(), h), "swz_attention")
-    _keep(stream, work)
     return out, lse
 
 
@@ -209,26 +203,22 @@ def attention_backward(dout, q, k, v, out, lse, cu_q, cu_k=None, dq=None, dk=Non
     cu_k = _check_prompt(q, k, v, cu_q, cu_k)
     assert _is_heads(dout, *q.shape) and _is_heads(out, *q.shape)
     assert lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (q.shape[1], q.shape[0])
-    dq, dk, dv = _out(dq, q), _out(dk, k), _out(dv, v)
+    dq, dk, dv = _out(dq, q, stream), _out(dk, k, stream), _out(dv, v, stream)
     h = _launch_stream(stream, dout, q, k, v, out, lse, cu_q, cu_k, dq, dk, dv)
     if q.shape[0] == 0 or k.shape[0] == 0:                # gradients of nothing
         for t in (dq, dk, dv):
             _fill_zero(t, stream)
         return dq, dk, dv
     a = _attention_args(q, k, v, out, lse, cu_q, cu_k, causal, scale)
-    work = _workspace(lib.swz_attention_backward_workspace(ctypes.byref(a)), "swz_attention_backward", q)
+    work = _workspace(lib.swz_attention_backward_workspace(ctypes.byref(a)), "swz_attention_backward", q, stream)
     _check(lib.swz_attention_backward(ctypes.byref(a), *(ctypes.byref(_heads(t)) for t in (dout, dq, dk, dv)), work.data_ptr(), work.numel(), h),
            "swz_attention_backward")
-    _keep(stream, work)
     return dq, dk, dv
 
 
 def _fill_zero(t, stream) -> None:
-    if stream is None:
+    with _on(stream):
         t.zero_()
-    else:
-        with torch.cuda.stream(stream):
-            t.zero_()
 
 
 class Cache4(NamedTuple):
@@ -289,8 +279,8 @@ def cache4_read(cache: Cache4, cu, first, block_table, tokens: int, k=None, v=No
     assert _is_ints(first, n) and _is_ints(cu, n + 1) and block_table.dim() == 2 and _is_ints(block_table, n, block_table.shape[1])
     shape = (int(tokens), c.k_heads, c.head_dim)
     like = torch.empty(shape, dtype=torch.bfloat16, device="meta") if k is None or v is None else k
-    k = torch.empty(shape, dtype=torch.bfloat16, device=cu.device) if k is None else _out(k, like)
-    v = torch.empty(shape, dtype=torch.bfloat16, device=cu.device) if v is None else _out(v, like)
+    k = _empty(stream, shape, torch.bfloat16, cu.device) if k is None else _out(k, like, stream)
+    v = _empty(stream, shape, torch.bfloat16, cu.device) if v is None else _out(v, like, stream)
     assert tuple(k.shape) == tuple(v.shape) == shape
     h = _launch_stream(stream, k, v, cu, first, block_table, *cache)
     if shape[0] > 0:
@@ -310,14 +300,13 @@ def cache4_attention(q, cache: Cache4, lengths, block_table, max_length: int = 0
     assert _is_heads(q, None, None, c.head_dim)
     n, q_heads, dim = q.shape
     assert _is_ints(lengths, n) and block_table.dim() == 2 and _is_ints(block_table, n, block_table.shape[1])
-    out = _out(out, q)
+    out = _out(out, q, stream)
     h = _launch_stream(stream, q, out, lengths, block_table, *cache)
     if n == 0:
         return out
     width, longest = block_table.shape[1], int(max_length)
-    work = _workspace(lib.swz_cache4_attention_workspace(ctypes.byref(c), n, q_heads, width, longest), "swz_cache4_attention", q)
+    work = _workspace(lib.swz_cache4_attention_workspace(ctypes.byref(c), n, q_heads, width, longest), "swz_cache4_attention", q, stream)
     _check(lib.swz_cache4_attention(ctypes.byref(c), ctypes.byref(_heads(q)), ctypes.byref(_heads(out)), lengths.data_ptr(), block_table.data_ptr(), width, n, q_heads,
                                     longest, dim ** -0.5 if scale is None else float(scale), _pointer(work), 0 if work is None else work.numel(), h),
            "swz_cache4_attention")
-    _keep(stream, work)
     return out

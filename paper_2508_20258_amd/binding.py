@@ -5,6 +5,7 @@ torch is used for device memory (``tensor.data_ptr()``) and streams only.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import warnings
@@ -161,6 +162,28 @@ def _launch_stream(stream, *tensors) -> int:
             return torch._C._cuda_getCurrentRawStream(cur)
     _same_current_device(stream, *tensors)
     return _stream_handle(stream)
+
+
+def _on(stream):
+    """What is allocated or filled within belongs to the stream that works on it.  A stream may be any object with `cuda_stream`."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = int(stream.cuda_stream)
+        stream = torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
+    return torch.cuda.stream(stream)
+
+
+def _empty(stream, shape, dtype, device, result: bool = True):
+    """Memory for work on `stream`: from that stream's own, as a block that was freed on another one may still be in use there.  A result may be used on the
+    caller's current stream too (ordered by the caller, as ever) and is not handed out again before that is done."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with _on(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if result:
+        t.record_stream(torch.cuda.current_stream(device))
+    return t
 
 
 def _params_ref(params):

@@ -660,6 +660,38 @@ def test_another_stream(swz):
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+def test_a_stream_that_is_a_handle_alone(swz):
+    class Handle:
+        def __init__(self, stream):
+            self.cuda_stream = stream.cuda_stream
+
+    t = layer_inputs(swz, 2)
+    want = layer_pass(swz, t)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for stream in (side, torch.cuda.default_stream()):
+        got = layer_pass(swz, t, stream=Handle(stream))
+        stream.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_memory_still_in_use_on_the_current_stream(swz):
+    """Blocks that were freed on the current stream while work on it waits, of the sizes that a pass makes: the pass on another stream gets none of them."""
+    t = layer_inputs(swz, 3)
+    want = layer_pass(swz, t)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20_000_000)
+    for _ in range(3):
+        junk = [torch.empty_like(x) for x in want] + [torch.empty(1 << n, dtype=torch.uint8, device="cuda") for n in range(9, 21)]
+        for x in junk:
+            x.fill_(77)
+        del junk, x
+    got = layer_pass(swz, t, stream=side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_captured_in_a_graph(swz):
     t = layer_inputs(swz, 5)
     layer_pass(swz, t)
