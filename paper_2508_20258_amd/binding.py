@@ -174,15 +174,21 @@ def _on(stream):
     return torch.cuda.stream(stream)
 
 
+def _handed_out(stream, *results) -> None:
+    """Results made on `stream` may be used on the caller's current stream too (ordered by the caller, as ever): their memory is not handed out again before that is done."""
+    if stream is not None:
+        for t in results:
+            t.record_stream(torch.cuda.current_stream(t.device))
+
+
 def _empty(stream, shape, dtype, device, result: bool = True):
-    """Memory for work on `stream`: from that stream's own, as a block that was freed on another one may still be in use there.  A result may be used on the
-    caller's current stream too (ordered by the caller, as ever) and is not handed out again before that is done."""
+    """Memory for work on `stream`: from that stream's own, as a block that was freed on another one may still be in use there."""
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=device)
     with _on(stream):
         t = torch.empty(shape, dtype=dtype, device=device)
     if result:
-        t.record_stream(torch.cuda.current_stream(device))
+        _handed_out(stream, t)
     return t
 
 
@@ -215,8 +221,10 @@ def pid_map_device(grid_m: int, grid_n: int, num_xcd: int, group_m: int, mode: i
     n = int(grid_m) * int(grid_n)
     if not 0 < n < (1 << 31):
         n = 1  # let the library report the error; keep the buffers valid
-    tile = torch.full((n,), -1, dtype=torch.int32, device="cuda")
-    xcc = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    with _on(stream):
+        tile = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+        xcc = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    _handed_out(stream, tile, xcc)
     _check(lib.swz_pid_map_device(int(grid_m), int(grid_n), int(num_xcd), int(group_m), int(mode), tile.data_ptr(),
                                   xcc.data_ptr(), _stream_handle(stream)), "swz_pid_map_device")
     return tile, xcc
@@ -258,7 +266,7 @@ def gemm(a, b, c=None, mode: int = MODE_XCD_GROUPM, stream=None, **params):
     M, K = a.shape
     N = b.shape[1]
     if c is None:
-        c = torch.empty((M, N), dtype=torch.bfloat16, device=a.device)
+        c = _empty(stream, (M, N), torch.bfloat16, a.device)
     assert c.is_cuda and c.dtype == torch.bfloat16 and c.is_contiguous() and tuple(c.shape) == (M, N)
     h = _launch_stream(stream, a, b, c)
     if params:
@@ -283,12 +291,14 @@ def gemm_probe(a, b, c=None, mode: int = MODE_XCD_GROUPM, stream=None, probe=Non
     M, K = a.shape
     N = b.shape[1]
     if c is None:
-        c = torch.empty((M, N), dtype=torch.bfloat16, device=a.device)
+        c = _empty(stream, (M, N), torch.bfloat16, a.device)
     assert c.is_cuda and c.dtype == torch.bfloat16 and c.is_contiguous() and tuple(c.shape) == (M, N)
     _same_current_device(stream, a, b, c)
     plan = gemm_plan(M, N, K, **params)
     if probe is None:
-        probe = torch.full((plan["grid_m"] * plan["grid_n"], PROBE_WORDS), -1, dtype=torch.int64, device=a.device)
+        with _on(stream):
+            probe = torch.full((plan["grid_m"] * plan["grid_n"], PROBE_WORDS), -1, dtype=torch.int64, device=a.device)
+        _handed_out(stream, probe)
     assert probe.is_cuda and probe.is_contiguous() and probe.dtype == torch.int64
     p = _params(**params)
     _check(lib.swz_gemm_probe(a.data_ptr(), b.data_ptr(), c.data_ptr(), M, N, K, DTYPE_BF16, int(mode), ctypes.byref(p),
@@ -321,8 +331,10 @@ def pid_map_persistent(grid_m: int, grid_n: int, num_xcd: int, group_m: int, mod
 def pid_map_persistent_device(grid_m: int, grid_n: int, num_xcd: int, group_m: int, mode: int, num_wg: int, stream=None):
     """Device PID map of the persistent launch: (tile [rounds x num_wg], xcc [num_wg]) int32 CUDA tensors."""
     rounds = _rounds(grid_m, grid_n, num_wg)
-    tile = torch.full((rounds, max(int(num_wg), 1)), -2, dtype=torch.int32, device="cuda")
-    xcc = torch.full((max(int(num_wg), 1),), -1, dtype=torch.int32, device="cuda")
+    with _on(stream):
+        tile = torch.full((rounds, max(int(num_wg), 1)), -2, dtype=torch.int32, device="cuda")
+        xcc = torch.full((max(int(num_wg), 1),), -1, dtype=torch.int32, device="cuda")
+    _handed_out(stream, tile, xcc)
     _check(lib.swz_pid_map_persistent_device(int(grid_m), int(grid_n), int(num_xcd), int(group_m), int(mode), int(num_wg),
                                              tile.data_ptr(), xcc.data_ptr(), _stream_handle(stream)),
            "swz_pid_map_persistent_device")
@@ -342,7 +354,7 @@ def transpose(x, out=None, tile: int = 64, mode: int = MODE_XCD_GROUPM + MODE_SK
     assert x.is_cuda and x.is_contiguous() and x.dim() == 2 and x.element_size() in (2, 4)
     M, N = x.shape
     if out is None:
-        out = torch.empty((N, M), dtype=x.dtype, device=x.device)
+        out = _empty(stream, (N, M), x.dtype, x.device)
     assert out.is_cuda and out.is_contiguous() and tuple(out.shape) == (N, M) and out.dtype == x.dtype
     h = _launch_stream(stream, x, out)
     _check(lib.swz_transpose(x.data_ptr(), out.data_ptr(), M, N, x.element_size(), int(tile), int(mode), _params_ref(params),
@@ -350,10 +362,10 @@ def transpose(x, out=None, tile: int = 64, mode: int = MODE_XCD_GROUPM + MODE_SK
     return out
 
 
-def _row_args(x, out):
+def _row_args(x, out, stream):
     assert x.is_cuda and x.is_contiguous() and x.dim() == 2 and x.dtype == torch.bfloat16
     if out is None:
-        out = torch.empty_like(x)
+        out = _empty(stream, x.shape, x.dtype, x.device)
     assert out.is_cuda and out.is_contiguous() and out.shape == x.shape and out.dtype == x.dtype
     return out
 
@@ -366,7 +378,7 @@ def softmax(x, out=None, chunks: int = 1, mode: int = MODE_XCD, stream=None, **p
         if st is not None:
             _check(st, "swz_softmax")
             return out
-    out = _row_args(x, out)
+    out = _row_args(x, out, stream)
     h = _launch_stream(stream, x, out)
     M, N = x.shape
     _check(lib.swz_softmax(x.data_ptr(), out.data_ptr(), M, N, int(chunks), int(mode), _params_ref(params), h), "swz_softmax")
@@ -380,7 +392,7 @@ def layernorm(x, gamma, beta, out=None, eps: float = 1e-5, chunks: int = 1, mode
         if st is not None:
             _check(st, "swz_layernorm")
             return out
-    out = _row_args(x, out)
+    out = _row_args(x, out, stream)
     for t in (gamma, beta):
         assert t.is_cuda and t.is_contiguous() and t.dtype == x.dtype and t.numel() == x.shape[1]
     h = _launch_stream(stream, x, out, gamma, beta)

@@ -6,7 +6,10 @@ import pytest
 torch = pytest.importorskip("torch")
 
 import paper_2508_20258_amd as swz  # noqa: E402
-from paper_2508_20258_amd import attention_layer as layer  # noqa: E402
+from paper_2508_20258_amd import attention_layer as layer, binding  # noqa: E402
+
+
+REAL = binding.lib
 
 
 class OnDevice(torch.Tensor):
@@ -26,6 +29,8 @@ class Side:                       # a stream of another library: a handle alone
 
 class Library:
     def __getattr__(self, name):
+        if name in ("swz_status_string", "swz_gemm_plan"):
+            return getattr(REAL, name)
         return (lambda *args: 64) if name.endswith("_workspace") else (lambda *args: 0)
 
 
@@ -33,7 +38,7 @@ class World:
     def __init__(self, monkeypatch):
         World.now = self
         self.inside, self.made, self.filled, self.recorded = None, [], [], []
-        empty = torch.empty
+        empty, full = torch.empty, torch.full
 
         @contextlib.contextmanager
         def stream(s):
@@ -46,12 +51,20 @@ class World:
                 self.made.append(self.inside)
             return empty(*args, **kw).as_subclass(OnDevice)
 
+        def filled(*args, **kw):
+            self.made.append(self.inside)
+            return full(*args, **{**kw, "device": "cpu"}).as_subclass(OnDevice)
+
         monkeypatch.setattr(torch, "empty", made)
+        monkeypatch.setattr(torch, "full", filled)
         monkeypatch.setattr(torch.cuda, "stream", stream)
         monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle: ("external", handle))
         monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: "current")
-        monkeypatch.setattr(layer, "lib", Library())
-        monkeypatch.setattr(layer, "_launch_stream", lambda s, *tensors: 0)
+        for module in (binding, layer):
+            monkeypatch.setattr(module, "lib", Library())
+            monkeypatch.setattr(module, "_launch_stream", lambda s, *tensors: 0)
+        monkeypatch.setattr(binding, "_same_current_device", lambda s, *tensors: None)
+        monkeypatch.setattr(binding, "_stream_handle", lambda s: 0)
 
 
 @pytest.fixture
@@ -80,6 +93,14 @@ def lse(n):
     return torch.zeros((2, n)).as_subclass(OnDevice)
 
 
+def matrix(m, n):
+    return torch.zeros((m, n), dtype=torch.bfloat16).as_subclass(OnDevice)
+
+
+def row(n):
+    return torch.zeros(n, dtype=torch.bfloat16).as_subclass(OnDevice)
+
+
 CALLS = {   # a call on `stream`, how many results and workspaces it makes
     "qk_norm_rope": (lambda s: swz.qk_norm_rope(*norm_inputs(3), stream=s), 2, 0),
     "qk_norm_rope_backward": (lambda s: swz.qk_norm_rope_backward(heads(3), heads(3, 1), *norm_inputs(3), stream=s), 3, 1),
@@ -87,6 +108,13 @@ CALLS = {   # a call on `stream`, how many results and workspaces it makes
     "attention_backward": (lambda s: swz.attention_backward(heads(3), heads(3), heads(3), heads(3), heads(3), lse(3), ints(0, 3), stream=s), 3, 1),
     "cache4_read": (lambda s: swz.cache4_read(cache(), ints(0, 3), ints(0), ints(0)[None], 3, stream=s), 2, 0),
     "cache4_attention": (lambda s: swz.cache4_attention(heads(1), cache(), ints(1), ints(0)[None], stream=s), 1, 1),
+    "gemm": (lambda s: swz.gemm(matrix(8, 16), matrix(16, 8), stream=s), 1, 0),
+    "gemm_probe": (lambda s: swz.gemm_probe(matrix(8, 16), matrix(16, 8), stream=s, num_xcd=8), 2, 0),
+    "transpose": (lambda s: swz.transpose(matrix(8, 16), stream=s), 1, 0),
+    "softmax": (lambda s: swz.softmax(matrix(8, 16), stream=s), 1, 0),
+    "layernorm": (lambda s: swz.layernorm(matrix(8, 16), row(16), row(16), stream=s), 1, 0),
+    "pid_map_device": (lambda s: swz.pid_map_device(2, 2, 8, 1, 0, stream=s), 2, 0),
+    "pid_map_persistent_device": (lambda s: swz.pid_map_persistent_device(2, 2, 8, 1, 0, 4, stream=s), 2, 0),
 }
 
 
