@@ -54,18 +54,22 @@ __device__ __forceinline__ u32x4 pack8(const float (&x)[8]) {
   return v;
 }
 
-// Which lane has the other halves of a lane's pairs.
+// Which lane has the other halves of a lane's pairs, and whether the lane's dimensions have any.
+struct Partner {
+  int lane;
+  uint32_t bits;                     // all where the lane's dimensions are turned, else none
+};
 template <int D, bool INTERLEAVED>
-__device__ __forceinline__ int partner_lane(int rotary, int lane) {
+__device__ __forceinline__ Partner partner_of(int rotary, int lane) {
   const int d = (lane % (D / 8)) * 8, half = rotary / 2;
-  return INTERLEAVED || d >= rotary ? lane : d < half ? lane + half / 8 : lane - half / 8;
+  return {INTERLEAVED || d >= rotary ? lane : d < half ? lane + half / 8 : lane - half / 8, d < rotary ? ~0u : 0u};
 }
-// The halves: of other lanes, or (interleaved) the neighbours.
+// The halves: of other lanes, or (interleaved) the neighbours.  0 for dimensions that are not turned: a sine of 0 would not keep an infinity or NaN out.
 template <bool INTERLEAVED>
-__device__ __forceinline__ void others(const u32x4& v, int partner, float (&other)[8]) {
+__device__ __forceinline__ void others(const u32x4& v, Partner partner, float (&other)[8]) {
   u32x4 w;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) w[e] = INTERLEAVED ? v[e] << 16 | v[e] >> 16 : (uint32_t)__builtin_amdgcn_ds_bpermute(partner * 4, (int)v[e]);
+  for (int e = 0; e < 4; ++e) w[e] = (INTERLEAVED ? v[e] << 16 | v[e] >> 16 : (uint32_t)__builtin_amdgcn_ds_bpermute(partner.lane * 4, (int)v[e])) & partner.bits;
   unpack8(w, other);
 }
 
@@ -110,7 +114,7 @@ __global__ void __launch_bounds__(kNormThreads) qk_norm_kernel(NormArgs n) {
 #pragma unroll
   for (int i = 0; i < kNormHeads; ++i) x[i] = *reinterpret_cast<const u32x4*>(side.x.at(p.token, min(p.head0 + i, side.heads - 1)) + d);
   const u32x4 weight = *reinterpret_cast<const u32x4*>(side.weight + d);
-  const int partner = partner_lane<D, INTERLEAVED>(n.rotary, lane);
+  const Partner partner = partner_of<D, INTERLEAVED>(n.rotary, lane);
   Angles a;
   load_angles<D, INTERLEAVED>(a, n, position, lane, false);
   float w[8], w_other[8];
@@ -142,7 +146,7 @@ __global__ void __launch_bounds__(kNormThreads, 4) qk_norm_backward_kernel(NormA
   constexpr int kLanes = D / 8, kItems = kNormThreads / kLanes;
   __shared__ float sums[kItems][D];
   const int lane = threadIdx.x & 63, d = ((int)threadIdx.x % kLanes) * 8, mine = (int)threadIdx.x / kLanes;
-  const int partner = partner_lane<D, INTERLEAVED>(n.rotary, lane);
+  const Partner partner = partner_of<D, INTERLEAVED>(n.rotary, lane);
   for (int keys = 0; keys < 2; ++keys) {
     const NormSide side = keys ? n.k : n.q;
     float w[8], dw[8];

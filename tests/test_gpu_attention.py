@@ -377,6 +377,31 @@ def test_norm_positions_outside_the_tables(swz):
         assert torch.isnan(out[[1, 3, 4]]).all() and torch.isfinite(out[[0, 2, 5]]).all()
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dim,r", [(64, 32), (64, 48), (128, 16), (128, 96)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("where", ["x", "gradient", "weight"])
+def test_norm_of_what_is_not_finite_where_nothing_turns(swz, where, bad, dim, r, interleaved):
+    """An infinity or NaN in a dimension that is not turned reaches what the formula says, not its neighbour."""
+    tokens, heads, at = 5, 3, (3, 1, r + 2)
+    x, dz, w = randn(dim, tokens, heads, dim), randn(dim + 1, tokens, heads, dim), randn(dim + 2, dim)
+    cos, sin = tables(50, r)
+    positions = torch.tensor([7, 0, 49, 23, 11], dtype=torch.int32, device="cuda")
+    {"x": x[at[0], at[1]], "gradient": dz[at[0], at[1]], "weight": w}[where][at[2]] = bad
+    outs = swz.qk_norm_rope(x, x, w, w, cos, sin, positions, interleaved=interleaved)
+    back = swz.qk_norm_rope_backward(dz, dz, x, x, w, w, cos, sin, positions, interleaved=interleaved)
+    xs, zs, ws, c, s, p = f64(x), f64(dz), f64(w), f64(cos), f64(sin), positions.cpu().numpy()
+    with np.errstate(invalid="ignore"):
+        want = np.stack([ar.norm_rope(xs[t], ws, c[p[t]], s[p[t]], interleaved, 1e-6) for t in range(tokens)])
+        pairs = [ar.norm_rope_backward(zs[t], xs[t], ws, c[p[t]], s[p[t]], interleaved, 1e-6) for t in range(tokens)]
+        dx, dw = np.stack([g for g, _ in pairs]), sum(g for _, g in pairs)
+    for side in range(2):
+        for got, exact, tolerance in ((outs[side], want, ar.ROUND), (back[side], dx, ar.ROUND), (back[2 + side], dw, 1e-5)):
+            got, some = f64(got), np.isfinite(exact)
+            assert np.array_equal(np.isnan(got), np.isnan(exact)) and np.array_equal(got[np.isinf(exact)], exact[np.isinf(exact)])
+            assert (np.abs(got[some] - exact[some]) <= 1.02 * tolerance * np.abs(exact[some]) + 1e-4).all()
+
+
 def test_norm_weights_over_many_rows(swz):
     # more rows than the launch has places for: workgroups go over them in turns
     tokens, heads, dim = 40000, 8, 64
