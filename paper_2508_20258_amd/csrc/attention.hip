@@ -312,6 +312,8 @@ int swz_attention(const swz_attention_args* args, void* workspace, int64_t works
   swz::PromptArgs p = prompt_args(*args);
   p.part_sums = static_cast<float*>(workspace);
   p.part_stats = p.part_sums + (floats > 0 ? floats / (args->head_dim + 2) * args->head_dim : 0);
+  const int64_t join_slots = slots_of(args->total_q, args->sequences, swz::kJoinRows);
+  if (splits > 1 && too_many_threads(join_slots, args->q_heads, 1, p.num_xcd, 64 * swz::kJoinRows)) return SWZ_ERR_OVERFLOW;
   return for_head_dim(args->head_dim, [&](auto dim) {
     return for_flag(args->causal != 0, [&](auto causal) {
       constexpr int D = decltype(dim)::value;
@@ -323,10 +325,8 @@ int swz_attention(const swz_attention_args* args, void* workspace, int64_t works
       });
       if (status != SWZ_OK || splits == 1) return status;
       p.sets = swz::prompt_sets(args->q_heads, p.num_xcd);
-      const int64_t slots = slots_of(args->total_q, args->sequences, swz::kJoinRows);
-      if (slots >= kTokens || swz::prompt_workgroups(slots, args->q_heads, 1, p.num_xcd) >= kTokens) return (int)SWZ_ERR_OVERFLOW;
-      p.slots = (int)slots;
-      return launch(swz::attention_join_kernel<D>, dim3((unsigned)swz::prompt_workgroups(slots, args->q_heads, 1, p.num_xcd)), dim3(64 * swz::kJoinRows), 0, stream, p);
+      p.slots = (int)join_slots;
+      return launch(swz::attention_join_kernel<D>, dim3((unsigned)swz::prompt_workgroups(join_slots, args->q_heads, 1, p.num_xcd)), dim3(64 * swz::kJoinRows), 0, stream, p);
     });
   });
 }

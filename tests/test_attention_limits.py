@@ -1,0 +1,29 @@
+"""What the attention entry points say at the ends of their ranges, before anything is launched or written.  No GPU: pointers that are never used."""
+import ctypes
+
+import pytest
+
+from paper_2508_20258_amd import attention_layer as layer
+
+P = 0x1000
+OK, INVALID, OVERFLOW = 0, -1, -3
+
+
+def heads(token=256, head=128):
+    return layer._Heads(P, token, head)
+
+
+def prompt_args(**change):
+    a = dict(q=heads(), k=heads(), v=heads(), out=heads(), lse=P, cu_q=P, cu_k=P, total_q=3, total_k=3, sequences=1, q_heads=2, k_heads=1, head_dim=128, causal=1, scale=0.1)
+    a.update(change)
+    return layer._AttentionArgs(*(a[n] for n, _ in layer._AttentionArgs._fields_))
+
+
+@pytest.mark.parametrize("causal", [0, 1])
+@pytest.mark.parametrize("head_dim", [64, 128])
+def test_no_launch_where_a_later_one_is_too_large(head_dim, causal):
+    # two million sequences of about 1070 keys: cut in two, which 12 million workgroups do, and joined for each of 12 heads by twice as many of as many threads
+    a = prompt_args(total_q=100, total_k=(1 << 31) - 5000, sequences=2000000, q_heads=12, k_heads=3, head_dim=head_dim, causal=causal)
+    need = layer.lib.swz_attention_workspace(ctypes.byref(a))
+    assert need > 0
+    assert layer.lib.swz_attention(ctypes.byref(a), P, need, None) == OVERFLOW
