@@ -82,7 +82,7 @@ int swz_attention(const swz_attention_args* args, void* workspace, int64_t works
 /* The gradient of swz_attention: args as in the forward call, with its out and lse (read).
  *   dout : gradient of out.   dq, dk, dv : receive those of q, k, v, for all tokens of the sequences (must not overlap anything that is read).
  *   Weights and their gradients are rounded to bfloat16 for the products.  No atomics: the bits do not depend on the run.
- *   workspace : swz_attention_backward_workspace(args) bytes, 16-byte aligned. */
+ *   workspace : swz_attention_backward_workspace(args) bytes, 16-byte aligned; may be null where that is 0. */
 int64_t swz_attention_backward_workspace(const swz_attention_args* args);
 int swz_attention_backward(const swz_attention_args* args, const swz_heads* dout, const swz_heads* dq, const swz_heads* dk, const swz_heads* dv,
                            void* workspace, int64_t workspace_bytes, hipStream_t stream);

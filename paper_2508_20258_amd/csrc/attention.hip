@@ -340,11 +340,12 @@ int swz_attention_backward(const swz_attention_args* args, const swz_heads* dout
                            void* workspace, int64_t workspace_bytes, hipStream_t stream) {
   int st = check_prompt(args);
   if (st != SWZ_OK) return st;
-  if (dout == nullptr || dq == nullptr || dk == nullptr || dv == nullptr || workspace == nullptr) return SWZ_ERR_INVALID_ARG;
+  if (dout == nullptr || dq == nullptr || dk == nullptr || dv == nullptr) return SWZ_ERR_INVALID_ARG;
   st = check_heads(*dout, *dq, *dk, *dv);
   if (st != SWZ_OK) return st;
   if (!aligned(workspace, 16) || dout->token >= kRowDistance) return SWZ_ERR_UNSUPPORTED;
-  if (workspace_bytes < swz_attention_backward_workspace(args)) return SWZ_ERR_INVALID_ARG;
+  const int64_t bytes = swz_attention_backward_workspace(args);
+  if (bytes > 0 && (workspace == nullptr || workspace_bytes < bytes)) return SWZ_ERR_INVALID_ARG;
   swz::PromptBackArgs p{};
   p.f = prompt_args(*args);
   p.dout = device_heads(*dout), p.dq = device_heads(*dq), p.dk = device_heads(*dk), p.dv = device_heads(*dv);

@@ -27,3 +27,13 @@ def test_no_launch_where_a_later_one_is_too_large(head_dim, causal):
     need = layer.lib.swz_attention_workspace(ctypes.byref(a))
     assert need > 0
     assert layer.lib.swz_attention(ctypes.byref(a), P, need, None) == OVERFLOW
+
+
+@pytest.mark.parametrize("head_dim", [64, 128])
+def test_no_workspace_where_none_is_needed(head_dim):
+    a, h = ctypes.byref(prompt_args(total_q=0, total_k=0, head_dim=head_dim)), ctypes.byref(heads())
+    assert layer.lib.swz_attention_workspace(a) == layer.lib.swz_attention_backward_workspace(a) == 0
+    assert layer.lib.swz_attention(a, None, 0, None) == layer.lib.swz_attention_backward(a, h, h, h, h, None, 0, None) == OK
+    a = ctypes.byref(prompt_args(head_dim=head_dim))
+    need = layer.lib.swz_attention_backward_workspace(a)
+    assert need > 0 and layer.lib.swz_attention_backward(a, h, h, h, h, None, need, None) == INVALID
