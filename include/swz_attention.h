@@ -47,7 +47,7 @@ typedef struct {
 } swz_norm_args;
 
 /* Errors (all functions here): INVALID_ARG (null pointer, a size or count < 0, heads or sequences < 1, heads not a multiple of one
- * another, eps < 0 or a scale that is not finite and > 0), UNSUPPORTED (head_dim, rotary_dim, page size, alignment, distances), OVERFLOW (tokens >= 2^31, or a
+ * another, eps < 0 or a scale that is not finite and > 0), UNSUPPORTED (head_dim, rotary_dim, page size, alignment, distances), OVERFLOW (tokens >= 2^31, for attention tokens or a table's positions > 2^31 - 4096, or a
  * launch of 2^32 threads or more), HIP.  No tokens at all: SWZ_OK, and gradients of weights are 0. */
 int swz_qk_norm_rope(const swz_norm_args* args, hipStream_t stream);
 

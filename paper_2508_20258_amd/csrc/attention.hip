@@ -20,6 +20,7 @@ using swz::launch;
 using swz::query_device;
 
 constexpr int64_t kTokens = (int64_t)1 << 31;      // fewer than these
+constexpr int64_t kMostKeys = kTokens - 4096;      // of what is looked at (and looks): tiles and steps past the last one are 32-bit numbers too, and so is the sum of the steps of 64 sequences
 constexpr int64_t kRowDistance = (int64_t)1 << 28;      // less than this from one token to the next, where tiles of tokens are loaded (RowLoader)
 
 swz::Heads device_heads(const swz_heads& h) { return {static_cast<uint16_t*>(h.data), h.token, h.head}; }
@@ -102,7 +103,7 @@ int check_prompt(const swz_attention_args* a) {
   if (st != SWZ_OK) return st;
   if (a->q.token >= kRowDistance || a->k.token >= kRowDistance || a->v.token >= kRowDistance) return SWZ_ERR_UNSUPPORTED;
   if (!head_dim_ok(a->head_dim) || !aligned(a->lse, 4) || !aligned(a->cu_q, 4) || !aligned(a->cu_k, 4)) return SWZ_ERR_UNSUPPORTED;
-  return a->total_q >= kTokens || a->total_k >= kTokens ? SWZ_ERR_OVERFLOW : SWZ_OK;
+  return a->total_q > kMostKeys || a->total_k > kMostKeys ? SWZ_ERR_OVERFLOW : SWZ_OK;
 }
 
 swz::PromptArgs prompt_args(const swz_attention_args& a) {
@@ -245,7 +246,7 @@ int check_decode(const swz_cache4* c, int sequences, int q_heads, int table_widt
   const int st = check_cache(c);
   if (st != SWZ_OK) return st;
   if (sequences < 1 || q_heads < 1 || q_heads % c->k_heads != 0 || table_width < 1 || max_length < 0) return SWZ_ERR_INVALID_ARG;
-  if ((int64_t)table_width * c->page_tokens >= kTokens || (int64_t)sequences * q_heads >= kTokens) return SWZ_ERR_OVERFLOW;
+  if ((int64_t)table_width * c->page_tokens > kMostKeys || (int64_t)sequences * q_heads >= kTokens) return SWZ_ERR_OVERFLOW;
   return SWZ_OK;
 }
 

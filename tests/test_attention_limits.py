@@ -37,3 +37,29 @@ def test_no_workspace_where_none_is_needed(head_dim):
     a = ctypes.byref(prompt_args(head_dim=head_dim))
     need = layer.lib.swz_attention_backward_workspace(a)
     assert need > 0 and layer.lib.swz_attention_backward(a, h, h, h, h, None, need, None) == INVALID
+
+
+# Tiles and steps reach past the last token by less than 4096, in 32-bit numbers: beyond that they would wrap, and a loop over them would not end.
+MOST = (1 << 31) - 4096
+
+
+@pytest.mark.parametrize("head_dim", [64, 128])
+def test_tokens_whose_tiles_would_pass_32_bits(head_dim):
+    lib, r = layer.lib, ctypes.byref
+    for which in ("total_q", "total_k"):
+        h = r(heads())
+        for tokens in (MOST + 1, (1 << 31) - 1):
+            a = prompt_args(head_dim=head_dim, **{which: tokens})
+            assert lib.swz_attention_workspace(r(a)) == lib.swz_attention_backward_workspace(r(a)) == OVERFLOW
+            assert lib.swz_attention(r(a), P, 1 << 60, None) == lib.swz_attention_backward(r(a), h, h, h, h, P, 1 << 60, None) == OVERFLOW
+        a = prompt_args(head_dim=head_dim, **{which: MOST})
+        assert lib.swz_attention_workspace(r(a)) >= 0 and lib.swz_attention_backward_workspace(r(a)) > 0
+
+
+@pytest.mark.parametrize("page", [32, 64, 1024])
+def test_tables_whose_steps_would_pass_32_bits(page):
+    c, h, lib = ctypes.byref(layer._Cache4(P, P, P, P, 4, page, 1, 128)), ctypes.byref(heads()), layer.lib
+    for width in (MOST // page + 1, (1 << 31) // page - 1):
+        assert lib.swz_cache4_attention_workspace(c, 1, 2, width, 0) == lib.swz_cache4_attention_workspace(c, 1, 2, width, 100) == OVERFLOW
+        assert lib.swz_cache4_attention(c, h, h, P, P, width, 1, 2, 0, 0.1, P, 1 << 60, None) == OVERFLOW
+    assert lib.swz_cache4_attention_workspace(c, 1, 2, MOST // page, 0) > 0

@@ -669,6 +669,24 @@ def test_cache_words_beyond_32_bits(swz):
     assert torch.equal(swz.cache4_attention(q, cache, lengths, table), swz.cache4_attention(q, small, lengths, near))
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+def test_cache_attention_of_the_longest_table(swz, dim):
+    """All positions that a table may have, in one page that it names over and over: the weights of the page's tokens are those of the page alone, and so is the result."""
+    page = 1024
+    cache, _, q = decode_case(swz, [page], 4, 1, dim, page)
+    cache = swz.Cache4(*(t[:1].contiguous() for t in cache))
+    k, v = randn(1, page, 1, dim), randn(2, page, 1, dim)
+    one = torch.zeros((1, 1), dtype=torch.int32, device="cuda")
+    swz.cache4_append(cache, k, v, cu_of([page]), one[0], one)
+    table = torch.zeros((1, ((1 << 31) - 4096) // page), dtype=torch.int32, device="cuda")
+    held = numbers_of(cache, one, [page], page)
+    for n in (1, 2, table.shape[1] - 1, table.shape[1]):
+        lengths = torch.tensor([n * page], dtype=torch.int32, device="cuda")
+        check_decode(swz.cache4_attention(q, cache, lengths, table), q, held, [page], 1, dim ** -0.5)
+    got = swz.cache4_attention(q, cache, torch.full_like(lengths, (1 << 31) - 1), table)       # cut to the table
+    assert torch.equal(got, swz.cache4_attention(q, cache, lengths, table))
+
+
 # ---------------------------------------------------------------- streams and graphs
 
 def layer_pass(swz, t, stream=None):
