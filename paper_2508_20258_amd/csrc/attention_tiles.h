@@ -127,13 +127,17 @@ __device__ __forceinline__ TurnPlace find_turn(const int32_t* cu, int total, con
           turn - __builtin_amdgcn_readlane(start, s)};
 }
 
+// Keeps the compiler from working a value out again where it is used.
+__device__ __forceinline__ void keep(uint32_t& x) { asm volatile("" : "+v"(x)); }
+
 template <int D>
 __device__ __forceinline__ int tile_key(int row) {
   if constexpr (D == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
   else return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
 }
 
-// ROWS rows of a head into LDS by NW waves, 1024 bytes an instruction.  Rows past the end are copies of the last one, which what uses them masks.  An instruction's rows
+// ROWS rows of a head into LDS by NW waves, 1024 bytes an instruction.  Rows past the end are zeros: they are masked where it matters, but a weight of 0 times an infinity is
+// NaN, so that copies of a real row would not do.  In whole tiles an instruction's rows
 // are named by a wave-uniform base and 32-bit offsets, so the distance between tokens is less than 2^28 elements (7 rows of it fit 2^32 bytes).
 template <int D, int ROWS, int NW>
 struct RowLoader {
@@ -159,15 +163,19 @@ struct RowLoader {
     } else {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
-        const int from = min(first + (wave * kLoads + i) * kRows, length - 1);
-        load(head + (int64_t)from * token, (uint32_t)min(lane / kChunks, length - 1 - from) * (uint32_t)(token * 2), i, to);
+        uint32_t l = (uint32_t)lane;
+        keep(l);                     // or what this needs, once for a sequence, has registers all along
+        const int from = first + (wave * kLoads + i) * kRows;
+        const unsigned char* at = reinterpret_cast<const unsigned char*>(head + from * token) + (l / kChunks * (uint32_t)(token * 2) + (chunk ^ key_of(i)));
+        load_to_lds(from + (int)(l / kChunks) < length ? at : reinterpret_cast<const unsigned char*>(&kZeroChunk), to + (uint32_t)(i * 1024));
       }
     }
   }
+  __device__ __forceinline__ uint32_t key_of(int i) const { return (uint32_t)(tile_key<D>((wave * kLoads + i) * kRows) << 4); }
   __device__ __forceinline__ void load(const uint16_t* row, uint32_t rows, int i, uint32_t to) const {
     const uint64_t at = reinterpret_cast<uint64_t>(row);
     const uint64_t base = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)at);
-    load_to_lds_base_off(reinterpret_cast<const void*>(base), rows + (chunk ^ (uint32_t)(tile_key<D>((wave * kLoads + i) * kRows) << 4)), to + (uint32_t)(i * 1024));
+    load_to_lds_base_off(reinterpret_cast<const void*>(base), rows + (chunk ^ key_of(i)), to + (uint32_t)(i * 1024));
   }
 };
 
@@ -227,9 +235,6 @@ __device__ __forceinline__ bf16x8 read_columns_at(uint32_t lane_part, uint32_t l
   const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr)(uintptr_t)(lane_part_8 + offset));
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
-// Keeps the compiler from working a value out again where it is used.
-__device__ __forceinline__ void keep(uint32_t& x) { asm volatile("" : "+v"(x)); }
-
 // A head's row as B (columns are rows of the tensor), dimensions 16 step + 8 h .. + 7 for all steps.
 template <int D>
 __device__ __forceinline__ void load_fragments(bf16x8 (&f)[D / 16], const uint16_t* row, int lane) {

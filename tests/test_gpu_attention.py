@@ -257,6 +257,33 @@ def test_gradients_of_what_is_not_looked_at(swz, dim, bad, q_heads):
             assert near(dq[:at, 0], clean[0][:at, 0]) and torch.equal(dq[:, 1:], clean[0][:, 1:]) and not torch.isfinite(dq[at, 0]).any()
 
 
+@pytest.mark.parametrize("q_heads", [2, 8])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("n", [1, 33, 100, 128, 190])
+def test_infinities_in_the_last_token(swz, n, dim, causal, q_heads):
+    """What a tile holds behind the last token must not turn an infinity of the last one, which is looked at, into NaN."""
+    group = q_heads // 2
+    q, k, v, dout = randn(n, n + 40, q_heads, dim), randn(n + 1, n + 40, 2, dim), randn(n + 2, n + 40, 2, dim), randn(n + 3, n + 40, q_heads, dim)
+    cu = cu_of([n, 40])
+    out, lse = swz.attention(q, k, v, cu, causal=causal)
+    clean = swz.attention_backward(dout, q, k, v, out, lse, cu, causal=causal)
+    for inf in (float("inf"), float("-inf")):
+        v2, d2 = v.clone(), dout.clone()
+        v2[n - 1, 0, 3] = inf
+        got, lse2 = swz.attention(q, k, v2, cu, causal=causal)
+        assert ((lse2 - lse).abs() <= 2e-5 * (1 + lse.abs())).all() and torch.equal(got[:, group:], out[:, group:]) and torch.equal(got[n:], out[n:])
+        looks = got[n - 1 if causal else 0:n, :group]
+        assert (looks[..., 3] == inf).all() and torch.isfinite(got[:n - 1 if causal else 0]).all()
+        rest = [d for d in range(dim) if d != 3]
+        assert (looks[..., rest].float() - out[n - 1 if causal else 0:n, :group][..., rest].float()).abs().max() <= 2 ** -6
+        d2[n - 1, 0, 5] = inf
+        dv = swz.attention_backward(d2, q, k, v, out, lse, cu, causal=causal)[2]
+        assert (dv[:n, 0, 5] == inf).all() and torch.equal(dv[:, 1], clean[2][:, 1]) and torch.equal(dv[n:], clean[2][n:])
+        rest = [d for d in range(dim) if d != 5]
+        assert (dv[:n, 0][..., rest].float() - clean[2][:n, 0][..., rest].float()).abs().max() <= 2 ** -6 * clean[2].float().abs().max()
+
+
 def test_distances_between_tokens(swz):
     # tiles are loaded with 32-bit offsets from their first row: longer distances are refused, not wrapped
     memory, cu = torch.zeros((1 << 28) + 64, dtype=torch.bfloat16, device="cuda"), cu_of([2])
