@@ -149,7 +149,8 @@ def qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, po
     weights = _empty(stream, (2, q.shape[2]), torch.float32, q.device)
     h = _launch_stream(stream, q, k, dq_out, dk_out, dq, dk, q_weight, k_weight, cos, sin, positions)
     if q.shape[0] == 0:
-        _fill_zero(weights, stream)
+        with _on(stream):
+            weights.zero_()
         return dq, dk, *weights
     work = _workspace(lib.swz_qk_norm_rope_backward_workspace(ctypes.byref(a)), "swz_qk_norm_rope_backward", q, stream)
     _check(lib.swz_qk_norm_rope_backward(ctypes.byref(a), ctypes.byref(_heads(dq)), ctypes.byref(_heads(dk)), weights[0].data_ptr(), weights[1].data_ptr(),
@@ -186,9 +187,11 @@ def attention(q, k, v, cu_q, cu_k=None, out=None, lse=None, causal: bool = True,
     h = _launch_stream(stream, q, k, v, out, lse, cu_q, cu_k)
     if q.shape[0] == 0:
         return out, lse
-    if k.shape[0] == 0:                                   # nothing to look at: no memory that a pointer could name either
-        k = v = q[:1, :1].expand(1, k.shape[1], -1)
+    keys = k.shape[0]
+    if keys == 0:
+        k = v = _of_no_tokens(k, q)
     a = _attention_args(q, k, v, out, lse, cu_q, cu_k, causal, scale)
+    a.total_k = keys
     work = _workspace(lib.swz_attention_workspace(ctypes.byref(a)), "swz_attention", q, stream)
     _check(lib.swz_attention(ctypes.byref(a), _pointer(work), 0 if work is None else work.numel(), h), "swz_attention")
     return out, lse
@@ -205,20 +208,24 @@ def attention_backward(dout, q, k, v, out, lse, cu_q, cu_k=None, dq=None, dk=Non
     assert lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (q.shape[1], q.shape[0])
     dq, dk, dv = _out(dq, q, stream), _out(dk, k, stream), _out(dv, v, stream)
     h = _launch_stream(stream, dout, q, k, v, out, lse, cu_q, cu_k, dq, dk, dv)
-    if q.shape[0] == 0 or k.shape[0] == 0:                # gradients of nothing
-        for t in (dq, dk, dv):
-            _fill_zero(t, stream)
-        return dq, dk, dv
+    queries, keys, grads = q.shape[0], k.shape[0], (dq, dk, dv)
+    if queries == 0 and keys == 0:
+        return grads
+    if keys == 0:
+        k = v = dk = dv = _of_no_tokens(k, q)
+    if queries == 0:
+        q = dout = out = dq = _of_no_tokens(q, k)
     a = _attention_args(q, k, v, out, lse, cu_q, cu_k, causal, scale)
+    a.total_q, a.total_k, a.lse = queries, keys, a.lse or q.data_ptr()
     work = _workspace(lib.swz_attention_backward_workspace(ctypes.byref(a)), "swz_attention_backward", q, stream)
-    _check(lib.swz_attention_backward(ctypes.byref(a), *(ctypes.byref(_heads(t)) for t in (dout, dq, dk, dv)), work.data_ptr(), work.numel(), h),
+    _check(lib.swz_attention_backward(ctypes.byref(a), *(ctypes.byref(_heads(t)) for t in (dout, dq, dk, dv)), _pointer(work), 0 if work is None else work.numel(), h),
            "swz_attention_backward")
-    return dq, dk, dv
+    return grads
 
 
-def _fill_zero(t, stream) -> None:
-    with _on(stream):
-        t.zero_()
+def _of_no_tokens(t, other):
+    """In the place of heads of no tokens, which have no memory: a pointer that the library takes, and that nothing is read from or written to."""
+    return other[:1, :1].expand(1, t.shape[1], -1)
 
 
 class Cache4(NamedTuple):

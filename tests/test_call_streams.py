@@ -135,5 +135,4 @@ def test_without_a_stream_nothing_is_switched(world, name):
 
 def test_gradients_of_no_tokens_are_filled_on_the_stream(world):
     swz.qk_norm_rope_backward(heads(0), heads(0, 1), *norm_inputs(0), stream=Side)
-    swz.attention_backward(heads(0), heads(0), heads(3), heads(3), heads(0), lse(0), ints(0, 0), ints(0, 3), stream=Side)
-    assert world.filled == [("external", 0x77)] * len(world.filled) and len(world.filled) >= 3
+    assert world.filled == [("external", 0x77)]

@@ -371,6 +371,29 @@ def test_no_tokens(swz):
     assert (dk == 0).all() and (dv == 0).all() and dk.shape == some.shape
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_tokens_of_no_sequence_beside_no_tokens(swz, dim, causal):
+    """No keys at all, or no queries: the tokens of the sequences get 0, those of none are left alone, as ever."""
+    some, none = randn(1, 8, 40, dim), torch.empty((0, 40, dim), dtype=torch.bfloat16, device="cuda")
+    cu, zero = torch.tensor([2, 5], dtype=torch.int32, device="cuda"), torch.tensor([0, 0], dtype=torch.int32, device="cuda")
+    inner = torch.tensor([2 <= i < 5 for i in range(8)], device="cuda")
+    out, lse = torch.full_like(some, 7.0), torch.full((40, 8), 7.0, device="cuda")
+    few = none[:, :1]
+    swz.attention(some, few, few, cu, zero, out=out, lse=lse, causal=causal)
+    assert (out[inner] == 0).all() and (out[~inner] == 7).all() and torch.isneginf(lse[:, inner]).all() and (lse[:, ~inner] == 7).all()
+    dq = torch.full_like(some, 7.0)
+    got = swz.attention_backward(some, some, few, few, out, lse, cu, zero, dq=dq, causal=causal)
+    assert got[0] is dq and (dq[inner] == 0).all() and (dq[~inner] == 7).all() and got[1].shape == got[2].shape == few.shape
+    keys = some[:, :1]
+    dk, dv = torch.full((8, 1, dim), 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((8, 1, dim), 7.0, dtype=torch.bfloat16, device="cuda")
+    got = swz.attention_backward(none, none, keys, keys, none, lse[:, :0].contiguous(), zero, cu, dk=dk, dv=dv, causal=causal)
+    assert got[0].shape == none.shape and got[1] is dk and got[2] is dv
+    for t in (dk, dv):
+        assert (t[inner] == 0).all() and (t[~inner] == 7).all()
+    assert [tuple(t.shape) for t in swz.attention_backward(none, none, few, few, none, lse[:, :0].contiguous(), zero, zero)] == [(0, 40, dim), (0, 1, dim), (0, 1, dim)]
+
+
 @pytest.mark.parametrize("dim", [64, 128])
 def test_gradient_of_no_queries_without_a_workspace(swz, dim):
     # the C call with what its own query of the size says
