@@ -162,9 +162,9 @@ struct DkvShape {
   static constexpr int kKeys = 32 * kKeyWaves, kThreads = 64 * kKeyWaves * kParts;
 };
 
-// How many workgroups share the queries of a tile of keys and leave their sums to another kernel: where tiles and key heads give less than a workgroup for half of the
-// compute units (a compute unit holds one of 512 threads, or three of 256), as many as give two (four of 256 threads) to each, or one for every eight rounds of the
-// queries of an average sequence, if that is fewer, as writing and reading the sums takes about as long as ten rounds.  8 query heads of one key head, 4096 causal tokens, the
+// How many workgroups share the queries of a tile of keys and leave their sums to another kernel.  Where tiles and key heads give no more workgroups than one for each compute unit (two of
+// 256 threads: a compute unit holds one of 512, or three of 256), as many as give two (four) to each, or one for every eight rounds of the
+// queries of an average sequence, if that is fewer, as writing and reading the sums takes about as long as ten rounds; at most 16.  8 query heads of one key head, 4096 causal tokens, the
 // whole gradient: 928 us whole, 268 with 15 splits; 32 heads of 8, 2048 tokens: 312 whole, 210 with 3; 16 of 2, 2007 tokens of four sequences: 263 whole, 103 with 7, 113 with 15.
 int dkv_splits(const swz_attention_args& a) {
   auto splits = [&](auto shape) {
@@ -234,7 +234,8 @@ DecodePlan decode_plan(const swz_cache4& c, int sequences, int q_heads, int tabl
   const int64_t cut = (int64_t)table_width * c.page_tokens, longest = max_length > 0 && max_length < cut ? max_length : cut;
   // Few tokens: one launch, a workgroup of 8 waves for each sequence and key head, not waves that share all steps and a second launch that joins them.  4 heads of 128 for each of 8 key
   // heads: 16 sequences of 256 tokens 8.1 us and 10.8, of 1000 11.5 and 15.0, of 2000 18.3 and 19.8, of 4000 28.8 and 26.0; one of 1000 10.8 and 10.9, of 2000 15.1 and 12.5; 64 of
-  // 1000 25.8 and 25.7.  16 heads of one key head, 8 of 1000: 13.6 and 12.9.  Heads of 64: 8 of 2000 10.1 and 13.5, of 4000 18.4 and 17.1.
+  // 1000 25.8 and 25.7.  16 heads of one key head, 8 of 1000: 13.6 and 12.9.  Heads of 64: 8 of 2000 10.1 and 13.5, of 4000 18.4 and 17.1.  The rule goes by the length alone; where the two
+  // cross also depends on sequences and heads, and of these it takes the slower one for 16 of 2000 and for the 16 heads of one key head, by 5 and 8 %.
   if (longest * c.head_dim <= 1 << 17) return {columns, rows, 0};
   // as many as run together; fewer where there are fewer steps
   const int64_t together = (int64_t)compute_units() * 4 * (c.head_dim == 64 ? 3 : rows >= 8 ? 2 : 3) / ((int64_t)c.k_heads * columns);

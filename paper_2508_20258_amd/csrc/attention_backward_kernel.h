@@ -5,8 +5,8 @@
 // would do), so that every sum has one owner and an order of its own, without atomics and without the scores in memory.
 // P and dS are rounded to bfloat16 for the products that sum over them, as the instruction takes nothing else: dq and dk have 0.0025 relative error, where rounding the result
 // alone has 0.0017; a second product with what the rounding leaves over would take a quarter more time.  delta comes from the rounded out: 0.0001 of that, 0.0002 with a few keys.
-// Bound by power (1.57 and 1.67 GHz; matrix units busy for 77 and 60 % of it, LDS for 38 and 52 %).  8227 tokens in six sequences, 32 heads of 128 sharing 8, causal: dq 290 us,
-// 1030 TFLOP/s, dk and dv 470 us, 850; 4 x 2048 tokens, 16 heads of 64: 77 to 84 and 95 to 105 us.
+// With heads of 128 bound by power (1.57 and 1.67 GHz).  8227 tokens in six sequences, 32 heads of 128 sharing 8, causal: dq 275 us, 1090 TFLOP/s, dk and dv 431 us, 930; matrix units busy
+// for 64 and 54 % of it, LDS for 32 and 41 %.  4 x 2048 tokens, 16 heads of 64: 70 and 85 us; matrix units 47 and 45 %, LDS 24 and 47 %, vector unit 60 and 50 %: none of them alone.
 #pragma once
 
 #include "attention_kernel.h"

@@ -7,10 +7,10 @@
 // rounding the result alone; their sum is taken before it.
 //
 // A wave has 32 rows, a workgroup four waves that share tiles of keys and values in LDS, two of each: the next ones load while these are used.  Two or three workgroups to a compute unit.
-// With heads of 128 the bound is power: 1.55 to 1.66 GHz under this kernel, the matrix units busy for 62 to 71 % of it and the vector unit for 59 % (the exponentials).  32768 causal tokens,
-// 16 heads of 128 sharing 4: 3.68 ms, 1195 TFLOP/s; 8192, 32 heads sharing 8: 479 us, 1147.  With heads of 64 a product has half the work for the same exponentials and the vector unit is
-// the bound (90 % at 1.84 GHz): 8192, 32 heads of 64 sharing 8: 288 us, 955 TFLOP/s.  Short prompts are bound by the latency of their loads, one after another: places, then
-// queries and keys, then values.  50 sequences of 1 to 512 tokens, 32 heads of 128 sharing 8: 44 us.
+// With heads of 128 the bound is power: 1.55 to 1.66 GHz under this kernel, the matrix units busy for 71 % of it and the vector unit for 59 % (the exponentials).  32768 causal tokens,
+// 16 heads of 128 sharing 4: 3.72 ms, 1183 TFLOP/s, one call after another (4.0 ms where there are 5 ms between them); 8192, 32 heads sharing 8: 487 us, 1129.  With heads of 64 a product has
+// half the work for the same exponentials: 8192, 32 heads of 64 sharing 8: 290 us, 947 TFLOP/s; five pieces of 1 to 2048 queries over 200 to 10000 keys 160 us, 800, the vector unit busy for
+// 70 %.  Short prompts are bound by the latency of their loads, one after another: places, then queries and keys, then values.  50 sequences of 1 to 512 tokens, 32 heads of 128 sharing 8: 40 us.
 #pragma once
 
 #include "attention_tiles.h"

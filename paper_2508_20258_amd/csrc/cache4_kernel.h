@@ -1,9 +1,9 @@
 // A cache of keys and values in 4 bits: writing it, reading it back, attention of single tokens over it.
 //
-// 64 values of a head share a step and a low, bfloat16 both: 36 bytes instead of 128.  16478 tokens of 8 heads of 128 (68 MB of keys and values, 19 MB of cache): writing 20 us, bound by the
-// vector unit (95 %: four instructions a value for its number alone, then words of eight tokens through LDS), reading 16.7 us, 5.2 TB/s.
-// Attention: the cache is read once, by all query heads of a key head together.  64 sequences of 512 to 8192 tokens, 32 heads of 128 sharing 8 (176 MB): 35 us, 5.0 TB/s, and
-// 6.7 for the join, call after call on the same cache; among other work, which leaves none of it in the memory-side cache, 51 us in all.
+// 64 values of a head share a step and a low, bfloat16 both: 36 bytes instead of 128.  16478 tokens of 8 heads of 128 (68 MB of keys and values, 19 MB of cache): writing 19 us, bound by the
+// vector unit (93 %: four instructions a value for its number alone, then words of eight tokens through LDS), reading 16.3 us, 5.3 TB/s.
+// Attention: the cache is read once, by all query heads of a key head together.  64 sequences of 512 to 8192 tokens, 32 heads of 128 sharing 8 (176 MB): 34 us, 5.1 TB/s, and
+// 6.6 for the join, call after call on the same cache; among other work, which leaves none of it in the memory-side cache, 51 us in all.
 #pragma once
 
 #include "qk_norm_kernel.h"

@@ -2,8 +2,8 @@
 //
 // With r = 1 / sqrt(mean(x^2) + eps) and R the rotation of a token's position: z = R (x r w).  Backward: dy = R^T dz, u = x r, dw = sum over tokens and heads of dy u, and
 // dx = r (dy w - u mean(dy w u)); r is worked out again from x, which is read anyway.  All of it in 32 bits, rounded once.
-// HBM is the bound: every element is read once and written once.  32768 tokens of 32 + 8 heads of 128: 126 us, 5.5 TB/s of 6.0 that a copy reaches.  Backward, 12345 tokens: 76 us, 5.1 TB/s, and 5 us for the
-// weights' sums; 4096 tokens of 16 + 16 heads of 64: 12.5 and 3.6.
+// HBM is the bound: every element is read once and written once.  32768 tokens of 32 + 8 heads of 128: 127 us, 5.4 TB/s of 6.0 that a copy reaches.  Backward, 12345 tokens: 75 us, 5.1 TB/s, and 5 us for the
+// weights' sums; 4096 tokens of 16 + 16 heads of 64: 12.6 and 3.5.
 #pragma once
 
 #include "attention_tiles.h"

@@ -594,17 +594,26 @@ def _operators():
 
 
 def cmd_attention(args):
+    import time
+
     import torch
 
     ops = _operators()
     case = next(c for c in ops.listed() if c["name"] == args.case)
     state = ops.prepare(case, 1)
+    until = time.monotonic() + args.warm_ms / 1e3
+    while time.monotonic() < until:
+        for _ in range(20):
+            ops.run(state)
+        torch.cuda.synchronize()
     for _ in range(args.launches):
         ops.run(state)
     torch.cuda.synchronize()
     print(f"ran {args.launches} x {args.case}", flush=True)
 
 
+# Work before the launches whose durations count.  Under load after a pause the device's clocks take 10 to 20 ms to settle: prompt_pieces 175 us at first, 190 to 212 from 2 to 5 ms on, then 161.
+ATTENTION_WARM_MS = 200
 ATTENTION_COUNTERS = ["SQ_BUSY_CU_CYCLES", "SQ_VALU_MFMA_BUSY_CYCLES", "SQ_LDS_IDX_ACTIVE", "SQ_LDS_BANK_CONFLICT", "SQ_ACTIVE_INST_VALU"]
 
 
@@ -620,7 +629,7 @@ def cmd_profile_attention(args):
             _rocprof(out, tag, "csv", ["--pmc", c], ["copy", "--mib", "1024", "--launches", "3"])
         for name in names:
             prog = ["attention", "--case", name]
-            _rocprof(out, name + "_kt", "csv", ["--kernel-trace", "--stats"], prog + ["--launches", str(args.launches + 10)])
+            _rocprof(out, name + "_kt", "csv", ["--kernel-trace", "--stats"], prog + ["--warm-ms", str(ATTENTION_WARM_MS), "--launches", str(args.launches + 10)])
             for tag, counters in passes:
                 _rocprof(out, f"{name}_{tag}", "csv", ["--pmc", *counters], prog + ["--launches", "3"], 90)
     fs = 1024 * 1024 / _one(f"{out}/copy_fetch", "copy")["counters"]["FETCH_SIZE"]
@@ -630,10 +639,10 @@ def cmd_profile_attention(args):
              "Written by (repository root, TMPDIR=/tmp):",
              f"  {H} profile-attention --out <dir>",
              "which runs, for CASE as in the table:",
-             f"  rocprofv3 --kernel-trace --stats --output-format csv -d <out> -- {H} attention --case CASE --launches {args.launches + 10}",
+             f"  rocprofv3 --kernel-trace --stats --output-format csv -d <out> -- {H} attention --case CASE --warm-ms {ATTENTION_WARM_MS} --launches {args.launches + 10}",
              f"  rocprofv3 --pmc {' '.join(ATTENTION_COUNTERS)} (then FETCH_SIZE, then WRITE_SIZE) --output-format csv -d <out> -- {H} attention --case CASE --launches 3",
              f"  and FETCH_SIZE, WRITE_SIZE on `{H} copy --mib 1024` (calibration: FETCH_SIZE x {fs:.3f}, WRITE_SIZE x {ws:.3f}).",
-             f"us = kernel duration in the trace, average over its last {args.launches} launches, over the same data.  MFMA: share of the matrix units' cycles, of busy compute units, in which one works;",
+             f"us = kernel duration in the trace, average over its last {args.launches} launches, over the same data, after {ATTENTION_WARM_MS} ms of them.  MFMA: share of the matrix units' cycles, of busy compute units, in which one works;",
              "LDS: share of these compute units' cycles in which LDS serves a read or write, conflicts among them; VALU: share of them in which vector instructions are issued.",
              "", f"{'case':14s} {'us':>8s} {'MFMA %':>7s} {'LDS %':>6s} {'conflict %':>10s} {'VALU %':>6s} {'fetch MiB':>10s} {'write MiB':>10s}  kernel"]
     for name in names:
@@ -1010,6 +1019,7 @@ def main(argv=None):
     pr.set_defaults(fn=cmd_profile_rows)
     at = sub.add_parser("attention")
     at.add_argument("--case", required=True)
+    at.add_argument("--warm-ms", type=int, default=0)
     at.add_argument("--launches", type=int, default=20)
     at.set_defaults(fn=cmd_attention)
     pa = sub.add_parser("profile-attention")
