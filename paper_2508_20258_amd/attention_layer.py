@@ -13,7 +13,7 @@ from __future__ import annotations
 import ctypes
 from typing import NamedTuple
 
-from .binding import _NoFast, _check, _empty, _fast, _launch_stream, _on, lib, torch
+from .binding import _NoFast, _check, _fast, _launch_stream, _run_on, lib, torch
 
 EXPORTS = ("swz_qk_norm_rope", "swz_qk_norm_rope_backward_workspace", "swz_qk_norm_rope_backward", "swz_attention_workspace", "swz_attention", "swz_attention_backward_workspace",
            "swz_attention_backward", "swz_cache4_append", "swz_cache4_read", "swz_cache4_attention_workspace", "swz_cache4_attention")
@@ -86,20 +86,20 @@ def _is_ints(t, *shape) -> bool:
     return t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == shape
 
 
-def _out(t, like, stream):
+def _out(t, like):
     """An output: `t`, or a new dense tensor; its tokens and heads must not share memory."""
     if t is None:
-        return _empty(stream, like.shape, like.dtype, like.device)
+        return torch.empty(like.shape, dtype=like.dtype, device=like.device)
     assert _is_heads(t, *like.shape)
     (n, h, d), (token, head, _) = t.shape, t.stride()
     assert (n < 2 or h < 2 or token >= h * head >= h * d or head >= n * token >= n * d) and (n < 2 or token >= d) and (h < 2 or head >= d), "tokens or heads of an output overlap"
     return t
 
 
-def _workspace(size: int, where: str, like, stream):
+def _workspace(size: int, where: str, like):
     if size < 0:
         _check(size, where)
-    return _empty(stream, size, torch.uint8, like.device, result=False) if size else None
+    return torch.empty(size, dtype=torch.uint8, device=like.device) if size else None
 
 
 def _pointer(t):
@@ -124,13 +124,15 @@ def qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions, q_out=None, k_ou
     q (tokens, q_heads, head_dim), k (tokens, k_heads, head_dim); weights (head_dim,) bfloat16; cos, sin (positions, rotary_dim / 2) float32 tables; positions
     (tokens,) int32.  Pairs are (i, i + rotary_dim / 2), or neighbours with `interleaved`; dimensions from rotary_dim on are not turned.  The outputs may be q and
     k themselves.  A position outside the tables gives NaN."""
-    if stream is None and q_out is None and k_out is None:
+    if stream is not None:
+        return _run_on(stream, qk_norm_rope, q, k, q_weight, k_weight, cos, sin, positions, q_out, k_out, eps, interleaved)
+    if q_out is None and k_out is None:
         done = _fast.qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
         if done is not None:
             return _done(done, "swz_qk_norm_rope")
-    q_out, k_out = _out(q_out, q, stream), _out(k_out, k, stream)
+    q_out, k_out = _out(q_out, q), _out(k_out, k)
     a = _norm_args(q, k, q_out, k_out, q_weight, k_weight, cos, sin, positions, eps, interleaved)
-    h = _launch_stream(stream, q, k, q_out, k_out, q_weight, k_weight, cos, sin, positions)
+    h = _launch_stream(None, q, k, q_out, k_out, q_weight, k_weight, cos, sin, positions)
     if q.shape[0] > 0:
         _check(lib.swz_qk_norm_rope(ctypes.byref(a), h), "swz_qk_norm_rope")
     return q_out, k_out
@@ -139,20 +141,20 @@ def qk_norm_rope(q, k, q_weight, k_weight, cos, sin, positions, q_out=None, k_ou
 def qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, positions, dq=None, dk=None, eps: float = 1e-6, interleaved: bool = False, stream=None):
     """(dq, dk, dq_weight, dk_weight) from the gradients of qk_norm_rope's outputs and its inputs; the weights' gradients are float32 sums over all tokens and
     heads.  dq, dk may be dq_out, dk_out themselves."""
-    if stream is None and dq is None and dk is None:
+    if stream is not None:
+        return _run_on(stream, qk_norm_rope_backward, dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, positions, dq, dk, eps, interleaved)
+    if dq is None and dk is None:
         done = _fast.qk_norm_rope_backward(dq_out, dk_out, q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
         if done is not None:
             return _done(done, "swz_qk_norm_rope_backward")
     assert _is_heads(dq_out, *q.shape) and _is_heads(dk_out, *k.shape)
-    dq, dk = _out(dq, q, stream), _out(dk, k, stream)
+    dq, dk = _out(dq, q), _out(dk, k)
     a = _norm_args(q, k, dq_out, dk_out, q_weight, k_weight, cos, sin, positions, eps, interleaved)
-    weights = _empty(stream, (2, q.shape[2]), torch.float32, q.device)
-    h = _launch_stream(stream, q, k, dq_out, dk_out, dq, dk, q_weight, k_weight, cos, sin, positions)
+    weights = torch.empty((2, q.shape[2]), dtype=torch.float32, device=q.device)
+    h = _launch_stream(None, q, k, dq_out, dk_out, dq, dk, q_weight, k_weight, cos, sin, positions)
     if q.shape[0] == 0:
-        with _on(stream):
-            weights.zero_()
-        return dq, dk, *weights
-    work = _workspace(lib.swz_qk_norm_rope_backward_workspace(ctypes.byref(a)), "swz_qk_norm_rope_backward", q, stream)
+        return dq, dk, *weights.zero_()
+    work = _workspace(lib.swz_qk_norm_rope_backward_workspace(ctypes.byref(a)), "swz_qk_norm_rope_backward", q)
     _check(lib.swz_qk_norm_rope_backward(ctypes.byref(a), ctypes.byref(_heads(dq)), ctypes.byref(_heads(dk)), weights[0].data_ptr(), weights[1].data_ptr(),
                                          work.data_ptr(), work.numel(), h), "swz_qk_norm_rope_backward")
     return dq, dk, weights[0], weights[1]
@@ -175,16 +177,18 @@ def attention(q, k, v, cu_q, cu_k=None, out=None, lse=None, causal: bool = True,
 
     q (tokens, q_heads, head_dim), k and v (key tokens, k_heads, head_dim), q_heads a multiple of k_heads; cu_k where keys belong to other tokens than queries.
     causal: the last query of a sequence looks at all its keys, each before at one fewer.  scale: head_dim ** -0.5 by default."""
-    if stream is None and out is None and lse is None:
+    if stream is not None:
+        return _run_on(stream, attention, q, k, v, cu_q, cu_k, out, lse, causal, scale)
+    if out is None and lse is None:
         done = _fast.attention(q, k, v, cu_q, cu_k, causal, scale)
         if done is not None:
             return _done(done, "swz_attention")
     cu_k = _check_prompt(q, k, v, cu_q, cu_k)
-    out = _out(out, q, stream)
+    out = _out(out, q)
     if lse is None:
-        lse = _empty(stream, (q.shape[1], q.shape[0]), torch.float32, q.device)
+        lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
     assert lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (q.shape[1], q.shape[0])
-    h = _launch_stream(stream, q, k, v, out, lse, cu_q, cu_k)
+    h = _launch_stream(None, q, k, v, out, lse, cu_q, cu_k)
     if q.shape[0] == 0:
         return out, lse
     keys = k.shape[0]
@@ -192,22 +196,24 @@ def attention(q, k, v, cu_q, cu_k=None, out=None, lse=None, causal: bool = True,
         k = v = _of_no_tokens(k, q)
     a = _attention_args(q, k, v, out, lse, cu_q, cu_k, causal, scale)
     a.total_k = keys
-    work = _workspace(lib.swz_attention_workspace(ctypes.byref(a)), "swz_attention", q, stream)
+    work = _workspace(lib.swz_attention_workspace(ctypes.byref(a)), "swz_attention", q)
     _check(lib.swz_attention(ctypes.byref(a), _pointer(work), 0 if work is None else work.numel(), h), "swz_attention")
     return out, lse
 
 
 def attention_backward(dout, q, k, v, out, lse, cu_q, cu_k=None, dq=None, dk=None, dv=None, causal: bool = True, scale: float | None = None, stream=None):
     """(dq, dk, dv) from the gradient of attention's out, its arguments and what it returned."""
-    if stream is None and dq is None and dk is None and dv is None:
+    if stream is not None:
+        return _run_on(stream, attention_backward, dout, q, k, v, out, lse, cu_q, cu_k, dq, dk, dv, causal, scale)
+    if dq is None and dk is None and dv is None:
         done = _fast.attention_backward(dout, q, k, v, out, lse, cu_q, cu_k, causal, scale)
         if done is not None:
             return _done(done, "swz_attention_backward")
     cu_k = _check_prompt(q, k, v, cu_q, cu_k)
     assert _is_heads(dout, *q.shape) and _is_heads(out, *q.shape)
     assert lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (q.shape[1], q.shape[0])
-    dq, dk, dv = _out(dq, q, stream), _out(dk, k, stream), _out(dv, v, stream)
-    h = _launch_stream(stream, dout, q, k, v, out, lse, cu_q, cu_k, dq, dk, dv)
+    dq, dk, dv = _out(dq, q), _out(dk, k), _out(dv, v)
+    h = _launch_stream(None, dout, q, k, v, out, lse, cu_q, cu_k, dq, dk, dv)
     queries, keys, grads = q.shape[0], k.shape[0], (dq, dk, dv)
     if queries == 0 and keys == 0:
         return grads
@@ -217,7 +223,7 @@ def attention_backward(dout, q, k, v, out, lse, cu_q, cu_k=None, dq=None, dk=Non
         q = dout = out = dq = _of_no_tokens(q, k)
     a = _attention_args(q, k, v, out, lse, cu_q, cu_k, causal, scale)
     a.total_q, a.total_k, a.lse = queries, keys, a.lse or q.data_ptr()
-    work = _workspace(lib.swz_attention_backward_workspace(ctypes.byref(a)), "swz_attention_backward", q, stream)
+    work = _workspace(lib.swz_attention_backward_workspace(ctypes.byref(a)), "swz_attention_backward", q)
     _check(lib.swz_attention_backward(ctypes.byref(a), *(ctypes.byref(_heads(t)) for t in (dout, dq, dk, dv)), _pointer(work), 0 if work is None else work.numel(), h),
            "swz_attention_backward")
     return grads
@@ -277,7 +283,9 @@ def cache4_append(cache: Cache4, k, v, cu, before, block_table, stream=None) -> 
 
 def cache4_read(cache: Cache4, cu, first, block_table, tokens: int, k=None, v=None, stream=None):
     """(k, v): positions first[b] .. of every sequence, cu[b + 1] - cu[b] of them, as bfloat16 (tokens, k_heads, head_dim); tokens is cu's last entry."""
-    if stream is None and k is None and v is None:
+    if stream is not None:
+        return _run_on(stream, cache4_read, cache, cu, first, block_table, tokens, k, v)
+    if k is None and v is None:
         done = _fast.cache4_read(cache, cu, first, block_table, tokens)
         if done is not None:
             return _done(done, "swz_cache4_read")
@@ -286,10 +294,10 @@ def cache4_read(cache: Cache4, cu, first, block_table, tokens: int, k=None, v=No
     assert _is_ints(first, n) and _is_ints(cu, n + 1) and block_table.dim() == 2 and _is_ints(block_table, n, block_table.shape[1])
     shape = (int(tokens), c.k_heads, c.head_dim)
     like = torch.empty(shape, dtype=torch.bfloat16, device="meta") if k is None or v is None else k
-    k = _empty(stream, shape, torch.bfloat16, cu.device) if k is None else _out(k, like, stream)
-    v = _empty(stream, shape, torch.bfloat16, cu.device) if v is None else _out(v, like, stream)
+    k = torch.empty(shape, dtype=torch.bfloat16, device=cu.device) if k is None else _out(k, like)
+    v = torch.empty(shape, dtype=torch.bfloat16, device=cu.device) if v is None else _out(v, like)
     assert tuple(k.shape) == tuple(v.shape) == shape
-    h = _launch_stream(stream, k, v, cu, first, block_table, *cache)
+    h = _launch_stream(None, k, v, cu, first, block_table, *cache)
     if shape[0] > 0:
         _check(lib.swz_cache4_read(ctypes.byref(c), ctypes.byref(_heads(k)), ctypes.byref(_heads(v)), shape[0], cu.data_ptr(), first.data_ptr(),
                                    block_table.data_ptr(), block_table.shape[1], n, h), "swz_cache4_read")
@@ -299,7 +307,9 @@ def cache4_read(cache: Cache4, cu, first, block_table, tokens: int, k=None, v=No
 def cache4_attention(q, cache: Cache4, lengths, block_table, max_length: int = 0, out=None, scale: float | None = None, stream=None):
     """Attention of one token of each sequence (q: (sequences, q_heads, head_dim)) over the first lengths[b] positions of the cache, its own appended before.
     A sequence of length 0 gets 0.  max_length: the longest length if the program knows it; it decides how sequences are split over the device."""
-    if stream is None and out is None:
+    if stream is not None:
+        return _run_on(stream, cache4_attention, q, cache, lengths, block_table, max_length, out, scale)
+    if out is None:
         done = _fast.cache4_attention(q, cache, lengths, block_table, max_length, scale)
         if done is not None:
             return _done(done, "swz_cache4_attention")
@@ -307,12 +317,12 @@ def cache4_attention(q, cache: Cache4, lengths, block_table, max_length: int = 0
     assert _is_heads(q, None, None, c.head_dim)
     n, q_heads, dim = q.shape
     assert _is_ints(lengths, n) and block_table.dim() == 2 and _is_ints(block_table, n, block_table.shape[1])
-    out = _out(out, q, stream)
-    h = _launch_stream(stream, q, out, lengths, block_table, *cache)
+    out = _out(out, q)
+    h = _launch_stream(None, q, out, lengths, block_table, *cache)
     if n == 0:
         return out
     width, longest = block_table.shape[1], int(max_length)
-    work = _workspace(lib.swz_cache4_attention_workspace(ctypes.byref(c), n, q_heads, width, longest), "swz_cache4_attention", q, stream)
+    work = _workspace(lib.swz_cache4_attention_workspace(ctypes.byref(c), n, q_heads, width, longest), "swz_cache4_attention", q)
     _check(lib.swz_cache4_attention(ctypes.byref(c), ctypes.byref(_heads(q)), ctypes.byref(_heads(out)), lengths.data_ptr(), block_table.data_ptr(), width, n, q_heads,
                                     longest, dim ** -0.5 if scale is None else float(scale), _pointer(work), 0 if work is None else work.numel(), h),
            "swz_cache4_attention")

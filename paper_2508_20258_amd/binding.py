@@ -5,7 +5,6 @@ torch is used for device memory (``tensor.data_ptr()``) and streams only.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 import warnings
@@ -164,32 +163,29 @@ def _launch_stream(stream, *tensors) -> int:
     return _stream_handle(stream)
 
 
-def _on(stream):
-    """What is allocated or filled within belongs to the stream that works on it.  A stream may be any object with `cuda_stream`."""
-    if stream is None:
-        return contextlib.nullcontext()
+def _run_on(stream, call, *args, **params):
+    """call(...) with `stream` as the current stream, so that what it allocates and fills belongs to the stream that works on it: a block that was freed on
+    another one may still be in use there.  Results may be used on the caller's current stream too (ordered by the caller, as ever): their memory is not handed
+    out again before that is done.  A stream may be any object with `cuda_stream`."""
+    _same_current_device(stream)
     if not isinstance(stream, torch.cuda.Stream):
         handle = int(stream.cuda_stream)
         stream = torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
-    return torch.cuda.stream(stream)
+    here = torch.cuda.current_stream()
+    torch.cuda.set_stream(stream)
+    try:
+        results = call(*args, **params)
+    finally:
+        torch.cuda.set_stream(here)
+    for t in results if isinstance(results, tuple) else (results,):
+        if t is not None:
+            t.record_stream(here)
+    return results
 
 
-def _handed_out(stream, *results) -> None:
-    """Results made on `stream` may be used on the caller's current stream too (ordered by the caller, as ever): their memory is not handed out again before that is done."""
-    if stream is not None:
-        for t in results:
-            t.record_stream(torch.cuda.current_stream(t.device))
-
-
-def _empty(stream, shape, dtype, device, result: bool = True):
-    """Memory for work on `stream`: from that stream's own, as a block that was freed on another one may still be in use there."""
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with _on(stream):
-        t = torch.empty(shape, dtype=dtype, device=device)
-    if result:
-        _handed_out(stream, t)
-    return t
+def _made(stream, make, *args, **params):
+    """make(...), memory for work on `stream`."""
+    return make(*args, **params) if stream is None else _run_on(stream, make, *args, **params)
 
 
 def _params_ref(params):
@@ -221,10 +217,8 @@ def pid_map_device(grid_m: int, grid_n: int, num_xcd: int, group_m: int, mode: i
     n = int(grid_m) * int(grid_n)
     if not 0 < n < (1 << 31):
         n = 1  # let the library report the error; keep the buffers valid
-    with _on(stream):
-        tile = torch.full((n,), -1, dtype=torch.int32, device="cuda")
-        xcc = torch.full((n,), -1, dtype=torch.int32, device="cuda")
-    _handed_out(stream, tile, xcc)
+    tile = _made(stream, torch.full, (n,), -1, dtype=torch.int32, device="cuda")
+    xcc = _made(stream, torch.full, (n,), -1, dtype=torch.int32, device="cuda")
     _check(lib.swz_pid_map_device(int(grid_m), int(grid_n), int(num_xcd), int(group_m), int(mode), tile.data_ptr(),
                                   xcc.data_ptr(), _stream_handle(stream)), "swz_pid_map_device")
     return tile, xcc
@@ -266,7 +260,7 @@ def gemm(a, b, c=None, mode: int = MODE_XCD_GROUPM, stream=None, **params):
     M, K = a.shape
     N = b.shape[1]
     if c is None:
-        c = _empty(stream, (M, N), torch.bfloat16, a.device)
+        c = _made(stream, torch.empty, (M, N), dtype=torch.bfloat16, device=a.device)
     assert c.is_cuda and c.dtype == torch.bfloat16 and c.is_contiguous() and tuple(c.shape) == (M, N)
     h = _launch_stream(stream, a, b, c)
     if params:
@@ -291,14 +285,12 @@ def gemm_probe(a, b, c=None, mode: int = MODE_XCD_GROUPM, stream=None, probe=Non
     M, K = a.shape
     N = b.shape[1]
     if c is None:
-        c = _empty(stream, (M, N), torch.bfloat16, a.device)
+        c = _made(stream, torch.empty, (M, N), dtype=torch.bfloat16, device=a.device)
     assert c.is_cuda and c.dtype == torch.bfloat16 and c.is_contiguous() and tuple(c.shape) == (M, N)
     _same_current_device(stream, a, b, c)
     plan = gemm_plan(M, N, K, **params)
     if probe is None:
-        with _on(stream):
-            probe = torch.full((plan["grid_m"] * plan["grid_n"], PROBE_WORDS), -1, dtype=torch.int64, device=a.device)
-        _handed_out(stream, probe)
+        probe = _made(stream, torch.full, (plan["grid_m"] * plan["grid_n"], PROBE_WORDS), -1, dtype=torch.int64, device=a.device)
     assert probe.is_cuda and probe.is_contiguous() and probe.dtype == torch.int64
     p = _params(**params)
     _check(lib.swz_gemm_probe(a.data_ptr(), b.data_ptr(), c.data_ptr(), M, N, K, DTYPE_BF16, int(mode), ctypes.byref(p),
@@ -331,10 +323,8 @@ def pid_map_persistent(grid_m: int, grid_n: int, num_xcd: int, group_m: int, mod
 def pid_map_persistent_device(grid_m: int, grid_n: int, num_xcd: int, group_m: int, mode: int, num_wg: int, stream=None):
     """Device PID map of the persistent launch: (tile [rounds x num_wg], xcc [num_wg]) int32 CUDA tensors."""
     rounds = _rounds(grid_m, grid_n, num_wg)
-    with _on(stream):
-        tile = torch.full((rounds, max(int(num_wg), 1)), -2, dtype=torch.int32, device="cuda")
-        xcc = torch.full((max(int(num_wg), 1),), -1, dtype=torch.int32, device="cuda")
-    _handed_out(stream, tile, xcc)
+    tile = _made(stream, torch.full, (rounds, max(int(num_wg), 1)), -2, dtype=torch.int32, device="cuda")
+    xcc = _made(stream, torch.full, (max(int(num_wg), 1),), -1, dtype=torch.int32, device="cuda")
     _check(lib.swz_pid_map_persistent_device(int(grid_m), int(grid_n), int(num_xcd), int(group_m), int(mode), int(num_wg),
                                              tile.data_ptr(), xcc.data_ptr(), _stream_handle(stream)),
            "swz_pid_map_persistent_device")
@@ -354,7 +344,7 @@ def transpose(x, out=None, tile: int = 64, mode: int = MODE_XCD_GROUPM + MODE_SK
     assert x.is_cuda and x.is_contiguous() and x.dim() == 2 and x.element_size() in (2, 4)
     M, N = x.shape
     if out is None:
-        out = _empty(stream, (N, M), x.dtype, x.device)
+        out = _made(stream, torch.empty, (N, M), dtype=x.dtype, device=x.device)
     assert out.is_cuda and out.is_contiguous() and tuple(out.shape) == (N, M) and out.dtype == x.dtype
     h = _launch_stream(stream, x, out)
     _check(lib.swz_transpose(x.data_ptr(), out.data_ptr(), M, N, x.element_size(), int(tile), int(mode), _params_ref(params),
@@ -365,7 +355,7 @@ def transpose(x, out=None, tile: int = 64, mode: int = MODE_XCD_GROUPM + MODE_SK
 def _row_args(x, out, stream):
     assert x.is_cuda and x.is_contiguous() and x.dim() == 2 and x.dtype == torch.bfloat16
     if out is None:
-        out = _empty(stream, x.shape, x.dtype, x.device)
+        out = _made(stream, torch.empty_like, x)
     assert out.is_cuda and out.is_contiguous() and out.shape == x.shape and out.dtype == x.dtype
     return out
 

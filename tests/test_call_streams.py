@@ -1,6 +1,4 @@
 """Which stream the memory belongs to that the entry points make for themselves: the one that works on it.  No GPU: tensors that say they are on one, a library that does nothing."""
-import contextlib
-
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -40,11 +38,8 @@ class World:
         self.inside, self.made, self.filled, self.recorded = None, [], [], []
         empty, full = torch.empty, torch.full
 
-        @contextlib.contextmanager
-        def stream(s):
-            before, self.inside = self.inside, s
-            yield
-            self.inside = before
+        def switch(s):
+            self.inside = None if s == "current" else s
 
         def made(*args, **kw):
             if str(kw.get("device")) != "meta":
@@ -56,10 +51,11 @@ class World:
             return full(*args, **{**kw, "device": "cpu"}).as_subclass(OnDevice)
 
         monkeypatch.setattr(torch, "empty", made)
+        monkeypatch.setattr(torch, "empty_like", lambda x: made(x.shape, dtype=x.dtype))
         monkeypatch.setattr(torch, "full", filled)
-        monkeypatch.setattr(torch.cuda, "stream", stream)
+        monkeypatch.setattr(torch.cuda, "set_stream", switch)
         monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle: ("external", handle))
-        monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: "current")
+        monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: self.inside or "current")
         for module in (binding, layer):
             monkeypatch.setattr(module, "lib", Library())
             monkeypatch.setattr(module, "_launch_stream", lambda s, *tensors: 0)
@@ -123,7 +119,8 @@ def test_memory_made_here_belongs_to_the_stream(world, name):
     call, results, workspaces = CALLS[name]
     call(Side)
     assert world.made == [("external", 0x77)] * (results + workspaces)
-    assert world.recorded == ["current"] * results       # what the caller gets may be used on the current stream too
+    assert set(world.recorded) == {"current"} and len(world.recorded) >= results       # what the caller gets may be used on the current stream too
+    assert world.inside is None
 
 
 @pytest.mark.parametrize("name", CALLS)
@@ -136,3 +133,9 @@ def test_without_a_stream_nothing_is_switched(world, name):
 def test_gradients_of_no_tokens_are_filled_on_the_stream(world):
     swz.qk_norm_rope_backward(heads(0), heads(0, 1), *norm_inputs(0), stream=Side)
     assert world.filled == [("external", 0x77)]
+
+
+def test_a_refusal_leaves_the_current_stream(world):
+    with pytest.raises(AssertionError):
+        swz.attention(heads(3), heads(3, 1), heads(3), ints(0, 3), stream=Side)
+    assert world.inside is None and world.recorded == []
