@@ -12,3 +12,4 @@ from .binding import (  # noqa: F401
 from .attention_layer import (  # noqa: F401
     CACHE_GROUP, Cache4, attention, attention_backward, cache4_append, cache4_attention, cache4_read, kv_cache4, qk_norm_rope, qk_norm_rope_backward,
 )
+from .drafts import Cache16, cache16_append, cache16_attention, cache16_keep, draft_tree, kv_cache16, verify_drafts  # noqa: F401

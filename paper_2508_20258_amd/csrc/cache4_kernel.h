@@ -6,26 +6,13 @@
 // 6.6 for the join, call after call on the same cache; among other work, which leaves none of it in the memory-side cache, 51 us in all.
 #pragma once
 
+#include "paged.h"
 #include "qk_norm_kernel.h"
 
 namespace swz {
 
-struct CacheArgs {
+struct CacheArgs : PageTable {
   uint32_t *k_words, *v_words, *k_scales, *v_scales;       // a scale: step in the low half, low in the high half
-  const int32_t* table;
-  int64_t pages;
-  int page_shift, k_heads, table_width;
-  // The page of a position, or -1.
-  __device__ __forceinline__ int page_of(int sequence, int position) const {
-    const int j = position >> page_shift;
-    if (j >= table_width) return -1;
-    const int page = table[(int64_t)sequence * table_width + j];
-    return page >= 0 && page < pages ? page : -1;
-  }
-  // Tokens of a head before this one in the cache.
-  __device__ __forceinline__ int64_t token_at(int page, int head, int position) const {
-    return (((int64_t)page * k_heads + head) << page_shift) + (position & ((1 << page_shift) - 1));
-  }
 };
 
 // Bits of a word that hold number e.

@@ -1,0 +1,232 @@
+// libswz: C-ABI entry points of a step with drafted tokens (declared in include/swz_drafts.h).  Host side: argument checks, the split of the
+// work, launches.  Nothing here allocates device memory or synchronises.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/swz_drafts.h"
+#include "cache16_kernel.h"
+#include "draft_attention_kernel.h"
+#include "host_checks.h"
+#include "verify_kernel.h"
+
+namespace {
+
+using namespace swz::host;
+using swz::launch;
+
+int check_cache(const swz_cache16* c) {
+  if (c == nullptr || c->k == nullptr || c->v == nullptr || c->pages < 1 || c->k_heads < 1) return SWZ_ERR_INVALID_ARG;
+  if (!head_dim_ok(c->head_dim) || c->page_tokens < 16 || (c->page_tokens & (c->page_tokens - 1)) != 0 || !aligned(c->k, 16) || !aligned(c->v, 16)) return SWZ_ERR_UNSUPPORTED;
+  return c->pages >= kTokens || c->k_heads > kMostHeads ? SWZ_ERR_OVERFLOW : SWZ_OK;
+}
+
+int check_blocks(const int32_t* cu, const int32_t* table, int64_t tokens, int32_t sequences, int32_t table_width) {
+  if (cu == nullptr || table == nullptr || tokens < 0 || sequences < 1 || table_width < 1) return SWZ_ERR_INVALID_ARG;
+  if (!aligned(cu, 4) || !aligned(table, 4)) return SWZ_ERR_UNSUPPORTED;
+  return tokens > kMostKeys ? SWZ_ERR_OVERFLOW : SWZ_OK;
+}
+
+swz::PageTable page_table(const swz_cache16& c, const int32_t* table, int table_width) {
+  return {table, c.pages, __builtin_ctz((unsigned)c.page_tokens), c.k_heads, table_width};
+}
+
+int check_append(const swz_cache16* cache, const swz_append16_args* a) {
+  int st = check_cache(cache);
+  if (st != SWZ_OK) return st;
+  if (a == nullptr || a->before == nullptr) return SWZ_ERR_INVALID_ARG;
+  st = check_blocks(a->cu, a->block_table, a->tokens, a->sequences, a->table_width);
+  if (st != SWZ_OK) return st;
+  const bool turned = a->cos != nullptr, queries = a->q.data != nullptr;
+  if ((a->sin != nullptr) != turned || (queries && !turned) || (queries && a->q_heads < 1) || (turned && a->table_rows < 0)) return SWZ_ERR_INVALID_ARG;
+  if (a->tokens == 0) return SWZ_OK;
+  st = check_heads(a->k, a->v);
+  if (st != SWZ_OK) return st;
+  if (queries && (st = check_heads(a->q, a->q_out)) != SWZ_OK) return st;
+  if (!aligned(a->before, 4) || !aligned(a->positions, 4) || !aligned(a->cos, 16) || !aligned(a->sin, 16)) return SWZ_ERR_UNSUPPORTED;
+  if (turned && (a->rotary_dim < 16 || a->rotary_dim > cache->head_dim || a->rotary_dim % 16 != 0)) return SWZ_ERR_UNSUPPORTED;
+  return queries && a->q_heads > kMostHeads ? SWZ_ERR_OVERFLOW : SWZ_OK;
+}
+
+// ---------------------------------------------------------------- attention
+
+int check_attention(const swz_cache16* cache, const swz_attention16_args* a) {
+  int st = check_cache(cache);
+  if (st != SWZ_OK) return st;
+  if (a == nullptr || a->lengths == nullptr) return SWZ_ERR_INVALID_ARG;
+  st = check_blocks(a->cu, a->block_table, a->tokens, a->sequences, a->table_width);
+  if (st == SWZ_ERR_INVALID_ARG) return st;
+  if (a->q_heads < 1 || a->q_heads % cache->k_heads != 0 || a->max_length < 0 || !(a->scale > 0.f) || !isfinite(a->scale)) return SWZ_ERR_INVALID_ARG;
+  if (st != SWZ_OK) return st;
+  if (!aligned(a->lengths, 4) || !aligned(a->tree, 8)) return SWZ_ERR_UNSUPPORTED;
+  if (a->q_heads > kMostHeads || (int64_t)a->table_width * cache->page_tokens > kMostKeys || a->tokens * a->q_heads >= kTokens) return SWZ_ERR_OVERFLOW;
+  return SWZ_OK;
+}
+
+struct AttentionPlan {
+  int row_waves, shares;             // shares 0: a workgroup for each tile of rows and key head
+  int64_t items;                     // tiles of rows, at most
+};
+
+// f(integral_constant<int, D>, integral_constant<int, RW>)
+template <class F>
+auto for_shape(int d, int row_waves, F&& f) {
+  return for_head_dim(d, [&](auto dim) { return row_waves == 1 ? f(dim, std::integral_constant<int, 1>{}) : f(dim, std::integral_constant<int, 4>{}); });
+}
+
+AttentionPlan attention_plan(const swz_cache16& c, const swz_attention16_args& a) {
+  const int64_t group = a.q_heads / c.k_heads, rows = (a.tokens + a.sequences - 1) / a.sequences * group;          // of an average block
+  const int64_t cut = (int64_t)a.table_width * c.page_tokens, longest = a.max_length > 0 && a.max_length < cut ? a.max_length : cut;
+  AttentionPlan p{};
+  p.row_waves = rows <= 32 ? 1 : 4;
+  for_shape(c.head_dim, p.row_waves, [&](auto dim, auto waves) {
+    using S = swz::DraftShape<decltype(dim)::value, decltype(waves)::value>;
+    p.items = a.tokens * group / S::kRows + a.sequences;
+    const int64_t together = (int64_t)compute_units() * S::kPerCu / c.k_heads, steps = (longest + S::kStep - 1) / S::kStep;
+    if (steps <= 4 || p.items >= 4 * together) return 0;
+    const int64_t shares = together < 1 ? 1 : together;
+    p.shares = (int)(p.items * steps < shares ? p.items * steps : shares);
+    return 0;
+  });
+  return p;
+}
+// Steps of all tiles of rows fit 32 bits, whatever the lengths.
+bool too_many_steps(const swz_cache16& c, const swz_attention16_args& a, const AttentionPlan& p) {
+  const int64_t steps = ((int64_t)a.table_width * c.page_tokens + swz::kDraftKeys - 1) / swz::kDraftKeys;
+  return p.items >= kTokens || steps * p.items >= kTokens;
+}
+int64_t attention_places(const swz_cache16& c, const AttentionPlan& p) { return (int64_t)p.shares * c.k_heads * 2 * 32 * p.row_waves; }
+int64_t attention_bytes(const swz_cache16& c, const AttentionPlan& p) { return p.shares == 0 ? 0 : 4 * attention_places(c, p) * (c.head_dim + 2) + 8 * p.items * c.k_heads; }
+
+// ---------------------------------------------------------------- verification
+
+int check_verify(const swz_verify_args* a) {
+  if (a == nullptr || a->target == nullptr || a->tokens == nullptr || a->cu == nullptr || a->uniforms == nullptr || a->accepted == nullptr || a->path == nullptr || a->token == nullptr) return SWZ_ERR_INVALID_ARG;
+  if (a->vocab < 1 || a->total < 0 || a->sequences < 1 || a->target_pitch < a->vocab || (a->draft != nullptr && a->draft_pitch < a->vocab)) return SWZ_ERR_INVALID_ARG;
+  if ((a->elem_bytes != 2 && a->elem_bytes != 4) || !aligned(a->target, a->elem_bytes) || !aligned(a->draft, a->elem_bytes)) return SWZ_ERR_UNSUPPORTED;
+  if (!aligned(a->tokens, 4) || !aligned(a->cu, 4) || !aligned(a->uniforms, 4) || !aligned(a->accepted, 4) || !aligned(a->path, 4) || !aligned(a->token, 4) || !aligned(a->parents, 4)) return SWZ_ERR_UNSUPPORTED;
+  if (a->vocab >= (1 << 30) || a->total >= kTokens || a->target_pitch >= kTokens || (a->draft != nullptr && a->draft_pitch >= kTokens)) return SWZ_ERR_OVERFLOW;
+  const int64_t pieces = (a->vocab + swz::kPieceValues - 1) / swz::kPieceValues;
+  return pieces * a->sequences * swz::kVerifyThreads > swz::kLaunchThreads || (int64_t)a->sequences * swz::kWalkThreads > swz::kLaunchThreads ? SWZ_ERR_OVERFLOW : SWZ_OK;
+}
+int verify_pieces(const swz_verify_args& a) { return (int)((a.vocab + swz::kPieceValues - 1) / swz::kPieceValues); }
+
+template <class T, bool DRAWN>
+int launch_verify(const swz::VerifyArgs& v, hipStream_t stream) {
+  const dim3 block(swz::kVerifyThreads), grid((unsigned)((int64_t)v.sequences * v.pieces));
+  int st;
+  if (DRAWN && v.parents != nullptr) {
+    st = launch(swz::verify_walk_kernel<T>, dim3((unsigned)v.sequences), dim3(swz::kWalkThreads), 0, stream, v);
+    if (st == SWZ_OK) st = launch(swz::verify_sums_kernel<T, true, true>, grid, block, 0, stream, v);
+  } else {
+    st = launch(swz::verify_sums_kernel<T, DRAWN, false>, grid, block, 0, stream, v);
+  }
+  return st != SWZ_OK ? st : launch(swz::verify_token_kernel<T, DRAWN>, dim3((unsigned)v.sequences), block, 0, stream, v);
+}
+
+}  // namespace
+
+extern "C" {
+
+int swz_cache16_append(const swz_cache16* cache, const swz_append16_args* args, hipStream_t stream) {
+  const int st = check_append(cache, args);
+  if (st != SWZ_OK || args->tokens == 0) return st;
+  swz::Append16Args a{};
+  a.c = page_table(*cache, args->block_table, args->table_width);
+  a.k_pages = static_cast<uint16_t*>(cache->k), a.v_pages = static_cast<uint16_t*>(cache->v);
+  a.k = device_heads(args->k), a.v = device_heads(args->v);
+  if (args->q.data != nullptr) a.q = device_heads(args->q), a.q_out = device_heads(args->q_out), a.q_heads = args->q_heads;
+  a.cos = args->cos, a.sin = args->sin, a.positions = args->positions, a.cu = args->cu, a.before = args->before;
+  a.table_rows = args->table_rows, a.total = (int)args->tokens, a.sequences = args->sequences, a.rotary = args->cos != nullptr ? args->rotary_dim : 0;
+  return for_head_dim(cache->head_dim, [&](auto dim) {
+    return for_flag(args->interleaved != 0, [&](auto interleaved) {
+      constexpr int D = decltype(dim)::value, kHeads = 1024 / D, kWaves = swz::kAppendThreads / 64;
+      const int blocks = (a.q_heads + 2 * a.c.k_heads + kHeads - 1) / kHeads;
+      a.splits = args->tokens * blocks <= 32 * (int64_t)compute_units() ? blocks : 1;
+      const int64_t workgroups = (args->tokens * a.splits + kWaves - 1) / kWaves;
+      if (workgroups >= kTokens) return (int)SWZ_ERR_OVERFLOW;
+      return launch(swz::cache16_append_kernel<D, decltype(interleaved)::value>, dim3((unsigned)workgroups), dim3(swz::kAppendThreads), 0, stream, a);
+    });
+  });
+}
+
+int64_t swz_cache16_attention_workspace(const swz_cache16* cache, const swz_attention16_args* args) {
+  const int st = check_attention(cache, args);
+  if (st != SWZ_OK) return st;
+  const AttentionPlan p = attention_plan(*cache, *args);
+  return too_many_steps(*cache, *args, p) ? SWZ_ERR_OVERFLOW : attention_bytes(*cache, p);
+}
+
+int swz_cache16_attention(const swz_cache16* cache, const swz_attention16_args* args, void* workspace, int64_t workspace_bytes, hipStream_t stream) {
+  int st = check_attention(cache, args);
+  if (st != SWZ_OK || args->tokens == 0) return st;
+  st = check_heads(args->q, args->out);
+  if (st != SWZ_OK) return st;
+  const AttentionPlan p = attention_plan(*cache, *args);
+  if (too_many_steps(*cache, *args, p)) return SWZ_ERR_OVERFLOW;
+  const int64_t bytes = attention_bytes(*cache, p);
+  if (bytes > 0 && (workspace == nullptr || workspace_bytes < bytes)) return SWZ_ERR_INVALID_ARG;
+  if (!aligned(workspace, 16)) return SWZ_ERR_UNSUPPORTED;
+  swz::DraftArgs a{};
+  a.c = page_table(*cache, args->block_table, args->table_width);
+  a.k_pages = static_cast<const uint16_t*>(cache->k), a.v_pages = static_cast<const uint16_t*>(cache->v);
+  a.q = device_heads(args->q), a.out = device_heads(args->out);
+  a.cu = args->cu, a.lengths = args->lengths, a.tree = reinterpret_cast<const uint64_t*>(args->tree);
+  a.sums = static_cast<float*>(workspace);
+  a.stats = a.sums + attention_places(*cache, p) * cache->head_dim;
+  a.parts = reinterpret_cast<int2*>(a.stats + attention_places(*cache, p) * 2);
+  a.total = (int)args->tokens, a.sequences = args->sequences, a.q_heads = args->q_heads, a.items = (int)p.items, a.shares = p.shares, a.scale = args->scale;
+  const int64_t workgroups = (p.shares == 0 ? p.items : p.shares) * cache->k_heads, joins = (args->tokens * args->q_heads + 3) / 4;
+  if (workgroups * 256 > swz::kLaunchThreads || joins * 256 > swz::kLaunchThreads) return SWZ_ERR_OVERFLOW;
+  return for_shape(cache->head_dim, p.row_waves, [&](auto dim, auto waves) {
+    constexpr int D = decltype(dim)::value, RW = decltype(waves)::value;
+    const int status = launch(swz::draft_attention_kernel<D, RW>, dim3((unsigned)workgroups), dim3(64 * swz::kDraftWaves), 0, stream, a);
+    if (status != SWZ_OK || p.shares == 0) return status;
+    return launch(swz::draft_join_kernel<D, RW>, dim3((unsigned)joins), dim3(256), 0, stream, a);
+  });
+}
+
+int64_t swz_verify_drafts_workspace(const swz_verify_args* args) {
+  const int st = check_verify(args);
+  return st != SWZ_OK ? st : args->sequences * ((int64_t)sizeof(swz::VerifyState) + 16 * (int64_t)verify_pieces(*args));
+}
+
+int swz_verify_drafts(const swz_verify_args* args, void* workspace, int64_t workspace_bytes, hipStream_t stream) {
+  const int st = check_verify(args);
+  if (st != SWZ_OK) return st;
+  if (workspace == nullptr || workspace_bytes < swz_verify_drafts_workspace(args)) return SWZ_ERR_INVALID_ARG;
+  if (!aligned(workspace, 16)) return SWZ_ERR_UNSUPPORTED;
+  swz::VerifyArgs v{};
+  v.target = args->target, v.draft = args->draft, v.target_pitch = args->target_pitch, v.draft_pitch = args->draft_pitch;
+  v.tokens = args->tokens, v.parents = args->parents, v.cu = args->cu, v.uniforms = args->uniforms;
+  v.accepted = args->accepted, v.path = args->path, v.token = args->token;
+  v.total = (int)args->total, v.sequences = args->sequences, v.vocab = (int)args->vocab, v.pieces = verify_pieces(*args);
+  v.states = static_cast<swz::VerifyState*>(workspace);
+  v.sums = reinterpret_cast<double*>(v.states + args->sequences);
+  return for_flag(args->draft != nullptr, [&](auto drawn) {
+    constexpr bool kDrawn = decltype(drawn)::value;
+    return args->elem_bytes == 4 ? launch_verify<float, kDrawn>(v, stream) : launch_verify<uint16_t, kDrawn>(v, stream);
+  });
+}
+
+int swz_cache16_keep(const swz_cache16* cache, const int32_t* cu, const int32_t* before, const int32_t* path, const int32_t* accepted, int64_t tokens, const int32_t* block_table,
+                     int32_t table_width, int32_t sequences, hipStream_t stream) {
+  int st = check_cache(cache);
+  if (st != SWZ_OK) return st;
+  if (before == nullptr || path == nullptr || accepted == nullptr) return SWZ_ERR_INVALID_ARG;
+  st = check_blocks(cu, block_table, tokens, sequences, table_width);
+  if (st != SWZ_OK || tokens == 0) return st;
+  if (!aligned(before, 4) || !aligned(path, 4) || !aligned(accepted, 4)) return SWZ_ERR_UNSUPPORTED;
+  swz::Keep16Args a{};
+  a.c = page_table(*cache, block_table, table_width);
+  a.k_pages = static_cast<uint16_t*>(cache->k), a.v_pages = static_cast<uint16_t*>(cache->v);
+  a.cu = cu, a.before = before, a.path = path, a.accepted = accepted, a.total = (int)tokens, a.sequences = sequences;
+  const int64_t items = (int64_t)cache->k_heads * 2 * (cache->head_dim / 8);
+  a.blocks = (int)((items + swz::kKeepThreads - 1) / swz::kKeepThreads);
+  if ((int64_t)sequences * a.blocks >= kTokens) return SWZ_ERR_OVERFLOW;
+  return for_head_dim(cache->head_dim, [&](auto dim) {
+    return launch(swz::cache16_keep_kernel<decltype(dim)::value>, dim3((unsigned)(sequences * a.blocks)), dim3(swz::kKeepThreads), 0, stream, a);
+  });
+}
+
+}  // extern "C"

@@ -40,20 +40,6 @@ __device__ __forceinline__ float row_sum(float x) {
   return x;
 }
 
-__device__ __forceinline__ void unpack8(const u32x4& v, float (&x)[8]) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    x[2 * e] = __uint_as_float(v[e] << 16);
-    x[2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ u32x4 pack8(const float (&x)[8]) {
-  u32x4 v;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = pack_bf16(x[2 * e], x[2 * e + 1]);
-  return v;
-}
-
 // Which lane has the other halves of a lane's pairs, and whether the lane's dimensions have any.
 struct Partner {
   int lane;
