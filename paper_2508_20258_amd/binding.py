@@ -96,6 +96,7 @@ class _NoFast:
     """In the place of _fastcall.so: nothing is an ordinary call."""
     gemm = transpose = softmax = layernorm = staticmethod(lambda *args: None)
     qk_norm_rope = qk_norm_rope_backward = attention = attention_backward = cache4_append = cache4_read = cache4_attention = gemm
+    cache16_append = cache16_attention = verify_drafts = cache16_keep = gemm
 
 
 def _load_fast():

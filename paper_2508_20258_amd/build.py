@@ -32,7 +32,7 @@ FLAGS = [
 ]
 
 
-FAST_DEPS = [FAST_SOURCE, os.path.join(HERE, "..", "include", "swz.h"), os.path.join(HERE, "..", "include", "swz_attention.h")]
+FAST_DEPS = [FAST_SOURCE, *(os.path.join(HERE, "..", "include", h) for h in ("swz.h", "swz_attention.h", "swz_drafts.h"))]
 
 
 def rocm_include() -> str:

@@ -64,26 +64,28 @@ int check_attention(const swz_cache16* cache, const swz_attention16_args* a) {
 }
 
 struct AttentionPlan {
-  int row_waves, shares;             // shares 0: a workgroup for each tile of rows and key head
+  int rows, shares;                  // of a tile; shares 0: a workgroup for each tile of rows and key head
   int64_t items;                     // tiles of rows, at most
 };
 
-// f(integral_constant<int, D>, integral_constant<int, RW>)
+// f(integral_constant<int, D>, integral_constant<int, ROWS>)
 template <class F>
-auto for_shape(int d, int row_waves, F&& f) {
-  return for_head_dim(d, [&](auto dim) { return row_waves == 1 ? f(dim, std::integral_constant<int, 1>{}) : f(dim, std::integral_constant<int, 4>{}); });
+auto for_shape(int d, int rows, F&& f) {
+  return for_head_dim(d, [&](auto dim) {
+    return rows == 32 ? f(dim, std::integral_constant<int, 32>{}) : rows == 64 ? f(dim, std::integral_constant<int, 64>{}) : f(dim, std::integral_constant<int, 128>{});
+  });
 }
 
 AttentionPlan attention_plan(const swz_cache16& c, const swz_attention16_args& a) {
   const int64_t group = a.q_heads / c.k_heads, rows = (a.tokens + a.sequences - 1) / a.sequences * group;          // of an average block
   const int64_t cut = (int64_t)a.table_width * c.page_tokens, longest = a.max_length > 0 && a.max_length < cut ? a.max_length : cut;
   AttentionPlan p{};
-  p.row_waves = rows <= 32 ? 1 : 4;
-  for_shape(c.head_dim, p.row_waves, [&](auto dim, auto waves) {
-    using S = swz::DraftShape<decltype(dim)::value, decltype(waves)::value>;
-    p.items = a.tokens * group / S::kRows + a.sequences;
+  p.rows = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  for_shape(c.head_dim, p.rows, [&](auto dim, auto rows) {
+    using S = swz::DraftShape<decltype(dim)::value, decltype(rows)::value>;
+    p.items = a.tokens * group / p.rows + a.sequences;
     const int64_t together = (int64_t)compute_units() * S::kPerCu / c.k_heads, steps = (longest + S::kStep - 1) / S::kStep;
-    if (steps <= 4 || p.items >= 4 * together) return 0;
+    if (longest <= 1024) return 0;
     const int64_t shares = together < 1 ? 1 : together;
     p.shares = (int)(p.items * steps < shares ? p.items * steps : shares);
     return 0;
@@ -95,7 +97,7 @@ bool too_many_steps(const swz_cache16& c, const swz_attention16_args& a, const A
   const int64_t steps = ((int64_t)a.table_width * c.page_tokens + swz::kDraftKeys - 1) / swz::kDraftKeys;
   return p.items >= kTokens || steps * p.items >= kTokens;
 }
-int64_t attention_places(const swz_cache16& c, const AttentionPlan& p) { return (int64_t)p.shares * c.k_heads * 2 * 32 * p.row_waves; }
+int64_t attention_places(const swz_cache16& c, const AttentionPlan& p) { return (int64_t)p.shares * c.k_heads * 2 * p.rows; }
 int64_t attention_bytes(const swz_cache16& c, const AttentionPlan& p) { return p.shares == 0 ? 0 : 4 * attention_places(c, p) * (c.head_dim + 2) + 8 * p.items * c.k_heads; }
 
 // ---------------------------------------------------------------- verification
@@ -178,11 +180,15 @@ int swz_cache16_attention(const swz_cache16* cache, const swz_attention16_args* 
   a.total = (int)args->tokens, a.sequences = args->sequences, a.q_heads = args->q_heads, a.items = (int)p.items, a.shares = p.shares, a.scale = args->scale;
   const int64_t workgroups = (p.shares == 0 ? p.items : p.shares) * cache->k_heads, joins = (args->tokens * args->q_heads + 3) / 4;
   if (workgroups * 256 > swz::kLaunchThreads || joins * 256 > swz::kLaunchThreads) return SWZ_ERR_OVERFLOW;
-  return for_shape(cache->head_dim, p.row_waves, [&](auto dim, auto waves) {
-    constexpr int D = decltype(dim)::value, RW = decltype(waves)::value;
-    const int status = launch(swz::draft_attention_kernel<D, RW>, dim3((unsigned)workgroups), dim3(64 * swz::kDraftWaves), 0, stream, a);
+  return for_shape(cache->head_dim, p.rows, [&](auto dim, auto rows) {
+    constexpr int D = decltype(dim)::value, ROWS = decltype(rows)::value;
+    auto kernel = [] {
+      if constexpr (ROWS == 128) return swz::draft_attention_wide_kernel<D>;
+      else return swz::draft_attention_kernel<D, ROWS>;
+    }();
+    const int status = launch(kernel, dim3((unsigned)workgroups), dim3(64 * swz::kDraftWaves), 0, stream, a);
     if (status != SWZ_OK || p.shares == 0) return status;
-    return launch(swz::draft_join_kernel<D, RW>, dim3((unsigned)joins), dim3(256), 0, stream, a);
+    return launch(swz::draft_join_kernel<D, ROWS>, dim3((unsigned)joins), dim3(256), 0, stream, a);
   });
 }
 

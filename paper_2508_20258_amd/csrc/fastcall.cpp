@@ -19,6 +19,7 @@
 
 #include "../../include/swz.h"
 #include "../../include/swz_attention.h"
+#include "../../include/swz_drafts.h"
 
 namespace {
 
@@ -368,12 +369,143 @@ PyObject* cache4_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
   });
 }
 
-// The library's functions, in the order of AttentionFns.
-PyObject* bind_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  constexpr Py_ssize_t kCount = sizeof(AttentionFns) / sizeof(void*);
+// ---------------------------------------------------------------- a step with drafted tokens (include/swz_drafts.h, drafts.py)
+
+struct DraftFns {
+  decltype(&swz_cache16_append) append;
+  decltype(&swz_cache16_attention_workspace) attention_workspace;
+  decltype(&swz_cache16_attention) attention;
+  decltype(&swz_verify_drafts_workspace) verify_workspace;
+  decltype(&swz_verify_drafts) verify;
+  decltype(&swz_cache16_keep) keep;
+} g_drafts;
+
+bool cache16_of(PyObject* o, c10::DeviceIndex dev, swz_cache16* c) {
+  if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 2) return false;
+  const at::Tensor *k = plain(PyTuple_GET_ITEM(o, 0), dev), *v = plain(PyTuple_GET_ITEM(o, 1), dev);
+  if (!is_bf16(k, 4) || !is_bf16(v, 4) || k->sizes() != v->sizes() || k->size(1) > (1 << 20) || k->size(2) > (1 << 30) || k->size(3) > 1024) return false;
+  *c = {k->data_ptr(), v->data_ptr(), k->size(0), static_cast<int32_t>(k->size(2)), static_cast<int32_t>(k->size(1)), static_cast<int32_t>(k->size(3))};
+  return true;
+}
+
+// args: cache, k, v, cu, before, block_table, q, cos, sin, positions, interleaved; a status where there is no q
+PyObject* cache16_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    const c10::DeviceIndex dev = c10::hip::current_device();
+    swz_cache16 c;
+    Sequences s;
+    if (n != 11 || !cache16_of(args[0], dev, &c) || !sequences_of(args[3], args[4], args[5], dev, &s) || !PyBool_Check(args[10])) return nullptr;
+    const at::Tensor *k = on_device(args[1], dev), *v = on_device(args[2], dev);
+    if (!is_heads(k) || !is_heads(v) || k->sizes() != v->sizes() || k->size(1) != c.k_heads || k->size(2) != c.head_dim) return nullptr;
+    swz_append16_args a{};
+    a.k = heads_of(*k), a.v = heads_of(*v), a.cu = s.cu, a.before = s.counts, a.block_table = s.table;
+    a.tokens = k->size(0), a.sequences = s.n, a.table_width = s.width, a.interleaved = args[10] == Py_True;
+    const bool turned = args[7] != Py_None, queries = args[6] != Py_None;
+    if ((args[8] != Py_None) != turned || (!turned && (queries || args[9] != Py_None))) return nullptr;
+    if (turned) {
+      const at::Tensor *cos = plain(args[7], dev), *sin = plain(args[8], dev);
+      if (!is_type(cos, 2, at::kFloat) || !is_type(sin, 2, at::kFloat) || cos->sizes() != sin->sizes() || cos->size(1) > 1024) return nullptr;
+      a.cos = static_cast<const float*>(cos->data_ptr()), a.sin = static_cast<const float*>(sin->data_ptr());
+      a.table_rows = cos->size(0), a.rotary_dim = static_cast<int32_t>(2 * cos->size(1));
+    }
+    if (args[9] != Py_None) {
+      const at::Tensor* p = plain(args[9], dev);
+      if (!is_ints(p, a.tokens)) return nullptr;
+      a.positions = static_cast<const int32_t*>(p->data_ptr());
+    }
+    at::Tensor out;
+    if (queries) {
+      const at::Tensor* q = on_device(args[6], dev);
+      if (!is_heads(q) || q->size(0) != a.tokens || q->size(2) != c.head_dim || q->size(1) > (1 << 20)) return nullptr;
+      out = dense_like(*q);
+      a.q = heads_of(*q), a.q_out = heads_of(out), a.q_heads = static_cast<int32_t>(q->size(1));
+    }
+    return result_of(dev, [&](hipStream_t st) { return g_drafts.append(&c, &a, st); }, [&] { return queries ? THPVariable_Wrap(out) : PyLong_FromLong(0); });
+  });
+}
+
+// args: q, cache, cu, lengths, block_table, tree, max_length, scale
+PyObject* cache16_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    const c10::DeviceIndex dev = c10::hip::current_device();
+    swz_cache16 c;
+    Sequences s;
+    int longest;
+    if (n != 8 || !cache16_of(args[1], dev, &c) || !sequences_of(args[2], args[3], args[4], dev, &s) || !as_int(args[6], &longest)) return nullptr;
+    const at::Tensor* q = on_device(args[0], dev);
+    float scale = static_cast<float>(1.0 / std::sqrt(static_cast<double>(c.head_dim)));
+    if (!is_heads(q) || q->size(2) != c.head_dim || q->size(1) > (1 << 20) || (args[7] != Py_None && !as_float(args[7], &scale))) return nullptr;
+    swz_attention16_args a{heads_of(*q), {}, s.cu, s.counts, s.table, nullptr, q->size(0), s.n, s.width, static_cast<int32_t>(q->size(1)), longest, scale};
+    if (args[5] != Py_None) {
+      const at::Tensor* tree = plain(args[5], dev);
+      if (!is_type(tree, 1, at::kLong) || tree->size(0) != a.tokens) return nullptr;
+      a.tree = static_cast<const int64_t*>(tree->data_ptr());
+    }
+    const int64_t bytes = g_drafts.attention_workspace(&c, &a);
+    if (bytes < 0) return nullptr;
+    const at::Tensor out = dense_like(*q), work = bytes > 0 ? workspace(bytes, *q) : at::Tensor();
+    a.out = heads_of(out);
+    return result_of(dev, [&](hipStream_t st) { return g_drafts.attention(&c, &a, bytes > 0 ? work.data_ptr() : nullptr, bytes, st); }, [&] { return THPVariable_Wrap(out); });
+  });
+}
+
+// args: target_probs, tokens, cu, uniforms, draft_probs, parents
+PyObject* verify_drafts(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    const c10::DeviceIndex dev = c10::hip::current_device();
+    if (n != 6) return nullptr;
+    const at::Tensor *target = on_device(args[0], dev), *tokens = plain(args[1], dev), *cu = plain(args[2], dev), *uniforms = plain(args[3], dev);
+    auto is_rows = [](const at::Tensor* t) {
+      return (is_bf16(t, 2) || is_type(t, 2, at::kFloat)) && t->numel() > 0 && (t->size(1) == 1 || t->stride(1) == 1) && (t->size(0) == 1 || t->stride(0) >= t->size(1));
+    };
+    if (!is_rows(target)) return nullptr;
+    const int64_t total = target->size(0), vocab = target->size(1);
+    if (!is_ints(tokens, total) || !is_type(cu, 1, at::kInt) || cu->size(0) < 2 || cu->size(0) > (1 << 30) || !is_type(uniforms, 1, at::kFloat) || uniforms->size(0) != total) return nullptr;
+    swz_verify_args a{};
+    auto pitch = [&](const at::Tensor& t) { return total > 1 ? t.stride(0) : vocab; };
+    if (args[4] != Py_None) {
+      const at::Tensor* draft = on_device(args[4], dev);
+      if (!is_rows(draft) || draft->sizes() != target->sizes() || draft->scalar_type() != target->scalar_type()) return nullptr;
+      a.draft = draft->data_ptr(), a.draft_pitch = pitch(*draft);
+    }
+    if (args[5] != Py_None) {
+      const at::Tensor* parents = plain(args[5], dev);
+      if (!is_ints(parents, total)) return nullptr;
+      a.parents = static_cast<const int32_t*>(parents->data_ptr());
+    }
+    a.target = target->data_ptr(), a.target_pitch = pitch(*target), a.vocab = vocab, a.total = total;
+    a.tokens = static_cast<const int32_t*>(tokens->data_ptr()), a.cu = static_cast<const int32_t*>(cu->data_ptr()), a.uniforms = static_cast<const float*>(uniforms->data_ptr());
+    a.sequences = static_cast<int32_t>(cu->size(0) - 1), a.elem_bytes = static_cast<int32_t>(target->element_size());
+    const at::Tensor accepted = at::empty({a.sequences}, cu->options()), path = at::empty({total}, cu->options()), token = at::empty({a.sequences}, cu->options());
+    a.accepted = static_cast<int32_t*>(accepted.data_ptr()), a.path = static_cast<int32_t*>(path.data_ptr()), a.token = static_cast<int32_t*>(token.data_ptr());
+    const int64_t bytes = g_drafts.verify_workspace(&a);
+    if (bytes < 0) return nullptr;
+    const at::Tensor work = workspace(bytes, *cu);
+    return result_of(dev, [&](hipStream_t st) { return g_drafts.verify(&a, work.data_ptr(), bytes, st); }, [&] { return tuple_of({accepted, path, token}); });
+  });
+}
+
+// args: cache, cu, before, path, accepted, block_table; a status
+PyObject* cache16_keep(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    const c10::DeviceIndex dev = c10::hip::current_device();
+    swz_cache16 c;
+    Sequences s;
+    if (n != 6 || !cache16_of(args[0], dev, &c) || !sequences_of(args[1], args[2], args[5], dev, &s)) return nullptr;
+    const at::Tensor *path = plain(args[3], dev), *accepted = plain(args[4], dev);
+    if (!is_type(path, 1, at::kInt) || path->numel() == 0 || !is_ints(accepted, s.n)) return nullptr;
+    const int64_t tokens = path->size(0);
+    const int32_t *p = static_cast<const int32_t*>(path->data_ptr()), *m = static_cast<const int32_t*>(accepted->data_ptr());
+    return launch(dev, [&](hipStream_t st) { return g_drafts.keep(&c, s.cu, s.counts, p, m, tokens, s.table, s.width, s.n, st); });
+  });
+}
+
+template <class Fns>
+PyObject* bind_all(Fns* to, PyObject* const* args, Py_ssize_t n) {
+  constexpr Py_ssize_t kCount = sizeof(Fns) / sizeof(void*);
   void* p[kCount];
   if (n != kCount) {
-    PyErr_SetString(PyExc_TypeError, "bind_attention takes one address for each function");
+    PyErr_SetString(PyExc_TypeError, "one address for each function");
     return nullptr;
   }
   for (Py_ssize_t i = 0; i < kCount; ++i) {
@@ -383,9 +515,12 @@ PyObject* bind_attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
       return nullptr;
     }
   }
-  std::memcpy(&g_attention, p, sizeof p);
+  std::memcpy(to, p, sizeof p);
   Py_RETURN_NONE;
 }
+// The library's functions, in the order of AttentionFns and DraftFns.
+PyObject* bind_attention(PyObject*, PyObject* const* args, Py_ssize_t n) { return bind_all(&g_attention, args, n); }
+PyObject* bind_drafts(PyObject*, PyObject* const* args, Py_ssize_t n) { return bind_all(&g_drafts, args, n); }
 
 // The library's functions, as ctypes found them: this module links to no second copy of it.
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -413,7 +548,8 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define SWZ_FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {SWZ_FAST(gemm), SWZ_FAST(transpose), SWZ_FAST(softmax), SWZ_FAST(layernorm), SWZ_FAST(bind),
                           SWZ_FAST(qk_norm_rope), SWZ_FAST(qk_norm_rope_backward), SWZ_FAST(attention), SWZ_FAST(attention_backward), SWZ_FAST(cache4_append),
-                          SWZ_FAST(cache4_read), SWZ_FAST(cache4_attention), SWZ_FAST(bind_attention), {nullptr, nullptr, 0, nullptr}};
+                          SWZ_FAST(cache4_read), SWZ_FAST(cache4_attention), SWZ_FAST(bind_attention), SWZ_FAST(cache16_append), SWZ_FAST(cache16_attention),
+                          SWZ_FAST(verify_drafts), SWZ_FAST(cache16_keep), SWZ_FAST(bind_drafts), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -15,8 +15,8 @@ from __future__ import annotations
 import ctypes
 from typing import NamedTuple
 
-from .attention_layer import _Heads, _heads, _is_heads, _is_ints, _out, _pointer, _workspace
-from .binding import _check, _launch_stream, _run_on, lib, torch
+from .attention_layer import _Heads, _done, _heads, _is_heads, _is_ints, _out, _pointer, _workspace
+from .binding import _NoFast, _check, _fast, _launch_stream, _run_on, lib, torch
 
 EXPORTS = ("swz_cache16_append", "swz_cache16_attention_workspace", "swz_cache16_attention", "swz_verify_drafts_workspace", "swz_verify_drafts", "swz_cache16_keep")
 
@@ -56,6 +56,8 @@ def _declare() -> None:
 
 
 _declare()
+if _fast is not _NoFast:
+    _fast.bind_drafts(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in EXPORTS))
 
 
 class Cache16(NamedTuple):
@@ -92,6 +94,10 @@ def cache16_append(cache: Cache16, k, v, cu, before, block_table, q=None, cos=No
     turned.  q_out may be q itself.  Positions beyond the table and entries that name no page (-1) are not written.  A page belongs to one sequence of a call."""
     if stream is not None:
         return _run_on(stream, cache16_append, cache, k, v, cu, before, block_table, q, cos, sin, positions, q_out, interleaved)
+    if q_out is None:
+        done = _fast.cache16_append(cache, k, v, cu, before, block_table, q, cos, sin, positions, interleaved)
+        if done is not None:
+            return _check(done, "swz_cache16_append") if done.__class__ is int else done
     c = _cache(cache)
     assert _is_heads(k, None, c.k_heads, c.head_dim) and _is_heads(v, *k.shape)
     n, tokens = _check_blocks(cu, before, block_table), k.shape[0]
@@ -127,6 +133,10 @@ def cache16_attention(q, cache: Cache16, cu, lengths, block_table, tree=None, ma
     scale: head_dim ** -0.5 by default."""
     if stream is not None:
         return _run_on(stream, cache16_attention, q, cache, cu, lengths, block_table, tree, max_length, out, scale)
+    if out is None:
+        done = _fast.cache16_attention(q, cache, cu, lengths, block_table, tree, max_length, scale)
+        if done is not None:
+            return _done(done, "swz_cache16_attention")
     c = _cache(cache)
     assert _is_heads(q, None, None, c.head_dim)
     n, (tokens, q_heads, dim) = _check_blocks(cu, lengths, block_table), q.shape
@@ -152,6 +162,9 @@ def verify_drafts(target_probs, tokens, cu, uniforms, draft_probs=None, parents=
     probabilities have no sum.  The exact rule is in include/swz_drafts.h."""
     if stream is not None:
         return _run_on(stream, verify_drafts, target_probs, tokens, cu, uniforms, draft_probs, parents)
+    done = _fast.verify_drafts(target_probs, tokens, cu, uniforms, draft_probs, parents)
+    if done is not None:
+        return _done(done, "swz_verify_drafts")
     used = [target_probs, tokens, cu, uniforms]
     total, vocab = target_probs.shape
     for t in (target_probs, draft_probs):
@@ -188,6 +201,10 @@ def verify_drafts(target_probs, tokens, cu, uniforms, draft_probs=None, parents=
 def cache16_keep(cache: Cache16, cu, before, path, accepted, block_table, stream=None) -> None:
     """Keeps the accepted path of every sequence's block, whose tokens were appended after its first before[b] positions: position before[b] + path[cu[b] + i] moves to before[b] + i, i up to
     accepted[b].  path and accepted as verify_drafts returns them (a path rises); the sequences then have before + accepted + 1 positions."""
+    if stream is None:
+        status = _fast.cache16_keep(cache, cu, before, path, accepted, block_table)
+        if status is not None:
+            return _check(status, "swz_cache16_keep")
     c = _cache(cache)
     n, total = _check_blocks(cu, before, block_table), path.shape[0]
     assert _is_ints(path, total) and _is_ints(accepted, n)

@@ -583,10 +583,14 @@ def cmd_profile_rows(args):
         f.write(text)
 
 
-def _operators():
-    """perf/operators.py, whose cases the attention layers are measured on."""
+# What is measured on the cases of a file under perf/: what they are, and where the summary goes.
+OPERATORS = {"operators": ("the attention layers", "attention_layers.txt"), "more_operators": ("a step with drafted tokens", "drafted_tokens.txt")}
+
+
+def _operators(name="operators"):
+    """perf/<name>.py, whose cases the operators are measured on."""
     import importlib.util
-    spec = importlib.util.spec_from_file_location("swz_operators", os.path.join(os.path.dirname(HERE), "perf", "operators.py"))
+    spec = importlib.util.spec_from_file_location("swz_" + name, os.path.join(os.path.dirname(HERE), "perf", name + ".py"))
     module = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(module)
     module.own = True
@@ -598,7 +602,7 @@ def cmd_attention(args):
 
     import torch
 
-    ops = _operators()
+    ops = _operators(args.operators)
     case = next(c for c in ops.listed() if c["name"] == args.case)
     state = ops.prepare(case, 1)
     until = time.monotonic() + args.warm_ms / 1e3
@@ -618,29 +622,32 @@ ATTENTION_COUNTERS = ["SQ_BUSY_CU_CYCLES", "SQ_VALU_MFMA_BUSY_CYCLES", "SQ_LDS_I
 
 
 def cmd_profile_attention(args):
-    """rocprofv3 passes for every listed case of perf/operators.py, as child processes; prints the summary table."""
+    """rocprofv3 passes for every listed case of a file of operators, as child processes; prints the summary table."""
     out = os.path.abspath(args.out)
     os.makedirs(out, exist_ok=True)
-    ops = _operators()
+    ops = _operators(args.operators)
+    what, summary = OPERATORS[args.operators]
+    chosen = [] if args.operators == "operators" else ["--operators", args.operators]
     names = [c["name"] for c in ops.listed()]
     passes = (("sq", ATTENTION_COUNTERS), ("fetch", ["FETCH_SIZE"]), ("write", ["WRITE_SIZE"]))
     if not args.table_only:
         for c, tag in (("FETCH_SIZE", "copy_fetch"), ("WRITE_SIZE", "copy_write")):
             _rocprof(out, tag, "csv", ["--pmc", c], ["copy", "--mib", "1024", "--launches", "3"])
         for name in names:
-            prog = ["attention", "--case", name]
+            prog = ["attention", "--case", name, *chosen]
             _rocprof(out, name + "_kt", "csv", ["--kernel-trace", "--stats"], prog + ["--warm-ms", str(ATTENTION_WARM_MS), "--launches", str(args.launches + 10)])
             for tag, counters in passes:
                 _rocprof(out, f"{name}_{tag}", "csv", ["--pmc", *counters], prog + ["--launches", "3"], 90)
     fs = 1024 * 1024 / _one(f"{out}/copy_fetch", "copy")["counters"]["FETCH_SIZE"]
     ws = 1024 * 1024 / _one(f"{out}/copy_write", "copy")["counters"]["WRITE_SIZE"]
     H = "python3 -m paper_2508_20258_amd.harness"
-    lines = ["rocprofv3 summary: the kernels of the attention layers on the listed cases of perf/operators.py, MI355X, one GPU.",
+    named = "".join(" " + x for x in chosen)
+    lines = [f"rocprofv3 summary: the kernels of {what} on the listed cases of perf/{args.operators}.py, MI355X, one GPU.",
              "Written by (repository root, TMPDIR=/tmp):",
-             f"  {H} profile-attention --out <dir>",
+             f"  {H} profile-attention{named} --out <dir>",
              "which runs, for CASE as in the table:",
-             f"  rocprofv3 --kernel-trace --stats --output-format csv -d <out> -- {H} attention --case CASE --warm-ms {ATTENTION_WARM_MS} --launches {args.launches + 10}",
-             f"  rocprofv3 --pmc {' '.join(ATTENTION_COUNTERS)} (then FETCH_SIZE, then WRITE_SIZE) --output-format csv -d <out> -- {H} attention --case CASE --launches 3",
+             f"  rocprofv3 --kernel-trace --stats --output-format csv -d <out> -- {H} attention --case CASE{named} --warm-ms {ATTENTION_WARM_MS} --launches {args.launches + 10}",
+             f"  rocprofv3 --pmc {' '.join(ATTENTION_COUNTERS)} (then FETCH_SIZE, then WRITE_SIZE) --output-format csv -d <out> -- {H} attention --case CASE{named} --launches 3",
              f"  and FETCH_SIZE, WRITE_SIZE on `{H} copy --mib 1024` (calibration: FETCH_SIZE x {fs:.3f}, WRITE_SIZE x {ws:.3f}).",
              f"us = kernel duration in the trace, average over its last {args.launches} launches, over the same data, after {ATTENTION_WARM_MS} ms of them.  MFMA: share of the matrix units' cycles, of busy compute units, in which one works;",
              "LDS: share of these compute units' cycles in which LDS serves a read or write, conflicts among them; VALU: share of them in which vector instructions are issued.",
@@ -656,7 +663,7 @@ def cmd_profile_attention(args):
                          f"{write[kernel]['counters']['WRITE_SIZE'] * ws / 1024:10.1f}  {kernel.split('(')[0].replace('void ', '').replace('swz::', '')}")
     text = "\n".join(lines) + "\n"
     print(text, flush=True)
-    with open(os.path.join(out, "attention_layers.txt"), "w") as f:
+    with open(os.path.join(out, summary), "w") as f:
         f.write(text)
 
 
@@ -1021,11 +1028,13 @@ def main(argv=None):
     at.add_argument("--case", required=True)
     at.add_argument("--warm-ms", type=int, default=0)
     at.add_argument("--launches", type=int, default=20)
+    at.add_argument("--operators", default="operators", choices=sorted(OPERATORS))
     at.set_defaults(fn=cmd_attention)
     pa = sub.add_parser("profile-attention")
     pa.add_argument("--out", required=True)
     pa.add_argument("--launches", type=int, default=10)
     pa.add_argument("--table-only", action="store_true")
+    pa.add_argument("--operators", default="operators", choices=sorted(OPERATORS))
     pa.set_defaults(fn=cmd_profile_attention)
     ck = sub.add_parser("clocks")
     ck.add_argument("--workload", default="cfg2_4096")
