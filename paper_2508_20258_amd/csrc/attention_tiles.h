@@ -179,6 +179,12 @@ struct RowLoader {
   }
 };
 
+// As load_to_lds_base_off, for what is read once: the caches do not keep it.
+__device__ __forceinline__ void stream_to_lds(const void* base, uint32_t off, uint32_t lds_base) {
+  const uint32_t lds_addr = __builtin_amdgcn_readfirstlane(lds_base);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" : : "s"(lds_addr), "v"(off), "s"(base) : "memory", "m0");
+}
+
 // 4 bytes a lane, global -> LDS at lds + lane * 4 (load_to_lds has 16).
 __device__ __forceinline__ void load_word_to_lds(const void* gptr, uint32_t lds_base) {
   const uint32_t lds_addr = __builtin_amdgcn_readfirstlane(lds_base);

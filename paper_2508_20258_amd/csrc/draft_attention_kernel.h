@@ -2,10 +2,11 @@
 // that a mask of 64 bits names, or (no masks) at those up to its own.
 //
 // The query heads of a key head look at the same keys, so a row is a token of one query head and the rows of a block are n * group.  Scores come as S^T = k q^T and out^T += v^T P^T, as for prompts
-// (attention_tiles.h): a lane has 32 scores of one row.  Two kernels, by the rows of a tile:
-// 32 or 64 (draft_attention_kernel): the four waves of a workgroup take every fourth tile of 64 keys each, for all the rows.  A wave has a tile of keys and one of values in LDS for itself and waits for nothing but
-// its own loads, the next keys being fetched when the scores are done and the next values when those are used up; the four join what they have in LDS.
-// 128 (draft_attention_wide_kernel): the waves have 32 rows each and share tiles, two of each, as for prompts: the scores of the next tile beside the weights and values of this one.
+// (attention_tiles.h).  A step over the keys is a tile of 64.  Two kernels, by the rows of a tile:
+// 32 (draft_attention_kernel): the four waves of a workgroup take every fourth tile of keys each.  A wave has a tile of keys and one of values in LDS for itself and waits for nothing but its own loads, the next
+// keys being fetched when the scores are done and the next values when those are used up; the four join what they have in LDS.
+// 64 or 128 (draft_attention_wide_kernel): the waves have 32 rows each, or 32 rows and half of the keys, and share tiles, two of each: the scores of the next tile beside the weights and values of this one, in
+// slots of one product, as for prompts (attention_kernel.h).
 //
 // The steps of all tiles of rows, in the sequences' order, are dealt evenly to the workgroups that a key head has, whatever the lengths: of `shares`, workgroup i has steps total * i / shares and up.  What it has
 // of a tile of rows goes to `out` where that is all of it, else into one of two places of its own (the first it works on, or the last), and draft_join_kernel joins them.
@@ -30,13 +31,12 @@ struct DraftArgs {
   float scale;
 };
 
-constexpr int kDraftKeys = 64, kDraftWaves = 4;
+constexpr int kDraftKeys = 64, kDraftWaves = 4;        // keys of a tile; waves of a workgroup
 
-// ROWS: 32 and 64, or 128 for the kernel whose waves share tiles.
 template <int D, int ROWS>
 struct DraftShape {
-  static constexpr bool kWide = ROWS == 128;
-  static constexpr int kStep = kDraftKeys * (kWide ? 1 : kDraftWaves);
+  static constexpr bool kWide = ROWS > 32;
+  static constexpr int kStep = kDraftKeys * (kWide ? 1 : kDraftWaves);       // keys that the workgroup takes at a time
   static constexpr int kTileBytes = kDraftKeys * 2 * D, kLdsBytes = 4 * kTileBytes * (kWide ? 1 : 2);
   static constexpr int kJoinPitch = D + 4;                  // floats of a row in LDS when waves join
   static constexpr int kPerCu = kWide || D == 64 ? 2 : 1;   // workgroups of a compute unit
@@ -93,8 +93,9 @@ __device__ __forceinline__ uint64_t shift_up(uint64_t x, int by) { return by >= 
 
 __device__ const u32x4 kNanChunk = {0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
 
-// 64 positions of a head from their pages into LDS, 16 rows at a time (a page has 16 or more): those past the length are zeros, those without a page NaN.
-template <int D>
+// Positions of a head from their pages into LDS, 16 rows at a time (a page has 16 or more): those from `length` on are zeros, those without a page NaN.
+// STREAM: they are read once.
+template <int D, bool STREAM>
 struct PageLoader {
   static constexpr int kChunks = D / 8, kRows = 64 / kChunks, kLoads = 16 / kRows;          // of 16 rows
   const PageTable& c;
@@ -105,22 +106,26 @@ struct PageLoader {
     const int r = lane / kChunks;
     lane_part = (uint32_t)(r * 2 * D) + (uint32_t)(((lane % kChunks) ^ tile_key<D>(r)) << 4);
   }
-  // position: of the first of 16, less than 2^31; page: theirs
-  __device__ __forceinline__ void operator()(const uint16_t* pages, int64_t position, int page, uint32_t lds) const {
-    const uint16_t* base = pages + c.token_at(max(page, 0), k_head, (int)position) * D;
-    if (page >= 0 && position + 16 <= length) {
-      const uint64_t at = reinterpret_cast<uint64_t>(base);
+  // Where 16 positions are: elements from the start of the pages, -1 where they have no page.
+  __device__ __forceinline__ int64_t place(int64_t position, int page) const { return page < 0 ? -1 : c.token_at(page, k_head, (int)position) * D; }
+  __device__ __forceinline__ void operator()(const uint16_t* pages, int64_t position, int64_t place, uint32_t lds) const {
+    if (place >= 0 && position + 16 <= length) {
+      const uint64_t at = reinterpret_cast<uint64_t>(pages + place);
       const uint64_t uniform = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)at);
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) load_to_lds_base_off(reinterpret_cast<const void*>(uniform), (uint32_t)(i * kRows * 2 * D) + (lane_part ^ key_of(i)), lds + (uint32_t)(i * 1024));
+      for (int i = 0; i < kLoads; ++i) {
+        const uint32_t off = (uint32_t)(i * kRows * 2 * D) + (lane_part ^ key_of(i)), to = lds + (uint32_t)(i * 1024);
+        if constexpr (STREAM) stream_to_lds(reinterpret_cast<const void*>(uniform), off, to);
+        else load_to_lds_base_off(reinterpret_cast<const void*>(uniform), off, to);
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         uint32_t l = (uint32_t)lane;
         keep(l);                     // or what this needs, once or twice for a sequence, has registers all along
         const int r = i * kRows + (int)l / kChunks;
-        const unsigned char* at = reinterpret_cast<const unsigned char*>(base) + (uint32_t)(r * 2 * D) + ((l % kChunks ^ (uint32_t)tile_key<D>(r)) << 4);
-        if (page < 0) at = reinterpret_cast<const unsigned char*>(&kNanChunk);
+        const unsigned char* at = reinterpret_cast<const unsigned char*>(pages + max(place, (int64_t)0)) + (uint32_t)(r * 2 * D) + ((l % kChunks ^ (uint32_t)tile_key<D>(r)) << 4);
+        if (place < 0) at = reinterpret_cast<const unsigned char*>(&kNanChunk);
         if (position + r >= length) at = reinterpret_cast<const unsigned char*>(&kZeroChunk);
         load_to_lds(at, lds + (uint32_t)(i * 1024));
       }
@@ -129,15 +134,15 @@ struct PageLoader {
   static __device__ __forceinline__ uint32_t key_of(int i) { return (uint32_t)(tile_key<D>(i * kRows) << 4); }
 };
 
-// The positions of a tile of which a value is no finite number.
-template <int D>
+// Of 32 NB positions, those of which a value is no finite number.
+template <int D, int NB>
 __device__ __forceinline__ uint64_t odd_positions(const unsigned char* tile, int lane) {
   constexpr int kChunks = D / 8, kRows = 64 / kChunks;
   uint32_t l = (uint32_t)lane;
   keep(l);
   uint64_t odd = 0;
 #pragma unroll 1
-  for (int i = 0; i < kDraftKeys / kRows; ++i) {
+  for (int i = 0; i < 32 * NB / kRows; ++i) {
     const u32x4 x = *reinterpret_cast<const u32x4*>(tile + i * 1024 + l * 16);
     bool mine = false;
 #pragma unroll
@@ -150,11 +155,11 @@ __device__ __forceinline__ uint64_t odd_positions(const unsigned char* tile, int
   return odd;
 }
 
-// o += p x for a tile that rows look at in part.  A product carries 0 times an infinity into rows that do not look at it: positions with values that are no finite numbers are left out of it, and then
-// taken one at a time, by a product of their own that only the rows keep that look at them.
-template <int D>
-__device__ __forceinline__ void add_seen(f32x16 (&o)[D / 32], const u32x4 (&p)[4], const unsigned char* tile, uint32_t lds, uint64_t seen, int lane) {
-  const uint64_t odd = odd_positions<D>(tile, lane);
+// o += p x for 32 NB positions that rows look at in part.  A product carries 0 times an infinity into rows that do not look at it: positions with values that are no finite numbers are left out of it, and
+// then taken one at a time, by a product of their own that only the rows keep that look at them.
+template <int D, int NB>
+__device__ __forceinline__ void add_seen(f32x16 (&o)[D / 32], const u32x4 (&p)[2 * NB], const unsigned char* tile, uint32_t lds, uint64_t seen, int lane) {
+  const uint64_t odd = odd_positions<D, NB>(tile, lane);
   uint32_t l = (uint32_t)lane;
   keep(l);
   const uint32_t column = column_address<D>(lds, (int)l);
@@ -170,7 +175,7 @@ __device__ __forceinline__ void add_seen(f32x16 (&o)[D / 32], const u32x4 (&p)[4
     return __builtin_bit_cast(bf16x8, w);
   };
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
+  for (int k = 0; k < 2 * NB; ++k)
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
       o[i] = mfma32(only(read_columns<D>(column, k, i), (uint32_t)(~odd >> (16 * k)) & 0xffffu), __builtin_bit_cast(bf16x8, p[k]), o[i]);
@@ -182,7 +187,9 @@ __device__ __forceinline__ void add_seen(f32x16 (&o)[D / 32], const u32x4 (&p)[4
     const bool looks = seen >> at & 1;
     u32x4 w = p[0];
 #pragma unroll
-    for (int e = 1; e < 4; ++e) w = k == e ? p[e] : w;
+    for (int j = 1; j < 2 * NB; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = k == j ? p[j][e] : w[e];
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
       const f32x16 with = mfma32(only(read_columns<D>(column + (uint32_t)(k * 32 * D), 0, i), 1u << (at & 15)), __builtin_bit_cast(bf16x8, w), o[i]);
@@ -234,17 +241,16 @@ struct DraftSums {
     for (int i = 0; i < D / 32; ++i) o[i] *= less;
     top = now;
   }
-  // Scores of a tile to weights, rounded for the product.
-  __device__ __forceinline__ void weigh(f32x16 (&x)[2], float c, u32x4 (&p)[4]) {
-    float high = x[0][0];
+  // Scores of 32 NB positions to weights, rounded for the product.
+  template <int NB>
+  __device__ __forceinline__ void weigh(f32x16 (&x)[NB], float c, u32x4 (&p)[2 * NB]) {
+    float high[2] = {x[0][0], x[0][1]};
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) high = fmaxf(high, x[b][r]);
-    raise(high, c);
+    for (int r = 2; r < 16 * NB; ++r) high[r % 2] = fmaxf(high[r % 2], x[r / 16][r % 16]);
+    raise(fmaxf(high[0], high[1]), c);
     float sums[2] = {sum, 0.f};
 #pragma unroll
-    for (int m = 0; m < 16; ++m) {
+    for (int m = 0; m < 8 * NB; ++m) {
       const float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[m / 8][m % 8 * 2], c, -top)), w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[m / 8][m % 8 * 2 + 1], c, -top));
       sums[0] += w0;
       sums[1] += w1;
@@ -254,10 +260,11 @@ struct DraftSums {
   }
 };
 // Scores of positions that a row does not look at.
-__device__ __forceinline__ void hide(f32x16 (&x)[2], uint64_t seen, int h) {
+template <int NB>
+__device__ __forceinline__ void hide(f32x16 (&x)[NB], uint64_t seen, int h) {
   const uint64_t mine = seen >> (4 * h);
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
+  for (int b = 0; b < NB; ++b) {
     const uint32_t bits = (uint32_t)(mine >> (32 * b));
 #pragma unroll
     for (int r = 0; r < 16; ++r) x[b][r] = bits & (1u << (8 * (r / 4) + r % 4)) ? x[b][r] : -INFINITY;
@@ -278,7 +285,7 @@ struct PagesAhead {
   __device__ __forceinline__ void advance(int tile) {        // to `tile`, the one after that of `entry`
     if (++entry == 64 >> bits) look_up(tile);
   }
-  // Of position `place` of a tile, `ahead` tiles after that of `entry`.
+  // Of position `place` of the tile.
   __device__ __forceinline__ int operator()(int place) const { return __builtin_amdgcn_readlane(pages, (entry << bits) + (place >> c.page_shift)); }
 };
 
@@ -364,12 +371,13 @@ __device__ __forceinline__ void deal(const DraftArgs& a, int share, int k_head, 
   }
 }
 
-template <int D, int ROWS>
-__global__ void __launch_bounds__(64 * kDraftWaves, (DraftShape<D, ROWS>::kPerCu)) draft_attention_kernel(DraftArgs a) {
+template <int D>
+__global__ void __launch_bounds__(64 * kDraftWaves, (DraftShape<D, 32>::kPerCu)) draft_attention_kernel(DraftArgs a) {
+  constexpr int ROWS = 32;
   using S = DraftShape<D, ROWS>;
-  constexpr int kParts = D / 32, kSteps = D / 16, kTileLoads = S::kTileBytes / 1024, kBlocks = ROWS / 32;
+  constexpr int kParts = D / 32, kSteps = D / 16, kTileLoads = S::kTileBytes / 1024;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[S::kLdsBytes];
-  __shared__ float wave_stats[kDraftWaves][32][2];
+  __shared__ float wave_stats[kDraftWaves][ROWS][2];
   const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   unsigned char *const k_tile = smem + 2 * wave * S::kTileBytes, *const v_tile = k_tile + S::kTileBytes;
   const uint32_t k_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)k_tile, v_lds = k_lds + (uint32_t)S::kTileBytes;
@@ -378,82 +386,72 @@ __global__ void __launch_bounds__(64 * kDraftWaves, (DraftShape<D, ROWS>::kPerCu
 
   deal<D, ROWS>(a, share, k_head, group, [&](const DraftItem& item, int from, int to, int all, int place) {
     const int rows = item.tokens.length * group, first_row = item.tile * ROWS;
-    bf16x8 qf[kBlocks][kSteps];
-    DraftSums<D> sums[kBlocks];
-#pragma unroll
-    for (int i = 0; i < kBlocks; ++i) {
-      const DraftRows r(a, item, first_row + 32 * i + (lane & 31), k_head, group);
-      load_fragments<D>(qf[i], a.q.at(item.tokens.first + r.token, r.head), lane);
-      sums[i].clear();
-    }
     const int end = min(to * kDraftWaves, (item.length + kDraftKeys - 1) / kDraftKeys);
-    const int whole = min(item.length - item.tokens.length, item.length) / kDraftKeys;      // tiles that all rows look at whole (none where the block is longer than the sequence)
+    const int whole = min(min(item.length - item.tokens.length, item.length) / kDraftKeys, end);      // tiles that all rows look at whole (none where the block is longer than the sequence)
     int t = from * kDraftWaves + wave;
-    const PageLoader<D> loader(a.c, k_head, item.length, lane);
+    const PageLoader<D, true> loader(a.c, k_head, item.length, lane);
     PagesAhead<kDraftWaves> pages(a.c, item, lane);
+    int64_t places[4];
     auto fetch = [&](const uint16_t* from_pages, int tile, uint32_t lds) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) loader(from_pages, (int64_t)tile * kDraftKeys + 16 * i, pages(16 * i), lds + (uint32_t)(16 * i * 2 * D));
+      for (int i = 0; i < 4; ++i) loader(from_pages, (int64_t)tile * kDraftKeys + 16 * i, places[i], lds + (uint32_t)(16 * i * 2 * D));
+    };
+    auto fetch_keys = [&](int tile) {                        // and note where the values are
+#pragma unroll
+      for (int i = 0; i < 4; ++i) places[i] = loader.place((int64_t)tile * kDraftKeys + 16 * i, pages(16 * i));
+      fetch(a.k_pages, tile, k_lds);
     };
     if (t < end) {
       pages.look_up(t);
-      fetch(a.k_pages, t, k_lds);
+      fetch_keys(t);
       fetch(a.v_pages, t, v_lds);
     }
+    const DraftRows row(a, item, first_row + (lane & 31), k_head, group);
+    bf16x8 qf[kSteps];
+    load_fragments<D>(qf, a.q.at(item.tokens.first + row.token, row.head), lane);
+    DraftSums<D> sums;
+    sums.clear();
     auto take = [&](auto is_masked) __attribute__((always_inline)) {
       constexpr bool masked = decltype(is_masked)::value;
       const int then = t + kDraftWaves;
       const bool more = then < end;
-      f32x16 x[kBlocks][2];
-      u32x4 p[kBlocks][4];
+      f32x16 x[2];
+      u32x4 p[4];
       __builtin_amdgcn_sched_barrier(0);
       wait_vmcnt<kTileLoads>();                              // the keys have landed, the values may be on their way
       __builtin_amdgcn_sched_barrier(0);
       const uint32_t k_lane = row_address<D>(k_lds, lane);
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
+        x[b] = f32x16{};
 #pragma unroll
-        for (int j = 0; j < kBlocks; ++j) x[j][b] = f32x16{};
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-          const bf16x8 f = read_rows<D>(k_lane, b, i);
-#pragma unroll
-          for (int j = 0; j < kBlocks; ++j) x[j][b] = mfma32(f, qf[j][i], x[j][b]);
-        }
+        for (int i = 0; i < kSteps; ++i) x[b] = mfma32(read_rows<D>(k_lane, b, i), qf[i], x[b]);
       }
       __builtin_amdgcn_sched_barrier(0);
       wait_vmcnt_lgkmcnt<63, 0>();
       __builtin_amdgcn_sched_barrier(0);
       if (more) {
         pages.advance(then);
-        fetch(a.k_pages, then, k_lds);
+        fetch_keys(then);
       }
-      uint64_t seen[kBlocks];
-#pragma unroll
-      for (int j = 0; j < kBlocks; ++j) {
-        if constexpr (masked) {
-          seen[j] = DraftRows(a, item, first_row + 32 * j + (lane & 31), k_head, group).seen(a, item, t);
-          hide(x[j], seen[j], h);
-        }
-        sums[j].weigh(x[j], c, p[j]);
+      uint64_t seen = 0;
+      if constexpr (masked) {
+        seen = row.seen(a, item, t);
+        hide(x, seen, h);
       }
+      sums.weigh(x, c, p);
       __builtin_amdgcn_sched_barrier(0);
       if (more) wait_vmcnt<kTileLoads>();
       else wait_vmcnt<0>();
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (masked) {
-#pragma unroll
-        for (int j = 0; j < kBlocks; ++j) add_seen<D>(sums[j].o, p[j], v_tile, v_lds, seen[j], lane);
+        add_seen<D, 2>(sums.o, p, v_tile, v_lds, seen, lane);
       } else {
         const uint32_t v_lane = column_address<D>(v_lds, lane);
 #pragma unroll
         for (int k = 0; k < 4; ++k)
 #pragma unroll
-          for (int i = 0; i < kParts; ++i) {
-            const bf16x8 f = read_columns<D>(v_lane, k, i);
-#pragma unroll
-            for (int j = 0; j < kBlocks; ++j) sums[j].o[i] = mfma32(f, __builtin_bit_cast(bf16x8, p[j][k]), sums[j].o[i]);
-          }
+          for (int i = 0; i < kParts; ++i) sums.o[i] = mfma32(read_columns<D>(v_lane, k, i), __builtin_bit_cast(bf16x8, p[k]), sums.o[i]);
       }
       __builtin_amdgcn_sched_barrier(0);
       wait_vmcnt_lgkmcnt<63, 0>();
@@ -461,223 +459,314 @@ __global__ void __launch_bounds__(64 * kDraftWaves, (DraftShape<D, ROWS>::kPerCu
       if (more) fetch(a.v_pages, then, v_lds);
       t = then;
     };
-    while (t < min(whole, end)) take(std::false_type{});
+    while (t < whole) take(std::false_type{});
     while (t < end) take(std::true_type{});
 
-    // 32 rows at a time: every wave's into its own tiles, then a row by 8 threads
-    const bool entire = from == 0 && to == all;
+    // every wave's sums into its own tiles, then a row by 8 threads
+    const float sum = across_halves(sums.sum, [](float y, float z) { return y + z; });
+    float* mine = reinterpret_cast<float*>(k_tile) + (lane & 31) * S::kJoinPitch;
 #pragma unroll
-    for (int j = 0; j < kBlocks; ++j) {
-      const float sum = across_halves(sums[j].sum, [](float y, float z) { return y + z; });
-      float* mine = reinterpret_cast<float*>(k_tile) + (lane & 31) * S::kJoinPitch;
+    for (int i = 0; i < kParts; ++i)
 #pragma unroll
-      for (int i = 0; i < kParts; ++i)
+      for (int r = 0; r < 16; r += 4) *reinterpret_cast<f32x4*>(mine + 32 * i + 2 * r + 4 * h) = f32x4{sums.o[i][r], sums.o[i][r + 1], sums.o[i][r + 2], sums.o[i][r + 3]};
+    if (h == 0) wave_stats[wave][lane & 31][0] = sums.top, wave_stats[wave][lane & 31][1] = sum;
+    __syncthreads();
+    const int r = (int)threadIdx.x / 8, d = (int)threadIdx.x % 8 * (D / 8), its = first_row + r;
+    if (its < rows) {
+      float factor[kDraftWaves], high = -FLT_MAX, total = 0.f;
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) *reinterpret_cast<f32x4*>(mine + 32 * i + 2 * r + 4 * h) = f32x4{sums[j].o[i][r], sums[j].o[i][r + 1], sums[j].o[i][r + 2], sums[j].o[i][r + 3]};
-      if (h == 0) wave_stats[wave][lane & 31][0] = sums[j].top, wave_stats[wave][lane & 31][1] = sum;
-      __syncthreads();
-      const int r = (int)threadIdx.x / 8, d = (int)threadIdx.x % 8 * (D / 8), its = first_row + 32 * j + r;
-      if (its < rows) {
-        float factor[kDraftWaves], high = -FLT_MAX, total = 0.f;
+      for (int w = 0; w < kDraftWaves; ++w) high = fmaxf(high, wave_stats[w][r][0]);
 #pragma unroll
-        for (int w = 0; w < kDraftWaves; ++w) high = fmaxf(high, wave_stats[w][r][0]);
-#pragma unroll
-        for (int w = 0; w < kDraftWaves; ++w) {
-          factor[w] = __builtin_amdgcn_exp2f(wave_stats[w][r][0] - high);
-          total = __builtin_fmaf(wave_stats[w][r][1], factor[w], total);
-        }
-        const float f = !entire ? 1.f : total == 0.f ? 0.f : 1.f / total;
-        float y[D / 8];
-#pragma unroll
-        for (int e = 0; e < D / 8; ++e) {
-          y[e] = 0.f;
-#pragma unroll
-          for (int w = 0; w < kDraftWaves; ++w) y[e] = __builtin_fmaf(reinterpret_cast<const float*>(smem + 2 * w * S::kTileBytes)[r * S::kJoinPitch + d + e], factor[w], y[e]);
-          y[e] *= f;
-        }
-        if (entire) {
-          uint16_t* to_row = a.out.at(item.tokens.first + its / group, k_head * group + its % group) + d;
-#pragma unroll
-          for (int e = 0; e < D / 8; e += 8) {
-            float z[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] = y[e + i];
-            *reinterpret_cast<u32x4*>(to_row + e) = pack8(z);
-          }
-        } else {
-          const int64_t at = (int64_t)place * ROWS + 32 * j + r;
-#pragma unroll
-          for (int e = 0; e < D / 8; e += 4) *reinterpret_cast<f32x4*>(a.sums + at * D + d + e) = f32x4{y[e], y[e + 1], y[e + 2], y[e + 3]};
-          if (d == 0) *reinterpret_cast<float2*>(a.stats + 2 * at) = float2{high, total};
-        }
+      for (int w = 0; w < kDraftWaves; ++w) {
+        factor[w] = __builtin_amdgcn_exp2f(wave_stats[w][r][0] - high);
+        total = __builtin_fmaf(wave_stats[w][r][1], factor[w], total);
       }
-      __syncthreads();
+      const bool entire = from == 0 && to == all;
+      const float f = !entire ? 1.f : total == 0.f ? 0.f : 1.f / total;
+      float y[D / 8];
+#pragma unroll
+      for (int e = 0; e < D / 8; ++e) {
+        y[e] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kDraftWaves; ++w) y[e] = __builtin_fmaf(reinterpret_cast<const float*>(smem + 2 * w * S::kTileBytes)[r * S::kJoinPitch + d + e], factor[w], y[e]);
+        y[e] *= f;
+      }
+      if (entire) {
+        uint16_t* to_row = a.out.at(item.tokens.first + its / group, k_head * group + its % group) + d;
+#pragma unroll
+        for (int e = 0; e < D / 8; e += 8) {
+          float z[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) z[i] = y[e + i];
+          *reinterpret_cast<u32x4*>(to_row + e) = pack8(z);
+        }
+      } else {
+        const int64_t at = (int64_t)place * ROWS + r;
+#pragma unroll
+        for (int e = 0; e < D / 8; e += 4) *reinterpret_cast<f32x4*>(a.sums + at * D + d + e) = f32x4{y[e], y[e + 1], y[e + 2], y[e + 3]};
+        if (d == 0) *reinterpret_cast<float2*>(a.stats + 2 * at) = float2{high, total};
+      }
     }
+    __syncthreads();
   });
 }
 
-template <int D>
+// Pairs of weights taken before a slot, if all `pairs` of them are by slot `last`.
+constexpr int pairs_before(int slot, int pairs, int last) { return slot >= last ? pairs : (slot * pairs + last - 1) / last; }
+
+// STREAM: most blocks are one tile of rows, so that keys and values are read once.
+template <int D, int ROWS, bool STREAM>
 __global__ void __launch_bounds__(64 * kDraftWaves, 2) draft_attention_wide_kernel(DraftArgs a) {
-  constexpr int ROWS = 128;
   using S = DraftShape<D, ROWS>;
-  constexpr int kParts = D / 32, kSteps = D / 16;
+  constexpr int kParts = D / 32, kSteps = D / 16, kBlocks = ROWS / 64, kRowWaves = ROWS / 32;     // a wave has 32 kBlocks of a tile's keys
   __shared__ __attribute__((aligned(1024))) unsigned char smem[S::kLdsBytes];
-  const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
+  const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), row_wave = wave % kRowWaves, part = wave / kRowWaves;
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem, mine = (uint32_t)(part * 64 * D);      // of a tile: the wave's keys
   const int heads = a.c.k_heads, group = a.q_heads / heads, share = (int)blockIdx.x / heads, k_head = (int)blockIdx.x - share * heads;
   const float c = a.scale * kLog2E;
 
   deal<D, ROWS>(a, share, k_head, group, [&](const DraftItem& item, int from, int to, int all, int place) {
-    const DraftRows row(a, item, item.tile * ROWS + wave * 32 + (lane & 31), k_head, group);
+    const int whole = min(min(item.length - item.tokens.length, item.length) / kDraftKeys, to);
+    const PageLoader<D, STREAM> loader(a.c, k_head, item.length, lane);
+    PagesAhead<1> pages(a.c, item, lane);
+    // The keys of tile t are in slot (t - from) & 1, the values in 2 + that; a wave fetches a quarter of a tile.  Keys are fetched two tiles ahead, values one, from the places that the keys had.
+    int64_t key_place = 0, value_place = 0;
+    auto fetch_k = [&](int t) {
+      value_place = key_place;
+      key_place = loader.place((int64_t)t * kDraftKeys + 16 * wave, pages(16 * wave));
+      pages.advance(t + 1);
+      loader(a.k_pages, (int64_t)t * kDraftKeys + 16 * wave, key_place, lds + (uint32_t)(((t - from) & 1) * S::kTileBytes + 16 * wave * 2 * D));
+    };
+    auto fetch_v = [&](int t, int64_t at) { loader(a.v_pages, (int64_t)t * kDraftKeys + 16 * wave, at, lds + (uint32_t)((2 + ((t - from) & 1)) * S::kTileBytes + 16 * wave * 2 * D)); };
+    pages.look_up(from);
+    fetch_k(from);
+    fetch_v(from, key_place);
+    if (from + 1 < to) fetch_k(from + 1);
+    auto turn = [&](int t) __attribute__((always_inline)) {
+      publish();
+      if (t + 2 < to) {
+        fetch_k(t + 2);
+        fetch_v(t + 1, value_place);
+      } else if (t + 1 < to) {
+        fetch_v(t + 1, key_place);
+      }
+    };
+    const DraftRows row(a, item, item.tile * ROWS + row_wave * 32 + (lane & 31), k_head, group);
     bf16x8 qf[kSteps];
     load_fragments<D>(qf, a.q.at(item.tokens.first + row.token, row.head), lane);
     DraftSums<D> sums;
     sums.clear();
-    const int whole = min(item.length - item.tokens.length, item.length) / kDraftKeys;
-    const PageLoader<D> loader(a.c, k_head, item.length, lane);
-    PagesAhead<1> k_page(a.c, item, lane), v_page(a.c, item, lane);
-    // this wave's quarter of a tile
-    auto fetch = [&](const uint16_t* from_pages, const PagesAhead<1>& pages, int tile, int slot) {
-      loader(from_pages, (int64_t)tile * kDraftKeys + 16 * wave, pages(16 * wave), lds + (uint32_t)(slot * S::kTileBytes + 16 * wave * 2 * D));
-    };
-    auto fetch_k = [&](int t) { fetch(a.k_pages, k_page, t, (t - from) & 1); };
-    auto fetch_v = [&](int t) { fetch(a.v_pages, v_page, t, 2 + ((t - from) & 1)); };
-    // keys of a tile are fetched two tiles ahead, values one
-    k_page.look_up(from);
-    v_page.look_up(from);
-    fetch_k(from);
-    fetch_v(from);
-    if (from + 1 < to) {
-      k_page.advance(from + 1);
-      fetch_k(from + 1);
-    }
-    auto turn = [&](int t) {
-      publish();
-      if (t + 2 < to) {
-        k_page.advance(t + 2);
-        fetch_k(t + 2);
-      }
-      if (t + 1 < to) {
-        v_page.advance(t + 1);
-        fetch_v(t + 1);
-      }
-    };
-    f32x16 x[2];
+    f32x16 x[kBlocks], other[kBlocks];
     auto score = [&](int t) __attribute__((always_inline)) {
-      const uint32_t k_lane = row_address<D>(lds + (uint32_t)(((t - from) & 1) * S::kTileBytes), lane);
+      const uint32_t k_lane = row_address<D>(lds + mine + (uint32_t)(((t - from) & 1) * S::kTileBytes), lane);
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
+      for (int b = 0; b < kBlocks; ++b) {
         x[b] = f32x16{};
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) x[b] = mfma32(read_rows<D>(k_lane, b, i), qf[i], x[b]);
       }
     };
-    publish();
-    score(from);
+    // One tile that all rows look at whole, and the scores of the next one, another such: kSlots products with the vector unit's share of the work in each, in a fixed order.  The weights come in pairs, all of them by
+    // slot kLast, so that each is there before the products that take it.
+    constexpr int kScoreSlots = kBlocks * kSteps, kSlots = kScoreSlots + 2 * kBlocks * kParts, kPairs = 8 * kBlocks, kLast = kBlocks == 2 ? kSlots * 7 / 8 : kSlots * 3 / 4;
+    uint32_t k_at[kSteps], v_at[kParts][2];
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) keep(k_at[i] = row_address<D>(lds + mine, lane) ^ (uint32_t)(i << 5));
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+      keep(v_at[i][0] = column_address<D>(lds + mine, lane) ^ (uint32_t)(i << 6));
+      keep(v_at[i][1] = (column_address<D>(lds + mine, lane) ^ (uint32_t)(i << 6) ^ 32u) + 16u * D);
+    }
+    auto tile_pass = [&](f32x16 (&now)[kBlocks], f32x16 (&then)[kBlocks], auto parity) __attribute__((always_inline)) {
+      constexpr int PARITY = decltype(parity)::value;
+      constexpr uint32_t kKeysAt = (uint32_t)((PARITY ? 0 : 1) * S::kTileBytes), kValuesAt = (uint32_t)((2 + PARITY) * S::kTileBytes);
+      auto read = [&](auto slot) __attribute__((always_inline)) {
+        constexpr int i = decltype(slot)::value, v = i - kScoreSlots;
+        if constexpr (i < kScoreSlots) return read_rows_at<D>(k_at[i % kSteps], kKeysAt + (uint32_t)(i / kSteps * 64 * D));
+        else return read_columns_at<D>(v_at[v % kParts][0], v_at[v % kParts][1], kValuesAt + (uint32_t)(v / kParts * 32 * D));
+      };
+      u32x4 p[2 * kBlocks];
+      constexpr int kAhead = 2, kRing = kAhead + 1;          // reads on their way
+      bf16x8 f[kRing];
+      for_each_index([&](auto slot) __attribute__((always_inline)) { f[decltype(slot)::value] = read(slot); }, std::make_integer_sequence<int, kAhead>{});
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) then[b] = f32x16{};
+      float weights[2] = {sums.sum, 0.f}, high[2] = {-INFINITY, -INFINITY};
+      now[0][0] = __builtin_fmaf(now[0][0], c, -sums.top);
+      now[0][1] = __builtin_fmaf(now[0][1], c, -sums.top);
+      __builtin_amdgcn_sched_barrier(0);
+      for_each_index([&](auto slot) __attribute__((always_inline)) {
+        constexpr int i = decltype(slot)::value, v = i - kScoreSlots;
+        if constexpr (i + kAhead < kSlots) f[(i + kAhead) % kRing] = read(std::integral_constant<int, i + kAhead>{});
+        if constexpr (i < kScoreSlots) then[i / kSteps] = mfma32(f[i % kRing], qf[i % kSteps], then[i / kSteps]);
+        else sums.o[v % kParts] = mfma32(f[i % kRing], __builtin_bit_cast(bf16x8, p[v / kParts]), sums.o[v % kParts]);
+        constexpr int kTaken = pairs_before(i, kPairs, kLast), kThen = pairs_before(i + 1, kPairs, kLast);
+        static_assert(i < kScoreSlots || kTaken >= (v / kParts + 1) * 4, "weights are there before they are used");
+#pragma unroll
+        for (int n = kTaken; n < kThen; ++n) {
+          const int b = n / 8, r = n % 8 * 2, m = n + 1;
+          if (m < kPairs) {
+            now[m / 8][m % 8 * 2] = __builtin_fmaf(now[m / 8][m % 8 * 2], c, -sums.top);
+            now[m / 8][m % 8 * 2 + 1] = __builtin_fmaf(now[m / 8][m % 8 * 2 + 1], c, -sums.top);
+          }
+          const float w0 = __builtin_amdgcn_exp2f(now[b][r]), w1 = __builtin_amdgcn_exp2f(now[b][r + 1]);
+          weights[0] += w0;
+          weights[1] += w1;
+          p[n / 4][n % 4] = pack_bf16(w0, w1);
+        }
+        if constexpr (i >= kScoreSlots) {
+          constexpr int kValueSlots = kSlots - kScoreSlots;
+#pragma unroll
+          for (int e = v * 16 * kBlocks / kValueSlots; e < (v + 1) * 16 * kBlocks / kValueSlots; e += 2)
+            high[e / 2 % 2] = __builtin_elementwise_maximum(high[e / 2 % 2], __builtin_elementwise_maximum(then[e / 16][e % 16], then[e / 16][e % 16 + 1]));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }, std::make_integer_sequence<int, kSlots>{});
+      sums.sum = weights[0] + weights[1];
+      sums.raise(fmaxf(high[0], high[1]), c);
+    };
+    // A tile after the other, the scores of tile t being there.
     auto take = [&](int t, auto is_masked) __attribute__((always_inline)) {
       constexpr bool masked = decltype(is_masked)::value;
       turn(t);
-      uint64_t seen = 0;
+      const uint32_t values = mine + (uint32_t)((2 + ((t - from) & 1)) * S::kTileBytes);
+      u32x4 p[2 * kBlocks];
       if constexpr (masked) {
-        seen = row.seen(a, item, t);
+        const uint64_t seen = row.seen(a, item, t) >> (32 * part) & (~0ull >> (64 - 32 * kBlocks));
         hide(x, seen, h);
-      }
-      if (!masked || __any(seen != 0)) {
-        u32x4 p[4];
-        sums.weigh(x, c, p);
-        const int slot = 2 + ((t - from) & 1);
-        if constexpr (masked) {
-          add_seen<D>(sums.o, p, smem + slot * S::kTileBytes, lds + (uint32_t)(slot * S::kTileBytes), seen, lane);
-        } else {
-          const uint32_t v_lane = column_address<D>(lds + (uint32_t)(slot * S::kTileBytes), lane);
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-#pragma unroll
-            for (int i = 0; i < kParts; ++i) sums.o[i] = mfma32(read_columns<D>(v_lane, k, i), __builtin_bit_cast(bf16x8, p[k]), sums.o[i]);
+        if (__any(seen != 0)) {
+          sums.weigh(x, c, p);
+          add_seen<D, kBlocks>(sums.o, p, smem + values, lds + values, seen, lane);
         }
+      } else {
+        sums.weigh(x, c, p);
+        const uint32_t v_lane = column_address<D>(lds + values, lane);
+#pragma unroll
+        for (int k = 0; k < 2 * kBlocks; ++k)
+#pragma unroll
+          for (int i = 0; i < kParts; ++i) sums.o[i] = mfma32(read_columns<D>(v_lane, k, i), __builtin_bit_cast(bf16x8, p[k]), sums.o[i]);
       }
       if (t + 1 < to) score(t + 1);
     };
+    publish();
+    score(from);
     int t = from;
-    for (; t < min(whole, to); ++t) take(t, std::false_type{});
+    if (t + 2 < whole) {
+      float high = x[0][0];
+#pragma unroll
+      for (int r = 1; r < 16 * kBlocks; ++r) high = fmaxf(high, x[r / 16][r % 16]);
+      sums.raise(high, c);
+      for (; t + 2 < whole; t += 2) {
+        turn(t);
+        tile_pass(x, other, std::integral_constant<int, 0>{});
+        turn(t + 1);
+        tile_pass(other, x, std::integral_constant<int, 1>{});
+      }
+    }
+    for (; t < whole; ++t) take(t, std::false_type{});
     for (; t < to; ++t) take(t, std::true_type{});
     publish();                                               // the tiles have been read
 
-    const float sum = across_halves(sums.sum, [](float y, float z) { return y + z; });
-    if (from == 0 && to == all) {
-      store_columns<D>(sums.o, sum == 0.f ? 0.f : 1.f / sum, a.out.at(item.tokens.first + row.token, row.head), row.real, lane);
-    } else if (row.real) {
-      const int64_t at = (int64_t)place * ROWS + wave * 32 + (lane & 31);
-      if (h == 0) *reinterpret_cast<float2*>(a.stats + 2 * at) = float2{sums.top, sum};
+    sums.sum = across_halves(sums.sum, [](float y, float z) { return y + z; });
+    if constexpr (kRowWaves < kDraftWaves) {
+      // the other half of the keys
+      float* its = reinterpret_cast<float*>(smem) + (row_wave * 32 + (lane & 31)) * S::kJoinPitch;
+      float* its_stats = reinterpret_cast<float*>(smem) + ROWS * S::kJoinPitch + 2 * (row_wave * 32 + (lane & 31));
+      if (part == 1) {
 #pragma unroll
-      for (int i = 0; i < kParts; ++i)
+        for (int i = 0; i < kParts; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) *reinterpret_cast<f32x4*>(a.sums + at * D + 32 * i + 2 * r + 4 * h) = f32x4{sums.o[i][r], sums.o[i][r + 1], sums.o[i][r + 2], sums.o[i][r + 3]};
+          for (int r = 0; r < 16; r += 4) *reinterpret_cast<f32x4*>(its + 32 * i + 2 * r + 4 * h) = f32x4{sums.o[i][r], sums.o[i][r + 1], sums.o[i][r + 2], sums.o[i][r + 3]};
+        if (h == 0) its_stats[0] = sums.top, its_stats[1] = sums.sum;
+      }
+      __syncthreads();
+      if (part == 0) {
+        const float high = fmaxf(sums.top, its_stats[0]), f = __builtin_amdgcn_exp2f(sums.top - high), g = __builtin_amdgcn_exp2f(its_stats[0] - high);
+        sums.top = high;
+        sums.sum = __builtin_fmaf(its_stats[1], g, sums.sum * f);
+#pragma unroll
+        for (int i = 0; i < kParts; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; r += 4) {
+            const f32x4 y = *reinterpret_cast<const f32x4*>(its + 32 * i + 2 * r + 4 * h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sums.o[i][r + e] = __builtin_fmaf(y[e], g, sums.o[i][r + e] * f);
+          }
+      }
     }
+    if (part == 0) {
+      if (from == 0 && to == all) {
+        store_columns<D>(sums.o, sums.sum == 0.f ? 0.f : 1.f / sums.sum, a.out.at(item.tokens.first + row.token, row.head), row.real, lane);
+      } else if (row.real) {
+        const int64_t at = (int64_t)place * ROWS + row_wave * 32 + (lane & 31);
+        if (h == 0) *reinterpret_cast<float2*>(a.stats + 2 * at) = float2{sums.top, sums.sum};
+#pragma unroll
+        for (int i = 0; i < kParts; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; r += 4) *reinterpret_cast<f32x4*>(a.sums + at * D + 32 * i + 2 * r + 4 * h) = f32x4{sums.o[i][r], sums.o[i][r + 1], sums.o[i][r + 2], sums.o[i][r + 3]};
+      }
+    }
+    if constexpr (kRowWaves < kDraftWaves) __syncthreads();
   });
 }
 
-// What several workgroups have of a row joined, a wave for each token and query head, D / 64 dimensions a lane; and zeros for sequences without positions.
+// What several workgroups have of a tile of rows joined, a workgroup for each 32 of its rows and key head, 8 threads a row; and zeros for sequences without positions.
 template <int D, int ROWS>
 __global__ void __launch_bounds__(256) draft_join_kernel(DraftArgs a) {
-  constexpr int kPer = D / 64;
-  typedef __attribute__((ext_vector_type(kPer))) float vec;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int64_t id = (int64_t)blockIdx.x * 4 + wave;
-  const int token = (int)(id / a.q_heads), head = (int)(id - (int64_t)token * a.q_heads);
-  if (token >= a.total) return;
-  const int heads = a.c.k_heads, group = a.q_heads / heads, k_head = head / group;
+  constexpr int kStep = DraftShape<D, ROWS>::kStep, kPer = D / 8;
+  const int heads = a.c.k_heads, group = a.q_heads / heads, id = (int)blockIdx.x / heads, k_head = (int)blockIdx.x - id * heads, slot = id / (ROWS / 32), block = id - slot * (ROWS / 32);
   int64_t items = 0;
-  int sequence = -1, first_token = 0;
-  for (int first = 0; first < a.sequences && sequence < 0; first += 64) {
-    const int b = first + lane;
-    Span t = {0, 0};
-    if (b < a.sequences) t = span_of(a.cu[b], a.cu[b + 1], a.total);
-    const int tiles = (t.length * group + ROWS - 1) / ROWS;
+  int sequence = -1, tile = 0;
+  over_blocks<ROWS, kStep>(a, group, [&](int first, int tiles, int) {
     const uint32_t sum = rising_sum((uint32_t)tiles);
-    const uint64_t found = __ballot(t.first <= token && token < t.first + t.length);
+    const uint64_t found = __ballot(slot < items + sum);
     if (found == 0) {
       items += last_sum(sum);
-      continue;
+      return true;
     }
     const int s = __ffsll((unsigned long long)found) - 1;
     sequence = first + s;
-    items += sum_up_to(sum, s);
-    first_token = __builtin_amdgcn_readlane(t.first, s);
-  }
+    tile = (int)(slot - items - sum_up_to(sum, s));
+    return false;
+  });
   if (sequence < 0) return;
-  uint16_t* to = a.out.at(token, head) + lane * kPer;
-  if (__builtin_amdgcn_readfirstlane(draft_length(a, sequence)) == 0) {
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) to[i] = 0;
-    return;
+  const DraftItem item = draft_item(a, sequence, tile);
+  const int in_tile = block * 32 + (int)threadIdx.x / 8, row = tile * ROWS + in_tile, d = (int)threadIdx.x % 8 * kPer;
+  if (row >= item.tokens.length * group) return;
+  uint16_t* to = a.out.at(item.tokens.first + row / group, k_head * group + row % group) + d;
+  int last = -1, first_part = 0;
+  if (item.length > 0) {
+    const int2 parts = a.parts[(int64_t)slot * heads + k_head];
+    last = __builtin_amdgcn_readfirstlane(parts.y);
+    if (last < 0) return;                                    // one workgroup had all of it
+    first_part = __builtin_amdgcn_readfirstlane(parts.x);
   }
-  const int row = (token - first_token) * group + head - k_head * group;
-  const int64_t item = items + row / ROWS;
-  if (item >= a.items) return;                               // (not where cu rises)
-  const int2 parts = a.parts[item * heads + k_head];
-  const int last = __builtin_amdgcn_readfirstlane(parts.y);
-  if (last < 0) return;                                      // one workgroup had all of it
-  const int first_part = __builtin_amdgcn_readfirstlane(parts.x), first = first_part / 2 / heads;
-  if (last >= a.shares || first_part < 0 || first > last) return;
-  auto place = [&](int share) { return (int64_t)(share == first ? first_part : (share * heads + k_head) * 2) * ROWS + row % ROWS; };
-  float top = -FLT_MAX, sum = 0.f;
-  vec o = 0.f;
-  // 64 parts at a time, a lane each for their statistics
-  for (int from = first; from <= last; from += 64) {
-    float2 x = {-FLT_MAX, 0.f};
-    if (from + lane <= last) x = *reinterpret_cast<const float2*>(a.stats + 2 * place(from + lane));
-    const float now = fmaxf(top, over_wave(x.x, [](float y, float z) { return fmaxf(y, z); })), less = __builtin_amdgcn_exp2f(top - now);
-    const float weight = __builtin_amdgcn_exp2f(x.x - now);
-    sum = sum * less + over_wave(x.y * weight, [](float y, float z) { return y + z; });
-    o *= less;
+  const int first = first_part / 2 / heads;
+  if (last >= a.shares || first_part < 0) return;            // (not where cu rises)
+  float top = -FLT_MAX, sum = 0.f, o[kPer];
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) o[e] = 0.f;
+  for (int share = first; share <= last; ++share) {
+    const int64_t at = (int64_t)(share == first ? first_part : (share * heads + k_head) * 2) * ROWS + in_tile;
+    const float2 x = *reinterpret_cast<const float2*>(a.stats + 2 * at);
+    const float now = fmaxf(top, x.x), less = __builtin_amdgcn_exp2f(top - now), more = __builtin_amdgcn_exp2f(x.x - now);
+    sum = __builtin_fmaf(x.y, more, sum * less);
+#pragma unroll
+    for (int e = 0; e < kPer; e += 4) {
+      const f32x4 y = *reinterpret_cast<const f32x4*>(a.sums + at * D + d + e);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[e + i] = __builtin_fmaf(y[i], more, o[e + i] * less);
+    }
     top = now;
-    const int count = min(64, last - from + 1);
-    for (int p = 0; p < count; ++p) o += *reinterpret_cast<const vec*>(a.sums + place(from + p) * D + lane * kPer) * __int_as_float(__builtin_amdgcn_readlane(__float_as_int(weight), p));
   }
   const float f = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) to[i] = __builtin_bit_cast(uint16_t, (__bf16)(o[i] * f));
+  for (int e = 0; e < kPer; e += 8) {
+    float z[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[i] = o[e + i] * f;
+    *reinterpret_cast<u32x4*>(to + e) = pack8(z);
+  }
 }
 
 }  // namespace swz

@@ -66,6 +66,7 @@ int check_attention(const swz_cache16* cache, const swz_attention16_args* a) {
 struct AttentionPlan {
   int rows, shares;                  // of a tile; shares 0: a workgroup for each tile of rows and key head
   int64_t items;                     // tiles of rows, at most
+  bool once;                         // an average block is one tile of rows
 };
 
 // f(integral_constant<int, D>, integral_constant<int, ROWS>)
@@ -81,6 +82,7 @@ AttentionPlan attention_plan(const swz_cache16& c, const swz_attention16_args& a
   const int64_t cut = (int64_t)a.table_width * c.page_tokens, longest = a.max_length > 0 && a.max_length < cut ? a.max_length : cut;
   AttentionPlan p{};
   p.rows = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  p.once = rows <= p.rows;
   for_shape(c.head_dim, p.rows, [&](auto dim, auto rows) {
     using S = swz::DraftShape<decltype(dim)::value, decltype(rows)::value>;
     p.items = a.tokens * group / p.rows + a.sequences;
@@ -178,13 +180,13 @@ int swz_cache16_attention(const swz_cache16* cache, const swz_attention16_args* 
   a.stats = a.sums + attention_places(*cache, p) * cache->head_dim;
   a.parts = reinterpret_cast<int2*>(a.stats + attention_places(*cache, p) * 2);
   a.total = (int)args->tokens, a.sequences = args->sequences, a.q_heads = args->q_heads, a.items = (int)p.items, a.shares = p.shares, a.scale = args->scale;
-  const int64_t workgroups = (p.shares == 0 ? p.items : p.shares) * cache->k_heads, joins = (args->tokens * args->q_heads + 3) / 4;
+  const int64_t workgroups = (p.shares == 0 ? p.items : p.shares) * cache->k_heads, joins = p.items * (p.rows / 32) * cache->k_heads;
   if (workgroups * 256 > swz::kLaunchThreads || joins * 256 > swz::kLaunchThreads) return SWZ_ERR_OVERFLOW;
   return for_shape(cache->head_dim, p.rows, [&](auto dim, auto rows) {
     constexpr int D = decltype(dim)::value, ROWS = decltype(rows)::value;
-    auto kernel = [] {
-      if constexpr (ROWS == 128) return swz::draft_attention_wide_kernel<D>;
-      else return swz::draft_attention_kernel<D, ROWS>;
+    auto kernel = [&] {
+      if constexpr (ROWS == 32) return swz::draft_attention_kernel<D>;
+      else return p.once ? swz::draft_attention_wide_kernel<D, ROWS, true> : swz::draft_attention_wide_kernel<D, ROWS, false>;
     }();
     const int status = launch(kernel, dim3((unsigned)workgroups), dim3(64 * swz::kDraftWaves), 0, stream, a);
     if (status != SWZ_OK || p.shares == 0) return status;
