@@ -40,6 +40,7 @@ struct DraftShape {
   static constexpr int kTileBytes = kDraftKeys * 2 * D, kLdsBytes = 4 * kTileBytes * (kWide ? 1 : 2);
   static constexpr int kJoinPitch = D + 4;                  // floats of a row in LDS when waves join
   static constexpr int kPerCu = kWide || D == 64 ? 2 : 1;   // workgroups of a compute unit
+  static constexpr int kSwitch = kWide ? 2 : 1;             // see deal
 };
 
 // A tile of rows of a sequence.
@@ -69,22 +70,33 @@ __device__ __forceinline__ uint32_t rising_sum(uint32_t x) {
 __device__ __forceinline__ int64_t last_sum(uint32_t sum) { return (uint32_t)__builtin_amdgcn_readlane((int)sum, 63); }
 __device__ __forceinline__ int64_t sum_up_to(uint32_t sum, int lane) { return lane == 0 ? 0 : (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)sum, lane - 1); }
 
-// f(first sequence, tiles and steps of a tile of the lane's sequence) for 64 sequences at a time, until it says false.
-template <int ROWS, int STEP, class F>
-__device__ __forceinline__ void over_blocks(const DraftArgs& a, int group, F&& f) {
-  for (int first = 0; first < a.sequences; first += 64) {
-    const int b = first + (int)(threadIdx.x & 63);
-    int tiles = 0, steps = 0;
+// 64 sequences, a lane each: their tokens, their lengths.
+struct DraftWindow {
+  int first;                         // sequence of lane 0
+  Span tokens;
+  int length;
+  __device__ __forceinline__ void load(const DraftArgs& a, int from) {
+    first = from;
+    const int b = from + (int)(threadIdx.x & 63);
+    tokens = {0, 0};
+    length = 0;
     if (b < a.sequences) {
-      const Span t = span_of(a.cu[b], a.cu[b + 1], a.total);
-      tiles = (t.length * group + ROWS - 1) / ROWS;
-      steps = (draft_length(a, b) + STEP - 1) / STEP;
+      tokens = span_of(a.cu[b], a.cu[b + 1], a.total);
+      length = draft_length(a, b);
     }
-    if (!f(first, tiles, steps)) return;
   }
-}
-__device__ __forceinline__ DraftItem draft_item(const DraftArgs& a, int sequence, int tile) {
-  return {sequence, tile, sequence_span(a.cu, sequence, a.total), __builtin_amdgcn_readfirstlane(draft_length(a, sequence))};
+  __device__ __forceinline__ DraftItem item(int sequence, int tile) const {
+    const int lane = sequence - first;
+    return {sequence, tile, {__builtin_amdgcn_readlane(tokens.first, lane), __builtin_amdgcn_readlane(tokens.length, lane)}, __builtin_amdgcn_readlane(length, lane)};
+  }
+};
+// The window that holds f's sequence: f(window) for one after the other, until it says false.  (One window is loaded once.)
+template <class F>
+__device__ __forceinline__ void over_windows(const DraftArgs& a, DraftWindow& w, F&& f) {
+  for (int first = 0; first < a.sequences; first += 64) {
+    if (w.first != first) w.load(a, first);
+    if (!f()) return;
+  }
 }
 
 // The lowest c bits.
@@ -98,16 +110,15 @@ __device__ const u32x4 kNanChunk = {0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc
 template <int D, bool STREAM>
 struct PageLoader {
   static constexpr int kChunks = D / 8, kRows = 64 / kChunks, kLoads = 16 / kRows;          // of 16 rows
-  const PageTable& c;
-  int k_head, length, lane;
+  int length, lane;
   uint32_t lane_part;
 
-  __device__ __forceinline__ PageLoader(const PageTable& c_, int k_head_, int length_, int lane_) : c(c_), k_head(k_head_), length(length_), lane(lane_) {
+  __device__ __forceinline__ PageLoader(int length_, int lane_) : length(length_), lane(lane_) {
     const int r = lane / kChunks;
     lane_part = (uint32_t)(r * 2 * D) + (uint32_t)(((lane % kChunks) ^ tile_key<D>(r)) << 4);
   }
   // Where 16 positions are: elements from the start of the pages, -1 where they have no page.
-  __device__ __forceinline__ int64_t place(int64_t position, int page) const { return page < 0 ? -1 : c.token_at(page, k_head, (int)position) * D; }
+  static __device__ __forceinline__ int64_t place(const PageTable& c, int k_head, int64_t position, int page) { return page < 0 ? -1 : c.token_at(page, k_head, (int)position) * D; }
   __device__ __forceinline__ void operator()(const uint16_t* pages, int64_t position, int64_t place, uint32_t lds) const {
     if (place >= 0 && position + 16 <= length) {
       const uint64_t at = reinterpret_cast<uint64_t>(pages + place);
@@ -134,70 +145,86 @@ struct PageLoader {
   static __device__ __forceinline__ uint32_t key_of(int i) { return (uint32_t)(tile_key<D>(i * kRows) << 4); }
 };
 
-// Of 32 NB positions, those of which a value is no finite number.
+// Whether any value of a tile is no finite number: whose exponent is all ones.
+template <int D>
+__device__ __forceinline__ bool any_odd(const unsigned char* tile, int lane) {
+  typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+  uint32_t l = (uint32_t)lane;
+  keep(l);                           // or what this needs, once or twice for a sequence, has registers all along
+  u16x2 high[2] = {0, 0};
+#pragma unroll 1
+  for (int i = 0; i < kDraftKeys * 2 * D / 1024; i += 4) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(tile + (i + j) * 1024 + l * 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) high[e % 2] = __builtin_elementwise_max(high[e % 2], __builtin_bit_cast(u16x2, x[e] & 0x7fff7fffu));
+    }
+  }
+  const u16x2 m = __builtin_elementwise_max(high[0], high[1]);
+  return __any(m[0] >= 0x7f80 || m[1] >= 0x7f80);
+}
+
+// o += p x for 32 NB positions.
 template <int D, int NB>
-__device__ __forceinline__ uint64_t odd_positions(const unsigned char* tile, int lane) {
+__device__ __forceinline__ void add_values(f32x16 (&o)[D / 32], const u32x4 (&p)[2 * NB], uint32_t lds, int lane) {
+  const uint32_t column = column_address<D>(lds, lane);
+#pragma unroll
+  for (int k = 0; k < 2 * NB; ++k)
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) o[i] = mfma32(read_columns<D>(column, k, i), __builtin_bit_cast(bf16x8, p[k]), o[i]);
+}
+
+// A product carries 0 times an infinity into rows that do not look at it.  So the positions of a tile that have values that are no finite numbers are taken one at a time, by a product of their own that only those rows
+// keep that look at them (of the wave's 32 NB positions from 32 `part` NB on), and are zeros in the tile then.  sync(): of the waves that share the tile.
+template <int D, int NB, class F>
+__device__ __forceinline__ void take_odd(f32x16 (&o)[D / 32], const u32x4 (&p)[2 * NB], unsigned char* tile, uint32_t lds, int part, uint64_t seen, int lane, F&& sync) {
   constexpr int kChunks = D / 8, kRows = 64 / kChunks;
   uint32_t l = (uint32_t)lane;
   keep(l);
   uint64_t odd = 0;
 #pragma unroll 1
-  for (int i = 0; i < 32 * NB / kRows; ++i) {
+  for (int i = 0; i < kDraftKeys / kRows; ++i) {
     const u32x4 x = *reinterpret_cast<const u32x4*>(tile + i * 1024 + l * 16);
     bool mine = false;
 #pragma unroll
     for (int e = 0; e < 4; ++e) mine |= (x[e] & 0x7f80u) == 0x7f80u || (x[e] & 0x7f800000u) == 0x7f800000u;
     const uint64_t found = __ballot(mine);
-    if (found == 0) continue;
 #pragma unroll
     for (int r = 0; r < kRows; ++r) odd |= (found >> (r * kChunks) & ((1ull << kChunks) - 1)) != 0 ? 1ull << (i * kRows + r) : 0ull;
   }
-  return odd;
-}
-
-// o += p x for 32 NB positions that rows look at in part.  A product carries 0 times an infinity into rows that do not look at it: positions with values that are no finite numbers are left out of it, and
-// then taken one at a time, by a product of their own that only the rows keep that look at them.
-template <int D, int NB>
-__device__ __forceinline__ void add_seen(f32x16 (&o)[D / 32], const u32x4 (&p)[2 * NB], const unsigned char* tile, uint32_t lds, uint64_t seen, int lane) {
-  const uint64_t odd = odd_positions<D, NB>(tile, lane);
-  uint32_t l = (uint32_t)lane;
-  keep(l);
-  const uint32_t column = column_address<D>(lds, (int)l);
-  // of 16 positions, those that `bits` names: element e of lane half h is 8 (e / 4) + 4 h + e % 4
-  auto only = [&](bf16x8 f, uint32_t bits) __attribute__((always_inline)) {
-    u32x4 w = __builtin_bit_cast(u32x4, f);
-    bits >>= 4 * (l >> 5);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int at = 8 * (e / 2) + 2 * (e % 2);
-      w[e] &= (bits >> at & 1u ? 0xffffu : 0u) | (bits >> (at + 1) & 1u ? 0xffff0000u : 0u);
-    }
-    return __builtin_bit_cast(bf16x8, w);
-  };
-#pragma unroll
-  for (int k = 0; k < 2 * NB; ++k)
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-      o[i] = mfma32(only(read_columns<D>(column, k, i), (uint32_t)(~odd >> (16 * k)) & 0xffffu), __builtin_bit_cast(bf16x8, p[k]), o[i]);
-      __builtin_amdgcn_sched_barrier(0);
-    }
+  const uint32_t column = column_address<D>(lds + (uint32_t)(part * NB * 64 * D), (int)l);
 #pragma unroll 1
-  for (uint64_t rest = odd; rest != 0; rest &= rest - 1) {
+  for (uint64_t rest = odd >> (32 * NB * part) & (~0ull >> (64 - 32 * NB)); rest != 0; rest &= rest - 1) {
     const int at = __ffsll((unsigned long long)rest) - 1, k = at >> 4;
-    const bool looks = seen >> at & 1;
     u32x4 w = p[0];
 #pragma unroll
     for (int j = 1; j < 2 * NB; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) w[e] = k == j ? p[j][e] : w[e];
-#pragma unroll
+    // element e of lane half h is position 16 k + 8 (e / 4) + 4 h + e % 4
+    const int place = at & 15, word = place >> 3 << 1 | (place >> 1 & 1);
+    const uint32_t keeps = (place >> 2 & 1) == (int)(l >> 5) ? (place & 1 ? 0xffff0000u : 0xffffu) : 0u;
+    const bool looks = seen >> at & 1;
+#pragma unroll 1
     for (int i = 0; i < D / 32; ++i) {
-      const f32x16 with = mfma32(only(read_columns<D>(column + (uint32_t)(k * 32 * D), 0, i), 1u << (at & 15)), __builtin_bit_cast(bf16x8, w), o[i]);
+      u32x4 f = __builtin_bit_cast(u32x4, read_columns<D>((column ^ (uint32_t)(i << 6)) + (uint32_t)(k * 32 * D), 0, 0));
 #pragma unroll
-      for (int r = 0; r < 16; ++r) o[i][r] = looks ? with[r] : o[i][r];
-      __builtin_amdgcn_sched_barrier(0);
+      for (int e = 0; e < 4; ++e) f[e] &= e == word ? keeps : 0u;
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) {
+        if (j != i) continue;
+        const f32x16 with = mfma32(__builtin_bit_cast(bf16x8, f), __builtin_bit_cast(bf16x8, w), o[j]);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[j][r] = looks ? with[r] : o[j][r];
+      }
     }
   }
+  sync();
+#pragma unroll 1
+  for (uint64_t rest = odd; rest != 0; rest &= rest - 1)
+    if (l < (uint32_t)kChunks) *reinterpret_cast<u32x4*>(tile + (__ffsll((unsigned long long)rest) - 1) * 2 * D + l * 16) = u32x4{};
+  sync();
 }
 
 // The rows of a wave: 32 of a tile.
@@ -272,35 +299,54 @@ __device__ __forceinline__ void hide(f32x16 (&x)[NB], uint64_t seen, int h) {
 }
 
 // The pages of the tiles that a wave will take, EVERY tiles apart: lane l has number l of them, `bits` (a power of two) a tile.
+__device__ __forceinline__ int page_bits(const PageTable& c) { return max(0, 6 - c.page_shift); }
+template <int EVERY>
+__device__ __forceinline__ int look_up_pages(const PageTable& c, const DraftItem& item, int tile) {
+  const int lane = threadIdx.x & 63, bits = page_bits(c);
+  const int64_t position = ((int64_t)tile + (int64_t)(lane >> bits) * EVERY) * kDraftKeys + ((lane & ((1 << bits) - 1)) << c.page_shift);
+  return position < item.length ? c.page_of(item.sequence, (int)position) : -1;
+}
 template <int EVERY>
 struct PagesAhead {
   const PageTable& c;
-  int sequence, length, lane, bits, pages, entry;
-  __device__ __forceinline__ PagesAhead(const PageTable& c_, const DraftItem& item, int lane_) : c(c_), sequence(item.sequence), length(item.length), lane(lane_), bits(max(0, 6 - c_.page_shift)), pages(0), entry(0) {}
-  __device__ __forceinline__ void look_up(int tile) {
-    const int64_t position = ((int64_t)tile + (int64_t)(lane >> bits) * EVERY) * kDraftKeys + ((lane & ((1 << bits) - 1)) << c.page_shift);
-    pages = position < length ? c.page_of(sequence, (int)position) : -1;
-    entry = 0;
-  }
+  const DraftItem& item;
+  int bits, pages, entry;
+  __device__ __forceinline__ PagesAhead(const PageTable& c_, const DraftItem& item_, int pages_) : c(c_), item(item_), bits(page_bits(c_)), pages(pages_), entry(0) {}
   __device__ __forceinline__ void advance(int tile) {        // to `tile`, the one after that of `entry`
-    if (++entry == 64 >> bits) look_up(tile);
+    if (++entry == 64 >> bits) {
+      pages = look_up_pages<EVERY>(c, item, tile);
+      entry = 0;
+    }
   }
   // Of position `place` of the tile.
   __device__ __forceinline__ int operator()(int place) const { return __builtin_amdgcn_readlane(pages, (entry << bits) + (place >> c.page_shift)); }
 };
 
-// Deals the steps of all tiles of rows to workgroups: calls process(item, from, to, all, place) for each tile of rows of which steps from .. to - 1, of `all`, are this workgroup's; a part of one
-// goes to `place`.
-template <int D, int ROWS, class F>
-__device__ __forceinline__ void deal(const DraftArgs& a, int share, int k_head, int group, F&& process) {
+// What a workgroup does after a tile of rows: the next one, its steps from 0 to `to`, and its pages, which look_up() finds.
+struct DraftNext {
+  bool there;
+  DraftItem item;
+  int to, pages;
+};
+
+// Deals the steps of all tiles of rows to workgroups: calls process(item, from, to, all, place, pages, next, look_up_next) for each tile of rows of which steps from .. to - 1, of `all`, are this workgroup's; a part of
+// one goes to `place`.  pages: what look_up(item, from) gave, and look_up_next() looks up next.pages: process calls it when it has no more urgent loads.  A workgroup that goes on to another tile of rows loses the
+// time of about kSwitch steps; tiles of rows count as so many steps more.
+template <int D, int ROWS, class L, class F>
+__device__ __forceinline__ void deal(const DraftArgs& a, int share, int k_head, int group, L&& look_up, F&& process) {
   constexpr int kStep = DraftShape<D, ROWS>::kStep;
-  const int heads = a.c.k_heads;
+  const int heads = a.c.k_heads, kSwitch = a.shares == 0 ? 0 : DraftShape<D, ROWS>::kSwitch;
+  auto tiles_of = [&](int tokens) { return (tokens * group + ROWS - 1) / ROWS; };
+  auto steps_of = [&](int length) { return length == 0 ? 0 : (length + kStep - 1) / kStep + kSwitch; };
   // `before` steps are those of the tiles before the sequence's, `items` the tiles
   int64_t my_start = 0, my_end = 0, before = 0, items = 0;
   int sequence = -1;
+  DraftWindow w;
+  w.first = -1;
   if (a.shares == 0) {
     int tile = 0;
-    over_blocks<ROWS, kStep>(a, group, [&](int first, int tiles, int) {
+    over_windows(a, w, [&] {
+      const int tiles = tiles_of(w.tokens.length);
       const uint32_t sum = rising_sum((uint32_t)tiles);
       const uint64_t found = __ballot(share < items + sum);
       if (found == 0) {
@@ -308,14 +354,14 @@ __device__ __forceinline__ void deal(const DraftArgs& a, int share, int k_head, 
         return true;
       }
       const int s = __ffsll((unsigned long long)found) - 1;
-      sequence = first + s;
+      sequence = w.first + s;
       items += sum_up_to(sum, s);
       tile = (int)(share - items);
       return false;
     });
     if (sequence < 0) return;
-    const DraftItem item = draft_item(a, sequence, tile);
-    const int all = (item.length + kStep - 1) / kStep;
+    const DraftItem item = w.item(sequence, tile);
+    const int all = steps_of(item.length);
     my_start = (int64_t)tile * all;
     my_end = my_start + all;
     if (all == 0) {                                          // rows that look at nothing
@@ -328,16 +374,17 @@ __device__ __forceinline__ void deal(const DraftArgs& a, int share, int k_head, 
     }
   } else {
     int64_t total = 0;
-    over_blocks<ROWS, kStep>(a, group, [&](int, int tiles, int steps) {
-      total += last_sum(rising_sum((uint32_t)tiles * (uint32_t)steps));
+    over_windows(a, w, [&] {
+      total += last_sum(rising_sum((uint32_t)tiles_of(w.tokens.length) * (uint32_t)steps_of(w.length)));
       return true;
     });
     const int shares = (int)min((int64_t)a.shares, total);
     if (share >= shares) return;
     my_start = total * share / shares;
     my_end = total * (share + 1) / shares;
-    over_blocks<ROWS, kStep>(a, group, [&](int first, int tiles, int steps) {
-      const uint32_t sum = rising_sum((uint32_t)tiles * (uint32_t)steps), count = rising_sum((uint32_t)tiles);
+    over_windows(a, w, [&] {
+      const int tiles = tiles_of(w.tokens.length);
+      const uint32_t sum = rising_sum((uint32_t)tiles * (uint32_t)steps_of(w.length)), count = rising_sum((uint32_t)tiles);
       const uint64_t found = __ballot(my_start < before + sum);
       if (found == 0) {
         before += last_sum(sum);
@@ -345,29 +392,61 @@ __device__ __forceinline__ void deal(const DraftArgs& a, int share, int k_head, 
         return true;
       }
       const int s = __ffsll((unsigned long long)found) - 1;
-      sequence = first + s;
+      sequence = w.first + s;
       before += sum_up_to(sum, s);
       items += sum_up_to(count, s);
       return false;
     });
     if (sequence < 0) return;
   }
-  for (int64_t step = my_start; step < my_end && sequence < a.sequences; ++sequence) {
-    DraftItem item = draft_item(a, sequence, 0);
-    const int tiles = (item.tokens.length * group + ROWS - 1) / ROWS, all = (item.length + kStep - 1) / kStep;
-    for (item.tile = all > 0 ? (int)((step - before) / all) : tiles; item.tile < tiles && step < my_end; ++item.tile) {
-      const int from = (int)(step - before - (int64_t)item.tile * all), count = (int)min((int64_t)(all - from), my_end - step);
-      const int place = (share * heads + k_head) * 2 + (step == my_start ? 0 : 1);
-      process(item, from, from + count, all, place);
+  // the first tile of rows with steps of this workgroup's, then those after it
+  DraftItem item = w.item(sequence, 0);
+  int all = steps_of(item.length);
+  item.tile = (int)((my_start - before) / all);
+  int pages = 0;
+  bool looked_up = false;
+  for (int64_t step = my_start;;) {
+    const int64_t at = step - before - (int64_t)item.tile * all, count = min((int64_t)all - at, my_end - step);
+    const int from = max((int)at - kSwitch, 0), to = max((int)(at + count) - kSwitch, 0);
+    step += count;
+    DraftItem then = item;
+    int64_t then_before = before, then_items = items;
+    if (step < my_end && ++then.tile == tiles_of(item.tokens.length)) {
+      // the next sequence that has rows and positions
+      do {
+        then_items += tiles_of(then.tokens.length);
+        then_before += (int64_t)tiles_of(then.tokens.length) * steps_of(then.length);
+        const int next = then.sequence + 1;
+        if (next >= a.sequences) {
+          my_end = step;
+          break;
+        }
+        if (next - w.first >= 64) w.load(a, next & ~63);
+        then = w.item(next, 0);
+      } while (then.tokens.length == 0 || then.length == 0);
+    }
+    const bool more = step < my_end;
+    if (from < to) {
+      const int place = (share * heads + k_head) * 2 + (step - count == my_start ? 0 : 1), real = all - kSwitch;
+      if (!looked_up) pages = look_up(item, from);
+      DraftNext next = {more, then, more ? (int)min((int64_t)steps_of(then.length), my_end - step) - kSwitch : 0, 0};
+      next.there = next.to > 0;
+      process(item, from, to, real, place, pages, next, [&] {
+        if (next.there) next.pages = look_up(then, 0);
+      });
+      pages = next.pages;
+      looked_up = true;
       if (a.shares != 0 && threadIdx.x == 0 && items + item.tile < a.items) {
         int2* part = a.parts + (items + item.tile) * heads + k_head;
         if (from == 0) part->x = place;
-        if (from + count == all) part->y = from == 0 ? -1 : share;
+        if (to == real) part->y = from == 0 ? -1 : share;
       }
-      step += count;
     }
-    items += tiles;
-    before += (int64_t)tiles * all;
+    if (!more) return;
+    item = then;
+    before = then_before;
+    items = then_items;
+    all = steps_of(item.length);
   }
 }
 
@@ -384,31 +463,38 @@ __global__ void __launch_bounds__(64 * kDraftWaves, (DraftShape<D, 32>::kPerCu))
   const int heads = a.c.k_heads, group = a.q_heads / heads, share = (int)blockIdx.x / heads, k_head = (int)blockIdx.x - share * heads;
   const float c = a.scale * kLog2E;
 
-  deal<D, ROWS>(a, share, k_head, group, [&](const DraftItem& item, int from, int to, int all, int place) {
+  auto look_up = [&](const DraftItem& item, int from) { return look_up_pages<kDraftWaves>(a.c, item, from * kDraftWaves + wave); };
+  bool fetched = false;              // the first keys are on their way
+  int64_t places[4];                 // of the last keys that were fetched
+  deal<D, ROWS>(a, share, k_head, group, look_up, [&](const DraftItem& item, int from, int to, int all, int place, int first_pages, DraftNext& next, auto&& look_up_next) {
     const int rows = item.tokens.length * group, first_row = item.tile * ROWS;
     const int end = min(to * kDraftWaves, (item.length + kDraftKeys - 1) / kDraftKeys);
     const int whole = min(min(item.length - item.tokens.length, item.length) / kDraftKeys, end);      // tiles that all rows look at whole (none where the block is longer than the sequence)
     int t = from * kDraftWaves + wave;
-    const PageLoader<D, true> loader(a.c, k_head, item.length, lane);
-    PagesAhead<kDraftWaves> pages(a.c, item, lane);
-    int64_t places[4];
-    auto fetch = [&](const uint16_t* from_pages, int tile, uint32_t lds) {
+    PagesAhead<kDraftWaves> pages(a.c, item, first_pages);
+    auto fetch = [&](const uint16_t* from_pages, int length, int tile, uint32_t lds) {
+      const PageLoader<D, true> loader(length, lane);
 #pragma unroll
       for (int i = 0; i < 4; ++i) loader(from_pages, (int64_t)tile * kDraftKeys + 16 * i, places[i], lds + (uint32_t)(16 * i * 2 * D));
     };
-    auto fetch_keys = [&](int tile) {                        // and note where the values are
+    auto fetch_keys = [&](const PagesAhead<kDraftWaves>& pages, int length, int tile) {      // and note where the values are
 #pragma unroll
-      for (int i = 0; i < 4; ++i) places[i] = loader.place((int64_t)tile * kDraftKeys + 16 * i, pages(16 * i));
-      fetch(a.k_pages, tile, k_lds);
+      for (int i = 0; i < 4; ++i) places[i] = PageLoader<D, true>::place(a.c, k_head, (int64_t)tile * kDraftKeys + 16 * i, pages(16 * i));
+      fetch(a.k_pages, length, tile, k_lds);
+    };
+    auto fetch_next_keys = [&] {                             // of the next tile of rows: this wave's first
+      fetched = next.there && wave < min(next.to * kDraftWaves, (next.item.length + kDraftKeys - 1) / kDraftKeys);
+      if (fetched) fetch_keys(PagesAhead<kDraftWaves>(a.c, next.item, next.pages), next.item.length, wave);
+      return fetched;
     };
     if (t < end) {
-      pages.look_up(t);
-      fetch_keys(t);
-      fetch(a.v_pages, t, v_lds);
+      if (!fetched) fetch_keys(pages, item.length, t);
+      fetch(a.v_pages, item.length, t, v_lds);
     }
     const DraftRows row(a, item, first_row + (lane & 31), k_head, group);
     bf16x8 qf[kSteps];
     load_fragments<D>(qf, a.q.at(item.tokens.first + row.token, row.head), lane);
+    look_up_next();
     DraftSums<D> sums;
     sums.clear();
     auto take = [&](auto is_masked) __attribute__((always_inline)) {
@@ -430,9 +516,12 @@ __global__ void __launch_bounds__(64 * kDraftWaves, (DraftShape<D, 32>::kPerCu))
       __builtin_amdgcn_sched_barrier(0);
       wait_vmcnt_lgkmcnt<63, 0>();
       __builtin_amdgcn_sched_barrier(0);
+      bool behind = more;                                    // a tile of keys is on its way behind the values
       if (more) {
         pages.advance(then);
-        fetch_keys(then);
+        fetch_keys(pages, item.length, then);
+      } else {
+        behind = fetch_next_keys();
       }
       uint64_t seen = 0;
       if constexpr (masked) {
@@ -441,34 +530,31 @@ __global__ void __launch_bounds__(64 * kDraftWaves, (DraftShape<D, 32>::kPerCu))
       }
       sums.weigh(x, c, p);
       __builtin_amdgcn_sched_barrier(0);
-      if (more) wait_vmcnt<kTileLoads>();
+      if (behind) wait_vmcnt<kTileLoads>();
       else wait_vmcnt<0>();
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (masked) {
-        add_seen<D, 2>(sums.o, p, v_tile, v_lds, seen, lane);
-      } else {
-        const uint32_t v_lane = column_address<D>(v_lds, lane);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-          for (int i = 0; i < kParts; ++i) sums.o[i] = mfma32(read_columns<D>(v_lane, k, i), __builtin_bit_cast(bf16x8, p[k]), sums.o[i]);
+        if (__builtin_expect(any_odd<D>(v_tile, lane), 0)) take_odd<D, 2>(sums.o, p, v_tile, v_lds, 0, seen, lane, [] { wait_vmcnt_lgkmcnt<63, 0>(); });
       }
+      add_values<D, 2>(sums.o, p, v_lds, lane);
       __builtin_amdgcn_sched_barrier(0);
       wait_vmcnt_lgkmcnt<63, 0>();
       __builtin_amdgcn_sched_barrier(0);
-      if (more) fetch(a.v_pages, then, v_lds);
+      if (more) fetch(a.v_pages, item.length, then, v_lds);
       t = then;
     };
+    if (t >= end) fetch_next_keys();
     while (t < whole) take(std::false_type{});
     while (t < end) take(std::true_type{});
 
-    // every wave's sums into its own tiles, then a row by 8 threads
+    // Every wave's sums into its tile of values, then a row by 8 threads.  Four dimensions, c, of row r are in slot c ^ r of the row: 32 rows' are spread over all banks.
     const float sum = across_halves(sums.sum, [](float y, float z) { return y + z; });
-    float* mine = reinterpret_cast<float*>(k_tile) + (lane & 31) * S::kJoinPitch;
+    auto slot = [](int row, int dims) { return row * D + (dims / 4 ^ row % (D / 4)) * 4; };
+    float* mine = reinterpret_cast<float*>(v_tile);
 #pragma unroll
     for (int i = 0; i < kParts; ++i)
 #pragma unroll
-      for (int r = 0; r < 16; r += 4) *reinterpret_cast<f32x4*>(mine + 32 * i + 2 * r + 4 * h) = f32x4{sums.o[i][r], sums.o[i][r + 1], sums.o[i][r + 2], sums.o[i][r + 3]};
+      for (int r = 0; r < 16; r += 4) *reinterpret_cast<f32x4*>(mine + slot(lane & 31, 32 * i + 2 * r + 4 * h)) = f32x4{sums.o[i][r], sums.o[i][r + 1], sums.o[i][r + 2], sums.o[i][r + 3]};
     if (h == 0) wave_stats[wave][lane & 31][0] = sums.top, wave_stats[wave][lane & 31][1] = sum;
     __syncthreads();
     const int r = (int)threadIdx.x / 8, d = (int)threadIdx.x % 8 * (D / 8), its = first_row + r;
@@ -485,11 +571,12 @@ __global__ void __launch_bounds__(64 * kDraftWaves, (DraftShape<D, 32>::kPerCu))
       const float f = !entire ? 1.f : total == 0.f ? 0.f : 1.f / total;
       float y[D / 8];
 #pragma unroll
-      for (int e = 0; e < D / 8; ++e) {
-        y[e] = 0.f;
+      for (int e = 0; e < D / 8; e += 4) {
+        f32x4 z = f32x4{};
 #pragma unroll
-        for (int w = 0; w < kDraftWaves; ++w) y[e] = __builtin_fmaf(reinterpret_cast<const float*>(smem + 2 * w * S::kTileBytes)[r * S::kJoinPitch + d + e], factor[w], y[e]);
-        y[e] *= f;
+        for (int w = 0; w < kDraftWaves; ++w) z += *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(smem + (2 * w + 1) * S::kTileBytes) + slot(r, d + e)) * factor[w];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[e + i] = z[i] * f;
       }
       if (entire) {
         uint16_t* to_row = a.out.at(item.tokens.first + its / group, k_head * group + its % group) + d;
@@ -519,46 +606,68 @@ template <int D, int ROWS, bool STREAM>
 __global__ void __launch_bounds__(64 * kDraftWaves, 2) draft_attention_wide_kernel(DraftArgs a) {
   using S = DraftShape<D, ROWS>;
   constexpr int kParts = D / 32, kSteps = D / 16, kBlocks = ROWS / 64, kRowWaves = ROWS / 32;     // a wave has 32 kBlocks of a tile's keys
+  constexpr bool kFollow = kRowWaves == kDraftWaves;         // LDS is tiles alone
   __shared__ __attribute__((aligned(1024))) unsigned char smem[S::kLdsBytes];
   const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), row_wave = wave % kRowWaves, part = wave / kRowWaves;
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem, mine = (uint32_t)(part * 64 * D);      // of a tile: the wave's keys
   const int heads = a.c.k_heads, group = a.q_heads / heads, share = (int)blockIdx.x / heads, k_head = (int)blockIdx.x - share * heads;
   const float c = a.scale * kLog2E;
 
-  deal<D, ROWS>(a, share, k_head, group, [&](const DraftItem& item, int from, int to, int all, int place) {
+  auto look_up = [&](const DraftItem& item, int from) { return look_up_pages<1>(a.c, item, from); };
+  // Tiles of all tiles of rows are numbered on: the keys of number n are in slot n & 1, the values in 2 + that.
+  int number = 0;
+  bool fetched = false;              // the first keys and values and the second keys are on their way
+  int64_t key_place = 0, value_place = 0;
+  deal<D, ROWS>(a, share, k_head, group, look_up, [&](const DraftItem& item, int from, int to, int all, int place, int first_pages, DraftNext& next, auto&& look_up_next) {
     const int whole = min(min(item.length - item.tokens.length, item.length) / kDraftKeys, to);
-    const PageLoader<D, STREAM> loader(a.c, k_head, item.length, lane);
-    PagesAhead<1> pages(a.c, item, lane);
-    // The keys of tile t are in slot (t - from) & 1, the values in 2 + that; a wave fetches a quarter of a tile.  Keys are fetched two tiles ahead, values one, from the places that the keys had.
-    int64_t key_place = 0, value_place = 0;
-    auto fetch_k = [&](int t) {
+    PagesAhead<1> pages(a.c, item, first_pages);
+    const int first_number = number;
+    number += to - from;
+    auto slot_of = [&](int t) { return first_number + t - from & 1; };
+    // A wave fetches a quarter of a tile.  Keys are fetched two tiles ahead, values one, from the places that the keys had; towards the end those of the next tile of rows.
+    const bool follow = kFollow && next.there && next.to >= 2 && to - from >= 2;
+    auto fetch_k = [&](const DraftItem& item, PagesAhead<1>& pages, int t, int slot) {
       value_place = key_place;
-      key_place = loader.place((int64_t)t * kDraftKeys + 16 * wave, pages(16 * wave));
+      key_place = PageLoader<D, STREAM>::place(a.c, k_head, (int64_t)t * kDraftKeys + 16 * wave, pages(16 * wave));
       pages.advance(t + 1);
-      loader(a.k_pages, (int64_t)t * kDraftKeys + 16 * wave, key_place, lds + (uint32_t)(((t - from) & 1) * S::kTileBytes + 16 * wave * 2 * D));
+      PageLoader<D, STREAM>(item.length, lane)(a.k_pages, (int64_t)t * kDraftKeys + 16 * wave, key_place, lds + (uint32_t)(slot * S::kTileBytes + 16 * wave * 2 * D));
     };
-    auto fetch_v = [&](int t, int64_t at) { loader(a.v_pages, (int64_t)t * kDraftKeys + 16 * wave, at, lds + (uint32_t)((2 + ((t - from) & 1)) * S::kTileBytes + 16 * wave * 2 * D)); };
-    pages.look_up(from);
-    fetch_k(from);
-    fetch_v(from, key_place);
-    if (from + 1 < to) fetch_k(from + 1);
+    auto fetch_v = [&](const DraftItem& item, int t, int64_t at, int slot) {
+      PageLoader<D, STREAM>(item.length, lane)(a.v_pages, (int64_t)t * kDraftKeys + 16 * wave, at, lds + (uint32_t)((2 + slot) * S::kTileBytes + 16 * wave * 2 * D));
+    };
+    if (!fetched) {
+      fetch_k(item, pages, from, slot_of(from));
+      fetch_v(item, from, key_place, slot_of(from));
+      if (from + 1 < to) fetch_k(item, pages, from + 1, slot_of(from + 1));
+    } else {
+      pages.advance(from + 1);
+      pages.advance(from + 2);
+    }
+    fetched = follow;
     auto turn = [&](int t) __attribute__((always_inline)) {
       publish();
       if (t + 2 < to) {
-        fetch_k(t + 2);
-        fetch_v(t + 1, value_place);
+        fetch_k(item, pages, t + 2, slot_of(t));
+        fetch_v(item, t + 1, value_place, slot_of(t + 1));
+      } else if (follow) {
+        PagesAhead<1> its(a.c, next.item, next.pages);
+        const int then = its.entry = t + 2 - to;             // 0, then 1
+        fetch_k(next.item, its, then, slot_of(t));
+        if (then == 0) fetch_v(item, t + 1, value_place, slot_of(t + 1));
+        else fetch_v(next.item, 0, value_place, slot_of(t + 1));
       } else if (t + 1 < to) {
-        fetch_v(t + 1, key_place);
+        fetch_v(item, t + 1, key_place, slot_of(t + 1));
       }
     };
     const DraftRows row(a, item, item.tile * ROWS + row_wave * 32 + (lane & 31), k_head, group);
     bf16x8 qf[kSteps];
     load_fragments<D>(qf, a.q.at(item.tokens.first + row.token, row.head), lane);
+    look_up_next();
     DraftSums<D> sums;
     sums.clear();
     f32x16 x[kBlocks], other[kBlocks];
     auto score = [&](int t) __attribute__((always_inline)) {
-      const uint32_t k_lane = row_address<D>(lds + mine + (uint32_t)(((t - from) & 1) * S::kTileBytes), lane);
+      const uint32_t k_lane = row_address<D>(lds + mine + (uint32_t)(slot_of(t) * S::kTileBytes), lane);
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b) {
         x[b] = f32x16{};
@@ -629,29 +738,28 @@ __global__ void __launch_bounds__(64 * kDraftWaves, 2) draft_attention_wide_kern
     auto take = [&](int t, auto is_masked) __attribute__((always_inline)) {
       constexpr bool masked = decltype(is_masked)::value;
       turn(t);
-      const uint32_t values = mine + (uint32_t)((2 + ((t - from) & 1)) * S::kTileBytes);
+      const uint32_t values = (uint32_t)((2 + slot_of(t)) * S::kTileBytes);
       u32x4 p[2 * kBlocks];
       if constexpr (masked) {
         const uint64_t seen = row.seen(a, item, t) >> (32 * part) & (~0ull >> (64 - 32 * kBlocks));
         hide(x, seen, h);
-        if (__any(seen != 0)) {
-          sums.weigh(x, c, p);
-          add_seen<D, kBlocks>(sums.o, p, smem + values, lds + values, seen, lane);
-        }
+        sums.weigh(x, c, p);
+        if (__builtin_expect(any_odd<D>(smem + values, lane), 0))
+          take_odd<D, kBlocks>(sums.o, p, smem + values, lds + values, part, seen, lane, [] {
+            wait_vmcnt_lgkmcnt<63, 0>();
+            block_barrier();
+          });
       } else {
         sums.weigh(x, c, p);
-        const uint32_t v_lane = column_address<D>(lds + values, lane);
-#pragma unroll
-        for (int k = 0; k < 2 * kBlocks; ++k)
-#pragma unroll
-          for (int i = 0; i < kParts; ++i) sums.o[i] = mfma32(read_columns<D>(v_lane, k, i), __builtin_bit_cast(bf16x8, p[k]), sums.o[i]);
       }
+      add_values<D, kBlocks>(sums.o, p, lds + values + mine, lane);
       if (t + 1 < to) score(t + 1);
     };
     publish();
     score(from);
     int t = from;
-    if (t + 2 < whole) {
+    if (t + 3 < whole && slot_of(t) == 1) take(t++, std::false_type{});
+    if (t + 2 < whole && slot_of(t) == 0) {
       float high = x[0][0];
 #pragma unroll
       for (int r = 1; r < 16 * kBlocks; ++r) high = fmaxf(high, x[r / 16][r % 16]);
@@ -665,8 +773,7 @@ __global__ void __launch_bounds__(64 * kDraftWaves, 2) draft_attention_wide_kern
     }
     for (; t < whole; ++t) take(t, std::false_type{});
     for (; t < to; ++t) take(t, std::true_type{});
-    publish();                                               // the tiles have been read
-
+    if constexpr (!kFollow) publish();                       // the tiles have been read
     sums.sum = across_halves(sums.sum, [](float y, float z) { return y + z; });
     if constexpr (kRowWaves < kDraftWaves) {
       // the other half of the keys
@@ -710,30 +817,34 @@ __global__ void __launch_bounds__(64 * kDraftWaves, 2) draft_attention_wide_kern
   });
 }
 
-// What several workgroups have of a tile of rows joined, a workgroup for each 32 of its rows and key head, 8 threads a row; and zeros for sequences without positions.
-template <int D, int ROWS>
+// What several workgroups have of a tile of rows joined, a workgroup for each 32 / GROUPS of its rows and key head, 8 threads a row and GROUPS of them for its parts; and zeros for sequences without positions.
+template <int D, int ROWS, int GROUPS>
 __global__ void __launch_bounds__(256) draft_join_kernel(DraftArgs a) {
-  constexpr int kStep = DraftShape<D, ROWS>::kStep, kPer = D / 8;
-  const int heads = a.c.k_heads, group = a.q_heads / heads, id = (int)blockIdx.x / heads, k_head = (int)blockIdx.x - id * heads, slot = id / (ROWS / 32), block = id - slot * (ROWS / 32);
+  constexpr int kPer = D / 8, kRows = 32 / GROUPS;
+  __shared__ __attribute__((aligned(16))) float joined[GROUPS > 1 ? 32 : 1][D + 4];
+  const int heads = a.c.k_heads, group = a.q_heads / heads, id = (int)blockIdx.x / heads, k_head = (int)blockIdx.x - id * heads, slot = id / (ROWS / kRows), block = id - slot * (ROWS / kRows);
   int64_t items = 0;
   int sequence = -1, tile = 0;
-  over_blocks<ROWS, kStep>(a, group, [&](int first, int tiles, int) {
-    const uint32_t sum = rising_sum((uint32_t)tiles);
+  DraftWindow w;
+  w.first = -1;
+  over_windows(a, w, [&] {
+    const uint32_t sum = rising_sum((uint32_t)(w.tokens.length * group + ROWS - 1) / ROWS);
     const uint64_t found = __ballot(slot < items + sum);
     if (found == 0) {
       items += last_sum(sum);
       return true;
     }
     const int s = __ffsll((unsigned long long)found) - 1;
-    sequence = first + s;
+    sequence = w.first + s;
     tile = (int)(slot - items - sum_up_to(sum, s));
     return false;
   });
   if (sequence < 0) return;
-  const DraftItem item = draft_item(a, sequence, tile);
-  const int in_tile = block * 32 + (int)threadIdx.x / 8, row = tile * ROWS + in_tile, d = (int)threadIdx.x % 8 * kPer;
-  if (row >= item.tokens.length * group) return;
-  uint16_t* to = a.out.at(item.tokens.first + row / group, k_head * group + row % group) + d;
+  const DraftItem item = w.item(sequence, tile);
+  const int mine = (int)threadIdx.x / 8, part = mine / kRows, in_tile = block * kRows + mine % kRows, row = tile * ROWS + in_tile, d = (int)threadIdx.x % 8 * kPer;
+  if (tile * ROWS + block * kRows >= item.tokens.length * group) return;
+  const bool real = row < item.tokens.length * group;
+  uint16_t* to = a.out.at(item.tokens.first + (real ? row : 0) / group, k_head * group + (real ? row : 0) % group) + d;
   int last = -1, first_part = 0;
   if (item.length > 0) {
     const int2 parts = a.parts[(int64_t)slot * heads + k_head];
@@ -746,19 +857,39 @@ __global__ void __launch_bounds__(256) draft_join_kernel(DraftArgs a) {
   float top = -FLT_MAX, sum = 0.f, o[kPer];
 #pragma unroll
   for (int e = 0; e < kPer; ++e) o[e] = 0.f;
-  for (int share = first; share <= last; ++share) {
+  auto add = [&](float its_top, float its_sum, const f32x4 (&y)[kPer / 4]) {
+    const float now = fmaxf(top, its_top), less = __builtin_amdgcn_exp2f(top - now), more = __builtin_amdgcn_exp2f(its_top - now);
+    sum = __builtin_fmaf(its_sum, more, sum * less);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) o[e] = __builtin_fmaf(y[e / 4][e % 4], more, o[e] * less);
+    top = now;
+  };
+#pragma unroll 2
+  for (int share = first + part; share <= last; share += GROUPS) {
     const int64_t at = (int64_t)(share == first ? first_part : (share * heads + k_head) * 2) * ROWS + in_tile;
     const float2 x = *reinterpret_cast<const float2*>(a.stats + 2 * at);
-    const float now = fmaxf(top, x.x), less = __builtin_amdgcn_exp2f(top - now), more = __builtin_amdgcn_exp2f(x.x - now);
-    sum = __builtin_fmaf(x.y, more, sum * less);
+    f32x4 y[kPer / 4];
 #pragma unroll
-    for (int e = 0; e < kPer; e += 4) {
-      const f32x4 y = *reinterpret_cast<const f32x4*>(a.sums + at * D + d + e);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o[e + i] = __builtin_fmaf(y[i], more, o[e + i] * less);
-    }
-    top = now;
+    for (int e = 0; e < kPer / 4; ++e) y[e] = *reinterpret_cast<const f32x4*>(a.sums + at * D + d + 4 * e);
+    if (real) add(x.x, x.y, y);
   }
+  if constexpr (GROUPS > 1) {
+    if (part > 0) {
+#pragma unroll
+      for (int e = 0; e < kPer; e += 4) *reinterpret_cast<f32x4*>(&joined[mine][d + e]) = f32x4{o[e], o[e + 1], o[e + 2], o[e + 3]};
+      if (d == 0) joined[mine][D] = top, joined[mine][D + 1] = sum;
+    }
+    __syncthreads();
+    if (part > 0) return;
+    for (int p = 1; p < GROUPS; ++p) {
+      const float* its = joined[mine + p * kRows];
+      f32x4 y[kPer / 4];
+#pragma unroll
+      for (int e = 0; e < kPer / 4; ++e) y[e] = *reinterpret_cast<const f32x4*>(its + d + 4 * e);
+      add(its[D], its[D + 1], y);
+    }
+  }
+  if (!real) return;
   const float f = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
   for (int e = 0; e < kPer; e += 8) {

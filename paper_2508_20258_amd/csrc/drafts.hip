@@ -67,6 +67,7 @@ struct AttentionPlan {
   int rows, shares;                  // of a tile; shares 0: a workgroup for each tile of rows and key head
   int64_t items;                     // tiles of rows, at most
   bool once;                         // an average block is one tile of rows
+  int join_groups;
 };
 
 // f(integral_constant<int, D>, integral_constant<int, ROWS>)
@@ -83,6 +84,7 @@ AttentionPlan attention_plan(const swz_cache16& c, const swz_attention16_args& a
   AttentionPlan p{};
   p.rows = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
   p.once = rows <= p.rows;
+  p.join_groups = 1;
   for_shape(c.head_dim, p.rows, [&](auto dim, auto rows) {
     using S = swz::DraftShape<decltype(dim)::value, decltype(rows)::value>;
     p.items = a.tokens * group / p.rows + a.sequences;
@@ -90,13 +92,14 @@ AttentionPlan attention_plan(const swz_cache16& c, const swz_attention16_args& a
     if (longest <= 1024) return 0;
     const int64_t shares = together < 1 ? 1 : together;
     p.shares = (int)(p.items * steps < shares ? p.items * steps : shares);
+    p.join_groups = p.shares > 4 * (a.tokens * group / p.rows + 1) ? 8 : 1;          // parts of a tile of rows, about
     return 0;
   });
   return p;
 }
 // Steps of all tiles of rows fit 32 bits, whatever the lengths.
 bool too_many_steps(const swz_cache16& c, const swz_attention16_args& a, const AttentionPlan& p) {
-  const int64_t steps = ((int64_t)a.table_width * c.page_tokens + swz::kDraftKeys - 1) / swz::kDraftKeys;
+  const int64_t steps = ((int64_t)a.table_width * c.page_tokens + swz::kDraftKeys - 1) / swz::kDraftKeys + 8;       // and what a tile of rows counts more
   return p.items >= kTokens || steps * p.items >= kTokens;
 }
 int64_t attention_places(const swz_cache16& c, const AttentionPlan& p) { return (int64_t)p.shares * c.k_heads * 2 * p.rows; }
@@ -180,7 +183,7 @@ int swz_cache16_attention(const swz_cache16* cache, const swz_attention16_args* 
   a.stats = a.sums + attention_places(*cache, p) * cache->head_dim;
   a.parts = reinterpret_cast<int2*>(a.stats + attention_places(*cache, p) * 2);
   a.total = (int)args->tokens, a.sequences = args->sequences, a.q_heads = args->q_heads, a.items = (int)p.items, a.shares = p.shares, a.scale = args->scale;
-  const int64_t workgroups = (p.shares == 0 ? p.items : p.shares) * cache->k_heads, joins = p.items * (p.rows / 32) * cache->k_heads;
+  const int64_t workgroups = (p.shares == 0 ? p.items : p.shares) * cache->k_heads, joins = p.items * (p.rows / 32) * p.join_groups * cache->k_heads;
   if (workgroups * 256 > swz::kLaunchThreads || joins * 256 > swz::kLaunchThreads) return SWZ_ERR_OVERFLOW;
   return for_shape(cache->head_dim, p.rows, [&](auto dim, auto rows) {
     constexpr int D = decltype(dim)::value, ROWS = decltype(rows)::value;
@@ -190,7 +193,7 @@ int swz_cache16_attention(const swz_cache16* cache, const swz_attention16_args* 
     }();
     const int status = launch(kernel, dim3((unsigned)workgroups), dim3(64 * swz::kDraftWaves), 0, stream, a);
     if (status != SWZ_OK || p.shares == 0) return status;
-    return launch(swz::draft_join_kernel<D, ROWS>, dim3((unsigned)joins), dim3(256), 0, stream, a);
+    return launch(p.join_groups > 1 ? swz::draft_join_kernel<D, ROWS, 8> : swz::draft_join_kernel<D, ROWS, 1>, dim3((unsigned)joins), dim3(256), 0, stream, a);
   });
 }
 
