@@ -67,8 +67,7 @@ def verify(target, tokens, uniforms, draft=None, parents=None):
                 rest = p - draft[node]
                 rest = np.where(rest < 0, 0.0, rest)
                 total = rest.sum()
-                # (a sum that is no number stays one: the new token is none)
-                p = rest / total if total > 0 else rest if np.isnan(total) else p
+                p = rest / total if total > 0 else p
     total = p.sum()
     token = -1
     if total > 0 and np.isfinite(total):

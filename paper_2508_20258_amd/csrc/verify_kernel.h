@@ -20,9 +20,12 @@ struct Walked {
   int node, accepted, failed;
   uint64_t failed_nodes;
 };
+struct LeftSum {
+  double sum, inverse;
+};
 struct VerifyState {
   Walked walked;
-  double sums[kMostNodes];           // drawn children: of what each failed one left
+  LeftSum sums[kMostNodes];            // drawn children: of what each failed one left
 };
 
 struct VerifyArgs {
@@ -68,24 +71,56 @@ __device__ __forceinline__ void load_values(const void* p, int64_t row, int i, i
   }
 }
 
-// What is left of p after `failed` children failed, but for the last division.
+// What a failed child leaves of p, but for the division by its sum.
 __device__ __forceinline__ double take(double p, double q) {
   const double d = p - q;
   return d < 0. ? 0. : d;            // (NaN stays)
 }
-__device__ __forceinline__ double left_of(double p, double q, int failed, const double* sums) {
+// d / sum: with the rounded reciprocal of the sum a quotient that its remainder corrects is the rounded one (Markstein), at three instructions instead of the division's dozen.
+__device__ __forceinline__ LeftSum left_sum(double sum) { return {sum, 1. / sum}; }
+// What is left of values p after `failed` children failed.
+template <int N>
+__device__ __forceinline__ void leave(double (&p)[N], const double (&q)[N], int failed, const LeftSum* sums) {
+#pragma unroll 1
   for (int i = 0; i < failed; ++i) {
-    const double d = take(p, q);
-    p = sums[i] > 0. ? d / sums[i] : p;
+    const LeftSum s = sums[i];
+    if (!(s.sum > 0.)) continue;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const double d = take(p[e], q[e]), quotient = d * s.inverse;
+      p[e] = __builtin_fma(__builtin_fma(-quotient, s.sum, d), s.inverse, quotient);
+    }
   }
-  return p;
+}
+__device__ __forceinline__ double left_of(double p, double q, int failed, const LeftSum* sums) {
+  double x[1] = {p};
+  const double y[1] = {q};
+  leave<1>(x, y, failed, sums);
+  return x[0];
 }
 
-__device__ __forceinline__ double add_over_wave(double x) {
-#pragma unroll
-  for (int by = 1; by < 64; by *= 2) x += __shfl_xor(x, by);
+__device__ __forceinline__ double lane_value(double x, int lane) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  return __builtin_bit_cast(double, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(b >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)b, lane));
+}
+// x of another lane of the wave, 0 where there is none.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double from_lane(double x) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint32_t low = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)b, CTRL, ROWS, 0xf, false), high = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, ROWS, 0xf, false);
+  return __builtin_bit_cast(double, (uint64_t)high << 32 | low);
+}
+// Sum of x over this lane and those before it.
+__device__ __forceinline__ double sum_with(double x) {
+  x += from_lane<0x111, 0xf>(x);     // row_shr:1, 2, 4, 8
+  x += from_lane<0x112, 0xf>(x);
+  x += from_lane<0x114, 0xf>(x);
+  x += from_lane<0x118, 0xf>(x);
+  x += from_lane<0x142, 0xa>(x);     // row_bcast:15, to rows 1 and 3
+  x += from_lane<0x143, 0xc>(x);     // row_bcast:31, to rows 2 and 3
   return x;
 }
+__device__ __forceinline__ double add_over_wave(double x) { return lane_value(sum_with(x), 63); }
 
 // A sequence's tests, all lanes alike; a lane has a node.
 struct Nodes {
@@ -114,15 +149,11 @@ __device__ __forceinline__ Nodes load_nodes(const VerifyArgs& a, int sequence) {
   }
   return n;
 }
-__device__ __forceinline__ double lane_value(double x, int lane) {
-  const uint64_t b = __builtin_bit_cast(uint64_t, x);
-  return __builtin_bit_cast(double, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(b >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)b, lane));
-}
-
 // sum_left(node, failed): the sum of what is left of the node's row after that many failed children (drawn ones only), needed where another one is tested.
 // The lane's entry of the path is returned in *path.
-template <bool DRAWN, class F>
-__device__ __forceinline__ Walked walk(const Nodes& n, double* sums, int* path, F&& sum_left) {
+// SIBLINGS: a node may have more than one child.
+template <bool DRAWN, bool SIBLINGS, class F>
+__device__ __forceinline__ Walked walk(const Nodes& n, LeftSum* sums, int* path, F&& sum_left) {
   const int lane = threadIdx.x & 63;
   Walked s{};
   *path = lane == 0 ? 0 : -1;
@@ -135,9 +166,13 @@ __device__ __forceinline__ Walked walk(const Nodes& n, double* sums, int* path, 
     const double u = lane_value(n.uniform, at), p = lane_value(n.p, at);
     bool good;
     if constexpr (DRAWN) {
-      if (s.failed > 0) sums[s.failed - 1] = sum_left(s.node, s.failed);
       const double q = lane_value(n.q, at);
-      good = u * q < left_of(p, q, s.failed, sums);
+      if constexpr (SIBLINGS) {
+        if (s.failed > 0) sums[s.failed - 1] = left_sum(sum_left(s.node, s.failed));
+        good = u * q < left_of(p, q, s.failed, sums);
+      } else {
+        good = u * q < p;
+      }
     } else {
       const int token = __builtin_amdgcn_readlane(n.token, at);
       const double mine = __ballot(n.token == token && (s.failed_nodes >> lane & 1)) != 0 ? 0. : p, least = u * mass;
@@ -154,6 +189,7 @@ __device__ __forceinline__ Walked walk(const Nodes& n, double* sums, int* path, 
     } else {
       ++s.failed;
       s.failed_nodes |= 1ull << at;
+      if constexpr (!SIBLINGS) break;
     }
   }
   return s;
@@ -171,21 +207,44 @@ __device__ __forceinline__ void store_walk(const VerifyArgs& a, int sequence, co
 template <class T>
 __global__ void __launch_bounds__(kWalkThreads) verify_walk_kernel(VerifyArgs a) {
   constexpr int N = 16 / sizeof(T), kWaves = kWalkThreads / 64;
-  __shared__ double sums[kMostNodes], parts[kWaves];
+  __shared__ LeftSum sums[kMostNodes];
+  __shared__ double parts[kWaves];
   const int sequence = (int)blockIdx.x, lane = threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
   const Nodes n = load_nodes<T, true>(a, sequence);
   int path;
-  const Walked s = walk<true>(n, sums, &path, [&](int node, int failed) {
+  const Walked s = walk<true, true>(n, sums, &path, [&](int node, int failed) {
     const int64_t p_row = (int64_t)(n.first + node) * a.target_pitch, q_row = (int64_t)(n.first + node) * a.draft_pitch;
-    double sum = 0.;
-#pragma unroll 2
-    for (int i = (int)threadIdx.x * N; i < a.vocab; i += kWalkThreads * N) {
-      float p[N], q[N];
-      load_values<T>(a.target, p_row, i, a.vocab, p);
-      load_values<T>(a.draft, q_row, i, a.vocab, q);
+    constexpr int kRounds = 8 / N, kStride = kRounds * kWalkThreads * N;     // the next rounds' loads are on their way while these are added up
+    float p[2][kRounds][N], q[2][kRounds][N];
+    auto load = [&](int to, int i) __attribute__((always_inline)) {
 #pragma unroll
-      for (int e = 0; e < N; ++e) sum += take(left_of((double)p[e], (double)q[e], failed - 1, sums), (double)q[e]);
+      for (int j = 0; j < kRounds; ++j) {
+        load_values<T>(a.target, p_row, i + j * kWalkThreads * N, a.vocab, p[to][j]);
+        load_values<T>(a.draft, q_row, i + j * kWalkThreads * N, a.vocab, q[to][j]);
+      }
+    };
+    double more[2] = {0., 0.};
+    auto add = [&](int from) __attribute__((always_inline)) {
+#pragma unroll
+      for (int j = 0; j < kRounds; ++j) {
+        double x[N], y[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = (double)p[from][j][e], y[e] = (double)q[from][j][e];
+        leave<N>(x, y, failed - 1, sums);
+#pragma unroll
+        for (int e = 0; e < N; ++e) more[e % 2] += take(x[e], y[e]);
+      }
+    };
+    const int first = (int)threadIdx.x * N;
+    load(0, first);
+#pragma unroll 1
+    for (int64_t i = 0; i < a.vocab; i += 2 * kStride) {
+      load(1, (int)min(i + kStride + first, (int64_t)a.vocab));
+      add(0);
+      load(0, (int)min(i + 2 * kStride + first, (int64_t)a.vocab));
+      add(1);
     }
+    double sum = more[0] + more[1];
     sum = add_over_wave(sum);
     __syncthreads();                                         // what was there has been read
     if (lane == 0) parts[wave] = sum;
@@ -196,25 +255,27 @@ __global__ void __launch_bounds__(kWalkThreads) verify_walk_kernel(VerifyArgs a)
   });
   __syncthreads();
   VerifyState* to = a.states + sequence;
-  if (threadIdx.x < kMostNodes) to->sums[threadIdx.x] = (int)threadIdx.x < s.failed - 1 ? sums[threadIdx.x] : 0.;
+  if (threadIdx.x < kMostNodes) to->sums[threadIdx.x] = (int)threadIdx.x < s.failed - 1 ? sums[threadIdx.x] : LeftSum{0., 0.};
   if (wave == 0) {
     if (lane == 0) to->walked = s;
     store_walk(a, sequence, n, s, path);
   }
 }
 
-// Value i of the row that the new token is drawn from: what is left after the last failed child, and before it.
-struct Left {
-  double now, before;
-};
-template <bool DRAWN>
-__device__ __forceinline__ Left left_at(double p, double q, const Walked& s, const double* sums) {
+// Values of the row that the new token is drawn from: what is left after the last failed child, and before it.
+template <bool DRAWN, int N>
+__device__ __forceinline__ void left_at(const float (&p)[N], const float (&q)[N], const Walked& s, const LeftSum* sums, double (&now)[N], double (&before)[N]) {
+#pragma unroll
+  for (int e = 0; e < N; ++e) now[e] = before[e] = (double)p[e];
   if constexpr (DRAWN) {
-    if (s.failed == 0) return {p, p};
-    const double before = left_of(p, q, s.failed - 1, sums);
-    return {take(before, q), before};
+    if (s.failed == 0) return;
+    double y[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) y[e] = (double)q[e];
+    leave<N>(before, y, s.failed - 1, sums);
+#pragma unroll
+    for (int e = 0; e < N; ++e) now[e] = take(before[e], y[e]);
   }
-  return {p, p};
 }
 // Whether token x is that of a failed child (points).
 template <int N>
@@ -241,8 +302,7 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_sums_kernel(VerifyArgs 
   } else {
     const Nodes n = load_nodes<T, DRAWN>(a, sequence);
     int path;
-    double none[1] = {0.};                                   // a chain: no node has a second child
-    s = walk<DRAWN>(n, none, &path, [](int, int) { return 0.; });
+    s = walk<DRAWN, !DRAWN>(n, nullptr, &path, [](int, int) { return 0.; });         // drawn children: of a chain
     if (piece == 0 && wave == 0) {
       if (lane == 0) state->walked = s;
       store_walk(a, sequence, n, s, path);
@@ -261,12 +321,10 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_sums_kernel(VerifyArgs 
 #pragma unroll
   for (int i = 0; i < kTurns; ++i) {
     if constexpr (!DRAWN) drop_failed<N>(a, t.first, s.failed_nodes, first + i * kVerifyThreads * N, p[i]);
+    double x[N], y[N];
+    left_at<DRAWN, N>(p[i], q[i], s, state->sums, x, y);
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const Left x = left_at<DRAWN>((double)p[i][e], (double)q[i][e], s, state->sums);
-      now += x.now;
-      before += x.before;
-    }
+    for (int e = 0; e < N; ++e) now += x[e], before += y[e];
   }
   now = add_over_wave(now);
   before = add_over_wave(before);
@@ -280,66 +338,79 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_sums_kernel(VerifyArgs 
   }
 }
 
-// The first of `count` numbers (value(i), not negative) with which their sum exceeds r, and the sum before it; -1: none.  The last one above 0 goes to *last.  A thread has `per` neighbours of
-// kVerifyThreads * per >= count; all threads return the same.
-struct Found {
+// Numbers that are not negative, `mine` for each thread of a workgroup: the sum of those of the threads before it, and of all.
+struct Before {
+  double before, all;
+};
+__device__ __forceinline__ Before sum_before_threads(double mine, double (&waves)[kVerifyThreads / 64]) {
+  const int lane = threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+  const double with = sum_with(mine), before = from_lane<0x138, 0xf>(with);      // wave_shr:1
+  if (lane == 63) waves[wave] = with;
+  __syncthreads();
+  double first = 0., all = 0.;
+#pragma unroll
+  for (int w = 0; w < kVerifyThreads / 64; ++w) {
+    first = w < wave ? first + waves[w] : first;
+    all += waves[w];
+  }
+  return {first + before, all};
+}
+
+// The first of a workgroup's numbers (N for each thread, from `first` on) with which their sum exceeds r, and the sum before it; where there is none (rounding may leave none at the very end of a piece) the last one above 0,
+// and infinity.
+struct Share {
   int at;
   double before;
 };
-template <class F>
-__device__ __forceinline__ Found find_share(int count, int per, double r, int* last, double* total, F&& value) {
-  __shared__ double waves[kVerifyThreads / 64], found_before;
-  __shared__ int found_at, last_at;
-  const int lane = threadIdx.x & 63, wave = (int)threadIdx.x >> 6, first = (int)threadIdx.x * per, end = min(first + per, count);
-  double mine = 0.;
-  int above = -1;
-  for (int i = first; i < end; ++i) {
-    const double x = value(i);
-    mine += x;
-    above = x > 0. ? i : above;
-  }
-  double with = mine;                // of this thread and those of its wave before it
+struct WaveShare {
+  int found, last;
+  double before;
+};
+template <int N>
+__device__ __forceinline__ Share find_share(const double (&x)[N], double before, int first, double r, WaveShare (&waves)[kVerifyThreads / 64]) {
+  const int lane = threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+  int at = -1, above = -1;
+  double sum = before, at_before = 0.;
 #pragma unroll
-  for (int by = 1; by < 64; by *= 2) {
-    const double other = __shfl_up(with, by);
-    if (lane >= by) with += other;
+  for (int i = 0; i < N; ++i) {
+    if (x[i] > 0.) above = first + i;
+    if (at < 0 && x[i] > 0. && sum + x[i] > r) at = first + i, at_before = sum;
+    sum += x[i];
   }
-  double without = __shfl_up(with, 1);
-  without = lane > 0 ? without : 0.;
+  // a wave's first is its first lane's that has one
+  const uint64_t found = __ballot(at >= 0), some = __ballot(above >= 0);
+  const int its = found != 0 ? __ffsll((unsigned long long)found) - 1 : 0, last = some != 0 ? 63 - __clzll((unsigned long long)some) : 0;
+  if (lane == its) waves[wave].found = at, waves[wave].before = at_before;
+  if (lane == last) waves[wave].last = above;
   __syncthreads();
-  if (lane == 63) waves[wave] = with;
-  if (threadIdx.x == 0) found_at = 0x7fffffff, last_at = -1;
-  __syncthreads();
-  double before = 0., all = 0.;
+  Share s = {-1, INFINITY};
 #pragma unroll
-  for (int w = 0; w < kVerifyThreads / 64; ++w) {
-    before = w < wave ? before + waves[w] : before;
-    all += waves[w];
+  for (int w = kVerifyThreads / 64 - 1; w >= 0; --w)
+    if (waves[w].found >= 0) s = {waves[w].found, waves[w].before};
+  if (s.at < 0)
+#pragma unroll
+    for (int w = 0; w < kVerifyThreads / 64; ++w) s.at = waves[w].last >= 0 ? waves[w].last : s.at;
+  return s;
+}
+
+// T consecutive values of a row as numbers, those from `end` on 0.
+template <class T, int COUNT>
+__device__ __forceinline__ void load_run(const void* p, int64_t row, int i, int end, float (&x)[COUNT]) {
+  constexpr int N = 16 / sizeof(T);
+#pragma unroll
+  for (int j = 0; j < COUNT; j += N) {
+    float v[N];
+    load_values<T>(p, row, i + j, end, v);
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[j + e] = v[e];
   }
-  before += without;
-  *total = all;
-  if (above >= 0) atomicMax(&last_at, above);
-  // rounding may leave sums that do not rise from thread to thread, by parts in 10^16: the first that exceeds counts
-  double sum = before;
-  int at = 0x7fffffff;
-  double at_before = 0.;
-  for (int i = first; i < end; ++i) {
-    const double x = value(i);
-    if (at == 0x7fffffff && sum + x > r && x > 0.) at = i, at_before = sum;
-    sum += x;
-  }
-  if (at != 0x7fffffff) atomicMin(&found_at, at);
-  __syncthreads();
-  if (at != 0x7fffffff && at == found_at) found_before = at_before;
-  __syncthreads();
-  *last = last_at;
-  const Found f = {found_at == 0x7fffffff ? -1 : found_at, found_before};
-  return f;
 }
 
 template <class T, bool DRAWN>
 __global__ void __launch_bounds__(kVerifyThreads) verify_token_kernel(VerifyArgs a) {
   constexpr int kPer = kPieceValues / kVerifyThreads;
+  __shared__ double waves[3][kVerifyThreads / 64];
+  __shared__ WaveShare shares[2][kVerifyThreads / 64];
   const int sequence = (int)blockIdx.x;
   const Span t = sequence_span(a.cu, sequence, a.total);
   if (t.length == 0) {
@@ -347,37 +418,59 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_token_kernel(VerifyArgs
     return;
   }
   const VerifyState* state = a.states + sequence;
-  const Walked s = state->walked;
   const double* sums = a.sums + (int64_t)sequence * a.pieces * 2;
+  // a thread's pieces: one, where there are no more pieces than threads
+  const int per = (a.pieces + kVerifyThreads - 1) / kVerifyThreads, first_piece = (int)threadIdx.x * per, end_piece = min(first_piece + per, a.pieces);
+  double now = 0., was = 0.;
+  for (int i = first_piece; i < end_piece; ++i) now += sums[2 * i], was += sums[2 * i + 1];
+  const Walked s = state->walked;
   const double u = (double)a.uniforms[t.first];
-  int last;
-  double total;
-  const int per = (a.pieces + kVerifyThreads - 1) / kVerifyThreads;
-  bool before = false;               // the last failed child left nothing: what there was before it
-  find_share(a.pieces, per, 0., &last, &total, [&](int i) { return sums[2 * i]; });
-  if (DRAWN && s.failed > 0 && !(total > 0.) && total == total) {
-    before = true;
-    find_share(a.pieces, per, 0., &last, &total, [&](int i) { return sums[2 * i + 1]; });
+  Before b = sum_before_threads(now, waves[0]);
+  const bool before = DRAWN && s.failed > 0 && !(b.all > 0.); // the last failed child left nothing: what there was before it
+  if (before) {
+    b = sum_before_threads(was, waves[1]);
+    now = was;
   }
-  if (!(total > 0.) || !(total < INFINITY)) {
+  if (!(b.all > 0.) || !(b.all < INFINITY)) {
     if (threadIdx.x == 0) a.token[sequence] = -1;
     return;
   }
-  double r = u * total;
-  Found f = find_share(a.pieces, per, r, &last, &total, [&](int i) { return sums[2 * i + (before ? 1 : 0)]; });
-  const int piece = f.at < 0 ? last : f.at;
-  r = f.at < 0 ? INFINITY : r - f.before;
+  double r = u * b.all;
+  const double mine[1] = {now};
+  const Share found = find_share<1>(mine, b.before, (int)threadIdx.x, r, shares[0]);
+  const int thread = found.at;
+  r = found.before < INFINITY ? r - found.before : INFINITY;
+  int piece = thread * per;
+  if (per > 1) {                     // of the thread's pieces
+    int last = piece;
+    for (const int end = min(piece + per, a.pieces); piece < end; ++piece) {
+      const double x = sums[2 * piece + (before ? 1 : 0)];
+      if (x > r) break;
+      last = x > 0. ? piece : last;
+      r -= x;
+      if (piece + 1 == end) {
+        piece = last;
+        r = INFINITY;
+        break;
+      }
+    }
+  }
   const int64_t p_row = (int64_t)(t.first + s.node) * a.target_pitch, q_row = (int64_t)(t.first + s.node) * a.draft_pitch;
-  const int start = piece * kPieceValues, count = min(kPieceValues, a.vocab - start);
-  f = find_share(count, kPer, r, &last, &total, [&](int i) {
-    float p[1] = {(float)probability<T>(a.target, p_row + start + i)};
-    double q = 0.;
-    if constexpr (DRAWN) q = s.failed > 0 ? probability<T>(a.draft, q_row + start + i) : 0.;
-    else drop_failed<1>(a, t.first, s.failed_nodes, start + i, p);
-    const Left x = left_at<DRAWN>((double)p[0], q, s, state->sums);
-    return before ? x.before : x.now;
-  });
-  if (threadIdx.x == 0) a.token[sequence] = start + (f.at < 0 ? last : f.at);
+  const int first = piece * kPieceValues + (int)threadIdx.x * kPer;
+  float p[kPer], q[kPer];
+  load_run<T, kPer>(a.target, p_row, first, a.vocab, p);
+  if (DRAWN && s.failed > 0) load_run<T, kPer>(a.draft, q_row, first, a.vocab, q);
+  if constexpr (!DRAWN) drop_failed<kPer>(a, t.first, s.failed_nodes, first, p);
+  double x[kPer], y[kPer], sum = 0.;
+  left_at<DRAWN, kPer>(p, q, s, state->sums, x, y);
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) {
+    x[e] = before ? y[e] : x[e];
+    sum += x[e];
+  }
+  const Before c = sum_before_threads(sum, waves[2]);
+  const Share token = find_share<kPer>(x, c.before, first, r, shares[1]);
+  if (threadIdx.x == 0) a.token[sequence] = token.at;
 }
 
 }  // namespace swz
