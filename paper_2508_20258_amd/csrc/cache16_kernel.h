@@ -35,11 +35,14 @@ struct Append16Args {
   int total, sequences, q_heads, rotary, splits;   // rotary 0: nothing is turned
 };
 
-constexpr int kAppendThreads = 256;
+constexpr int kAppendThreads = 256, kAppendAhead = 3;
 
+// HBM is the bound where tokens are many: 32768 of 32 + 8 + 8 heads of 128 in 139 us, 5.9 TB/s, in streaming loads and stores (159 without them), which are slower where all fits the memory-side cache (8192 tokens
+// of 8 + 8 heads, 67 MB: 17.8 us, and 12.8 with regular ones).  A step's few tokens take 3.6 us, three loads one after another.
+//
 // A wave for each token, or for each of `splits` parts of its heads (queries, then keys, then values): 64 / kLanes heads at a time, 16 dimensions a lane.  The lane's two chunks of 8 hold both halves of its pairs: c and
 // c + rotary / 16 of those that are turned, neighbours of the others.
-template <int D, bool INTERLEAVED>
+template <int D, bool INTERLEAVED, bool STREAM>
 __global__ void __launch_bounds__(kAppendThreads) cache16_append_kernel(Append16Args a) {
   constexpr int kLanes = D / 16, kHeads = 64 / kLanes;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -67,42 +70,59 @@ __global__ void __launch_bounds__(kAppendThreads) cache16_append_kernel(Append16
       s[0] = *reinterpret_cast<const f32x4*>(sin + first), s[1] = *reinterpret_cast<const f32x4*>(sin + second);
     }
   }
-  for (int head = split * kHeads + mine; head < heads; head += a.splits * kHeads) {
-    const int k_head = head - a.q_heads, v_head = k_head - a.c.k_heads;
-    const uint16_t* from = k_head < 0 ? a.q.at(token, head) : v_head < 0 ? a.k.at(token, k_head) : a.v.at(token, v_head);
-    u32x4 x = *reinterpret_cast<const u32x4*>(from + d0), y = *reinterpret_cast<const u32x4*>(from + d1);
-    if (turned && v_head < 0) {
-      float p[8], q[8];
-      unpack8(x, p);
-      unpack8(y, q);
-      if constexpr (INTERLEAVED) {
-        auto turn = [&](float (&z)[8], const f32x4& c, const f32x4& s) {
+  // kAppendAhead turns' loads are on their way together
+  for (int first = split * kHeads + mine; first < heads; first += kAppendAhead * a.splits * kHeads) {
+    u32x4 x[kAppendAhead], y[kAppendAhead];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float u = z[2 * e], w = z[2 * e + 1];
-            z[2 * e] = u * c[e] - w * s[e];
-            z[2 * e + 1] = w * c[e] + u * s[e];
+    for (int i = 0; i < kAppendAhead; ++i) {
+      const int head = min(first + i * a.splits * kHeads, heads - 1), k_head = head - a.q_heads, v_head = k_head - a.c.k_heads;
+      const uint16_t* from = k_head < 0 ? a.q.at(token, head) : v_head < 0 ? a.k.at(token, k_head) : a.v.at(token, v_head);
+      auto load = [](const uint16_t* p) { return STREAM ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)) : *reinterpret_cast<const u32x4*>(p); };
+      x[i] = load(from + d0);
+      y[i] = load(from + d1);
+    }
+#pragma unroll
+    for (int i = 0; i < kAppendAhead; ++i) {
+      const int head = first + i * a.splits * kHeads, k_head = head - a.q_heads, v_head = k_head - a.c.k_heads;
+      if (head >= heads) break;
+      if (turned && v_head < 0) {
+        float p[8], q[8];
+        unpack8(x[i], p);
+        unpack8(y[i], q);
+        if constexpr (INTERLEAVED) {
+          auto turn = [&](float (&z)[8], const f32x4& c, const f32x4& s) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float u = z[2 * e], w = z[2 * e + 1];
+              z[2 * e] = u * c[e] - w * s[e];
+              z[2 * e + 1] = w * c[e] + u * s[e];
+            }
+          };
+          turn(p, c[0], s[0]);
+          turn(q, c[1], s[1]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float u = p[e], w = q[e], cosine = c[e / 4][e % 4], sine = s[e / 4][e % 4];
+            p[e] = u * cosine - w * sine;
+            q[e] = w * cosine + u * sine;
           }
-        };
-        turn(p, c[0], s[0]);
-        turn(q, c[1], s[1]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float u = p[e], w = q[e], cosine = c[e / 4][e % 4], sine = s[e / 4][e % 4];
-          p[e] = u * cosine - w * sine;
-          q[e] = w * cosine + u * sine;
+        }
+        x[i] = pack8(p);
+        y[i] = pack8(q);
+      }
+      uint16_t* to = nullptr;
+      if (k_head < 0) to = a.q_out.at(token, head);
+      else if (page >= 0) to = v_head < 0 ? a.k_pages + a.c.token_at(page, k_head, (int)position) * D : a.v_pages + a.c.token_at(page, v_head, (int)position) * D;
+      if (to != nullptr) {
+        if constexpr (STREAM) {
+          __builtin_nontemporal_store(x[i], reinterpret_cast<u32x4*>(to + d0));
+          __builtin_nontemporal_store(y[i], reinterpret_cast<u32x4*>(to + d1));
+        } else {
+          *reinterpret_cast<u32x4*>(to + d0) = x[i];
+          *reinterpret_cast<u32x4*>(to + d1) = y[i];
         }
       }
-      x = pack8(p);
-      y = pack8(q);
-    }
-    uint16_t* to = nullptr;
-    if (k_head < 0) to = a.q_out.at(token, head);
-    else if (page >= 0) to = v_head < 0 ? a.k_pages + a.c.token_at(page, k_head, (int)position) * D : a.v_pages + a.c.token_at(page, v_head, (int)position) * D;
-    if (to != nullptr) {
-      *reinterpret_cast<u32x4*>(to + d0) = x;
-      *reinterpret_cast<u32x4*>(to + d1) = y;
     }
   }
 }

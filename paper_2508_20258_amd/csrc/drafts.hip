@@ -15,6 +15,8 @@ namespace {
 using namespace swz::host;
 using swz::launch;
 
+constexpr int64_t kCacheBytes = (int64_t)256 << 20;          // the memory-side cache: what is more is not found there again
+
 int check_cache(const swz_cache16* c) {
   if (c == nullptr || c->k == nullptr || c->v == nullptr || c->pages < 1 || c->k_heads < 1) return SWZ_ERR_INVALID_ARG;
   if (!head_dim_ok(c->head_dim) || c->page_tokens < 16 || (c->page_tokens & (c->page_tokens - 1)) != 0 || !aligned(c->k, 16) || !aligned(c->v, 16)) return SWZ_ERR_UNSUPPORTED;
@@ -152,7 +154,9 @@ int swz_cache16_append(const swz_cache16* cache, const swz_append16_args* args, 
       a.splits = args->tokens * blocks <= 32 * (int64_t)compute_units() ? blocks : 1;
       const int64_t workgroups = (args->tokens * a.splits + kWaves - 1) / kWaves;
       if (workgroups >= kTokens) return (int)SWZ_ERR_OVERFLOW;
-      return launch(swz::cache16_append_kernel<D, decltype(interleaved)::value>, dim3((unsigned)workgroups), dim3(swz::kAppendThreads), 0, stream, a);
+      constexpr bool kInterleaved = decltype(interleaved)::value;
+      const bool stream_out = args->tokens * (a.q_heads + 2 * a.c.k_heads) * D * 4 > kCacheBytes;
+      return launch(stream_out ? swz::cache16_append_kernel<D, kInterleaved, true> : swz::cache16_append_kernel<D, kInterleaved, false>, dim3((unsigned)workgroups), dim3(swz::kAppendThreads), 0, stream, a);
     });
   });
 }
