@@ -105,45 +105,38 @@ __device__ __forceinline__ uint64_t shift_up(uint64_t x, int by) { return by >= 
 
 __device__ const u32x4 kNanChunk = {0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
 
-// Positions of a head from their pages into LDS, 16 rows at a time (a page has 16 or more): those from `length` on are zeros, those without a page NaN.
-// STREAM: they are read once.
-template <int D, bool STREAM>
-struct PageLoader {
-  static constexpr int kChunks = D / 8, kRows = 64 / kChunks, kLoads = 16 / kRows;          // of 16 rows
-  int length, lane;
-  uint32_t lane_part;
-
-  __device__ __forceinline__ PageLoader(int length_, int lane_) : length(length_), lane(lane_) {
-    const int r = lane / kChunks;
-    lane_part = (uint32_t)(r * 2 * D) + (uint32_t)(((lane % kChunks) ^ tile_key<D>(r)) << 4);
-  }
-  // Where 16 positions are: elements from the start of the pages, -1 where they have no page.
-  static __device__ __forceinline__ int64_t place(const PageTable& c, int k_head, int64_t position, int page) { return page < 0 ? -1 : c.token_at(page, k_head, (int)position) * D; }
-  __device__ __forceinline__ void operator()(const uint16_t* pages, int64_t position, int64_t place, uint32_t lds) const {
-    if (place >= 0 && position + 16 <= length) {
-      const uint64_t at = reinterpret_cast<uint64_t>(pages + place);
+// Positions of a head from their pages into LDS: GROUPS times 16, as a page has 16 or more.  page(i): of the i-th 16.  Positions from `length` on are zeros, those without a page NaN.  STREAM: they are read once.
+template <int D, int GROUPS, bool STREAM, class F>
+__device__ __forceinline__ void load_positions(const PageTable& c, const uint16_t* pages, int k_head, int64_t position, int length, uint32_t lds, F&& page) {
+  constexpr int kChunks = D / 8, kRows = 64 / kChunks, kLoads = 16 / kRows;          // rows of an instruction; instructions of 16 rows
+  constexpr int kUnroll = GROUPS == 1 ? 1 : kLoads;          // where a wave has the one group, the kernel has no room for more of the rarer path
+  uint32_t l = threadIdx.x & 63;
+  const uint32_t part = (l / kChunks) * (uint32_t)(2 * D) + (((l % kChunks) ^ (uint32_t)tile_key<D>((int)l / kChunks)) << 4);
+#pragma unroll 1
+  for (int i = 0; i < GROUPS; ++i) {
+    const int its = page(i);
+    const int64_t from = position + 16 * i;
+    if (its >= 0 && from + 16 <= length) {
+      const uint64_t at = reinterpret_cast<uint64_t>(pages + c.token_at(its, k_head, (int)from) * D);
       const uint64_t uniform = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)at);
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const uint32_t off = (uint32_t)(i * kRows * 2 * D) + (lane_part ^ key_of(i)), to = lds + (uint32_t)(i * 1024);
+      for (int j = 0; j < kLoads; ++j) {
+        const uint32_t off = (uint32_t)(j * kRows * 2 * D) + (part ^ (uint32_t)(tile_key<D>(j * kRows) << 4)), to = lds + (uint32_t)(i * 32 * D + j * 1024);
         if constexpr (STREAM) stream_to_lds(reinterpret_cast<const void*>(uniform), off, to);
         else load_to_lds_base_off(reinterpret_cast<const void*>(uniform), off, to);
       }
     } else {
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        uint32_t l = (uint32_t)lane;
-        keep(l);                     // or what this needs, once or twice for a sequence, has registers all along
-        const int r = i * kRows + (int)l / kChunks;
-        const unsigned char* at = reinterpret_cast<const unsigned char*>(pages + max(place, (int64_t)0)) + (uint32_t)(r * 2 * D) + ((l % kChunks ^ (uint32_t)tile_key<D>(r)) << 4);
-        if (place < 0) at = reinterpret_cast<const unsigned char*>(&kNanChunk);
-        if (position + r >= length) at = reinterpret_cast<const unsigned char*>(&kZeroChunk);
-        load_to_lds(at, lds + (uint32_t)(i * 1024));
+      keep(l);                       // or what this needs, once or twice for a sequence, has registers all along
+      const unsigned char* real = reinterpret_cast<const unsigned char*>(its < 0 ? reinterpret_cast<const uint16_t*>(&kNanChunk) : pages + c.token_at(its, k_head, (int)from) * D);
+#pragma unroll kUnroll
+      for (int j = 0; j < kLoads; ++j) {
+        const int r = j * kRows + (int)l / kChunks;
+        const uint32_t off = its < 0 ? 0u : (uint32_t)(r * 2 * D) + ((l % kChunks ^ (uint32_t)tile_key<D>(r)) << 4);
+        load_to_lds(from + r < length ? real + off : reinterpret_cast<const unsigned char*>(&kZeroChunk), lds + (uint32_t)(i * 32 * D + j * 1024));
       }
     }
   }
-  static __device__ __forceinline__ uint32_t key_of(int i) { return (uint32_t)(tile_key<D>(i * kRows) << 4); }
-};
+}
 
 // Whether any value of a tile is no finite number: whose exponent is all ones.
 template <int D>
@@ -306,21 +299,8 @@ __device__ __forceinline__ int look_up_pages(const PageTable& c, const DraftItem
   const int64_t position = ((int64_t)tile + (int64_t)(lane >> bits) * EVERY) * kDraftKeys + ((lane & ((1 << bits) - 1)) << c.page_shift);
   return position < item.length ? c.page_of(item.sequence, (int)position) : -1;
 }
-template <int EVERY>
-struct PagesAhead {
-  const PageTable& c;
-  const DraftItem& item;
-  int bits, pages, entry;
-  __device__ __forceinline__ PagesAhead(const PageTable& c_, const DraftItem& item_, int pages_) : c(c_), item(item_), bits(page_bits(c_)), pages(pages_), entry(0) {}
-  __device__ __forceinline__ void advance(int tile) {        // to `tile`, the one after that of `entry`
-    if (++entry == 64 >> bits) {
-      pages = look_up_pages<EVERY>(c, item, tile);
-      entry = 0;
-    }
-  }
-  // Of position `place` of the tile.
-  __device__ __forceinline__ int operator()(int place) const { return __builtin_amdgcn_readlane(pages, (entry << bits) + (place >> c.page_shift)); }
-};
+// Of position `place` of the entry-th of those tiles.
+__device__ __forceinline__ int page_at(const PageTable& c, int pages, int entry, int place) { return __builtin_amdgcn_readlane(pages, (entry << page_bits(c)) + (place >> c.page_shift)); }
 
 // What a workgroup does after a tile of rows: the next one, its steps from 0 to `to`, and its pages, which look_up() finds.
 struct DraftNext {
@@ -465,32 +445,31 @@ __global__ void __launch_bounds__(64 * kDraftWaves, (DraftShape<D, 32>::kPerCu))
 
   auto look_up = [&](const DraftItem& item, int from) { return look_up_pages<kDraftWaves>(a.c, item, from * kDraftWaves + wave); };
   bool fetched = false;              // the first keys are on their way
-  int64_t places[4];                 // of the last keys that were fetched
-  deal<D, ROWS>(a, share, k_head, group, look_up, [&](const DraftItem& item, int from, int to, int all, int place, int first_pages, DraftNext& next, auto&& look_up_next) {
+  deal<D, ROWS>(a, share, k_head, group, look_up, [&](const DraftItem& item, int from, int to, int all, int place, int pages, DraftNext& next, auto&& look_up_next) {
     const int rows = item.tokens.length * group, first_row = item.tile * ROWS;
     const int end = min(to * kDraftWaves, (item.length + kDraftKeys - 1) / kDraftKeys);
     const int whole = min(min(item.length - item.tokens.length, item.length) / kDraftKeys, end);      // tiles that all rows look at whole (none where the block is longer than the sequence)
-    int t = from * kDraftWaves + wave;
-    PagesAhead<kDraftWaves> pages(a.c, item, first_pages);
-    auto fetch = [&](const uint16_t* from_pages, int length, int tile, uint32_t lds) {
-      const PageLoader<D, true> loader(length, lane);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) loader(from_pages, (int64_t)tile * kDraftKeys + 16 * i, places[i], lds + (uint32_t)(16 * i * 2 * D));
+    int t = from * kDraftWaves + wave, entry = 0;            // the wave's tile, and which of `pages` is its
+    auto fetch = [&](const uint16_t* from_pages, int length, int tile, int pages, int entry, uint32_t lds) {
+      load_positions<D, 4, true>(a.c, from_pages, k_head, (int64_t)tile * kDraftKeys, length, lds, [&](int i) { return page_at(a.c, pages, entry, 16 * i); });
     };
-    auto fetch_keys = [&](const PagesAhead<kDraftWaves>& pages, int length, int tile) {      // and note where the values are
-#pragma unroll
-      for (int i = 0; i < 4; ++i) places[i] = PageLoader<D, true>::place(a.c, k_head, (int64_t)tile * kDraftKeys + 16 * i, pages(16 * i));
-      fetch(a.k_pages, length, tile, k_lds);
-    };
-    auto fetch_next_keys = [&] {                             // of the next tile of rows: this wave's first
-      fetched = next.there && wave < min(next.to * kDraftWaves, (next.item.length + kDraftKeys - 1) / kDraftKeys);
-      if (fetched) fetch_keys(PagesAhead<kDraftWaves>(a.c, next.item, next.pages), next.item.length, wave);
-      return fetched;
+    // the keys after those of tile t: of the next tile, or the first of the next tile of rows; whether there are any
+    auto fetch_more = [&] {
+      const int then = t + kDraftWaves;
+      const bool more = then < end;
+      if (more && ++entry == 64 >> page_bits(a.c)) {
+        pages = look_up_pages<kDraftWaves>(a.c, item, then);
+        entry = 0;
+      }
+      if (!more) fetched = next.there && wave < min(next.to * kDraftWaves, (next.item.length + kDraftKeys - 1) / kDraftKeys);
+      if (more || fetched) fetch(a.k_pages, more ? item.length : next.item.length, more ? then : wave, more ? pages : next.pages, more ? entry : 0, k_lds);
+      return more || fetched;
     };
     if (t < end) {
-      if (!fetched) fetch_keys(pages, item.length, t);
-      fetch(a.v_pages, item.length, t, v_lds);
+      if (!fetched) fetch(a.k_pages, item.length, t, pages, 0, k_lds);
+      fetch(a.v_pages, item.length, t, pages, 0, v_lds);
     }
+    fetched = false;
     const DraftRows row(a, item, first_row + (lane & 31), k_head, group);
     bf16x8 qf[kSteps];
     load_fragments<D>(qf, a.q.at(item.tokens.first + row.token, row.head), lane);
@@ -499,8 +478,6 @@ __global__ void __launch_bounds__(64 * kDraftWaves, (DraftShape<D, 32>::kPerCu))
     sums.clear();
     auto take = [&](auto is_masked) __attribute__((always_inline)) {
       constexpr bool masked = decltype(is_masked)::value;
-      const int then = t + kDraftWaves;
-      const bool more = then < end;
       f32x16 x[2];
       u32x4 p[4];
       __builtin_amdgcn_sched_barrier(0);
@@ -516,13 +493,7 @@ __global__ void __launch_bounds__(64 * kDraftWaves, (DraftShape<D, 32>::kPerCu))
       __builtin_amdgcn_sched_barrier(0);
       wait_vmcnt_lgkmcnt<63, 0>();
       __builtin_amdgcn_sched_barrier(0);
-      bool behind = more;                                    // a tile of keys is on its way behind the values
-      if (more) {
-        pages.advance(then);
-        fetch_keys(pages, item.length, then);
-      } else {
-        behind = fetch_next_keys();
-      }
+      const bool behind = fetch_more();                      // a tile of keys is on its way behind the values
       uint64_t seen = 0;
       if constexpr (masked) {
         seen = row.seen(a, item, t);
@@ -540,10 +511,10 @@ __global__ void __launch_bounds__(64 * kDraftWaves, (DraftShape<D, 32>::kPerCu))
       __builtin_amdgcn_sched_barrier(0);
       wait_vmcnt_lgkmcnt<63, 0>();
       __builtin_amdgcn_sched_barrier(0);
-      if (more) fetch(a.v_pages, item.length, then, v_lds);
-      t = then;
+      if (t + kDraftWaves < end) fetch(a.v_pages, item.length, t + kDraftWaves, pages, entry, v_lds);
+      t += kDraftWaves;
     };
-    if (t >= end) fetch_next_keys();
+    if (t >= end) fetch_more();
     while (t < whole) take(std::false_type{});
     while (t < end) take(std::true_type{});
 
@@ -617,47 +588,42 @@ __global__ void __launch_bounds__(64 * kDraftWaves, 2) draft_attention_wide_kern
   // Tiles of all tiles of rows are numbered on: the keys of number n are in slot n & 1, the values in 2 + that.
   int number = 0;
   bool fetched = false;              // the first keys and values and the second keys are on their way
-  int64_t key_place = 0, value_place = 0;
-  deal<D, ROWS>(a, share, k_head, group, look_up, [&](const DraftItem& item, int from, int to, int all, int place, int first_pages, DraftNext& next, auto&& look_up_next) {
+  int key_page = 0, value_page = 0;  // of the last keys that were fetched, and of those before them
+  deal<D, ROWS>(a, share, k_head, group, look_up, [&](const DraftItem& item, int from, int to, int all, int place, int pages, DraftNext& next, auto&& look_up_next) {
     const int whole = min(min(item.length - item.tokens.length, item.length) / kDraftKeys, to);
-    PagesAhead<1> pages(a.c, item, first_pages);
     const int first_number = number;
     number += to - from;
     auto slot_of = [&](int t) { return first_number + t - from & 1; };
-    // A wave fetches a quarter of a tile.  Keys are fetched two tiles ahead, values one, from the places that the keys had; towards the end those of the next tile of rows.
+    // A wave fetches a quarter of a tile.  Keys are fetched two tiles ahead, values one, from the pages that the keys had; towards the end those of the next tile of rows.
     const bool follow = kFollow && next.there && next.to >= 2 && to - from >= 2;
-    auto fetch_k = [&](const DraftItem& item, PagesAhead<1>& pages, int t, int slot) {
-      value_place = key_place;
-      key_place = PageLoader<D, STREAM>::place(a.c, k_head, (int64_t)t * kDraftKeys + 16 * wave, pages(16 * wave));
-      pages.advance(t + 1);
-      PageLoader<D, STREAM>(item.length, lane)(a.k_pages, (int64_t)t * kDraftKeys + 16 * wave, key_place, lds + (uint32_t)(slot * S::kTileBytes + 16 * wave * 2 * D));
+    int entry = 0;                                           // of `pages`: that of the keys to come
+    auto fetch_k = [&](bool mine, int t, int slot) {
+      const int length = mine ? item.length : next.item.length;
+      value_page = key_page;
+      key_page = page_at(a.c, mine ? pages : next.pages, mine ? entry : t, 16 * wave);
+      if (mine && ++entry == 64 >> page_bits(a.c)) {
+        pages = look_up_pages<1>(a.c, item, t + 1);
+        entry = 0;
+      }
+      load_positions<D, 1, STREAM>(a.c, a.k_pages, k_head, (int64_t)t * kDraftKeys + 16 * wave, length, lds + (uint32_t)(slot * S::kTileBytes + 16 * wave * 2 * D), [&](int) { return key_page; });
     };
-    auto fetch_v = [&](const DraftItem& item, int t, int64_t at, int slot) {
-      PageLoader<D, STREAM>(item.length, lane)(a.v_pages, (int64_t)t * kDraftKeys + 16 * wave, at, lds + (uint32_t)((2 + slot) * S::kTileBytes + 16 * wave * 2 * D));
+    auto fetch_v = [&](bool mine, int t, int page, int slot) {
+      load_positions<D, 1, STREAM>(a.c, a.v_pages, k_head, (int64_t)t * kDraftKeys + 16 * wave, mine ? item.length : next.item.length,
+                                   lds + (uint32_t)((2 + slot) * S::kTileBytes + 16 * wave * 2 * D), [&](int) { return page; });
     };
     if (!fetched) {
-      fetch_k(item, pages, from, slot_of(from));
-      fetch_v(item, from, key_place, slot_of(from));
-      if (from + 1 < to) fetch_k(item, pages, from + 1, slot_of(from + 1));
+      fetch_k(true, from, slot_of(from));
+      fetch_v(true, from, key_page, slot_of(from));
+      if (from + 1 < to) fetch_k(true, from + 1, slot_of(from + 1));
     } else {
-      pages.advance(from + 1);
-      pages.advance(from + 2);
+      entry = 2;                                             // (a table of 64 has the pages of 16 tiles or more)
     }
     fetched = follow;
     auto turn = [&](int t) __attribute__((always_inline)) {
       publish();
-      if (t + 2 < to) {
-        fetch_k(item, pages, t + 2, slot_of(t));
-        fetch_v(item, t + 1, value_place, slot_of(t + 1));
-      } else if (follow) {
-        PagesAhead<1> its(a.c, next.item, next.pages);
-        const int then = its.entry = t + 2 - to;             // 0, then 1
-        fetch_k(next.item, its, then, slot_of(t));
-        if (then == 0) fetch_v(item, t + 1, value_place, slot_of(t + 1));
-        else fetch_v(next.item, 0, value_place, slot_of(t + 1));
-      } else if (t + 1 < to) {
-        fetch_v(item, t + 1, key_place, slot_of(t + 1));
-      }
+      const bool k_mine = t + 2 < to, v_mine = t + 1 < to;
+      if (k_mine || follow) fetch_k(k_mine, k_mine ? t + 2 : t + 2 - to, slot_of(t));
+      if (v_mine || follow) fetch_v(v_mine, v_mine ? t + 1 : 0, k_mine || follow ? value_page : key_page, slot_of(t + 1));
     };
     const DraftRows row(a, item, item.tile * ROWS + row_wave * 32 + (lane & 31), k_head, group);
     bf16x8 qf[kSteps];
