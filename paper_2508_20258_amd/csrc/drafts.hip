@@ -80,20 +80,31 @@ auto for_shape(int d, int rows, F&& f) {
   });
 }
 
+// Rows of a tile.  32 heads of 128 sharing 8, us in tiles of 32, 64 and 128 rows: blocks of 32 rows, 32 sequences of 3000 positions 71, 74 and 91; of 64 rows 135, 74 and 88; of 192 381, 225 and 122.  Blocks of 128, 32 sequences
+// of 512 to 8192 positions: 138 in tiles of 64, 96 in tiles of 128 (as two tiles of a block read its positions at different times; at the same time, in 32 sequences of 3000, 89 and 92).  Few positions are soon read
+// again: blocks of 192 rows, 4 sequences of 500 positions 13, 14 and 17.
+int tile_rows(int64_t rows, int64_t longest) { return rows <= 32 ? 32 : rows <= 64 || longest <= 1024 ? 64 : 128; }
+
+// A workgroup for each tile of rows and key head, or the steps of all of them dealt evenly and the parts joined.  The latter takes another launch and the parts' traffic, 6 us and theirs, the former as long as the longest tile, of
+// about 2.7 us for 256 positions (4.2 with 128 rows); lengths are taken to be 0.6 of the longest on average.  Single tokens of 32 heads of 128 sharing 8, the one and the other: 16 sequences of 256 positions 8.8 us and 12.0,
+// of 1024 21.0 and 21.7, of 2048 34.7 and 30.5; one of 512 11.4 and 13.7, of 1024 16.6 and 15.1, of 4096 49 and 18.  Blocks of 128 rows: 16 of 1024 28 and 41, one 25 and 16.
 AttentionPlan attention_plan(const swz_cache16& c, const swz_attention16_args& a) {
   const int64_t group = a.q_heads / c.k_heads, rows = (a.tokens + a.sequences - 1) / a.sequences * group;          // of an average block
   const int64_t cut = (int64_t)a.table_width * c.page_tokens, longest = a.max_length > 0 && a.max_length < cut ? a.max_length : cut;
   AttentionPlan p{};
-  p.rows = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  p.rows = tile_rows(rows, longest);
   p.once = rows <= p.rows;
   p.join_groups = 1;
-  for_shape(c.head_dim, p.rows, [&](auto dim, auto rows) {
-    using S = swz::DraftShape<decltype(dim)::value, decltype(rows)::value>;
+  for_shape(c.head_dim, p.rows, [&](auto dim, auto of_tile) {
+    using S = swz::DraftShape<decltype(dim)::value, decltype(of_tile)::value>;
     p.items = a.tokens * group / p.rows + a.sequences;
-    const int64_t together = (int64_t)compute_units() * S::kPerCu / c.k_heads, steps = (longest + S::kStep - 1) / S::kStep;
-    if (longest <= 1024) return 0;
-    const int64_t shares = together < 1 ? 1 : together;
-    p.shares = (int)(p.items * steps < shares ? p.items * steps : shares);
+    const int64_t room = (int64_t)compute_units() * S::kPerCu, steps = (longest + S::kStep - 1) / S::kStep + S::kSwitch;
+    const int64_t tiles = (a.tokens * group + p.rows - 1) / p.rows > a.sequences ? (a.tokens * group + p.rows - 1) / p.rows : a.sequences;       // about as many as there are
+    const int64_t shares = room / c.k_heads < 1 ? 1 : room / c.k_heads < tiles * steps ? room / c.k_heads : tiles * steps;
+    const double whole = (p.rows == 128 ? 4.2 : 2.7) / 256 * longest, filled = (double)tiles * c.k_heads / room;
+    const double parts = (double)shares * c.k_heads * p.rows * c.head_dim * 4 * 2 / 5e6;
+    if (whole * (filled > 1 ? filled : 1) <= 0.6 * whole * filled + 6 + parts) return 0;
+    p.shares = (int)shares;
     p.join_groups = p.shares > 4 * (a.tokens * group / p.rows + 1) ? 8 : 1;          // parts of a tile of rows, about
     return 0;
   });
