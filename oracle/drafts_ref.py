@@ -29,14 +29,12 @@ def looked_at(n: int, length: int, masks=None) -> np.ndarray:
 def attention(q, k, v, scale, seen):
     """(out, bound) of one head: q (n, d), k, v (length, d) float64, seen (n, length)."""
     out, size = np.zeros(q.shape), np.zeros(q.shape)
-    for i in range(len(q)):
-        j = np.flatnonzero(seen[i])
-        if len(j) == 0:
-            continue
-        s = scale * (k[j] @ q[i])
-        e = np.exp(s - s.max())
-        e /= e.sum()
-        out[i], size[i] = e @ v[j], e @ np.abs(v[j])
+    rows = seen.any(1)
+    if rows.any():
+        s = np.where(seen[rows], scale * (q[rows] @ k.T), -np.inf)
+        e = np.exp(s - s.max(1, keepdims=True))
+        e /= e.sum(1, keepdims=True)
+        out[rows], size[rows] = e @ v, e @ np.abs(v)
     return out, 1.02 * ROUND * (size + np.abs(out)) + SLACK * size + 1e-30
 
 

@@ -198,7 +198,7 @@ int swz_cache16_attention(const swz_cache16* cache, const swz_attention16_args* 
   a.stats = a.sums + attention_places(*cache, p) * cache->head_dim;
   a.parts = reinterpret_cast<int2*>(a.stats + attention_places(*cache, p) * 2);
   a.total = (int)args->tokens, a.sequences = args->sequences, a.q_heads = args->q_heads, a.items = (int)p.items, a.shares = p.shares, a.scale = args->scale;
-  const int64_t workgroups = (p.shares == 0 ? p.items : p.shares) * cache->k_heads, joins = p.items * (p.rows / 32) * p.join_groups * cache->k_heads;
+  const int64_t workgroups = (p.shares == 0 ? p.items : p.shares) * cache->k_heads, joins = p.shares == 0 ? 0 : p.items * (p.rows / 32) * p.join_groups * cache->k_heads;
   if (workgroups * 256 > swz::kLaunchThreads || joins * 256 > swz::kLaunchThreads) return SWZ_ERR_OVERFLOW;
   return for_shape(cache->head_dim, p.rows, [&](auto dim, auto rows) {
     constexpr int D = decltype(dim)::value, ROWS = decltype(rows)::value;

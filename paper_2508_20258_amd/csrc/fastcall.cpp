@@ -404,7 +404,7 @@ PyObject* cache16_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if ((args[8] != Py_None) != turned || (!turned && (queries || args[9] != Py_None))) return nullptr;
     if (turned) {
       const at::Tensor *cos = plain(args[7], dev), *sin = plain(args[8], dev);
-      if (!is_type(cos, 2, at::kFloat) || !is_type(sin, 2, at::kFloat) || cos->sizes() != sin->sizes() || cos->size(1) > 1024) return nullptr;
+      if (!is_type(cos, 2, at::kFloat) || !is_type(sin, 2, at::kFloat) || cos->sizes() != sin->sizes() || cos->size(1) > 1024 || cos->numel() == 0) return nullptr;
       a.cos = static_cast<const float*>(cos->data_ptr()), a.sin = static_cast<const float*>(sin->data_ptr());
       a.table_rows = cos->size(0), a.rotary_dim = static_cast<int32_t>(2 * cos->size(1));
     }

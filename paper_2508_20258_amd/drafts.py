@@ -107,7 +107,7 @@ def cache16_append(cache: Cache16, k, v, cu, before, block_table, q=None, cos=No
     assert (cos is None) == (sin is None) and (cos is not None or (q is None and positions is None)) and (q is not None or q_out is None)
     if cos is not None:
         for t in (cos, sin):
-            assert t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.dim() == 2 and t.shape == cos.shape
+            assert t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.dim() == 2 and t.shape == cos.shape and t.numel() > 0
         a.cos, a.sin, a.rotary_dim, a.table_rows = cos.data_ptr(), sin.data_ptr(), 2 * cos.shape[1], cos.shape[0]
         used += [cos, sin]
     if positions is not None:

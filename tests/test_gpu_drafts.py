@@ -222,6 +222,30 @@ def test_attention(swz, nodes, lens, q_heads, k_heads, page, dim, known, branch)
 
 
 @pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("nodes,lens,q_heads,k_heads", [
+    ([1] * 20 + [0, 3, 2], [700, 1, 0, 64, 65, 256, 257, 300, 30, 511, 513, 90, 800, 12, 128, 129, 640, 33, 1000, 5, 70, 3, 900], 64, 64),
+    ([40, 64, 33, 0, 50, 12, 60, 41, 64, 38, 1, 55], [64, 600, 90, 500, 50, 700, 128, 129, 1000, 320, 640, 200], 64, 64),
+    ([64, 1, 50, 64, 0, 40, 64, 33, 64, 64], [1100, 900, 70, 128, 300, 40, 700, 64, 129, 66], 128, 64),
+    ([64, 20, 64, 31, 64], [300, 1500, 64, 200, 257], 128, 32),
+    ([30] * 70, [30 + (i * 53) % 400 for i in range(70)], 32, 16)])
+def test_tiles_of_rows_one_after_another(swz, nodes, lens, q_heads, k_heads, dim):
+    """Many key heads, so that a workgroup goes from one tile of rows to the next, of one step or many, and from sequence to sequence."""
+    page = 16
+    rows, pages = table_of(lens, page, width=400)
+    cache = filled(swz, pages, k_heads, dim, page, math.nan)
+    for b, n in enumerate(lens):
+        for p in range(0, n, page):
+            for x, s in zip(cache, (1, 2)):
+                x[rows[b][p // page], :, :min(page, n - p)] = randn(100 * b + p + s, k_heads, min(page, n - p), dim)
+    q = randn(5, sum(nodes), q_heads, dim, scale=2.0)
+    masks = masks_of(nodes, 2)
+    args = (q, cache, cu_of(nodes), ints(lens), ints(rows))
+    for m in (masks, None):
+        out = swz.cache16_attention(*args, tree=None if m is None else ints([x for block in m for x in block], torch.int64))
+        check_attention(q, cache, out, nodes, lens, rows, m)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("nodes,lens", [([100, 65, 1], [100, 300, 70]), ([200], [1000]), ([300], [200])])
 def test_pieces_of_prompts(swz, nodes, lens, dim):
     """Blocks of any length without masks; with masks the tokens from the 65th on are looked at by none."""
