@@ -52,7 +52,7 @@ int swz_cache16_append(const swz_cache16* cache, const swz_append16_args* args, 
  * before: token j of n is position lengths[b] - n + j.  A token looks at all positions before the block, and
  *   tree null     : at the block's tokens up to itself (a chain, or the next piece of a prompt, of any length);
  *   tree not null : at token j of its block where bit j of the token's 64-bit mask is set; at those from the 65th on none looks.
- * A token that looks at nothing gets 0.  A length is cut to the table's positions; pages that the cache has not give NaN to what looks at them.  Infinities and NaN in keys and
+ * A token that looks at nothing gets 0, and so does one whose scores are all minus infinity.  A length is cut to the table's positions; pages that the cache has not give NaN to what looks at them.  Infinities and NaN in keys and
  * values that a token does not look at do not reach its output.  The weights are rounded to bfloat16 for their product with v, their sum is not.
  *   q, out : `tokens` tokens of q_heads heads, query head h looking at key head h / (q_heads / k_heads).
  *   max_length : the longest length, or more (0: the table's); it decides how many workgroups share the work, no more: longer lengths are right too, and slower.

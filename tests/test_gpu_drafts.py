@@ -347,6 +347,50 @@ def test_attention_layouts(swz, dim):
         swz.cache16_attention(q, *args, tree=torch.zeros(14, dtype=torch.int64, device="cuda"))
 
 
+@pytest.mark.parametrize("max_length", [0, 64])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("q_heads,nodes", [(1, [6, 2, 1, 0]), (8, [8, 7, 5, 1]), (16, [20, 40, 9, 8])])
+def test_sequences_that_share_pages(swz, dim, q_heads, nodes, max_length):
+    """A prompt that several sequences begin with stands in the cache once; one of them has a page of it twice."""
+    lens, page = [300, 217, 160, 256], 16
+    rows, pages = table_of(lens, page, width=300)
+    for r in rows[1:]:
+        r[:8] = rows[0][:8]
+    rows[2][3] = rows[2][2]
+    cache = swz.Cache16(randn(1, pages, 1, page, dim), randn(2, pages, 1, page, dim))
+    q = randn(3, sum(nodes), q_heads, dim, scale=2.0)
+    masks = masks_of(nodes, 2)
+    out = swz.cache16_attention(q, cache, cu_of(nodes), ints(lens), ints(rows), tree=ints([m for block in masks for m in block], torch.int64), max_length=max_length)
+    check_attention(q, cache, out, nodes, lens, rows, masks)
+
+
+@pytest.mark.parametrize("max_length", [0, 64])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("q_heads", [1, 8, 16])
+def test_scores_of_minus_infinity(swz, dim, q_heads, max_length):
+    """As if the position were not looked at; nothing but such scores: 0."""
+    nodes, lens, page = [9, 12], [400, 130], 16
+    rows, pages = table_of(lens, page, width=300)
+    cache = swz.Cache16(randn(1, pages, 1, page, dim), randn(2, pages, 1, page, dim))
+    q = randn(3, sum(nodes), q_heads, dim)
+    q[..., 3] = 1
+    gone = [(0, p) for p in range(400) if p % 7 == 0 or 64 <= p < 200 or p < 20] + [(1, p) for p in range(130)]
+    for b, p in gone:
+        cache.k[rows[b][p // page], 0, p % page, 3] = -math.inf
+    out = swz.cache16_attention(q, cache, cu_of(nodes), ints(lens), ints(rows), max_length=max_length)
+    assert not out[9:].any()
+    # the others' alone: the positions before the block that are left, and a chain of its tokens that misses some
+    left = [p for p in range(391) if (0, p) not in gone]
+    dense = swz.kv_cache16(40, 1, dim, page)
+    places = left + list(range(391, 400))
+    for i, p in enumerate(places):
+        for x, y in zip(dense, cache):
+            x[i // page, 0, i % page] = y[rows[0][p // page], 0, p % page]
+    dense.k[:, :, :, 3].clamp_(min=-100)
+    masks = [[sum(1 << j for j in range(i + 1) if (0, 391 + j) not in gone) for i in range(9)]]
+    check_attention(q[:9], dense, out[:9], [9], [len(places)], [list(range(40))], masks)
+
+
 @pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("scale,size", [(0.02, 1.0), (1.0, 3.0)])
 def test_attention_scales(swz, dim, scale, size):
@@ -630,3 +674,36 @@ def test_a_step_in_a_graph(swz):
             assert all(torch.equal(a, b) for a, b in zip(outs, wants[seed])), (turn, [torch.equal(a, b) for a, b in zip(outs, wants[seed])])
         step(inputs(seed))
         torch.cuda.synchronize()
+
+
+def test_steps_on_two_streams_at_once(swz):
+    """Two batches with a cache each, every call on a stream of its own, none waiting for the other's: the results of one after the other."""
+    q_heads, k_heads, dim, page, vocab, nodes = 8, 2, 64, 32, 20000, [6] * 12
+    n, lens = sum(nodes), [100 + 150 * i for i in range(12)]
+    rows, pages = table_of([m + 6 for m in lens], page)
+    table, cu, before, after = ints(rows), cu_of(nodes), ints(lens), ints([m + 6 for m in lens])
+    cos, sin = angles(2000, dim // 2)
+    parents = ints([max(0, (i - 1) // 2) for m in nodes for i in range(m)])
+    tree = ints([m for block in masks_of(nodes, 2) for m in block], torch.int64)
+    tokens = torch.randint(0, vocab, (n,), generator=torch.Generator().manual_seed(3)).to(torch.int32).cuda()
+
+    def state(seed):
+        target, draft = probabilities(seed, n, vocab, False)
+        return dict(cache=swz.Cache16(randn(seed, pages, k_heads, page, dim), randn(seed + 1, pages, k_heads, page, dim)), k=randn(seed + 2, n, k_heads, dim), v=randn(seed + 3, n, k_heads, dim),
+                    q=randn(seed + 4, n, q_heads, dim), target=target, draft=draft, uniforms=torch.rand(n, generator=torch.Generator().manual_seed(seed)).cuda())
+
+    def step(s, stream):
+        q = swz.cache16_append(s["cache"], s["k"], s["v"], cu, before, table, q=s["q"], cos=cos, sin=sin, stream=stream)
+        out = swz.cache16_attention(q, s["cache"], cu, after, table, tree=tree, stream=stream)
+        results = swz.verify_drafts(s["target"], tokens, cu, s["uniforms"], draft_probs=s["draft"], parents=parents, stream=stream)
+        swz.cache16_keep(s["cache"], cu, before, results[1], results[0], table, stream=stream)
+        return [q, out, *results, *s["cache"]]
+
+    wants = [step(state(seed), None) for seed in (1, 2)]
+    states, streams = [[state(seed) for _ in range(5)] for seed in (1, 2)], [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[step(states[i][turn], streams[i]) for i in range(2)] for turn in range(5)]
+    torch.cuda.synchronize()
+    for turn in got:
+        for mine, want in zip(turn, wants):
+            assert all(torch.equal(a, b) for a, b in zip(mine, want))
