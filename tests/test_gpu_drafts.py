@@ -707,3 +707,46 @@ def test_steps_on_two_streams_at_once(swz):
     for turn in got:
         for mine, want in zip(turn, wants):
             assert all(torch.equal(a, b) for a, b in zip(mine, want))
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_a_cache_beyond_32_bits(swz, dim):
+    """Pages, and their elements, past 2^32 of the cache's start: the results of a small cache."""
+    k_heads, page, nodes, lens = 2, 64, [5, 3], [200, 90]
+    rows, pages = table_of([205, 93], page)
+    far = (1 << 32) // (k_heads * page * dim) + 7
+    small = swz.Cache16(*(randn(i, pages, k_heads, page, dim) for i in range(2)))
+    big = swz.Cache16(*(torch.empty((far + pages, k_heads, page, dim), dtype=torch.bfloat16, device="cuda") for _ in range(2)))
+    k, v, q = randn(3, 8, k_heads, dim), randn(4, 8, k_heads, dim), randn(5, 8, 8, dim)
+    cos, sin = angles(300, dim // 2)
+    path, accepted = ints([0, 2, 4, -1, -1, 0, 2, -1]), ints([2, 1])
+    results, held = [], [x.clone() for x in small]
+    for x, y in zip(big, small):
+        x[far:] = y
+    for cache, first in ((small, 0), (big, far)):
+        table = ints([[p + first if p >= 0 else -1 for p in r] for r in rows])
+        turned = swz.cache16_append(cache, k, v, cu_of(nodes), ints(lens), table, q=q, cos=cos, sin=sin)
+        out = [swz.cache16_attention(turned, cache, cu_of(nodes), ints([a + b for a, b in zip(lens, nodes)]), table, max_length=m) for m in (0, 64)]
+        swz.cache16_keep(cache, cu_of(nodes), ints(lens), path, accepted, table)
+        results.append([turned, *out, *(x[first:] for x in cache)])
+    assert not any(torch.equal(a, b) for a, b in zip(held, small))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+@pytest.mark.parametrize("drawn", [False, True])
+def test_probabilities_beyond_32_bits(swz, drawn):
+    """Rows that start past 2^32 elements from the first one."""
+    vocab, pitch, total = 5000, (1 << 31) - 8, 5
+    target, draft = probabilities(7, total, vocab, True)
+    wide = torch.empty(pitch * (total - 1) + vocab, dtype=torch.bfloat16, device="cuda").as_strided((total, vocab), (pitch, 1))
+    parents = ints([0, 0, 0, 2, 2])
+    tokens = ints([0, int(draft[0].argmin()), int(target[0].argmax()), int(target[2].argmin()), int(target[2].argmax())])
+    uniforms = torch.tensor([0.7, 0.9, 0.01, 0.99, 0.01], device="cuda")
+    call = dict(parents=parents, draft_probs=draft if drawn else None)
+    want = swz.verify_drafts(target, tokens, cu_of([total]), uniforms, **call)
+    check_verify(want, target, tokens, uniforms, [total], draft if drawn else None, parents)
+    wide.copy_(target)
+    assert all(torch.equal(a, b) for a, b in zip(swz.verify_drafts(wide, tokens, cu_of([total]), uniforms, **call), want))
+    if drawn:
+        wide.copy_(draft)
+        assert all(torch.equal(a, b) for a, b in zip(swz.verify_drafts(target, tokens, cu_of([total]), uniforms, parents=parents, draft_probs=wide), want))
