@@ -13,8 +13,8 @@
 //
 // What bounds it: the cache's bytes up to about 250 rows of a block (4 D bytes and 4 D operations a row for each position and key head, at 6.4 TB/s and 1600 TFLOP/s), products beyond.  With 32 query heads of 128:
 // 64 single tokens, sharing 8 key heads, over 151000 positions in all (620 MB) 98 us, 6.3 TB/s, and 4.6 for the join; one over 131072 positions (537 MB) 84 us, 6.4 TB/s, and 5.  32 blocks of 32 tokens over 94000
-// positions (388 MB) 87 us, 4.4 TB/s, and 11: the parts of 512 workgroups, 52 MB, are written and read beside it.  A block of 64 tokens, sharing 4 key heads, over 131072 positions, 137 GFLOP, 148 us and 9,
-// 0.93 PFLOP/s: the matrix units work for 52 % of the cycles, the vector unit for 46 %, at 1.76 GHz.
+// positions (388 MB) 87 us, 4.4 TB/s, and 11: the parts of 512 workgroups, 52 MB, are written and read beside it.  A block of 64 tokens, sharing 4 key heads, over 131072 positions, 137 GFLOP, 142 us and 8.4,
+// 0.97 PFLOP/s: the matrix units work for 53 % of the cycles, the vector unit for 46 %, at 1.76 GHz.
 //
 // Loads go straight to LDS.  Streaming ones, where positions are read once: 64 single tokens 105 us, with regular ones 121.  More tiles on their way in LDS, or fewer bytes a wave and more waves, changed
 // nothing: 5.8 TB/s was what regular loads reach in a kernel that does nothing else.
@@ -577,6 +577,11 @@ __global__ void __launch_bounds__(64 * kDraftWaves, (DraftShape<D, 32>::kPerCu))
   });
 }
 
+// Where the waves of wide tiles leave their sums of 32 rows, from row `at` of all places on: as they have them, a lane's four dimensions of `chunk` beside the next lane's, which are another row's (row by row, 16 bytes
+// of 64 rows with a store: 148 us for 142 with a block of 64 tokens over 131072 positions).
+template <int D>
+__device__ __forceinline__ f32x4* wide_sums(const DraftArgs& a, int64_t at, int chunk, int lane) { return reinterpret_cast<f32x4*>(a.sums + at * D + (chunk * 64 + lane) * 4); }
+
 // Pairs of weights taken before a slot, if all `pairs` of them are by slot `last`.
 constexpr int pairs_before(int slot, int pairs, int last) { return slot >= last ? pairs : (slot * pairs + last - 1) / last; }
 
@@ -784,19 +789,22 @@ __global__ void __launch_bounds__(64 * kDraftWaves, 2) draft_attention_wide_kern
 #pragma unroll
         for (int i = 0; i < kParts; ++i)
 #pragma unroll
-          for (int r = 0; r < 16; r += 4) *reinterpret_cast<f32x4*>(a.sums + at * D + 32 * i + 2 * r + 4 * h) = f32x4{sums.o[i][r], sums.o[i][r + 1], sums.o[i][r + 2], sums.o[i][r + 3]};
+          for (int r = 0; r < 16; r += 4) *wide_sums<D>(a, at - (lane & 31), 4 * i + r / 4, lane) = f32x4{sums.o[i][r], sums.o[i][r + 1], sums.o[i][r + 2], sums.o[i][r + 3]};
       }
     }
     if constexpr (kRowWaves < kDraftWaves) __syncthreads();
   });
 }
 
-// What several workgroups have of a tile of rows joined, a workgroup for each 32 / GROUPS of its rows and key head, 8 threads a row and GROUPS of them for its parts; and zeros for sequences without positions.
+// What several workgroups have of a tile of rows joined, and zeros for sequences without positions: GROUPS workgroups for each 32 of its rows and key head.  Tiles of 32 rows: a workgroup has 32 / GROUPS rows, 8 threads
+// a row and GROUPS of them for its parts.  Wide ones: a lane has a row, and four dimensions of each of its chunks of 8; a workgroup has 1 / GROUPS of the chunks, and a wave a quarter of those, or (GROUPS 8) of the parts.
 template <int D, int ROWS, int GROUPS>
 __global__ void __launch_bounds__(256) draft_join_kernel(DraftArgs a) {
-  constexpr int kPer = D / 8, kRows = 32 / GROUPS;
-  __shared__ __attribute__((aligned(16))) float joined[GROUPS > 1 ? 32 : 1][D + 4];
-  const int heads = a.c.k_heads, group = a.q_heads / heads, id = (int)blockIdx.x / heads, k_head = (int)blockIdx.x - id * heads, slot = id / (ROWS / kRows), block = id - slot * (ROWS / kRows);
+  constexpr bool kWide = ROWS > 32, kSplit = GROUPS > 1;
+  constexpr int kPer = kWide && kSplit ? D / 16 : D / 8, kRows = kWide ? 32 : 32 / GROUPS, kParts = !kSplit ? 1 : kWide ? 4 : GROUPS;       // numbers of a thread; rows of a workgroup; parts that it takes at a time
+  constexpr int kJoined = !kSplit ? 1 : kWide ? 256 : 32, kJoinedPitch = kWide ? kPer + 4 : D + 4;
+  __shared__ __attribute__((aligned(16))) float joined[kJoined][kJoinedPitch];
+  const int heads = a.c.k_heads, group = a.q_heads / heads, id = (int)blockIdx.x / heads, k_head = (int)blockIdx.x - id * heads, slot = id / (ROWS / 32 * GROUPS), block = id - slot * (ROWS / 32 * GROUPS);
   int64_t items = 0;
   int sequence = -1, tile = 0;
   DraftWindow w;
@@ -815,8 +823,10 @@ __global__ void __launch_bounds__(256) draft_join_kernel(DraftArgs a) {
   });
   if (sequence < 0) return;
   const DraftItem item = w.item(sequence, tile);
-  const int mine = (int)threadIdx.x / 8, part = mine / kRows, in_tile = block * kRows + mine % kRows, row = tile * ROWS + in_tile, d = (int)threadIdx.x % 8 * kPer;
-  if (tile * ROWS + block * kRows >= item.tokens.length * group) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), mine = kWide ? (int)threadIdx.x : (int)threadIdx.x / 8, part = kWide ? (kSplit ? wave : 0) : mine / kRows;
+  const int first_row = kWide ? block / GROUPS * 32 : block * kRows, in_tile = first_row + (kWide ? lane & 31 : mine % kRows), row = tile * ROWS + in_tile;
+  const int chunk = kSplit ? block % GROUPS * (kPer / 4) : wave * (kPer / 4), d = kWide ? 8 * chunk + 4 * (lane >> 5) : (int)threadIdx.x % 8 * kPer;
+  if (tile * ROWS + first_row >= item.tokens.length * group) return;
   const bool real = row < item.tokens.length * group;
   uint16_t* to = a.out.at(item.tokens.first + (real ? row : 0) / group, k_head * group + (real ? row : 0) % group) + d;
   int last = -1, first_part = 0;
@@ -839,38 +849,55 @@ __global__ void __launch_bounds__(256) draft_join_kernel(DraftArgs a) {
     top = now;
   };
 #pragma unroll 2
-  for (int share = first + part; share <= last; share += GROUPS) {
+  for (int share = first + part; share <= last; share += kParts) {
     const int64_t at = (int64_t)(share == first ? first_part : (share * heads + k_head) * 2) * ROWS + in_tile;
     const float2 x = *reinterpret_cast<const float2*>(a.stats + 2 * at);
     f32x4 y[kPer / 4];
 #pragma unroll
-    for (int e = 0; e < kPer / 4; ++e) y[e] = *reinterpret_cast<const f32x4*>(a.sums + at * D + d + 4 * e);
+    for (int e = 0; e < kPer / 4; ++e) y[e] = kWide ? *wide_sums<D>(a, at - (lane & 31), chunk + e, lane) : *reinterpret_cast<const f32x4*>(a.sums + at * D + d + 4 * e);
     if (real) add(x.x, x.y, y);
   }
-  if constexpr (GROUPS > 1) {
+  if constexpr (kSplit) {
+    constexpr int kStats = kJoinedPitch - 4;
+    const int at = kWide ? 0 : d;
     if (part > 0) {
 #pragma unroll
-      for (int e = 0; e < kPer; e += 4) *reinterpret_cast<f32x4*>(&joined[mine][d + e]) = f32x4{o[e], o[e + 1], o[e + 2], o[e + 3]};
-      if (d == 0) joined[mine][D] = top, joined[mine][D + 1] = sum;
+      for (int e = 0; e < kPer; e += 4) *reinterpret_cast<f32x4*>(&joined[mine][at + e]) = f32x4{o[e], o[e + 1], o[e + 2], o[e + 3]};
+      if (at == 0) joined[mine][kStats] = top, joined[mine][kStats + 1] = sum;
     }
     __syncthreads();
     if (part > 0) return;
-    for (int p = 1; p < GROUPS; ++p) {
-      const float* its = joined[mine + p * kRows];
+    for (int p = 1; p < kParts; ++p) {
+      const float* its = joined[mine + p * (kWide ? 64 : kRows)];
       f32x4 y[kPer / 4];
 #pragma unroll
-      for (int e = 0; e < kPer / 4; ++e) y[e] = *reinterpret_cast<const f32x4*>(its + d + 4 * e);
-      add(its[D], its[D + 1], y);
+      for (int e = 0; e < kPer / 4; ++e) y[e] = *reinterpret_cast<const f32x4*>(its + at + 4 * e);
+      add(its[kStats], its[kStats + 1], y);
     }
   }
   if (!real) return;
   const float f = sum == 0.f ? 0.f : 1.f / sum;
+  if constexpr (kWide) {
+    typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+    if constexpr (kPer == 4) {
+      *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(o[0] * f, o[1] * f), pack_bf16(o[2] * f, o[3] * f)};
+    } else {
+      // the halves trade registers so that each lane has a whole chunk, the first or the second of two
 #pragma unroll
-  for (int e = 0; e < kPer; e += 8) {
-    float z[8];
+      for (int e = 0; e < kPer; e += 8) {
+        const auto x = __builtin_amdgcn_permlane32_swap(pack_bf16(o[e] * f, o[e + 1] * f), pack_bf16(o[e + 4] * f, o[e + 5] * f), false, false);
+        const auto y = __builtin_amdgcn_permlane32_swap(pack_bf16(o[e + 2] * f, o[e + 3] * f), pack_bf16(o[e + 6] * f, o[e + 7] * f), false, false);
+        *reinterpret_cast<u32x4*>(to + 2 * e + 4 * (lane >> 5)) = u32x4{x[0], y[0], x[1], y[1]};
+      }
+    }
+  } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) z[i] = o[e + i] * f;
-    *reinterpret_cast<u32x4*>(to + e) = pack8(z);
+    for (int e = 0; e < kPer; e += 8) {
+      float z[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) z[i] = o[e + i] * f;
+      *reinterpret_cast<u32x4*>(to + e) = pack8(z);
+    }
   }
 }
 
