@@ -13,8 +13,8 @@
 //
 // What bounds it: the cache's bytes up to about 250 rows of a block (4 D bytes and 4 D operations a row for each position and key head, at 6.4 TB/s and 1600 TFLOP/s), products beyond.  With 32 query heads of 128:
 // 64 single tokens, sharing 8 key heads, over 151000 positions in all (620 MB) 98 us, 6.3 TB/s, and 4.6 for the join; one over 131072 positions (537 MB) 84 us, 6.4 TB/s, and 5.  32 blocks of 32 tokens over 94000
-// positions (388 MB) 87 us, 4.4 TB/s, and 11: the parts of 512 workgroups, 52 MB, are written and read beside it.  A block of 64 tokens, sharing 4 key heads, over 131072 positions, 137 GFLOP, 142 us and 8.4,
-// 0.97 PFLOP/s: the matrix units work for 53 % of the cycles, the vector unit for 46 %, at 1.76 GHz.
+// positions (388 MB) 87 us, 4.4 TB/s, and 11: the parts of 512 workgroups, 45 MB, are written and read beside it.  A block of 64 tokens, sharing 4 key heads, over 131072 positions, 137 GFLOP, 144 us and 8.3,
+// 0.95 PFLOP/s: the matrix units work for 54 % of the cycles, the vector unit for 47 %, at 1.76 GHz.
 //
 // Loads go straight to LDS.  Streaming ones, where positions are read once: 64 single tokens 105 us, with regular ones 121.  More tiles on their way in LDS, or fewer bytes a wave and more waves, changed
 // nothing: 5.8 TB/s was what regular loads reach in a kernel that does nothing else.
@@ -578,7 +578,7 @@ __global__ void __launch_bounds__(64 * kDraftWaves, (DraftShape<D, 32>::kPerCu))
 }
 
 // Where the waves of wide tiles leave their sums of 32 rows, from row `at` of all places on: as they have them, a lane's four dimensions of `chunk` beside the next lane's, which are another row's (row by row, 16 bytes
-// of 64 rows with a store: 148 us for 142 with a block of 64 tokens over 131072 positions).
+// of 64 rows with a store: 148 us for 144 with a block of 64 tokens over 131072 positions).
 template <int D>
 __device__ __forceinline__ f32x4* wide_sums(const DraftArgs& a, int64_t at, int chunk, int lane) { return reinterpret_cast<f32x4*>(a.sums + at * D + (chunk * 64 + lane) * 4); }
 
