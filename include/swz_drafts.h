@@ -34,8 +34,8 @@ typedef struct {
  *   q.data null: no queries (q_heads is not read).  q_out may be q itself (the same pointer and distances), else it must not overlap anything.
  *   Positions past the table's width, entries that name no page of the cache and sequences whose before is negative are not written to the cache.
  * Errors (all functions here): INVALID_ARG (null pointer, a size or count < 0, heads or sequences < 1, heads not a multiple of one another, a scale that is not finite and > 0, too small a
- * workspace), UNSUPPORTED (head_dim, rotary_dim, page size, element size, alignment, distances), OVERFLOW (counts that do not fit 32-bit indices, a launch of 2^32 threads or more),
- * HIP.  No tokens at all: SWZ_OK. */
+ * workspace), UNSUPPORTED (head_dim, rotary_dim, page size, element size, alignment, distances), OVERFLOW (counts that do not fit 32-bit indices, a table of more than 2^31 - 4096 positions, a launch
+ * of 2^32 threads or more), HIP.  No tokens at all: SWZ_OK. */
 typedef struct {
   swz_heads q, k, v, q_out;
   const float *cos, *sin;

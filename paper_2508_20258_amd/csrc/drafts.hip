@@ -29,6 +29,9 @@ int check_blocks(const int32_t* cu, const int32_t* table, int64_t tokens, int32_
   return tokens > kMostKeys ? SWZ_ERR_OVERFLOW : SWZ_OK;
 }
 
+// Positions are 32-bit numbers in the kernels, whatever starts and lengths the device has: those of a table have to be.
+bool too_many_positions(const swz_cache16& c, int32_t table_width) { return (int64_t)table_width * c.page_tokens > kMostKeys; }
+
 swz::PageTable page_table(const swz_cache16& c, const int32_t* table, int table_width) {
   return {table, c.pages, __builtin_ctz((unsigned)c.page_tokens), c.k_heads, table_width};
 }
@@ -47,7 +50,7 @@ int check_append(const swz_cache16* cache, const swz_append16_args* a) {
   if (queries && (st = check_heads(a->q, a->q_out)) != SWZ_OK) return st;
   if (!aligned(a->before, 4) || !aligned(a->positions, 4) || !aligned(a->cos, 16) || !aligned(a->sin, 16)) return SWZ_ERR_UNSUPPORTED;
   if (turned && (a->rotary_dim < 16 || a->rotary_dim > cache->head_dim || a->rotary_dim % 16 != 0)) return SWZ_ERR_UNSUPPORTED;
-  return queries && a->q_heads > kMostHeads ? SWZ_ERR_OVERFLOW : SWZ_OK;
+  return too_many_positions(*cache, a->table_width) || (queries && a->q_heads > kMostHeads) ? SWZ_ERR_OVERFLOW : SWZ_OK;
 }
 
 // ---------------------------------------------------------------- attention
@@ -61,7 +64,7 @@ int check_attention(const swz_cache16* cache, const swz_attention16_args* a) {
   if (a->q_heads < 1 || a->q_heads % cache->k_heads != 0 || a->max_length < 0 || !(a->scale > 0.f) || !isfinite(a->scale)) return SWZ_ERR_INVALID_ARG;
   if (st != SWZ_OK) return st;
   if (!aligned(a->lengths, 4) || !aligned(a->tree, 8)) return SWZ_ERR_UNSUPPORTED;
-  if (a->q_heads > kMostHeads || (int64_t)a->table_width * cache->page_tokens > kMostKeys || a->tokens * a->q_heads >= kTokens) return SWZ_ERR_OVERFLOW;
+  if (a->q_heads > kMostHeads || too_many_positions(*cache, a->table_width) || a->tokens * a->q_heads >= kTokens) return SWZ_ERR_OVERFLOW;
   return SWZ_OK;
 }
 
@@ -243,6 +246,7 @@ int swz_cache16_keep(const swz_cache16* cache, const int32_t* cu, const int32_t*
   st = check_blocks(cu, block_table, tokens, sequences, table_width);
   if (st != SWZ_OK || tokens == 0) return st;
   if (!aligned(before, 4) || !aligned(path, 4) || !aligned(accepted, 4)) return SWZ_ERR_UNSUPPORTED;
+  if (too_many_positions(*cache, table_width)) return SWZ_ERR_OVERFLOW;
   swz::Keep16Args a{};
   a.c = page_table(*cache, block_table, table_width);
   a.k_pages = static_cast<uint16_t*>(cache->k), a.v_pages = static_cast<uint16_t*>(cache->v);

@@ -10,7 +10,7 @@ struct PageTable {
   const int32_t* table;
   int64_t pages;
   int page_shift, k_heads, table_width;
-  // The page of a position, or -1.
+  // The page of a position (not negative), or -1.
   __device__ __forceinline__ int page_of(int sequence, int position) const {
     const int j = position >> page_shift;
     if (j >= table_width) return -1;

@@ -198,3 +198,30 @@ def test_verify_refuses_workspaces():
 def test_keep_refuses(change, status):
     a = {**dict(cu=P, before=P, path=P, accepted=P, tokens=3, table=P, width=2, sequences=1), **change}
     assert lib.swz_cache16_keep(ref(cache()), a["cu"], a["before"], a["path"], a["accepted"], a["tokens"], a["table"], a["width"], a["sequences"], None) == status
+
+
+MOST = (1 << 31) - 4096
+
+
+@pytest.mark.parametrize("page,width", [(16, (1 << 27) + 1), (64, (1 << 25) + 1), (1 << 16, 1 << 15), (1 << 30, 2), (1 << 30, (1 << 31) - 1), (4096, MOST // 4096 + 1)])
+def test_tables_of_positions_beyond_32_bits(page, width):
+    """Positions are 32-bit numbers on the device: a table that has more of them could be given a start (which the host does not see) from which they would be negative."""
+    c = ref(cache(page_tokens=page))
+    assert lib.swz_cache16_append(c, ref(append_args(table_width=width)), None) == OVERFLOW
+    assert lib.swz_cache16_append(c, ref(append_args(table_width=width, cos=None, sin=None, positions=None, q=heads(at=None))), None) == OVERFLOW
+    assert lib.swz_cache16_keep(c, P, P, P, P, 3, P, width, 1, None) == OVERFLOW
+    a = ref(attention_args(table_width=width))
+    assert lib.swz_cache16_attention_workspace(c, a) == lib.swz_cache16_attention(c, a, P, 1 << 60, None) == OVERFLOW
+    # nothing to do
+    assert lib.swz_cache16_append(c, ref(append_args(table_width=width, tokens=0)), None) == lib.swz_cache16_keep(c, P, P, P, P, 0, P, width, 1, None) == OK
+
+
+@pytest.mark.parametrize("page", [16, 4096])
+def test_tables_as_wide_as_32_bits_allow(page):
+    """(What comes after the checks: no device, no launch.)"""
+    widest = MOST // page
+    assert widest * page == MOST
+    c = ref(cache(page_tokens=page))
+    assert lib.swz_cache16_append(c, ref(append_args(table_width=widest, k=heads(at=None))), None) == INVALID
+    assert lib.swz_cache16_attention_workspace(c, ref(attention_args(table_width=widest, max_length=64))) >= 0
+    assert lib.swz_cache16_keep(c, P, P, P + 2, P, 3, P, widest, 1, None) == UNSUPPORTED
