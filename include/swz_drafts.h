@@ -77,7 +77,8 @@ int swz_cache16_attention(const swz_cache16* cache, const swz_attention16_args* 
  *   tokens, uniforms : what each node proposes, and a number of [0, 1) for each; the root's is the new token's.
  * From the root on, the children of the current node are tested in their order; the first that passes becomes the current node.  P is the target's row of the current node, at first.
  *   draft not null: child c, of token x, passes if uniforms[c] * Q(x) < P(x).  If it does not, P becomes max(P - Q, 0) / its sum (or stays, if that sum is not above 0).
- *   draft null    : it passes if P(x) > max(uniforms[c] * M, 0), M being 1 at first.  If it does not, M loses P(x), and P(x) becomes 0.
+ *   draft null    : it passes if P(x) > 0 and P(x) > uniforms[c] * M, M being 1 at first.  If it does not, M loses P(x), and P(x) becomes 0.
+ * A comparison with NaN is false: a child of such a probability fails, and so do all those after it under the same node where children are points, as M is NaN then.
  * Where no child passes, the new token is the first x where P(0) + .. + P(x) > uniforms[root] * sum(P), or the last x of P(x) > 0 where none is; -1 if sum(P) is no finite number above 0.
  * All in 64-bit arithmetic.  A token outside the vocabulary, one whose parent does not stand before it, and those of a block from the 65th on are not tested.  The order of the sums depends on
  * the sizes alone.

@@ -181,7 +181,7 @@ __device__ __forceinline__ Walked walk(const Nodes& n, LeftSum* sums, int* path,
     } else {
       const int token = __builtin_amdgcn_readlane(n.token, at);
       const double mine = __ballot(n.token == token && (s.failed_nodes >> lane & 1)) != 0 ? 0. : p, least = u * mass;
-      good = mine > (least > 0. ? least : 0.);
+      good = mine > 0. && mine > least;                      // (a NaN on either side: no)
       if (!good) mass -= mine;
     }
     if (good) {

@@ -95,6 +95,13 @@ def test_verify_closed_forms():
     assert dr.verify(p, [9, 0], [0.3, 0.5], p) == (0, [0, -1], 2)
 
 
+def test_no_child_passes_by_a_mass_that_is_no_number():
+    p = np.array([[np.nan, 0.01, 0.5, 0.49]] * 3)
+    # its probability is none, so what is left of the mass is none; the new token is drawn from the rest of the row
+    assert dr.verify(p, [9, 0, 1], [0.3, 0.9, 0.999], None, [0, 0, 0]) == (0, [0, -1, -1], 2)
+    assert dr.verify(p, [9, 0, 1], [0.6, 0.9, 0.0], None, [0, 0, 0]) == (0, [0, -1, -1], 3)
+
+
 # ---------------------------------------------------------------- refusals
 
 def heads(token=256, head=128, at=P):

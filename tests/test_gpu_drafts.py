@@ -506,6 +506,29 @@ def test_verify_odd_inputs(swz, branch, drawn):
 
 
 @pytest.mark.parametrize("half", [False, True])
+@pytest.mark.parametrize("u", [0.0, 0.9, 0.999])
+def test_verify_siblings_of_one_without_a_probability(swz, u, half):
+    """Points, and a failed one whose probability is NaN: no mass is left that a sibling could be tested against, so none passes.  At the root, further down, and where the NaN comes second."""
+    vocab, nodes = 5, [3, 6, 5, 4]
+    n = sum(nodes)
+    target = torch.full((n, vocab), 0.125, dtype=torch.bfloat16 if half else torch.float32)
+    target[:, 4] = 0.5
+    target[0] = torch.tensor([math.nan, 0.0078125, 0.5, 0.25, 0.0])
+    target[3 + 1, 0] = target[9, 1] = math.nan               # of the node that stands; of the second child
+    parents = [0, 0, 0, 0, 0, 1, 1, 1, 1, 0, 0, 0, 0, 0, 0, 0, 0, 0]
+    tokens = [0, 0, 1, 0, 4, 0, 1, 4, 2, 0, 0, 1, 4, 2, 0, 4, 4, 2]
+    uniforms = torch.full((n,), u, dtype=torch.float32)
+    uniforms[[0, 3, 9, 14]] = 0.4
+    uniforms[4] = 0.0                                        # passes
+    uniforms[10] = 0.9                                       # fails
+    uniforms[14 + 1] = math.nan                              # no number to test by: fails too
+    tokens, parents = ints(tokens), ints(parents)
+    got = swz.verify_drafts(target.cuda(), tokens, cu_of(nodes), uniforms.cuda(), parents=parents)
+    assert got[0].tolist()[:3] == [0, 1, 0]
+    check_verify(got, target, tokens, uniforms, nodes, None, parents)
+
+
+@pytest.mark.parametrize("half", [False, True])
 def test_verify_layouts(swz, half):
     """Rows apart, starting anywhere; tokens behind the last sequence; no tokens; another stream."""
     nodes, vocab = [4, 3], 1001
