@@ -773,3 +773,144 @@ def test_probabilities_beyond_32_bits(swz, drawn):
     if drawn:
         wide.copy_(draft)
         assert all(torch.equal(a, b) for a, b in zip(swz.verify_drafts(target, tokens, cu_of([total]), uniforms, parents=parents, draft_probs=wide), want))
+
+
+# ---------------------------------------------------------------- starts of sequences that make no sense
+
+# of 64 tokens: an end beyond them, a start before them, falling and overlapping starts, all that 32 bits hold, and more sequences than are looked at together
+SENSELESS = [[0, 1000], [-50, 30], [0, 60, 20, 64], [64, 0], [-(1 << 31), (1 << 31) - 1], [10, 5, 40, -7, 64, (1 << 31) - 1, 0], list(range(100, -40, -2)), [(i * 37) % 90 - 10 for i in range(140)]]
+
+
+class Fenced:
+    """Memory of a call between words that it must leave alone."""
+    def __init__(self):
+        self.all = []
+
+    def __call__(self, *shape, dtype=torch.bfloat16, value=7):
+        n, edge = math.prod(shape), 4096
+        whole = torch.full((n + 2 * edge,), value, dtype=dtype, device="cuda")
+        self.all.append((whole, edge, n, value))
+        return whole[edge:edge + n].view(shape)
+
+    def check(self):
+        torch.cuda.synchronize()
+        for whole, edge, n, value in self.all:
+            assert (whole[:edge] == value).all() and (whole[edge + n:] == value).all()
+
+
+def owned(cu, total):
+    """First token and length of each sequence, cut to the tokens there are."""
+    cut = [max(0, min(total, c)) for c in cu]
+    return [(a, max(0, b - a)) for a, b in zip(cut, cut[1:])]
+
+
+@pytest.mark.parametrize("cu", SENSELESS)
+@pytest.mark.parametrize("dim", [64, 128])
+def test_append_and_keep_stay_inside_the_tensors(swz, cu, dim):
+    total, page, heads = 64, 16, 2
+    spans, n = owned(cu, total), len(cu) - 1
+    fenced = Fenced()
+    rows = [[6 * b + j for j in range(6)] for b in range(n)]
+    cache = swz.Cache16(*(fenced(6 * n, heads, page, dim) for _ in range(2)))
+    k, v, q = randn(1, total, heads, dim), randn(2, total, heads, dim), randn(3, total, 3, dim)
+    cos, sin = angles(200, dim // 2)
+    q_out = fenced(total, 3, dim)
+    before = [(5 * b) % 20 for b in range(n)]
+    args = (ints(cu), ints(before), ints(rows))
+    swz.cache16_append(cache, k, v, *args, q=q, cos=cos, sin=sin, q_out=q_out)
+    fenced.check()
+    # a token belongs to the last sequence that starts at it or before, where starts rise; it is written to one place or to none
+    mine = torch.zeros(total, dtype=torch.bool)
+    for first, length in spans:
+        mine[first:first + length] = True
+    assert (q_out[~mine.cuda()] == 7).all()
+    written = (cache.v != 7).any(-1).any(1).sum()
+    assert int(written) <= int(mine.sum())
+    if all(a <= b for a, b in zip(cu, cu[1:])):
+        want = swz.Cache16(*(torch.full_like(x, 7) for x in cache))
+        got = swz.cache16_append(want, k, v, ints([max(0, min(total, c)) for c in cu]), *args[1:], q=q, cos=cos, sin=sin, q_out=torch.full_like(q_out, 7))
+        assert torch.equal(got, q_out) and torch.equal(want.k, cache.k) and torch.equal(want.v, cache.v)
+    # each sequence's nodes but the second one, in its places: where they overlap, the last sequence's
+    path = torch.zeros(total, dtype=torch.int32)
+    for first, length in spans:
+        path[first:first + length] = torch.tensor([0] + [i + 1 if i + 1 < length else -1 for i in range(1, length)])[:length]
+    held = [x.clone() for x in cache]
+    accepted = [[0, 5, 1000, -3, (1 << 31) - 1][b % 5] for b in range(n)]
+    path = path.tolist()
+    swz.cache16_keep(cache, args[0], args[1], ints(path), ints(accepted), args[2])
+    fenced.check()
+    for b, (first, length) in enumerate(spans):
+        moves = [(i, path[first + i]) for i in range(1, min(accepted[b], length - 1) + 1) if path[first + i] >= 0]
+        if any(node < i for i, node in moves) or any(y <= x for (_, x), (_, y) in zip(moves, moves[1:])):
+            continue                                         # a path that does not rise, of sequences that overlap: any order
+        for i, node in moves:
+            for x in held:
+                x[rows[b][(before[b] + i) // page], :, (before[b] + i) % page] = x[rows[b][(before[b] + node) // page], :, (before[b] + node) % page]
+        for x, y in zip(held, cache):
+            assert torch.equal(x[rows[b]], y[rows[b]]), b
+
+
+@pytest.mark.parametrize("cu", SENSELESS)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("q_heads", [1, 4, 8])
+@pytest.mark.parametrize("width,max_length", [(5, 0), (300, 0), (300, 64)])
+def test_attention_stays_inside_the_tensors(swz, cu, q_heads, dim, width, max_length):
+    """Tiles of 32, 64 and 128 rows, alone and dealt; lengths of all kinds, and longer ones than max_length says."""
+    from paper_2508_20258_amd import drafts
+    total, page, n = 64, 16, len(cu) - 1
+    fenced = Fenced()
+    lens = [[300, 70, 0, -5, (1 << 31) - 1, 33][b % 6] for b in range(n)]
+    rows = [[(7 * b + j) % 40 if j % 11 != 10 else -1 for j in range(width)] for b in range(n)]
+    cache = swz.Cache16(randn(1, 40, 1, page, dim), randn(2, 40, 1, page, dim))
+    q, out, tree = randn(3, total, q_heads, dim), fenced(total, q_heads, dim), ints([m for block in masks_of([32, 32], 2) for m in block], torch.int64)
+    c = drafts._cache(cache)
+    tensors = ints(cu), ints(lens), ints(rows)
+    for mask in (None, tree):
+        a = drafts._DraftAttentionArgs(drafts._heads(q), drafts._heads(out), *(t.data_ptr() for t in tensors), None if mask is None else mask.data_ptr(), total, n, width, q_heads, max_length, 0.1)
+        need = drafts.lib.swz_cache16_attention_workspace(drafts.ctypes.byref(c), drafts.ctypes.byref(a))
+        assert need >= 0
+        # what a part's place would be that nobody wrote: any numbers, other ones each time
+        for value in (0, 1, 255):
+            work = fenced(max(need, 16), dtype=torch.uint8, value=value)
+            out.fill_(7)
+            assert drafts.lib.swz_cache16_attention(drafts.ctypes.byref(c), drafts.ctypes.byref(a), work.data_ptr(), need, torch.cuda.current_stream().cuda_stream) == 0
+            fenced.check()
+        mine = torch.zeros(total, dtype=torch.bool)
+        for first, length in owned(cu, total):
+            mine[first:first + length] = True
+        assert (out[~mine.cuda()] == 7).all()
+        if all(a <= b for a, b in zip(cu, cu[1:])):
+            cut = ints([max(0, min(total, x)) for x in cu])
+            want = swz.cache16_attention(q, cache, cut, *tensors[1:], tree=mask, max_length=max_length, scale=0.1, out=torch.full_like(out, 7))
+            assert same(out, want)
+
+
+@pytest.mark.parametrize("cu", SENSELESS)
+@pytest.mark.parametrize("drawn", [False, True])
+@pytest.mark.parametrize("branch", [0, 2])
+def test_verification_stays_inside_the_tensors(swz, cu, branch, drawn):
+    from paper_2508_20258_amd import drafts
+    total, vocab, n = 64, 5000, len(cu) - 1
+    fenced = Fenced()
+    target, draft = probabilities(1, total, vocab, False)
+    tokens, uniforms = ints([int(t) for t in target.argmax(1).roll(1)]), torch.rand(total, generator=torch.Generator().manual_seed(1)).cuda() * 0.5
+    parents = ints([max(0, (i % 30 - 1) // 2) for i in range(total)]) if branch else None
+    accepted, path, token = fenced(n, dtype=torch.int32), fenced(total, dtype=torch.int32), fenced(n, dtype=torch.int32)
+    starts = ints(cu)
+    a = drafts._VerifyArgs(target.data_ptr(), draft.data_ptr() if drawn else None, vocab, vocab, vocab, total, tokens.data_ptr(), None if parents is None else parents.data_ptr(), starts.data_ptr(),
+                           uniforms.data_ptr(), accepted.data_ptr(), path.data_ptr(), token.data_ptr(), n, 4)
+    need = drafts.lib.swz_verify_drafts_workspace(drafts.ctypes.byref(a))
+    work = fenced(need, dtype=torch.uint8, value=255)
+    assert drafts.lib.swz_verify_drafts(drafts.ctypes.byref(a), work.data_ptr(), need, torch.cuda.current_stream().cuda_stream) == 0
+    fenced.check()
+    # each sequence's own, whatever the others; the path where no other one has its places
+    target, draft, spans = f64(target), f64(draft) if drawn else None, owned(cu, total)
+    many, path = np.zeros(total, dtype=int), path.tolist()
+    for first, length in spans:
+        many[first:first + length] += 1
+    for b, (first, length) in enumerate(spans):
+        part = slice(first, first + length)
+        want = dr.verify(target[part], tokens[part].tolist(), f64(uniforms[part]), None if draft is None else draft[part], None if parents is None else parents[part].tolist())
+        assert (int(accepted[b]), int(token[b])) == (want[0], want[2]), b
+        assert all(p == w for p, w, m in zip(path[part], want[1], many[part]) if m == 1), b
+    assert all(p == 7 for p, m in zip(path, many) if m == 0)
