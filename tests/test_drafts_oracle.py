@@ -72,6 +72,15 @@ def test_what_is_emitted_has_the_targets_distribution_drawn(children):
     assert np.abs(got - p[0]).max() <= 1e-12 if children == 1 else np.abs(got - p[0]).max() < 0.07
 
 
+@pytest.mark.parametrize("children", [1, 2])
+def test_what_is_left_over_is_divided_by_its_sum(children):
+    """Two tokens are left over, by unequal parts, one of which the draft draws more often than it is left before the division and less often than after it.  All borders (1/4, 2/3, 1/6) are lines of the grid, so
+    that each sum of its cells is the probability, but for one rounding an addition."""
+    p, q = np.array([[2, 5, 9]] * 3) / 16, np.array([[8, 4, 4]] * 3) / 16
+    got = emitted(p, q, [0] + [0] * children, None, 12)
+    assert np.abs(got - p[0]).max() <= 2 * 2.0 ** -53 * 3 ** children * 12 ** (children + 1)
+
+
 @pytest.mark.parametrize("first", [(0,), (2, 0), (1, 1), (0, 1, 2)])
 def test_what_is_emitted_has_the_targets_distribution_points(first):
     p = np.array([[0.5, 0.25, 0.25]] * 4)
