@@ -91,6 +91,8 @@ int tile_rows(int64_t rows, int64_t longest) { return rows <= 32 ? 32 : rows <= 
 // A workgroup for each tile of rows and key head, or the steps of all of them dealt evenly and the parts joined.  The latter takes another launch and the parts' traffic, 6 us and theirs, the former as long as the longest tile, of
 // about 2.7 us for 256 positions (4.2 with 128 rows); lengths are taken to be 0.6 of the longest on average.  Single tokens of 32 heads of 128 sharing 8, the one and the other: 16 sequences of 256 positions 8.8 us and 12.0,
 // of 1024 21.0 and 21.7, of 2048 34.7 and 30.5; one of 512 11.4 and 13.7, of 1024 16.6 and 15.1, of 4096 49 and 18.  Blocks of 128 rows: 16 of 1024 28 and 41, one 25 and 16.
+// A tile of rows whose parts are joined by one workgroup, or (of each 32 rows) by 8, each looking for the tile by itself.  Blocks of 1 and 8 tokens, both kinds of heads, us with the one and the other: where a tile has 5.3 parts
+// 26.3 and 25.4, 7 parts 12.8 and 11.4 to 15.8 and 15.8, 4 parts 31.2 and 31.4 to 56.5 and 57.5, 2 parts 50.5 and 51.6 to 97.4 and 103.4.
 AttentionPlan attention_plan(const swz_cache16& c, const swz_attention16_args& a) {
   const int64_t group = a.q_heads / c.k_heads, rows = (a.tokens + a.sequences - 1) / a.sequences * group;          // of an average block
   const int64_t cut = (int64_t)a.table_width * c.page_tokens, longest = a.max_length > 0 && a.max_length < cut ? a.max_length : cut;
@@ -108,7 +110,7 @@ AttentionPlan attention_plan(const swz_cache16& c, const swz_attention16_args& a
     const double parts = (double)shares * c.k_heads * p.rows * c.head_dim * 4 * 2 / 5e6;
     if (whole * (filled > 1 ? filled : 1) <= 0.6 * whole * filled + 6 + parts) return 0;
     p.shares = (int)shares;
-    p.join_groups = p.shares > 4 * (a.tokens * group / p.rows + 1) ? 8 : 1;          // parts of a tile of rows, about
+    p.join_groups = p.shares > 4 * tiles ? 8 : 1;          // by the parts of a tile of rows, about
     return 0;
   });
   return p;

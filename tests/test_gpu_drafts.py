@@ -528,6 +528,39 @@ def test_verify_siblings_of_one_without_a_probability(swz, u, half):
     check_verify(got, target, tokens, uniforms, nodes, None, parents)
 
 
+@pytest.mark.parametrize("drawn", [False, True])
+@pytest.mark.parametrize("vocab", [300, 9001])
+@pytest.mark.parametrize("failing", [1, 31, 32, 62, 63])
+def test_verify_many_siblings(swz, failing, vocab, drawn):
+    """Nodes of as many children as a block has room for, of which so many fail before one passes, or all do: of the root, and of its child."""
+    count = min(failing + 2, 64)
+    nodes = [count, count, 64]
+    n = sum(nodes)
+    target, draft = probabilities(failing + vocab, n, vocab, False)
+    draft = (0.7 * target + 0.3 * draft).contiguous()        # much of the target is left for long
+    rows = [target.float().cpu(), draft.float().cpu()]
+    parents = [0] * count + [0, 0] + [1] * (count - 2) + [0] * 64
+    tokens, first = [], 0
+    rng = np.random.default_rng(failing)
+    for m in nodes:
+        for i in range(m):
+            p, q = (x[first + parents[first + i]] for x in rows)
+            if first == count and i == 1 or first < 2 * count and i == failing + 1:
+                tokens.append(int((p / q).argmax()))         # of what is left
+            else:
+                tokens.append(int((p / q).topk(40 + i, largest=False).indices[-1 - int(rng.integers(0, 20))]))     # of what is not
+        first += m
+    uniforms = torch.tensor(0.9 + 0.1 * rng.random(n), dtype=torch.float32)
+    for at in (failing + 1, count + 1, count + failing + 1):
+        if at < 2 * count:
+            uniforms[at] = 0.0
+    uniforms[[0, count, 2 * count]] = torch.tensor([0.3, 0.5, 0.9])
+    tokens, parents, uniforms = ints(tokens), ints(parents), uniforms.cuda()
+    got = swz.verify_drafts(target, tokens, cu_of(nodes), uniforms, draft_probs=draft if drawn else None, parents=parents)
+    assert int(got[0][1]) >= 1 and int(got[0][2]) == 0 and (failing == 63 or int(got[0][0]) == 1)
+    check_verify(got, target, tokens, uniforms, nodes, draft if drawn else None, parents)
+
+
 @pytest.mark.parametrize("half", [False, True])
 def test_verify_layouts(swz, half):
     """Rows apart, starting anywhere; tokens behind the last sequence; no tokens; another stream."""
