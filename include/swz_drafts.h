@@ -50,9 +50,10 @@ int swz_cache16_append(const swz_cache16* cache, const swz_append16_args* args, 
 
 /* out = softmax(scale q k^T) v of every token and query head over the first lengths[b] positions of its sequence in the cache, of which the last ones are the block's own tokens, appended
  * before: token j of n is position lengths[b] - n + j.  A token looks at all positions before the block, and
- *   tree null     : at the block's tokens up to itself (a chain, or the next piece of a prompt, of any length);
+ *   tree null     : at the block's tokens up to itself (a chain, or the next piece of a prompt, of any length; every token costs the sequence's whole length, where swz_attention leaves out what is
+ *                   behind a token: a prompt of 8192 tokens by itself takes three times as long as there);
  *   tree not null : at token j of its block where bit j of the token's 64-bit mask is set; at those from the 65th on none looks.
- * A token that looks at nothing gets 0, and so does one whose scores are all minus infinity.  A length is cut to the table's positions; pages that the cache has not give NaN to what looks at them.  Infinities and NaN in keys and
+ * A token that looks at nothing gets 0, and so does one whose scores are all minus infinity, if the values are finite (0 times another one is NaN).  A length is cut to the table's positions; pages that the cache has not give NaN to what looks at them.  Infinities and NaN in keys and
  * values that a token does not look at do not reach its output.  The weights are rounded to bfloat16 for their product with v, their sum is not.
  *   q, out : `tokens` tokens of q_heads heads, query head h looking at key head h / (q_heads / k_heads).
  *   max_length : the longest length, or more (0: the table's); it decides how many workgroups share the work, no more: longer lengths are right too, and slower.

@@ -16,6 +16,9 @@
 // positions (388 MB) 87 us, 4.4 TB/s, and 11: the parts of 512 workgroups, 45 MB, are written and read beside it.  A block of 64 tokens, sharing 4 key heads, over 131072 positions, 137 GFLOP, 144 us and 8.3,
 // 0.95 PFLOP/s: the matrix units work for 54 % of the cycles, the vector unit for 47 %, at 1.76 GHz.
 //
+// The next piece of a prompt is a block as any other: every tile of its rows takes all positions of the sequence, those of the block's own tokens in the slower masked way, though a chain's first rows look at few of those.
+// With 32 heads of 128 sharing 8: 8192 tokens by themselves 1580 us (the causal products alone are 343 at 1604 TFLOP/s, and attention_kernel takes 511), 2048 over 16384 positions 562 (321), 512 over 8192 101 (42).
+//
 // Loads go straight to LDS.  Streaming ones, where positions are read once: 64 single tokens 105 us, with regular ones 121.  More tiles on their way in LDS, or fewer bytes a wave and more waves, changed
 // nothing: 5.8 TB/s was what regular loads reach in a kernel that does nothing else.
 #pragma once
@@ -269,7 +272,8 @@ struct DraftSums {
     for (int i = 0; i < D / 32; ++i) o[i] *= less;
     top = now;
   }
-  // Scores of 32 NB positions to weights, rounded for the product.
+  // Scores of 32 NB positions to weights, rounded to bfloat16 for the product: 2^-8 of a weight at most, as likely up as down; the sum is of the weights before.  With values of bfloat16 and an output that is
+  // rounded to it the error against 64 bits is 0.0023 where 32-bit weights leave 0.0017; they would take two products for one.
   template <int NB>
   __device__ __forceinline__ void weigh(f32x16 (&x)[NB], float c, u32x4 (&p)[2 * NB]) {
     float high[2] = {x[0][0], x[0][1]};

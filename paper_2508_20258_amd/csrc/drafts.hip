@@ -85,12 +85,15 @@ auto for_shape(int d, int rows, F&& f) {
 
 // Rows of a tile.  32 heads of 128 sharing 8, us in tiles of 32, 64 and 128 rows: blocks of 32 rows, 32 sequences of 3000 positions 71, 74 and 91; of 64 rows 135, 74 and 88; of 192 381, 225 and 122.  Blocks of 128, 32 sequences
 // of 512 to 8192 positions: 138 in tiles of 64, 96 in tiles of 128 (as two tiles of a block read its positions at different times; at the same time, in 32 sequences of 3000, 89 and 92).  Few positions are soon read
-// again: blocks of 192 rows, 4 sequences of 500 positions 13, 14 and 17.
+// again: blocks of 192 rows, 4 sequences of 500 positions 13, 14 and 17.  Heads of 64, 32 sequences of 3000: 32 rows 41, 39 and 51; 64 rows 46, 41 and 50; 128 rows 88, 47 and 52; 192 rows 133, 93 and 70, the slower one being taken for 65
+// to 128 rows, by a tenth; and so it is for 32 rows in many sequences (heads of 128, 64 of 2000: 93, 84 and 99).  The average is of all blocks: one of 512 tokens over 4096 positions beside 64 single tokens over 2000 193, 134 and 151 (64 taken), one of 2048 over 8192 beside them 983, 465 and 435 (128 taken); heads of 64,
+// sharing in twos, 64, 66 and 82 (32 taken), 217, 170 and 176 (128 taken).
 int tile_rows(int64_t rows, int64_t longest) { return rows <= 32 ? 32 : rows <= 64 || longest <= 1024 ? 64 : 128; }
 
 // A workgroup for each tile of rows and key head, or the steps of all of them dealt evenly and the parts joined.  The latter takes another launch and the parts' traffic, 6 us and theirs, the former as long as the longest tile, of
 // about 2.7 us for 256 positions (4.2 with 128 rows); lengths are taken to be 0.6 of the longest on average.  Single tokens of 32 heads of 128 sharing 8, the one and the other: 16 sequences of 256 positions 8.8 us and 12.0,
 // of 1024 21.0 and 21.7, of 2048 34.7 and 30.5; one of 512 11.4 and 13.7, of 1024 16.6 and 15.1, of 4096 49 and 18.  Blocks of 128 rows: 16 of 1024 28 and 41, one 25 and 16.
+// Heads of 64, by the same figures: 16 sequences of 512 9.5 and 12.0, of 1024 13.0 and 15.4 (where the rule takes the latter, as for one, 12.5 and 10.8), of 2048 22 and 19; 64 of 1024 25.0 and 27.5, of 4096 89 and 88.
 // A tile of rows whose parts are joined by one workgroup, or (of each 32 rows) by 8, each looking for the tile by itself.  Blocks of 1 and 8 tokens, both kinds of heads, us with the one and the other: where a tile has 5.3 parts
 // 26.3 and 25.4, 7 parts 12.8 and 11.4 to 15.8 and 15.8, 4 parts 31.2 and 31.4 to 56.5 and 57.5, 2 parts 50.5 and 51.6 to 97.4 and 103.4.
 AttentionPlan attention_plan(const swz_cache16& c, const swz_attention16_args& a) {

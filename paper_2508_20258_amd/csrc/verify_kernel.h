@@ -5,10 +5,12 @@
 // random number's share, and in it the token.  Where children were drawn from a draft's probabilities and one fails that has siblings, what is left has to be summed before the next test: for trees of drawn
 // children a launch before these makes the tests, a workgroup for each sequence.  Sums are 64-bit, in an order that depends on the sizes alone.
 //
-// What bounds it: with many sequences the rows' bytes (64 of 128000 floats, of both kinds: the sums 14.7 us, 4.3 TB/s, in which the vector unit issues for 44 % of the cycles: 64-bit additions; pieces of 4096
-// values are 4 loads of 16 bytes a thread and row, all on their way); with few the waits: places, nodes, their probabilities and the row one after another (16 sequences of 32000 values in bfloat16: 4.8 us), and the token's launch
-// alike (4.9 us: sums, place in them, a piece of the row).  Trees of drawn children: 8 sequences of 50257 floats 26 us for the tests, residuals of a row summed one after the other by a workgroup alone, whose
-// compute unit's vector unit issues for 65 % of the cycles (512 threads, or a division for each value: slower).
+// What bounds it: the waits, and with many sequences the rows' bytes behind them.  Places, nodes, their probabilities and the row are loaded one after another: 16 sequences of 32000 values in bfloat16, next to no bytes,
+// 4.7 us.  64 of 128000 floats, of both kinds, are 10.3 us at a copy's rate, and the sums take 15.0: every workgroup waits as long before its row's loads (pieces of 4096 values are 4 loads of 16 bytes a thread and row, all on their
+// way), and all of them at the same time, while the vector unit issues for 44 % of the cycles.  The token's launch waits alike (4.9 us: sums, place in them, a piece of the row).
+// Trees of drawn children: 8 sequences of 50257 floats 26 us for the tests, residuals of a row summed one after the other by a workgroup alone, whose compute unit's vector unit issues for 65 % of the cycles (512
+// threads, or a division for each value: slower).  Each sum starts from the rows again and takes off all the failed children before it, so that the time goes with the square of their number: 8 trees whose root has 1, 2, 4, 8, 16, 32
+// and 62 children that fail, and one more that passes, take 20, 33, 73, 202, 666, 2410 and 8650 us in all.  (The sums of a node follow from its two rows alone, whatever is drawn; they could be made for all nodes at once.)
 #pragma once
 
 #include <hip/hip_runtime.h>
