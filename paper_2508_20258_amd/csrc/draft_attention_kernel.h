@@ -13,8 +13,8 @@
 //
 // What bounds it: the cache's bytes up to about 250 rows of a block (4 D bytes and 4 D operations a row for each position and key head, at 6.4 TB/s and 1600 TFLOP/s), products beyond.  With 32 query heads of 128:
 // 64 single tokens, sharing 8 key heads, over 151000 positions in all (620 MB) 98 us, 6.3 TB/s, and 4.6 for the join; one over 131072 positions (537 MB) 84 us, 6.4 TB/s, and 5.  32 blocks of 32 tokens over 94000
-// positions (388 MB) 87 us, 4.4 TB/s, and 11: the parts of 512 workgroups, 45 MB, are written and read beside it.  A block of 64 tokens, sharing 4 key heads, over 131072 positions, 137 GFLOP, 144 us and 8.3,
-// 0.95 PFLOP/s: the matrix units work for 54 % of the cycles, the vector unit for 47 %, at 1.76 GHz.
+// positions (388 MB) 87 us, 4.4 TB/s, and 11: the parts of 512 workgroups, 45 MB, are written and read beside it.  A block of 64 tokens, sharing 4 key heads, over 131072 positions, 137 GFLOP, 142 to 144 us and 8.3,
+// 0.96 PFLOP/s: the matrix units work for 54 % of the cycles, the vector unit for 47 %, at 1.76 GHz.
 //
 // The next piece of a prompt is a block as any other: every tile of its rows takes all positions of the sequence, those of the block's own tokens in the slower masked way, though a chain's first rows look at few of those.
 // With 32 heads of 128 sharing 8: 8192 tokens by themselves 1580 us (the causal products alone are 343 at 1604 TFLOP/s, and attention_kernel takes 511), 2048 over 16384 positions 562 (321), 512 over 8192 101 (42).
