@@ -129,7 +129,8 @@ def cache16_attention(q, cache: Cache16, cu, lengths, block_table, tree=None, ma
     """Attention of every sequence's tokens (q: (tokens, q_heads, head_dim), packed) over the first lengths[b] positions of the cache, of which the last are the tokens' own, appended before.
 
     A token looks at all positions before its block, and at the block's tokens up to itself, or, with `tree` ((tokens,) int64), at token j of its block where bit j is set (draft_tree gives such
-    masks); at those from the 65th on none looks then.  A token that looks at nothing gets 0.  max_length: the longest length if the program knows it; it decides how sequences are split over the device.
+    masks); at those from the 65th on none looks then.  A token that looks at nothing gets 0.  A long block (the next piece of a prompt) is right, and costs its products with the whole sequence: `attention` takes a
+    third of the time for a prompt by itself.  max_length: the longest length if the program knows it; it decides how sequences are split over the device.
     scale: head_dim ** -0.5 by default."""
     if stream is not None:
         return _run_on(stream, cache16_attention, q, cache, cu, lengths, block_table, tree, max_length, out, scale)
